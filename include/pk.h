@@ -461,6 +461,145 @@ int pk_store_noalloc(const pk_config *cfg, const uint8_t *keys_dev, const uint32
                      const int64_t *key_off_dev, const int32_t *hit_chunks_dev, uint32_t R,
                      int32_t *result_dev, uint32_t *slot_out_dev, int32_t *status_dev, pk_stream stream);
 
+/* KV pages: what lies behind a slot, and what a serving step does with it.
+ * The paper keeps page payloads opaque (Sec. 2.1: a hit loads stored KV state
+ * and skips that prefill, a miss computes and writes new state); these calls
+ * are one such payload, held in 4 bits, with the attention that reads it.
+ *
+ * A page holds page_tokens tokens of every KV head:
+ *     page    = [kv_heads][page_tokens / 16] granules
+ *     granule = 16 consecutive tokens of one head, 16 * (D + D/8) bytes:
+ *               K codes [16][D/2] | V codes [16][D/2] |
+ *               K scales [16][D/16] | V scales [16][D/16]       (D = head_dim)
+ * Codes are e2m1 (sign, 2 exponent bits, 1 mantissa bit: 0, .5, 1, 1.5, 2, 3,
+ * 4, 6), dimension 2i in the low and 2i+1 in the high half of byte i; a scale
+ * is e4m3 and serves 16 consecutive dimensions of one token:
+ *     value = code * scale * k_scale (v_scale).
+ * A scale of NaN marks a block that held an infinity or NaN: its 16 values
+ * read as NaN.  k_scale and v_scale belong to the KV representation: bind
+ * them, with the format, in the descriptor's kv_format. */
+typedef struct {
+    void *pool_dev;       /* n_slots pages of pk_kv_page_bytes each; 16-byte aligned */
+    uint64_t n_slots;     /* >= 1 */
+    uint32_t page_tokens; /* a multiple of 16, 16..32768 */
+    uint32_t kv_heads;    /* 1..1024 */
+    uint32_t head_dim;    /* 64 or 128 */
+    float k_scale;        /* finite, > 0 */
+    float v_scale;        /* finite, > 0 */
+} pk_kv_cache;
+
+/* A strided [tokens][heads][head_dim] array of 16-bit values: strides in
+ * elements, the last dimension contiguous.  p 16-byte aligned, strides
+ * multiples of 8 (every row starts on a 16-byte boundary), not negative. */
+typedef struct {
+    void *p;
+    int64_t tok_stride;
+    int64_t head_stride;
+} pk_heads;
+
+#define PK_BF16 0u
+#define PK_FP16 1u
+
+/* Bytes of one page (0 if a field of the geometry is out of range). */
+size_t pk_kv_page_bytes(uint32_t page_tokens, uint32_t kv_heads, uint32_t head_dim);
+
+/* Device.  Quantise the K and V of new tokens into their pages.
+ *   k, v         [n_tokens][kv_heads][head_dim] of dtype (PK_BF16, PK_FP16)
+ *   tok_off_dev  int64[R+1], non-decreasing, 0 <= tok_off[0], tok_off[R] <=
+ *                n_tokens: request r's new tokens are [tok_off[r], tok_off[r+1])
+ *   start_dev    int32[R] >= 0: tokens that request r holds already; its
+ *                token i goes to position start[r] + i
+ *   pages_dev    uint32[R][page_stride]: position p of request r lies in the
+ *                page of slot pages[r][p / page_tokens]
+ * Per block of 16 dimensions, with a the largest magnitude and g the tensor's
+ * scale, in 32-bit arithmetic: s = e4m3(min(a * fl(1/6) / g, 448)), code =
+ * e2m1(x / (s * g)), both to nearest even and saturating (0 where s = 0).
+ * Only the bytes of the named positions are written; two tokens given the
+ * same place in one call leave either's bytes.  Device errors: offsets,
+ * start, or a slot out of range (PK_ERR_ARG; that token is not written). */
+int pk_kv_write(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *k, const pk_heads *v, uint64_t n_tokens,
+                const int64_t *tok_off_dev, const int32_t *start_dev, uint32_t R, const uint32_t *pages_dev,
+                uint64_t page_stride, int32_t *status_dev, pk_stream stream);
+
+/* Device.  The reverse: tokens of pages as 16-bit values, packed for
+ * pk_attend_prompt (a hit's prefix).  Request r's positions [start[r],
+ * start[r] + tok_off[r+1] - tok_off[r]) go to rows [tok_off[r], tok_off[r+1])
+ * of k and v (OUT), each value code * (s * g) in 32 bits, rounded once.  Rows
+ * that belong to no request are not written.  Device errors as pk_kv_write
+ * (that token's row is left unwritten). */
+int pk_kv_read(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *k, const pk_heads *v, uint64_t n_tokens,
+               const int64_t *tok_off_dev, const int32_t *start_dev, uint32_t R, const uint32_t *pages_dev,
+               uint64_t page_stride, int32_t *status_dev, pk_stream stream);
+
+/* Device.  Causal attention over whole prompts, packed one after another,
+ * q_heads query heads sharing kv_heads KV heads in equal groups (query head h
+ * reads KV head h / (q_heads / kv_heads)):
+ *   q  [n_q][q_heads][head_dim], k, v [n_k][kv_heads][head_dim], of dtype
+ *   q_off_dev, k_off_dev  int64[R+1], non-decreasing, within n_q and n_k:
+ *       request r's queries and keys.  Its last query sits at its last key:
+ *       query i attends keys j <= i + Lk - Lq, so with Lk > Lq the first
+ *       Lk - Lq keys are a prefix that needs no queries (a hit).
+ *   out      OUT [n_q][q_heads][head_dim] of dtype:
+ *            sum_j softmax_j(scale * q.k_j) v_j
+ *   lse_dev  OUT float32[n_q][q_heads], ln sum_j exp(scale * q.k_j); may be
+ *            NULL
+ * A query without a key (Lk < Lq) gives 0 and -infinity.  Keys past a query's
+ * last one never reach its outputs, whatever they hold.  A query that attends
+ * a value of V that is infinite or NaN gets a non-finite output in that
+ * dimension.  Rows of q that belong to no request are not written.
+ * head_dim: 64 or 128; q_heads a multiple of kv_heads; scale finite.
+ * scratch_dev: pk_attend_prompt_scratch_bytes(R) bytes, 16-byte aligned.
+ * Device errors: offsets out of order or range (PK_ERR_ARG; nothing is
+ * written); PK_ERR_TIMEOUT. */
+size_t pk_attend_prompt_scratch_bytes(uint32_t R);
+int pk_attend_prompt(uint32_t dtype, const pk_heads *q, const pk_heads *k, const pk_heads *v, const pk_heads *out,
+                     float *lse_dev, uint64_t n_q, uint64_t n_k, const int64_t *q_off_dev, const int64_t *k_off_dev,
+                     uint32_t R, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, float scale,
+                     void *scratch_dev, size_t scratch_bytes, int32_t *status_dev, pk_stream stream);
+
+/* Device.  Attention of n_q tokens a request (1 for a decode step) over its
+ * pages.  Query i of request r sits at position kv_len[r] - n_q + i and
+ * attends the positions up to its own (the step's tokens are written first).
+ *   q        [R * n_q][q_heads][head_dim] of dtype; out OUT likewise
+ *   lse_dev  OUT float32[R * n_q][q_heads], or NULL
+ *   kv_len_dev int32[R], 0 <= kv_len <= page_stride * page_tokens
+ *   pages_dev  uint32[R][page_stride]
+ *   page_weight_dev  float32[R][page_stride] or NULL: page_weight[r][j] +=
+ *            the softmax weights on page j's tokens, summed over the heads and
+ *            queries (what pk_evict_pages ranks by).  Deterministic.
+ * A query before position 0 gives 0 and -infinity.  Bytes of positions at or
+ * past kv_len are never used.  q_heads a multiple of kv_heads, at most 65536;
+ * n_q >= 1.
+ * scratch_dev: pk_attend_cache_scratch_bytes(...) bytes for the same
+ * arguments, 16-byte aligned (weigh: page_weight_dev given).  Device errors: kv_len or a slot out of range (PK_ERR_ARG). */
+size_t pk_attend_cache_scratch_bytes(const pk_kv_cache *kv, uint32_t R, uint32_t n_q, uint32_t q_heads,
+                                     uint64_t page_stride, int weigh);
+int pk_attend_cache(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, const pk_heads *out, float *lse_dev,
+                    uint32_t R, uint32_t n_q, uint32_t q_heads, float scale, const int32_t *kv_len_dev,
+                    const uint32_t *pages_dev, uint64_t page_stride, float *page_weight_dev, void *scratch_dev,
+                    size_t scratch_bytes, int32_t *status_dev, pk_stream stream);
+
+/* Device.  Cut each request to `budget` pages by accumulated attention
+ * weight.  Request r holds n = ceil(kv_len[r] / page_tokens) pages.  n <=
+ * budget: all are kept.  Else its first `sinks` and last `recent` pages stay,
+ * and of the others the budget - sinks - recent heaviest; of equal weights the
+ * lower index stays, NaN counts as the lightest.  Kept pages keep their order.
+ *   pages_dev uint32[R][page_stride], weight_dev float32[R][page_stride]
+ *   pages_out_dev   OUT uint32[R][budget]: kept slots, then PK_NO_SLOT
+ *   weight_out_dev  OUT float32[R][budget]: their weights, then 0
+ *   kv_len_out_dev  OUT int32[R]: tokens held (only the last page, which is
+ *                   kept, can be partial)
+ *   evicted_dev     OUT uint32[R][page_stride]: dropped slots in index order,
+ *                   then PK_NO_SLOT; or NULL
+ * Outputs must not overlap inputs.  The pages' bytes are not touched: a slot
+ * may be another request's too.  recent >= 1, sinks + recent <= budget,
+ * page_stride < 2^31.  Device errors: kv_len out of range (PK_ERR_ARG; that
+ * request's outputs are empty). */
+int pk_evict_pages(const uint32_t *pages_dev, const float *weight_dev, const int32_t *kv_len_dev, uint32_t R,
+                   uint64_t page_stride, uint32_t page_tokens, uint32_t budget, uint32_t sinks, uint32_t recent,
+                   uint32_t *pages_out_dev, float *weight_out_dev, int32_t *kv_len_out_dev, uint32_t *evicted_dev,
+                   int32_t *status_dev, pk_stream stream);
+
 /* Host, synchronous.  Number of entries in the table (device counter read
  * after synchronising `stream`). */
 int pk_entries(pk_ctx *ctx, uint64_t *count, pk_stream stream);

@@ -1,0 +1,192 @@
+// pk_kv.cu -- the 4-bit page store: quantise new K/V into their pages
+// (pk_kv_write) and read pages back as 16-bit rows (pk_kv_read).
+#include <cuda_runtime.h>
+
+#include "pk_device.cuh"
+#include "pk_internal.h"
+#include "pk_kv.cuh"
+
+namespace {
+
+constexpr int kMoveThreads = 256;
+
+struct Move {
+    uint8_t *pool;
+    uint64_t page_bytes, n_slots;
+    uint32_t page_tokens, granules;  // granules of one head in a page
+    uint32_t heads, heads_per_warp;
+    float g[2];  // k_scale, v_scale
+    uint16_t *x[2];
+    int64_t ts[2], hs[2];
+    uint64_t n_tokens;
+    const int64_t *tok_off;
+    const int32_t *start;
+    uint32_t R;
+    const uint32_t *pages;
+    uint64_t page_stride;
+    int32_t *status;
+};
+
+// One block of 16 dimensions: 8 words of 16-bit values -> 8 code bytes and a
+// scale byte.  The largest magnitude is found on the bits (same order), which
+// also finds an infinity or NaN.  den = s * g and the true division x / den
+// are the format's definition (pk.h): a tie between two codes is then decided
+// by the values, not by a reciprocal's rounding.
+template <uint32_t DT>
+__device__ __forceinline__ void quantise16(const uint32_t (&w)[8], float g, uint2 *codes, uint32_t *scale) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+    m = max(m & 0xffffu, m >> 16);
+    const bool finite = m < pk::Elem<DT>::kInfBits;
+    const float a = pk::Elem<DT>::to1((uint16_t)m);
+    const uint32_t s = finite ? pk::e4m3_byte(fminf(__fdiv_rn(a * (1.0f / 6.0f), g), 448.0f)) : 0x7fu;
+    const float den = __fmul_rn(pk::e4m3_to_float(s), g);
+    const bool live = finite && den > 0.0f;
+    uint32_t out[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 x = pk::Elem<DT>::to2(w[i]);
+        const float lo = live ? __fdiv_rn(x.x, den) : copysignf(0.0f, x.x);
+        const float hi = live ? __fdiv_rn(x.y, den) : copysignf(0.0f, x.y);
+        out[i / 4] |= pk::e2m1_pair(lo, hi) << (8 * (i % 4));
+    }
+    *codes = make_uint2(out[0], out[1]);
+    *scale = s;
+}
+
+// D/16 lanes hold one token (16 dimensions each), so a warp takes 512/D tokens
+// at a time and walks over heads_per_warp heads: the search for the tokens'
+// requests is paid once.  Codes of a token are D/2 consecutive bytes and
+// consecutive tokens of a granule follow each other, so whole 32-byte sectors
+// are written where four tokens (two for D = 64's codes) lie together.
+// Bound by memory: 4 D bytes of K and V against 1.125 D bytes of pages a token
+// and head.
+template <int D, uint32_t DT, bool kWrite>
+__global__ void __launch_bounds__(kMoveThreads) k_kv_move(const Move a) {
+    constexpr uint32_t kLanes = D / 16, kTokens = 32 / kLanes;
+    using G = pk::Granule<D>;
+    const uint32_t lane = threadIdx.x & 31;
+    const uint64_t n_groups = (a.n_tokens + kTokens - 1) / kTokens;
+    const uint32_t head_parts = (a.heads + a.heads_per_warp - 1) / a.heads_per_warp;
+    const uint64_t wid = ((uint64_t)blockIdx.x * kMoveThreads + threadIdx.x) >> 5;
+    const uint64_t group = wid / head_parts;
+    const uint32_t h0 = (uint32_t)(wid % head_parts) * a.heads_per_warp;
+    const int64_t *tok_off = a.tok_off;
+    const int32_t *start = a.start;
+    const uint32_t *pages = a.pages;
+    uint8_t *pool = a.pool;
+    uint16_t *xk = a.x[0], *xv = a.x[1];
+    pk::pdl_wait(tok_off, start, pages, pool, xk, xv);
+
+    // every request's offsets are looked at once, whatever the tokens do
+    for (uint64_t r = (uint64_t)blockIdx.x * kMoveThreads + threadIdx.x; r < a.R;
+         r += (uint64_t)gridDim.x * kMoveThreads) {
+        const int64_t o0 = __ldcg(tok_off + r), o1 = __ldcg(tok_off + r + 1), s = __ldcg(start + r);
+        if (o0 < 0 || o1 < o0 || (uint64_t)o1 > a.n_tokens || s < 0 ||
+            (uint64_t)(s + (o1 - o0)) > a.page_stride * a.page_tokens)
+            pk::set_status(a.status, PK_ERR_ARG);
+    }
+    if (group >= n_groups) return;  // uniform per warp
+
+    const int64_t t0 = (int64_t)(group * kTokens);
+    const int64_t t = t0 + lane / kLanes;
+    const uint32_t r = pk::lane_request(tok_off, a.R, t0, __ldcg(tok_off + a.R), t);
+    const int64_t first = __ldcg(tok_off + r);
+    const int64_t pos = (int64_t)__ldcg(start + r) + (t - first);
+    bool on = (uint64_t)t < a.n_tokens && t >= first && t < __ldcg(tok_off + r + 1) && pos >= t - first &&
+              (uint64_t)pos < a.page_stride * a.page_tokens;
+    uint32_t slot = 0;
+    const uint32_t page = on ? (uint32_t)((uint64_t)pos / a.page_tokens) : 0;
+    if (on) {
+        slot = __ldcg(pages + (uint64_t)r * a.page_stride + page);
+        if (slot >= a.n_slots) {
+            pk::set_status(a.status, PK_ERR_ARG);
+            on = false;
+        }
+    }
+    pk::pdl_launch_dependents();
+    if (!on) return;  // no warp-wide step follows
+
+    const uint32_t in_page = (uint32_t)((uint64_t)pos - (uint64_t)page * a.page_tokens);
+    const uint32_t tok = in_page % pk::kGranTokens, block = lane % kLanes;
+    uint8_t *base = pool + (uint64_t)slot * a.page_bytes + (uint64_t)(in_page / pk::kGranTokens) * G::kBytes;
+    const uint32_t h1 = min(h0 + a.heads_per_warp, a.heads);
+#pragma unroll 2
+    for (uint32_t h = h0; h < h1; ++h) {
+        uint8_t *gran = base + (uint64_t)h * a.granules * G::kBytes;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            uint2 *codes = reinterpret_cast<uint2 *>(gran + (j ? G::kV : G::kK) + tok * G::kRow + block * 8);
+            uint8_t *scale = gran + (j ? G::kVs : G::kKs) + tok * G::kScales + block;
+            uint4 *row = reinterpret_cast<uint4 *>((j ? xv : xk) + t * a.ts[j] + (int64_t)h * a.hs[j] + block * 16);
+            if (kWrite) {
+                const uint4 u = __ldcg(row), v = __ldcg(row + 1);
+                const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+                uint2 c;
+                uint32_t s;
+                quantise16<DT>(w, a.g[j], &c, &s);
+                *codes = c;
+                *scale = (uint8_t)s;
+            } else {
+                const uint2 c = __ldcg(codes);
+                const float den = __fmul_rn(pk::e4m3_to_float(__ldcg(scale)), a.g[j]);
+                uint32_t half[8], w[8];
+                pk::e2m1x8_to_half2(c.x, *reinterpret_cast<uint32_t(*)[4]>(half));
+                pk::e2m1x8_to_half2(c.y, *reinterpret_cast<uint32_t(*)[4]>(half + 4));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&half[i]));
+                    w[i] = pk::Elem<DT>::from2(__fmul_rn(f.x, den), __fmul_rn(f.y, den));
+                }
+                row[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                row[1] = make_uint4(w[4], w[5], w[6], w[7]);
+            }
+        }
+    }
+}
+
+}  // namespace
+
+cudaError_t pk_launch_kv_move(bool write, const pk_kv_cache &kv, uint32_t dtype, const pk_heads &k, const pk_heads &v,
+                              uint64_t n_tokens, const int64_t *tok_off, const int32_t *start, uint32_t R,
+                              const uint32_t *pages, uint64_t page_stride, int32_t *status, cudaStream_t s) {
+    Move a;
+    a.pool = static_cast<uint8_t *>(kv.pool_dev);
+    a.page_bytes = pk_kv_page_bytes(kv.page_tokens, kv.kv_heads, kv.head_dim);
+    a.n_slots = kv.n_slots;
+    a.page_tokens = kv.page_tokens;
+    a.granules = kv.page_tokens / pk::kGranTokens;
+    a.heads = kv.kv_heads;
+    a.g[0] = kv.k_scale;
+    a.g[1] = kv.v_scale;
+    const pk_heads *x[2] = {&k, &v};
+    for (int j = 0; j < 2; ++j) {
+        a.x[j] = static_cast<uint16_t *>(x[j]->p);
+        a.ts[j] = x[j]->tok_stride;
+        a.hs[j] = x[j]->head_stride;
+    }
+    a.n_tokens = n_tokens;
+    a.tok_off = tok_off;
+    a.start = start;
+    a.R = R;
+    a.pages = pages;
+    a.page_stride = page_stride;
+    a.status = status;
+    const uint32_t tokens = 512 / kv.head_dim;
+    const uint64_t groups = (n_tokens + tokens - 1) / tokens;
+    // one head a warp while that leaves SMs without work, else up to 8
+    a.heads_per_warp = 1;
+    while (a.heads_per_warp < 8 && a.heads_per_warp < a.heads && groups * a.heads / a.heads_per_warp > 152 * 64)
+        a.heads_per_warp *= 2;
+    const uint64_t warps = groups * ((a.heads + a.heads_per_warp - 1) / a.heads_per_warp);
+    const uint64_t blocks = (warps + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
+    if (blocks > 0x7fffffffull) return cudaErrorInvalidValue;
+    void (*const kernels[2][2][2])(Move) = {
+        {{k_kv_move<64, PK_BF16, false>, k_kv_move<64, PK_BF16, true>},
+         {k_kv_move<64, PK_FP16, false>, k_kv_move<64, PK_FP16, true>}},
+        {{k_kv_move<128, PK_BF16, false>, k_kv_move<128, PK_BF16, true>},
+         {k_kv_move<128, PK_FP16, false>, k_kv_move<128, PK_FP16, true>}}};
+    const cudaError_t e = pk_launch(kernels[kv.head_dim == 128][dtype][write], (unsigned)blocks, kMoveThreads, s, a);
+    return e != cudaSuccess ? e : cudaGetLastError();
+}

@@ -38,6 +38,7 @@ PK_KEY_BYTES = 32
 PK_ENTRY_BYTES = 32
 PK_KEY_STRING_CHARS = 22
 PK_KEY_STRING_MAX_WIDTH = 256
+PK_BF16, PK_FP16 = 0, 1
 REGISTRY_V1 = ("model_id", "weight_precision", "weight_version", "adapter_id", "kv_format", "salt")
 
 
@@ -60,6 +61,16 @@ class pk_config(ctypes.Structure):
     _fields_ = [("chunk_tokens", ctypes.c_uint32), ("capacity_log2", ctypes.c_uint32),
                 ("max_probe", ctypes.c_uint32), ("table_dev", ctypes.c_void_p),
                 ("table_bytes", ctypes.c_size_t)]
+
+
+class pk_kv_cache(ctypes.Structure):
+    _fields_ = [("pool_dev", ctypes.c_void_p), ("n_slots", ctypes.c_uint64), ("page_tokens", ctypes.c_uint32),
+                ("kv_heads", ctypes.c_uint32), ("head_dim", ctypes.c_uint32), ("k_scale", ctypes.c_float),
+                ("v_scale", ctypes.c_float)]
+
+
+class pk_heads(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("tok_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -117,6 +128,17 @@ def lib() -> ctypes.CDLL:
             "pk_key_strings": (ctypes.c_int, [_VP, _U64, _VP, _U32, _U32, _VP, _VP]),
             "pk_table_save": (ctypes.c_int, [_VP, _VP, ctypes.c_size_t, _VP]),
             "pk_table_load": (ctypes.c_int, [_VP, _VP, ctypes.c_size_t, _VP]),
+            "pk_kv_page_bytes": (ctypes.c_size_t, [_U32, _U32, _U32]),
+            "pk_kv_write": (ctypes.c_int, [_VP, _U32, _VP, _VP, _U64, _VP, _VP, _U32, _VP, _U64, _VP, _VP]),
+            "pk_kv_read": (ctypes.c_int, [_VP, _U32, _VP, _VP, _U64, _VP, _VP, _U32, _VP, _U64, _VP, _VP]),
+            "pk_attend_prompt_scratch_bytes": (ctypes.c_size_t, [_U32]),
+            "pk_attend_prompt": (ctypes.c_int, [_U32, _VP, _VP, _VP, _VP, _VP, _U64, _U64, _VP, _VP, _U32, _U32, _U32,
+                                                _U32, ctypes.c_float, _VP, ctypes.c_size_t, _VP, _VP]),
+            "pk_attend_cache_scratch_bytes": (ctypes.c_size_t, [_VP, _U32, _U32, _U32, _U64, ctypes.c_int]),
+            "pk_attend_cache": (ctypes.c_int, [_VP, _U32, _VP, _VP, _VP, _U32, _U32, _U32, ctypes.c_float, _VP, _VP,
+                                               _U64, _VP, _VP, ctypes.c_size_t, _VP, _VP]),
+            "pk_evict_pages": (ctypes.c_int, [_VP, _VP, _VP, _U32, _U64, _U32, _U32, _U32, _U32, _VP, _VP, _VP, _VP,
+                                              _VP, _VP]),
             "pk_strerror": (ctypes.c_char_p, [ctypes.c_int]),
         }
         for name, (res, args) in sig.items():
@@ -465,6 +487,138 @@ def pk_table_save(ctx: int, dst: torch.Tensor, stream=None) -> None:
 
 def pk_table_load(ctx: int, src: torch.Tensor, stream=None) -> None:
     _check(lib().pk_table_load(ctx, _p(src), src.numel() * src.element_size(), _s(stream)), "pk_table_load")
+
+
+_KV_DTYPES = {torch.bfloat16: PK_BF16, torch.float16: PK_FP16}
+
+
+def _dtype(*tensors) -> int:
+    d = tensors[0].dtype
+    if d not in _KV_DTYPES or any(t.dtype != d for t in tensors):
+        raise PKError(PK_ERR_ARG, "16-bit tensors of one type (bfloat16 or float16)")
+    return _KV_DTYPES[d]
+
+
+def _heads(t: torch.Tensor) -> pk_heads:
+    """[tokens, heads, head_dim] (leading dimensions flattened by the caller), last dimension contiguous."""
+    if t.dim() == 3 and t.numel() == 0:
+        return pk_heads(None, 0, 0)
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise PKError(PK_ERR_ARG, "a [tokens, heads, head_dim] tensor with contiguous rows")
+    ts, hs = t.stride(0), t.stride(1)
+    return pk_heads(_p(t), ts if t.shape[0] > 1 else 0, hs if t.shape[1] > 1 else 0)
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise PKError(PK_ERR_ARG, what)
+
+
+def _i(t: torch.Tensor, dtype, n: int, what: str) -> Optional[int]:
+    """Pointer of a contiguous index array of n entries."""
+    _need(t.dtype == dtype and t.numel() == n and t.is_contiguous(), what)
+    return _p(t)
+
+
+def pk_kv_page_bytes(page_tokens: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib().pk_kv_page_bytes(page_tokens, kv_heads, head_dim))
+
+
+def _kv_move(fn: str, kv: pk_kv_cache, k, v, tok_off, start, pages, status, stream) -> None:
+    R = start.numel()
+    _need(k.shape == v.shape and k.dim() == 3 and tuple(k.shape[1:]) == (kv.kv_heads, kv.head_dim),
+          f"{fn}: k and v are [tokens, kv_heads, head_dim]")
+    _need(pages.dim() == 2 and pages.shape[0] == R, f"{fn}: pages is [R, page_stride]")
+    _check(getattr(lib(), fn)(ctypes.byref(kv), _dtype(k, v), ctypes.byref(_heads(k)), ctypes.byref(_heads(v)),
+                              k.shape[0], _i(tok_off, torch.int64, R + 1, f"{fn}: tok_off is int64[R+1]"),
+                              _i(start, torch.int32, R, f"{fn}: start is int32[R]"), R,
+                              _i(pages, torch.int32, pages.numel(), f"{fn}: pages is contiguous int32"),
+                              pages.shape[1], _p(status), _s(stream)), fn)
+
+
+def pk_kv_write(kv: pk_kv_cache, k: torch.Tensor, v: torch.Tensor, tok_off: torch.Tensor, start: torch.Tensor,
+                pages: torch.Tensor, status: torch.Tensor, stream=None) -> None:
+    """k, v: [tokens, kv_heads, head_dim] bf16 / fp16 (strided); tok_off: int64[R+1]; start: int32[R]; pages:
+    int32 [R, page_stride] holding uint32 slots."""
+    _kv_move("pk_kv_write", kv, k, v, tok_off, start, pages, status, stream)
+
+
+def pk_kv_read(kv: pk_kv_cache, k: torch.Tensor, v: torch.Tensor, tok_off: torch.Tensor, start: torch.Tensor,
+               pages: torch.Tensor, status: torch.Tensor, stream=None) -> None:
+    """k, v: outputs; the other arguments as pk_kv_write."""
+    _kv_move("pk_kv_read", kv, k, v, tok_off, start, pages, status, stream)
+
+
+def pk_attend_prompt_scratch_bytes(R: int) -> int:
+    return int(lib().pk_attend_prompt_scratch_bytes(R))
+
+
+def pk_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                     lse: Optional[torch.Tensor], q_off: torch.Tensor, k_off: torch.Tensor, scale: float,
+                     scratch: torch.Tensor, status: torch.Tensor, stream=None) -> None:
+    """q, out: [n_q, q_heads, D]; k, v: [n_k, kv_heads, D]; q_off, k_off: int64[R+1]; lse: float32 [n_q, q_heads]."""
+    R = q_off.numel() - 1
+    _need(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and q.shape == out.shape and q.shape[2] == k.shape[2],
+          "pk_attend_prompt: q, out [n_q, q_heads, D], k, v [n_k, kv_heads, D]")
+    _need(R >= 0, "pk_attend_prompt: q_off is int64[R+1]")
+    _need(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == tuple(q.shape[:2])),
+          "pk_attend_prompt: lse is contiguous float32 [n_q, q_heads]")
+    _check(lib().pk_attend_prompt(_dtype(q, k, v, out), ctypes.byref(_heads(q)), ctypes.byref(_heads(k)),
+                                  ctypes.byref(_heads(v)), ctypes.byref(_heads(out)), _p(lse), q.shape[0], k.shape[0],
+                                  _i(q_off, torch.int64, R + 1, "pk_attend_prompt: q_off is int64[R+1]"),
+                                  _i(k_off, torch.int64, R + 1, "pk_attend_prompt: k_off is int64[R+1]"), R,
+                                  q.shape[1], k.shape[1], q.shape[2], scale, _p(scratch), scratch.numel(), _p(status),
+                                  _s(stream)), "pk_attend_prompt")
+
+
+def pk_attend_cache_scratch_bytes(kv: pk_kv_cache, R: int, n_q: int, q_heads: int, page_stride: int,
+                                  weigh: bool) -> int:
+    return int(lib().pk_attend_cache_scratch_bytes(ctypes.byref(kv), R, n_q, q_heads, page_stride, int(weigh)))
+
+
+def pk_attend_cache(kv: pk_kv_cache, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor], n_q: int,
+                    kv_len: torch.Tensor, pages: torch.Tensor, scale: float, page_weight: Optional[torch.Tensor],
+                    scratch: torch.Tensor, status: torch.Tensor, stream=None) -> None:
+    """q, out: [R * n_q, q_heads, D]; lse: float32 [R * n_q, q_heads]; kv_len: int32[R]; pages: int32 and page_weight:
+    float32 [R, page_stride]."""
+    R = kv_len.numel()
+    _need(q.dim() == 3 and q.shape == out.shape and q.shape[0] == R * n_q and q.shape[2] == kv.head_dim,
+          "pk_attend_cache: q, out [R * n_q, q_heads, head_dim]")
+    _need(pages.dim() == 2 and pages.shape[0] == R, "pk_attend_cache: pages is [R, page_stride]")
+    _need(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == tuple(q.shape[:2])),
+          "pk_attend_cache: lse is contiguous float32 [R * n_q, q_heads]")
+    _need(page_weight is None or (page_weight.dtype == torch.float32 and page_weight.is_contiguous() and
+                                  page_weight.shape == pages.shape),
+          "pk_attend_cache: page_weight is contiguous float32 [R, page_stride]")
+    _check(lib().pk_attend_cache(ctypes.byref(kv), _dtype(q, out), ctypes.byref(_heads(q)), ctypes.byref(_heads(out)),
+                                 _p(lse), R, n_q, q.shape[1], scale,
+                                 _i(kv_len, torch.int32, R, "pk_attend_cache: kv_len is int32[R]"),
+                                 _i(pages, torch.int32, pages.numel(), "pk_attend_cache: pages is contiguous int32"),
+                                 pages.shape[1], _p(page_weight), _p(scratch), scratch.numel(), _p(status),
+                                 _s(stream)), "pk_attend_cache")
+
+
+def pk_evict_pages(pages: torch.Tensor, weight: torch.Tensor, kv_len: torch.Tensor, page_tokens: int, budget: int,
+                   sinks: int, recent: int, pages_out: torch.Tensor, weight_out: torch.Tensor,
+                   kv_len_out: torch.Tensor, evicted: Optional[torch.Tensor], status: torch.Tensor,
+                   stream=None) -> None:
+    """pages: int32 and weight: float32 [R, page_stride]; kv_len, kv_len_out: int32[R]; pages_out: int32 and
+    weight_out: float32 [R, budget]; evicted: int32 [R, page_stride] or None."""
+    R = kv_len.numel()
+    where = "pk_evict_pages"
+    _need(pages.dim() == 2 and pages.shape[0] == R and weight.shape == pages.shape and
+          (evicted is None or evicted.shape == pages.shape), f"{where}: pages, weight, evicted are [R, page_stride]")
+    _need(min(page_tokens, budget, sinks, recent) >= 0, f"{where}: counts are not negative")
+    _check(lib().pk_evict_pages(_i(pages, torch.int32, pages.numel(), f"{where}: pages is contiguous int32"),
+                                _i(weight, torch.float32, pages.numel(), f"{where}: weight is contiguous float32"),
+                                _i(kv_len, torch.int32, R, f"{where}: kv_len is int32[R]"), R, pages.shape[1],
+                                page_tokens, budget, sinks, recent,
+                                _i(pages_out, torch.int32, R * budget, f"{where}: pages_out is int32[R, budget]"),
+                                _i(weight_out, torch.float32, R * budget, f"{where}: weight_out is float32[R, budget]"),
+                                _i(kv_len_out, torch.int32, R, f"{where}: kv_len_out is int32[R]"),
+                                None if evicted is None else
+                                _i(evicted, torch.int32, pages.numel(), f"{where}: evicted is int32[R, page_stride]"),
+                                _p(status), _s(stream)), where)
 
 
 def pk_store_noalloc(table: torch.Tensor, capacity_log2: int, keys: torch.Tensor, slots: torch.Tensor,

@@ -9,6 +9,7 @@ per-batch buffers, all allocated with PyTorch, every step run by libpk.
 """
 from __future__ import annotations
 
+import contextlib
 from typing import Optional
 
 import numpy as np
@@ -29,6 +30,12 @@ def _dev(x, dtype, device) -> torch.Tensor:
     want = np.dtype(_NP_SIGNED[dtype])
     a = a.view(want) if a.dtype.itemsize == want.itemsize and a.dtype.kind in "ui" else a.astype(want)
     return torch.from_numpy(a).to(device=device)
+
+
+def _on(stream):
+    """Buffers made inside belong to `stream` (None: the current one), so that one freed while its kernel still runs
+    is only given out again to later work of that stream."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
 class KeyTable:
@@ -215,6 +222,98 @@ class KeyTable:
             self.store(filler[:need], np.arange(n_seed, n_seed + need, dtype=np.uint32))
         self.check("seed")
         return self.entries()
+
+
+class KVPages:
+    """What the slots of a KeyTable point at: a pool of KV pages held in 4 bits
+    (layout and format: pk.h), with its calls.  Page tables are int32
+    [R, page_stride] tensors of (uint32) slots, one row a request.
+
+        kv = KVPages(n_slots, page_tokens=kt.chunk_tokens, kv_heads=8, head_dim=128)
+        kv.write(k, v, tok_off, start, pages)          # the misses' chunks, or a decode step's tokens
+        k, v = kv.read(tok_off, start, pages, n)       # a hit's prefix, for attend_prompt
+        out, lse = kv.attend(q, kv_len, pages, scale, weight=weight)
+        pages, weight, kv_len, _ = evict_pages(pages, weight, kv_len, kv.page_tokens, budget, sinks, recent)
+
+    Bind ``kv.kv_format`` in the descriptors of what is stored here."""
+
+    def __init__(self, n_slots: int, page_tokens: int, kv_heads: int, head_dim: int, k_scale: float = 1.0,
+                 v_scale: float = 1.0, device="cuda", stream: Optional[torch.cuda.Stream] = None,
+                 pool: Optional[torch.Tensor] = None):
+        self.stream = stream
+        self.page_tokens, self.kv_heads, self.head_dim = int(page_tokens), int(kv_heads), int(head_dim)
+        nbytes = pk.pk_kv_page_bytes(page_tokens, kv_heads, head_dim) if min(page_tokens, kv_heads, head_dim) > 0 else 0
+        if nbytes == 0 or n_slots < 1:
+            raise pk.PKError(pk.PK_ERR_ARG, "KVPages")
+        if pool is None:
+            pool = torch.zeros((n_slots, nbytes), dtype=torch.uint8, device=device)
+        if pool.dtype != torch.uint8 or not pool.is_contiguous() or pool.numel() != n_slots * nbytes:
+            raise pk.PKError(pk.PK_ERR_ARG, "KVPages: pool is contiguous uint8 [n_slots, pk_kv_page_bytes]")
+        self.pool, self.device = pool, pool.device
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self.kv = pk.pk_kv_cache(pool.data_ptr(), n_slots, page_tokens, kv_heads, head_dim, k_scale, v_scale)
+
+    @property
+    def kv_format(self) -> str:
+        """The descriptor's kv_format for pages of this pool: format, block and tensor scales."""
+        return f"fp4_e2m1_b16_e4m3:k={self.kv.k_scale!r}:v={self.kv.v_scale!r}"
+
+    take_status, check = KeyTable.take_status, KeyTable.check
+
+    def write(self, k, v, tok_off, start, pages) -> None:
+        pk.pk_kv_write(self.kv, k, v, tok_off, start, pages, self.status, self.stream)
+
+    def read(self, tok_off, start, pages, n_tokens: int, dtype=torch.bfloat16):
+        """(k, v) [n_tokens, kv_heads, head_dim]; rows that belong to no request are unspecified."""
+        with _on(self.stream):
+            kv = torch.empty((2, n_tokens, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        pk.pk_kv_read(self.kv, kv[0], kv[1], tok_off, start, pages, self.status, self.stream)
+        return kv[0], kv[1]
+
+    def attend(self, q, kv_len, pages, scale: Optional[float] = None, weight: Optional[torch.Tensor] = None):
+        """q [R, n_q, q_heads, head_dim] over the pages: (out like q, lse float32 [R, n_q, q_heads]).  weight
+        (float32, like pages) gets each page's attention weight added."""
+        if q.dim() != 4:
+            raise pk.PKError(pk.PK_ERR_ARG, "KVPages.attend: q is [R, n_q, q_heads, head_dim]")
+        R, n_q, heads, D = q.shape
+        nbytes = pk.pk_attend_cache_scratch_bytes(self.kv, R, n_q, heads, pages.shape[-1], weight is not None)
+        with _on(self.stream):
+            out = torch.empty((R, n_q, heads, D), dtype=q.dtype, device=q.device)
+            lse = torch.empty((R, n_q, heads), dtype=torch.float32, device=q.device)
+            scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+        pk.pk_attend_cache(self.kv, q.flatten(0, 1), out.view(R * n_q, heads, D), lse.view(R * n_q, heads), n_q,
+                           kv_len, pages, D ** -0.5 if scale is None else scale, weight, scratch, self.status,
+                           self.stream)
+        return out, lse
+
+
+def attend_prompt(q, k, v, q_off, k_off, scale: Optional[float] = None, status: Optional[torch.Tensor] = None,
+                  stream=None):
+    """Causal attention over packed prompts (pk_attend_prompt): (out like q, lse float32 [n_q, q_heads]).  Without
+    ``status`` a device-reported error leaves the outputs unspecified and is not reported."""
+    nbytes = pk.pk_attend_prompt_scratch_bytes(max(q_off.numel() - 1, 0))
+    with _on(stream):
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    pk.pk_attend_prompt(q, k, v, out, lse, q_off, k_off, q.shape[-1] ** -0.5 if scale is None else scale, scratch,
+                        status, stream)
+    return out, lse
+
+
+def evict_pages(pages, weight, kv_len, page_tokens: int, budget: int, sinks: int, recent: int,
+                status: Optional[torch.Tensor] = None, stream=None):
+    """Cut each request to `budget` pages by accumulated attention weight (pk_evict_pages): (pages [R, budget],
+    weight [R, budget], kv_len [R], evicted slots like pages), unused places PK_NO_SLOT (-1) and 0."""
+    R = pages.shape[0]
+    with _on(stream):
+        pages_out = torch.empty((R, max(budget, 0)), dtype=torch.int32, device=pages.device)
+        weight_out = torch.empty((R, max(budget, 0)), dtype=torch.float32, device=pages.device)
+        kv_len_out = torch.empty(R, dtype=torch.int32, device=pages.device)
+        evicted = torch.empty(pages.shape, dtype=torch.int32, device=pages.device)
+    pk.pk_evict_pages(pages, weight, kv_len, page_tokens, budget, sinks, recent, pages_out, weight_out, kv_len_out,
+                      evicted, status, stream)
+    return pages_out, weight_out, kv_len_out, evicted
 
 
 def u32(t: torch.Tensor) -> np.ndarray:
