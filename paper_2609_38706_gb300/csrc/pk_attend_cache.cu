@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_cache(const Args a) {
 #pragma unroll 1
     for (uint32_t k = 0; k < mine; ++k) {
         const uint32_t st = k % kStages;
-        if (!pk::mbar_wait(bar_s + 8 * st, (k / kStages) & 1)) {
+        if (!pk::mbar_wait_warp(bar_s + 8 * st, (k / kStages) & 1)) {
             gave_up = true;
             for (uint32_t i = k + 1; i < min(k + kStages, mine); ++i)  // no copy of its own stays in flight
                 pk::mbar_wait(bar_s + 8 * (i % kStages), (i / kStages) & 1);

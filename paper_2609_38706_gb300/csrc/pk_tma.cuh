@@ -30,15 +30,27 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 
-// Waits for the phase of `parity` to complete.  A try suspends for a while in
-// hardware, so the limit is seconds; false: it gave up.
-constexpr uint32_t kMbarTries = 1u << 22;
+// Waits for the phase of `parity` to complete; false: it gave up, after
+// seconds (a try suspends for a while in hardware before it answers).
+constexpr uint64_t kMbarLimitNs = 4000000000ull;
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
+    uint64_t t0, t1;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+    do {
+        for (int i = 0; i < 64; ++i)
+            if (mbar_try(bar, parity)) return true;
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
+    } while (t1 - t0 < kMbarLimitNs);
+    return false;
+}
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
     if (mbar_try(bar, parity)) return true;
-#pragma unroll 1
-    for (uint32_t i = 0; i < kMbarTries; ++i)
-        if (mbar_try(bar, parity)) return true;
-    return false;
+    return mbar_wait_slow(bar, parity);
+}
+
+// The same by a whole warp, which gets one answer.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity));
 }
 
 // Untiled copy global -> shared memory of this CTA; both addresses 16-byte
@@ -47,6 +59,15 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
     asm volatile(
         "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
         "l"(src), "r"(bytes), "r"(bar)
+        : "memory");
+}
+
+// Tiled copy of a 3-D tensor map's box; x times the element size a multiple of 16 bytes.
+__device__ __forceinline__ void tile_load3(uint32_t dst, const void *map, int x, int y, int z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+            dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
         : "memory");
 }
 

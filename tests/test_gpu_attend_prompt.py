@@ -86,6 +86,23 @@ def test_long_prompt_sampled_rows():
     check(q, k, v, lq, lk, out, lse, "bf16", 128 ** -0.5, rows=np.array([0, 1, 63, 64, 127, 128, 1000, 2431, 2498, 2499]))
 
 
+@pytest.mark.parametrize("H,G,D,dtype", [(8, 4, 128, "bf16"), (4, 3, 64, "fp16")])
+def test_many_more_blocks_than_the_gpu_holds(H, G, D, dtype):
+    """Several rounds of blocks on every SM, calls back to back: the same bits each time, sampled rows against the
+    reference."""
+    from paper_2609_38706_gb300 import service
+    lq = [512, 341, 470, 375, 256, 314, 374, 452]
+    lk = [n + 300 * (i % 3) for i, n in enumerate(lq)]
+    q, k, v = inputs(lq, lk, H, G, D, dtype, 19)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    args = q.cuda(), k.cuda(), v.cuda(), dev(offs(lq)), dev(offs(lk))
+    res = [service.attend_prompt(*args, status=status) for _ in range(6)]
+    assert int(status.item()) == 0
+    for out, lse in res[1:]:
+        assert torch.equal(out, res[0][0]) and torch.equal(lse, res[0][1])
+    check(q, k, v, lq, lk, *res[0], dtype, D ** -0.5, rows=np.array([0, 31, 64, 200, 255, 256, 300, 511]))
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
 def test_scales_and_peaked_rows(scale):
     """A scale of 0 weighs all keys alike; a large one is decided by the maximum, which moves as keys come."""
