@@ -4,8 +4,6 @@
 #include <cuda_runtime.h>
 #include <float.h>
 
-#include <type_traits>
-
 #include "pk_device.cuh"
 #include "pk_internal.h"
 #include "pk_kv.cuh"
@@ -14,7 +12,7 @@
 
 namespace {
 
-constexpr int kTileRows = 256;  // (query token, head of the group) rows of a CTA: two tiles of 128
+constexpr int kRows = 128;      // (query token, head of the group) rows of a tile; an item is two tiles
 constexpr int kKeys = 128;      // keys of a tile
 constexpr int kThreads = 384;
 constexpr float kTop = 15.0f;   // p stays below 2^kTop (half: 2^16)
@@ -22,22 +20,22 @@ constexpr float kBase = 8.0f;   // the largest p when the reference moves: 2^kBa
 constexpr int kPlanThreads = 1024;
 
 struct Args {
-    const uint16_t *q;
     uint16_t *out;
-    int64_t q_ts, q_hs, o_ts, o_hs;
+    int64_t o_ts, o_hs;
     float *lse;
     const int64_t *q_off, *k_off;
-    uint64_t *tile_off;  // [R + 1]: tiles of the requests before r
+    uint64_t *tile_off;  // [R + 1]: items of one KV head in the requests before r
     uint32_t R, q_heads, kv_heads, group;
+    uint32_t tile_tokens, tile_heads, chunks;  // of a tile; tiles that it takes for a group's heads
     float scale2;  // scale * log2 e
     int32_t *status;
 };
 
-// tile_off: how many row tiles the requests before each one have; all zero
-// where an offset is out of order or range.
+// tile_off: how many items of one KV head the requests before each one have;
+// all zero where an offset is out of order or range.
 __global__ void __launch_bounds__(kPlanThreads)
-k_prompt_tiles(const int64_t *q_off, const int64_t *k_off, uint32_t R, uint64_t n_q, uint64_t n_k, uint32_t group,
-               uint32_t tile_rows, uint64_t *tile_off, int32_t *status) {
+k_prompt_tiles(const int64_t *q_off, const int64_t *k_off, uint32_t R, uint64_t n_q, uint64_t n_k,
+               uint32_t item_tokens, uint32_t chunks, uint64_t *tile_off, int32_t *status) {
     __shared__ uint64_t warp_sum[32];
     __shared__ uint32_t bad;
     const uint32_t tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
@@ -55,7 +53,7 @@ k_prompt_tiles(const int64_t *q_off, const int64_t *k_off, uint32_t R, uint64_t 
             if (a < 0 || b < a || (uint64_t)b > n_q || e < 0 || f < e || (uint64_t)f > n_k)
                 bad = 1;
             else
-                n = ((uint64_t)(b - a) * group + tile_rows - 1) / tile_rows;
+                n = ((uint64_t)(b - a) + item_tokens - 1) / item_tokens * chunks;
         }
         uint64_t scan = n;
 #pragma unroll
@@ -87,8 +85,7 @@ __device__ __forceinline__ float ex2(float x) {
     return r;
 }
 
-// Shared memory of a CTA, from a 1024-byte boundary: Q (two tiles), the ring
-// of K and V tiles, then the small things.
+// Shared memory of a CTA, from a 1024-byte boundary: Q (two tiles), then the ring of K and V tiles.
 template <int D>
 struct Layout {
     static constexpr uint32_t kTile = 128 * D * 2;  // 128 rows; blocks of [128][64] values, 16 KB each
@@ -99,20 +96,84 @@ struct Layout {
 
 struct Small {
     uint64_t full[8], empty[8];    // ring stages: tile ready (loaded, and an edge tile's V made finite); no longer read
+    uint64_t q_full[2], q_empty[2];
     uint64_t s_full[2], p_ready[2], o_done[2];
-    uint64_t q_ready, edge_v[4];   // Q in shared memory; an edge tile's V loaded, by edge tile
+    uint64_t edge_v[4];            // an edge tile's V loaded, by edge tile
     uint32_t tmem, abort;
-    int32_t bad_row[128];          // first key of an edge tile whose V is not finite, by dimension
+    uint32_t epilogues[8];         // by softmax warp: items whose outputs it has written
+    uint32_t any_bad[2][2];        // by item parity and half of the dimensions: bad_row holds something
+    int32_t bad_row[2][128];       // first key of an edge tile whose V is not finite, by dimension
 };
 
-using Yes = std::true_type;
-using No = std::false_type;
+// One item: 2 tiles of `tokens` query tokens times `heads` heads of one group.
+struct Item {
+    int32_t q0, k0, lq, lk, tok0, chunk, head;
+    int32_t n_tiles[2], first_last[2], n_all, first_edge;
+};
+
+__device__ __forceinline__ bool find_item(const Args &a, const uint64_t *tile_off, const int64_t *q_off,
+                                          const int64_t *k_off, uint64_t index, Item &it) {
+    const uint64_t tile = index / a.kv_heads;
+    if (tile >= __ldcg(tile_off + a.R)) return false;
+    const uint32_t r = pk::warp_find_request(reinterpret_cast<const int64_t *>(tile_off), a.R, (int64_t)tile);
+    it.head = (int32_t)(index % a.kv_heads);
+    it.q0 = (int32_t)__ldcg(q_off + r);
+    it.k0 = (int32_t)__ldcg(k_off + r);
+    it.lq = (int32_t)__ldcg(q_off + r + 1) - it.q0;
+    it.lk = (int32_t)__ldcg(k_off + r + 1) - it.k0;
+    // the last queries first: they have the most keys
+    const uint64_t x = __ldcg(tile_off + r + 1) - 1 - tile;
+    it.chunk = (int32_t)(x % a.chunks);
+    it.tok0 = (int32_t)(x / a.chunks) * 2 * (int32_t)a.tile_tokens;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int32_t t0 = it.tok0 + t * (int32_t)a.tile_tokens, t1 = min(t0 + (int32_t)a.tile_tokens, it.lq);
+        const int32_t keys = t1 > t0 ? t1 + it.lk - it.lq : 0;  // that some query of the tile sees
+        it.n_tiles[t] = keys > 0 ? (keys + kKeys - 1) / kKeys : 0;
+        it.first_last[t] = t0 + it.lk - it.lq;                  // last key of the tile's first query
+    }
+    it.n_all = max(it.n_tiles[0], it.n_tiles[1]);
+    // From this key tile on, some query does not see some key: p = 0 there, which must not meet an infinity or NaN
+    // of V.  At most three tiles, as an item has at most 256 queries.
+    it.first_edge = it.first_last[0] + 1 >= kKeys ? (it.first_last[0] + 1) / kKeys : 0;
+    return true;
+}
 
 constexpr uint32_t kWarpLoad = 8, kWarpMma = 9, kWarpClean = 10;  // warps 0-7: softmax
 
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// One CTA an SM walks over items.  Warp roles: one loads Q, K and V by TMA,
+// one issues the matrix products, two look after V at the causal edge, and
+// two warpgroups of four turn scores into weights, a thread a row, for one of
+// the item's two tiles each: while one tile's scores are weighed the other's
+// products run.  TMEM: scores of the tiles (128 columns each; the weights, two
+// to a column, take the place of scores that have been read), then their outputs
+// (D columns each).  Every counter of a barrier's use runs on over the items, so
+// the next item's loads and first products run under this one's end.
 template <int D, uint32_t DT>
 __global__ void __launch_bounds__(kThreads, 1)
-k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                const __grid_constant__ CUtensorMap map_v) {
     using L = Layout<D>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ Small sm;
@@ -126,331 +187,388 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_k, const _
             pk::mbar_init(pk::smem_addr(&sm.empty[i]), 1);
         }
         for (int t = 0; t < 2; ++t) {
+            pk::mbar_init(pk::smem_addr(&sm.q_full[t]), 1);
+            pk::mbar_init(pk::smem_addr(&sm.q_empty[t]), 1);
             pk::mbar_init(pk::smem_addr(&sm.s_full[t]), 1);
             pk::mbar_init(pk::smem_addr(&sm.p_ready[t]), 4);
             pk::mbar_init(pk::smem_addr(&sm.o_done[t]), 1);
         }
-        pk::mbar_init(pk::smem_addr(&sm.q_ready), 8);
         for (int i = 0; i < 4; ++i) pk::mbar_init(pk::smem_addr(&sm.edge_v[i]), 1);
         pk::mbar_fence_init();
         sm.abort = 0;
+        for (int i = 0; i < 8; ++i) sm.epilogues[i] = 0;
     }
-    if (tid < 128) sm.bad_row[tid] = 0x7fffffff;
-    const uint64_t *tile_off = a.tile_off;
-    const int64_t *q_off = a.q_off, *k_off = a.k_off;
-    const uint16_t *qp = a.q;
-    pk::pdl_wait(tile_off, q_off, k_off, qp);
-    pk::pdl_launch_dependents();
-    const uint32_t head = blockIdx.x % a.kv_heads;
-    const uint64_t tile = blockIdx.x / a.kv_heads;
-    if (tile >= __ldcg(tile_off + a.R)) return;  // uniform; nothing allocated yet
     if (warp == kWarpMma) pk::tmem_alloc(pk::smem_addr(&sm.tmem), 512);
-    const uint32_t r = pk::warp_find_request(reinterpret_cast<const int64_t *>(tile_off), a.R, (int64_t)tile);
-    const int64_t q0 = __ldcg(q_off + r), k0 = __ldcg(k_off + r);
-    const int32_t lq = (int32_t)(__ldcg(q_off + r + 1) - q0), lk = (int32_t)(__ldcg(k_off + r + 1) - k0);
-    // the last rows first: they have the most keys
-    const int64_t row0 = (int64_t)(__ldcg(tile_off + r + 1) - 1 - tile) * kTileRows;
-    const int64_t n_rows = (int64_t)lq * a.group;
-    // per tile of 128 rows: how many key tiles its rows see, and the first key that some row does not
-    int32_t n_tiles[2], first_last[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const int64_t r0 = row0 + 128 * t, r1 = min(r0 + 128, n_rows);  // [r0, r1)
-        const int32_t keys = r1 > r0 ? (int32_t)((r1 - 1) / a.group) + lk - lq + 1 : 0;
-        n_tiles[t] = keys > 0 ? (keys + kKeys - 1) / kKeys : 0;
-        first_last[t] = (int32_t)(r0 / a.group) + lk - lq;
-    }
-    const int32_t n_all = max(n_tiles[0], n_tiles[1]);
-    // From this key tile on, some row does not see some key: p = 0 there, which must not meet an infinity or NaN
-    // of V.  At most three tiles: 256 rows hold at most 256 queries.
-    const int32_t first_edge = first_last[0] + 1 >= kKeys ? (first_last[0] + 1) / kKeys : 0;
     pk::tmem_fence_before();
     __syncthreads();
     pk::tmem_fence_after();
     const uint32_t tmem = sm.tmem;
-    const uint32_t tmem_s[2] = {tmem, tmem + 128}, tmem_o[2] = {tmem + 256, tmem + 256 + D};
+    const uint64_t *tile_off = a.tile_off;
+    const int64_t *q_off = a.q_off, *k_off = a.k_off;
+    pk::pdl_wait(tile_off, q_off, k_off);
+    pk::pdl_launch_dependents();
+
+    volatile uint32_t *abort = &sm.abort;
     auto give_up = [&]() {
-        if (lane == 0) {
-            *reinterpret_cast<volatile uint32_t *>(&sm.abort) = 1;
-            pk::set_status(a.status, PK_ERR_TIMEOUT);
-        }
+        *abort = 1;
+        pk::set_status(a.status, PK_ERR_TIMEOUT);
     };
 
-    float inv = 0.0f;
-    int32_t last = -1;
+    Item it;
+    uint64_t index = blockIdx.x;
+    bool more = find_item(a, tile_off, q_off, k_off, index, it);
     if (warp == kWarpLoad) {
-        if (lane == 0) {
-            pk::fence_proxy_async();
-            uint32_t n = 0;
-            for (int32_t j = 0; j < n_all; ++j) {
-                bool ok = true;
+        uint32_t n = 0, edges = 0, nq[2] = {0, 0};  // ring stages, edge tiles and Q tiles loaded so far
+        bool ok = true;
+        pk::fence_proxy_async();
+        while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
+            if (lane == 0) {
+                const uint32_t q_bytes = a.tile_tokens * a.tile_heads * 128 * (D / 64);
+                for (int32_t j = 0; ok && j < it.n_all; ++j) {
 #pragma unroll
-                for (int kv = 0; kv < 2; ++kv, ++n) {
-                    const uint32_t st = n % L::kStages;
-                    const bool dirty = kv && j >= first_edge;
-                    const uint32_t bar = pk::smem_addr(dirty ? &sm.edge_v[(j - first_edge) & 3] : &sm.full[st]);
-                    ok = ok && (n < L::kStages || pk::mbar_wait(pk::smem_addr(&sm.empty[st]), (n / L::kStages + 1) & 1));
-                    if (!ok) break;
-                    // only now: the barrier's earlier phase is over, as the stage was read
-                    if (!dirty) pk::mbar_arrive(bar);
-                    pk::mbar_expect(bar, L::kTile);
+                    for (int kv = 0; kv < 2; ++kv) {
+                        const uint32_t st = n % L::kStages;
+                        const bool dirty = kv && j >= it.first_edge;
+                        const uint32_t bar = pk::smem_addr(dirty ? &sm.edge_v[edges & 3] : &sm.full[st]);
+                        ok = ok && (n < L::kStages ||
+                                    pk::mbar_wait(pk::smem_addr(&sm.empty[st]), (n / L::kStages + 1) & 1));
+                        if (!ok) break;
+                        // only now: the barrier's earlier phase is over, as the stage was read
+                        if (!dirty) pk::mbar_arrive(bar);
+                        pk::mbar_expect(bar, L::kTile);
 #pragma unroll
-                    for (int b = 0; b < D / 64; ++b)
-                        pk::tile_load3(smem + L::kRing + st * L::kTile + b * 16384, kv ? &map_v : &map_k, b * 64,
-                                       (int)head, (int)(k0 + (int64_t)j * kKeys), bar);
-                }
-                if (!ok) {
-                    give_up();
-                    break;
+                        for (int b = 0; b < D / 64; ++b)
+                            pk::tile_load3(smem + L::kRing + st * L::kTile + b * 16384, kv ? &map_v : &map_k, b * 64,
+                                           it.head, it.k0 + j * kKeys, bar);
+                        ++n;
+                        edges += dirty;
+                    }
+                    if (j == 0) {  // Q behind the first tiles, which need not wait for the last item's Q
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            if (!ok || it.n_tiles[t] == 0) continue;
+                            ok = nq[t] == 0 || pk::mbar_wait(pk::smem_addr(&sm.q_empty[t]), (nq[t] - 1) & 1);
+                            if (!ok) break;
+                            const uint32_t bar = pk::smem_addr(&sm.q_full[t]);
+                            pk::mbar_expect(bar, q_bytes);
+#pragma unroll
+                            for (int b = 0; b < D / 64; ++b)
+                                pk::tile_load3(smem + t * L::kTile + b * 16384, &map_q, b * 64,
+                                               it.head * (int)a.group + it.chunk * (int)a.tile_heads,
+                                               it.q0 + it.tok0 + t * (int)a.tile_tokens, bar);
+                            ++nq[t];
+                        }
+                    }
                 }
             }
+            ok = __all_sync(0xffffffffu, ok);
+            index += gridDim.x;
+            more = find_item(a, tile_off, q_off, k_off, index, it);
+        }
+        if (lane == 0) {
+            if (!ok) give_up();
             // no copy of its own stays in flight
             for (uint32_t i = n > L::kStages ? n - L::kStages : 0; i < n; ++i)
                 pk::mbar_wait(pk::smem_addr(&sm.full[i % L::kStages]), (i / L::kStages) & 1);
+            for (int t = 0; t < 2; ++t)
+                if (nq[t]) pk::mbar_wait(pk::smem_addr(&sm.q_full[t]), (nq[t] - 1) & 1);
         }
         __syncwarp();
     } else if (warp == kWarpMma) {
-        if (lane == 0) {
-            constexpr uint32_t kQk = pk::mma_idesc(DT == PK_BF16, 128, 128, false);
-            constexpr uint32_t kPv = pk::mma_idesc(DT == PK_BF16, 128, D, true);
-            bool ok = n_all == 0 || pk::mbar_wait(pk::smem_addr(&sm.q_ready), 0);
-            auto stage_of = [&](uint32_t n) { return smem + L::kRing + (n % L::kStages) * L::kTile; };
-            auto wait_full = [&](uint32_t n) {
-                return pk::mbar_wait(pk::smem_addr(&sm.full[n % L::kStages]), (n / L::kStages) & 1);
-            };
-            auto qk = [&](int t, uint32_t n) {
-                const uint32_t q = smem + t * L::kTile, k = stage_of(n);
+        const uint32_t qk_kind = pk::mma_idesc(DT == PK_BF16, 128, 128, false) |
+                                 (a.scale2 < 0.0f ? 1u << 13 : 0u);  // a negative scale negates Q
+        constexpr uint32_t kPv = pk::mma_idesc(DT == PK_BF16, 128, D, true);
+        uint32_t base = 0, ni[2] = {0, 0}, nq[2] = {0, 0};  // ring stages, key tiles and Q tiles used so far
+        bool ok = true;
+        auto stage_of = [&](uint32_t n) { return smem + L::kRing + (n % L::kStages) * L::kTile; };
+        auto wait_full = [&](uint32_t n) {
+            return pk::mbar_wait(pk::smem_addr(&sm.full[n % L::kStages]), (n / L::kStages) & 1);
+        };
+        auto qk = [&](int t, uint32_t n, bool last) {
+            const uint32_t q = smem + t * L::kTile, k = stage_of(n);
 #pragma unroll
-                for (int s = 0; s < D / 16; ++s)
-                    pk::mma_ss(tmem_s[t], pk::mma_desc(q + (s / 4) * 16384 + (s % 4) * 32, 16, 1024),
-                               pk::mma_desc(k + (s / 4) * 16384 + (s % 4) * 32, 16, 1024), kQk, s > 0);
-                pk::mma_commit(pk::smem_addr(&sm.s_full[t]));
-            };
-            if (ok && n_all) {
-                ok = wait_full(0);
-                pk::tmem_fence_after();
-                if (ok) {
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-                        if (n_tiles[t] > 0) qk(t, 0);
-                    pk::mma_commit(pk::smem_addr(&sm.empty[0]));
-                }
-            }
-            for (int32_t j = 0; ok && j < n_all; ++j) {
-                const uint32_t nv = 2 * j + 1, nk = 2 * j + 2;
-                ok = wait_full(nv);
+            for (int s = 0; s < D / 16; ++s)
+                pk::mma_ss(tmem + 128 * t, pk::mma_desc(q + (s / 4) * 16384 + (s % 4) * 32, 16, 1024),
+                           pk::mma_desc(k + (s / 4) * 16384 + (s % 4) * 32, 16, 1024), qk_kind, s > 0);
+            pk::mma_commit(pk::smem_addr(&sm.s_full[t]));
+            if (last) pk::mma_commit(pk::smem_addr(&sm.q_empty[t]));
+        };
+        while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
+            if (lane == 0 && it.n_all) {
+                ok = wait_full(base);
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    if (!ok || j >= n_tiles[t]) continue;
-                    ok = pk::mbar_wait(pk::smem_addr(&sm.p_ready[t]), j & 1);
+                    if (!ok || it.n_tiles[t] == 0) continue;
+                    ok = pk::mbar_wait(pk::smem_addr(&sm.q_full[t]), nq[t] & 1);
                     if (!ok) break;
                     pk::tmem_fence_after();
-                    const uint32_t v = stage_of(nv);
+                    ++nq[t];
+                    qk(t, base, it.n_tiles[t] == 1);
+                }
+                if (ok) pk::mma_commit(pk::smem_addr(&sm.empty[base % L::kStages]));
+            }
+            // the next item is looked up while the first scores are weighed
+            Item next;
+            index += gridDim.x;
+            more = find_item(a, tile_off, q_off, k_off, index, next);
+            if (lane == 0) {
+                for (int32_t j = 0; ok && j < it.n_all; ++j) {
+                    const uint32_t nv = base + 2 * j + 1, nk = nv + 1;
+                    ok = wait_full(nv);
 #pragma unroll
-                    for (int s = 0; s < 8; ++s)
-                        pk::mma_ts(tmem_o[t], tmem_s[t] + 8 * s, pk::mma_desc(v + s * 2048, 16384, 1024), kPv,
-                                   j > 0 || s > 0);
-                    pk::mma_commit(pk::smem_addr(&sm.o_done[t]));
-                    if (j + 1 < n_tiles[t]) {
-                        ok = wait_full(nk);
+                    for (int t = 0; t < 2; ++t) {
+                        if (!ok || j >= it.n_tiles[t]) continue;
+                        ok = pk::mbar_wait(pk::smem_addr(&sm.p_ready[t]), ni[t] & 1);
                         if (!ok) break;
-                        qk(t, nk);
+                        ++ni[t];
+                        pk::tmem_fence_after();
+                        const uint32_t v = stage_of(nv);
+#pragma unroll
+                        for (int s = 0; s < 8; ++s)
+                            pk::mma_ts(tmem + 256 + D * t, tmem + 128 * t + 64 * (s / 4) + 8 * (s % 4),
+                                       pk::mma_desc(v + s * 2048, 16384, 1024), kPv, j > 0 || s > 0);
+                        pk::mma_commit(pk::smem_addr(&sm.o_done[t]));
+                        if (j + 1 < it.n_tiles[t]) {
+                            ok = wait_full(nk);
+                            if (!ok) break;
+                            pk::tmem_fence_after();
+                            qk(t, nk, j + 2 == it.n_tiles[t]);
+                        }
+                    }
+                    if (ok) {
+                        pk::mma_commit(pk::smem_addr(&sm.empty[nv % L::kStages]));
+                        if (j + 1 < it.n_all) pk::mma_commit(pk::smem_addr(&sm.empty[nk % L::kStages]));
                     }
                 }
-                if (ok) {
-                    pk::mma_commit(pk::smem_addr(&sm.empty[nv % L::kStages]));
-                    if (j + 1 < n_all) pk::mma_commit(pk::smem_addr(&sm.empty[nk % L::kStages]));
-                }
+                base += 2 * it.n_all;
             }
-            if (!ok) give_up();
+            ok = __all_sync(0xffffffffu, ok);
+            it = next;
         }
-        __syncwarp();
+        if (!ok && lane == 0) give_up();
     } else if (warp >= kWarpClean) {
         // V of the tiles at the causal edge and at the request's end: rows past its last key become 0, and so do
-        // infinities and NaN, which are noted for the queries that do attend them
+        // infinities and NaN, which are noted for the queries that do attend them.  Each of the two warps has its
+        // own half of the dimensions.
+        constexpr uint32_t kChunks = D / 16;  // 16-byte chunks of a row that a warp looks at
+        const uint32_t half = warp - kWarpClean;
+        uint32_t base = 0, edges = 0, items = 0;
         bool ok = true;
-        for (int32_t j = first_edge; ok && j < n_all; ++j) {
-            const uint32_t st = (2 * j + 1) % L::kStages;
-            ok = pk::mbar_wait_warp(pk::smem_addr(&sm.edge_v[(j - first_edge) & 3]), 0);  // used once
-            if (!ok) break;
-            uint8_t *v = smem_p + L::kRing + st * L::kTile;
-            for (uint32_t x = tid - 32 * kWarpClean; x < L::kTile / 16; x += 64) {
-                const uint32_t row = x / 8 % 128, chunk = (x ^ row) & 7;
-                uint4 *at = reinterpret_cast<uint4 *>(v + x * 16);
-                uint4 u = *at;
-                const int32_t key = j * kKeys + (int32_t)row;
-                constexpr uint32_t kInf = pk::Elem<DT>::kInfBits;
-                if (key >= lk) {
-                    if (u.x | u.y | u.z | u.w) *at = make_uint4(0, 0, 0, 0);
-                    continue;
-                }
-                uint32_t w[4] = {u.x, u.y, u.z, u.w};
-                bool found = false;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t d = x / 1024 * 64 + chunk * 8 + 2 * i;
-                    if ((w[i] & 0x7fffu) >= kInf) {
-                        atomicMin(&sm.bad_row[d], key);
-                        w[i] &= 0xffff0000u;
-                        found = true;
-                    }
-                    if ((w[i] >> 16 & 0x7fffu) >= kInf) {
-                        atomicMin(&sm.bad_row[d + 1], key);
-                        w[i] &= 0xffffu;
-                        found = true;
+        while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
+            int32_t *bad_row = sm.bad_row[items & 1];
+            if (it.first_edge < it.n_all) {
+                // the item before the last one shared these notes: its outputs must have been written
+                uint64_t t0 = 0, t1 = 0;
+                while (items >= 2) {
+                    uint32_t done;
+                    asm volatile("ld.acquire.cta.shared.u32 %0, [%1];" : "=r"(done) : "r"(pk::smem_addr(&sm.epilogues[lane & 7])) : "memory");
+                    if (__all_sync(0xffffffffu, (int32_t)(done - (items - 1)) >= 0)) break;
+                    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
+                    t1 = __shfl_sync(0xffffffffu, t1, 0);
+                    if (t0 == 0) t0 = t1;
+                    if (t1 - t0 > pk::kMbarLimitNs) {
+                        ok = false;
+                        break;
                     }
                 }
-                if (found) *at = make_uint4(w[0], w[1], w[2], w[3]);
+                for (uint32_t d = lane; d < D / 2; d += 32) bad_row[half * (D / 2) + d] = 0x7fffffff;
+                if (lane == 0) sm.any_bad[items & 1][half] = 0;
+                __syncwarp();
             }
-            pk::fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.full[st]));
+            for (int32_t j = it.first_edge; ok && j < it.n_all; ++j, ++edges) {
+                const uint32_t st = (base + 2 * j + 1) % L::kStages;
+                ok = pk::mbar_wait_warp(pk::smem_addr(&sm.edge_v[edges & 3]), (edges >> 2) & 1);
+                if (!ok) break;
+                uint8_t *v = smem_p + L::kRing + st * L::kTile + (D == 128 ? half * 16384 : 0);
+                for (uint32_t x = lane; x < 128 * kChunks; x += 32) {
+                    const uint32_t row = x / kChunks, chunk = x % kChunks + (D == 128 ? 0 : half * kChunks);
+                    uint4 *at = reinterpret_cast<uint4 *>(v + row * 128 + ((chunk ^ (row & 7)) << 4));
+                    const uint4 u = *at;
+                    const int32_t key = j * kKeys + (int32_t)row;
+                    constexpr uint32_t kInf = pk::Elem<DT>::kInfBits;
+                    if (key >= it.lk) {
+                        *at = make_uint4(0, 0, 0, 0);
+                        continue;
+                    }
+                    uint32_t w[4] = {u.x, u.y, u.z, u.w}, m = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+                    if ((m & 0xffffu) < kInf && m >> 16 < kInf) continue;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t d = (D == 128 ? half * 64 : 0) + chunk * 8 + 2 * i;
+                        if ((w[i] & 0x7fffu) >= kInf) {
+                            atomicMin(&bad_row[d], key);
+                            w[i] &= 0xffff0000u;
+                        }
+                        if ((w[i] >> 16 & 0x7fffu) >= kInf) {
+                            atomicMin(&bad_row[d + 1], key);
+                            w[i] &= 0xffffu;
+                        }
+                    }
+                    *at = make_uint4(w[0], w[1], w[2], w[3]);
+                    sm.any_bad[items & 1][half] = 1;
+                }
+                pk::fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.full[st]));
+            }
+            base += 2 * it.n_all;
+            ++items;
+            index += gridDim.x;
+            more = find_item(a, tile_off, q_off, k_off, index, it);
         }
-        if (!ok) give_up();
+        if (!ok && lane == 0) give_up();
     } else {
         const uint32_t t = warp >> 2;
-        const int64_t row = row0 + tid;  // warps 0-3: tile 0, 4-7: tile 1; thread = row = TMEM lane
-        const uint32_t lane_base = (warp & 3) * 32 << 16;
-        const uint32_t flip = a.scale2 < 0.0f ? 0x80008000u : 0u;  // a negative scale goes into Q
-        const float scale2 = fabsf(a.scale2);
-        // Q: 8 lanes bring 128 bytes of a row; rows past the end are 0
-        if (n_tiles[t] > 0) {
-#pragma unroll 4
-            for (int i = 0; i < 32 * (D / 64) / 4; ++i) {
-                const uint32_t b = i / 8, rr = (warp & 3) * 32 + i % 8 * 4 + lane / 8, chunk = lane & 7;
-                const int64_t qr = row0 + 128 * t + rr;
-                uint4 u = make_uint4(0, 0, 0, 0);
-                if (qr < n_rows) {
-                    const int64_t i2 = qr / a.group;
-                    u = __ldcg(reinterpret_cast<const uint4 *>(qp + (q0 + i2) * a.q_ts +
-                                                               (int64_t)(head * a.group + (uint32_t)(qr - i2 * a.group)) * a.q_hs +
-                                                               b * 64 + chunk * 8));
-                    u.x ^= flip, u.y ^= flip, u.z ^= flip, u.w ^= flip;
-                }
-                *reinterpret_cast<uint4 *>(smem_p + t * L::kTile + b * 16384 + rr * 128 + ((chunk ^ (rr & 7)) << 4)) = u;
-            }
-            pk::fence_proxy_async();
-        }
-        __syncwarp();
-        if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.q_ready));
-
-        const bool on = row < n_rows;
-        const int64_t qi = on ? row / a.group : 0;
-        last = on ? (int32_t)qi + lk - lq : -1;
-        float ref = -FLT_MAX, sum = 0.0f;
+        const int32_t row = tid & 127;  // TMEM lane
+        const int32_t row_tok = row / (int32_t)a.tile_heads, row_head = row % (int32_t)a.tile_heads;
+        const uint32_t ts = tmem + 128 * t + ((warp & 3) * 32 << 16), to = tmem + 256 + D * t + ((warp & 3) * 32 << 16);
+        // a scale of 0 would make a masked -infinity NaN; the smallest normal one gives the same weights
+        const float scale2 = fmaxf(fabsf(a.scale2), FLT_MIN);
+        const uint64_t scale22 = pack2(scale2, scale2);
+        uint32_t ni = 0, items = 0;  // key tiles weighed so far
         bool ok = true;
-        const uint32_t ts = tmem_s[t] + lane_base, to = tmem_o[t] + lane_base;
+        while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
+            const int32_t n_tiles = t ? it.n_tiles[1] : it.n_tiles[0];
+            const int32_t first_last = t ? it.first_last[1] : it.first_last[0];
+            const int32_t tok = it.tok0 + (int32_t)(t * a.tile_tokens) + row_tok;
+            const int32_t gh = it.chunk * (int32_t)a.tile_heads + row_head;
+            const bool on = row_tok < (int32_t)a.tile_tokens && tok < it.lq && gh < (int32_t)a.group;
+            const int32_t last = on ? tok + it.lk - it.lq : -1;
+            const int64_t q_row = it.q0 + tok;
+            const uint32_t qh = it.head * a.group + gh;
+            const bool notes = it.first_edge < it.n_all;
+            index += gridDim.x;
+            more = find_item(a, tile_off, q_off, k_off, index, it);  // the next one
+            float ref = -FLT_MAX;
+            uint64_t sum2[2] = {0, 0};
 #pragma unroll 1
-        for (int32_t j = 0; j < n_tiles[t]; ++j) {
-            ok = pk::mbar_wait_warp(pk::smem_addr(&sm.s_full[t]), j & 1);
-            if (!ok) break;
-            pk::tmem_fence_after();
-            const bool edge = j * kKeys + kKeys - 1 > first_last[t];
-            const int32_t see = last - j * kKeys;  // columns up to here
-            float m = -INFINITY;
-            uint32_t x[32];
-            auto find_max = [&](auto masked) {
+            for (int32_t j = 0; j < n_tiles; ++j, ++ni) {
+                ok = pk::mbar_wait_warp(pk::smem_addr(&sm.s_full[t]), ni & 1);
+                if (!ok) break;
+                pk::tmem_fence_after();
+                // two chunks of 32 scores in registers: keys 0-63 pass once for the maximum and are read again after
+                // keys 64-127 have become weights
+                uint32_t x[2][32];
+                const bool edge = j * kKeys + kKeys - 1 > first_last;
+                const int32_t see = last - j * kKeys;  // columns up to here
+                auto mask = [&](uint32_t(&y)[32], int c) {
+                    if (edge) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    pk::tmem_load32(ts + 32 * c, x);
-                    pk::tmem_wait_load(x);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (!decltype(masked)::value || 32 * c + i <= see) m = fmaxf(m, __uint_as_float(x[i]));
-                }
-            };
-            edge ? find_max(Yes{}) : find_max(No{});
-            m *= scale2;
-            const bool over = m > ref + kTop;
-            if (__any_sync(0xffffffffu, over)) {
-                const float next = over ? ceilf(m) - kBase : ref;
-                const float f = ex2(ref - next);
-                ref = next;
-                sum *= f;
-                if (j > 0) {
-                    ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (j - 1) & 1);
-                    if (!ok) break;
-                    pk::tmem_fence_after();
-#pragma unroll
-                    for (int c = 0; c < D / 32; ++c) {
-                        pk::tmem_load32(to + 32 * c, x);
-                        pk::tmem_wait_load(x);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
-                        pk::tmem_store32(to + 32 * c, x);
+                        for (int i = 0; i < 32; ++i)
+                            if (32 * c + i > see) y[i] = 0xff800000u;
                     }
+                };
+                float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    pk::tmem_load32(ts + 64 * h, x[0]);
+                    pk::tmem_load32(ts + 64 * h + 32, x[1]);
+                    pk::tmem_wait_load(x[0]);
+                    pk::tmem_wait_load(x[1]);
+                    mask(x[0], 2 * h);
+                    mask(x[1], 2 * h + 1);
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) m4[i & 3] = fmaxf(m4[i & 3], __uint_as_float(x[i / 32][i % 32]));
                 }
-            }
-            float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            auto weigh = [&](auto masked) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t p[16];
-                    pk::tmem_load32(ts + 32 * c, x);
-                    pk::tmem_wait_load(x);
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        float p0 = ex2(fmaf(__uint_as_float(x[i]), scale2, -ref));
-                        float p1 = ex2(fmaf(__uint_as_float(x[i + 1]), scale2, -ref));
-                        if (decltype(masked)::value) {
-                            if (32 * c + i > see) p0 = 0.0f;
-                            if (32 * c + i + 1 > see) p1 = 0.0f;
-                        }
-                        part[i / 2 & 3] += p0 + p1;
-                        p[i / 2] = pk::Elem<DT>::from2(p0, p1);
-                    }
-                    pk::tmem_store16(ts + 16 * c, p);  // over scores that both passes have read
-                }
-            };
-            edge ? weigh(Yes{}) : weigh(No{});
-            sum += (part[0] + part[1]) + (part[2] + part[3]);
-            pk::tmem_wait_store();
-            pk::tmem_fence_before();
-            __syncwarp();
-            if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.p_ready[t]));
-        }
-        if (ok && n_tiles[t] > 0) ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (n_tiles[t] - 1) & 1);
-        if (!ok) give_up();
-        inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        if (on && a.lse)
-            a.lse[(q0 + qi) * a.q_heads + head * a.group + (uint32_t)(row - qi * a.group)] =
-                sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
-    }
-    __syncthreads();  // bad_row is final
-    pk::tmem_fence_after();
-    if (warp < 8 && sm.abort == 0) {
-        const uint32_t t = warp >> 2;
-        const int64_t row = row0 + tid;
-        const bool on = row < n_rows;
-        const int64_t qi = on ? row / a.group : 0;
-        uint16_t *dst = a.out + (q0 + qi) * a.o_ts + (int64_t)(head * a.group + (uint32_t)(on ? row - qi * a.group : 0)) * a.o_hs;
-        const bool any = n_tiles[t] > 0;  // else O was never written
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-            uint32_t x[32];
-            __syncwarp();
-            if (any) {
-                pk::tmem_load32(tmem_o[t] + ((warp & 3) * 32 << 16) + 32 * c, x);
-                pk::tmem_wait_load(x);
-            }
-            if (on) {
-                uint32_t w[16];
-#pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                    float y[2];
+                const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale2;
+                const bool over = m > ref + kTop;
+                if (__any_sync(0xffffffffu, over)) {
+                    const float next = over ? ceilf(m) - kBase : ref;
+                    const float f = ex2(ref - next);
+                    ref = next;
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        y[e] = any && inv != 0.0f ? __uint_as_float(x[i + e]) * inv : 0.0f;
-                        if (sm.bad_row[32 * c + i + e] <= last) y[e] = __int_as_float(0x7fffffff);
+                        const float2 y = unpack2(sum2[e]);
+                        sum2[e] = pack2(y.x * f, y.y * f);
                     }
-                    w[i / 2] = pk::Elem<DT>::from2(y[0], y[1]);
-                }
+                    if (j > 0) {
+                        ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
+                        if (!ok) break;
+                        pk::tmem_fence_after();
+#pragma unroll 1
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t y[32];
+                            pk::tmem_load32(to + 32 * c, y);
+                            pk::tmem_wait_load(y);
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    reinterpret_cast<uint4 *>(dst + 32 * c)[i] =
-                        make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                            for (int i = 0; i < 32; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * f);
+                            pk::tmem_store32(to + 32 * c, y);
+                        }
+                    }
+                }
+                const uint64_t ref2 = pack2(-ref, -ref);
+                // the weights of a chunk lie in the first half of its scores' columns' pair: keys 0-63 in columns 0-31,
+                // keys 64-127 in columns 64-95
+                auto weigh = [&](uint32_t(&y)[32], int c) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        float2 z = unpack2(fma2(pack2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), scale22, ref2));
+                        z.x = ex2(z.x);
+                        z.y = ex2(z.y);
+                        sum2[i / 2 & 1] = add2(sum2[i / 2 & 1], pack2(z.x, z.y));
+                        p[i / 2] = pk::Elem<DT>::from2(z.x, z.y);
+                    }
+                    pk::tmem_store16(ts + 64 * (c >> 1) + 16 * (c & 1), p);
+                };
+                weigh(x[0], 2);
+                pk::tmem_load32(ts, x[0]);
+                weigh(x[1], 3);
+                pk::tmem_load32(ts + 32, x[1]);
+                pk::tmem_wait_load(x[0]);
+                pk::tmem_wait_load(x[1]);
+                mask(x[0], 0);
+                mask(x[1], 1);
+                weigh(x[0], 0);
+                weigh(x[1], 1);
+                pk::tmem_wait_store();
+                pk::tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.p_ready[t]));
             }
+            if (ok && n_tiles > 0) ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
+            if (!ok) break;
+            const float2 s0 = unpack2(sum2[0]), s1 = unpack2(sum2[1]);
+            const float sum = (s0.x + s1.x) + (s0.y + s1.y);
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            if (on && a.lse)
+                a.lse[q_row * a.q_heads + qh] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+            uint16_t *dst = a.out + q_row * a.o_ts + (int64_t)qh * a.o_hs;
+            const bool bad = notes && (sm.any_bad[items & 1][0] | sm.any_bad[items & 1][1]) != 0;
+            pk::tmem_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t y[32];
+                __syncwarp();
+                if (n_tiles > 0) {  // else O was never written
+                    pk::tmem_load32(to + 32 * c, y);
+                    pk::tmem_wait_load(y);
+                }
+                if (on) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        float z = n_tiles > 0 && inv != 0.0f ? __uint_as_float(y[i]) * inv : 0.0f;
+                        if (bad && sm.bad_row[items & 1][32 * c + i] <= last) z = __int_as_float(0x7fffffff);
+                        y[i] = __float_as_uint(z);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            w[e] = pk::Elem<DT>::from2(__uint_as_float(y[8 * i + 2 * e]), __uint_as_float(y[8 * i + 2 * e + 1]));
+                        reinterpret_cast<uint4 *>(dst + 32 * c)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+            }
+            __syncwarp();
+            ++items;
+            if (lane == 0)
+                asm volatile("st.release.cta.shared.u32 [%0], %1;" ::"r"(pk::smem_addr(&sm.epilogues[warp])), "r"(items) : "memory");
         }
+        if (!ok && lane == 0) give_up();
     }
     pk::tmem_fence_before();
     __syncthreads();
@@ -474,15 +592,16 @@ EncodeTiled encoder() {
     return fn;
 }
 
-// [tokens][heads][D] as a 3-D map whose box is 128 tokens of one head and 64 dimensions, in the 128-byte swizzle;
-// tokens past the end read as 0.
-cudaError_t map_of(CUtensorMap *map, const pk_heads &h, uint64_t n, uint32_t heads, uint32_t D, uint32_t dtype) {
+// [tokens][heads][D] as a 3-D map whose box is box_tokens tokens of box_heads heads and 64 dimensions, in the 128-byte
+// swizzle; what lies past the end reads as 0.
+cudaError_t map_of(CUtensorMap *map, const pk_heads &h, uint64_t n, uint32_t heads, uint32_t D, uint32_t dtype,
+                   uint32_t box_tokens, uint32_t box_heads) {
     const EncodeTiled enc = encoder();
     if (!enc) return cudaErrorNotSupported;
     const cuuint64_t dims[3] = {D, heads, n};
     // a dimension of one entry has no stride
     const cuuint64_t strides[2] = {heads > 1 ? (cuuint64_t)h.head_stride * 2 : D * 2u, n > 1 ? (cuuint64_t)h.tok_stride * 2 : D * 2u};
-    const cuuint32_t box[3] = {64, 1, kKeys}, unit[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {64, box_heads, box_tokens}, unit[3] = {1, 1, 1};
     const CUresult e = enc(map, dtype == PK_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
                            h.p, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -490,10 +609,11 @@ cudaError_t map_of(CUtensorMap *map, const pk_heads &h, uint64_t n, uint32_t hea
 }
 
 template <int D, uint32_t DT>
-cudaError_t launch(const Args &a, unsigned grid, const CUtensorMap &mk, const CUtensorMap &mv, cudaStream_t s) {
+cudaError_t launch(const Args &a, unsigned grid, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv,
+                   cudaStream_t s) {
     constexpr size_t smem = Layout<D>::kBytes + 1024;
     const cudaError_t e = cudaFuncSetAttribute(k_attend_prompt<D, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    return e != cudaSuccess ? e : pk_launch_smem(k_attend_prompt<D, DT>, grid, kThreads, smem, s, a, mk, mv);
+    return e != cudaSuccess ? e : pk_launch_smem(k_attend_prompt<D, DT>, grid, kThreads, smem, s, a, mq, mk, mv);
 }
 
 }  // namespace
@@ -503,9 +623,7 @@ cudaError_t pk_launch_attend_prompt(uint32_t dtype, const pk_heads &q, const pk_
                                     const int64_t *k_off, uint32_t R, uint32_t q_heads, uint32_t kv_heads,
                                     uint32_t head_dim, float scale, void *scratch, int32_t *status, cudaStream_t s) {
     Args a;
-    a.q = static_cast<const uint16_t *>(q.p);
     a.out = static_cast<uint16_t *>(out.p);
-    a.q_ts = q.tok_stride, a.q_hs = q.head_stride;
     a.o_ts = out.tok_stride, a.o_hs = out.head_stride;
     a.lse = lse;
     a.q_off = q_off;
@@ -515,25 +633,32 @@ cudaError_t pk_launch_attend_prompt(uint32_t dtype, const pk_heads &q, const pk_
     a.q_heads = q_heads;
     a.kv_heads = kv_heads;
     a.group = q_heads / kv_heads;
+    // a tile: all heads of the group for as many tokens as fit 128 rows, or 128 heads of one token
+    a.tile_heads = a.group < kRows ? a.group : kRows;
+    a.tile_tokens = kRows / a.tile_heads;
+    a.chunks = (a.group + a.tile_heads - 1) / a.tile_heads;
     a.scale2 = (float)((double)scale * 1.4426950408889634);
     a.status = status;
-    cudaError_t e = pk_launch(k_prompt_tiles, 1, kPlanThreads, s, q_off, k_off, R, n_q, n_k, a.group,
-                              (uint32_t)kTileRows, a.tile_off, status);
+    int device = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     if (e != cudaSuccess) return e;
-    // every request rounds its rows up to whole tiles: at most one more tile each
-    const uint64_t tiles = (n_q * a.group + kTileRows - 1) / kTileRows + R;
-    if (tiles * kv_heads > 0x7fffffffull) return cudaErrorInvalidValue;
-    const unsigned grid = (unsigned)(tiles * kv_heads);
-    CUtensorMap mk, mv;
-    if (n_k == 0) {  // no key tile is ever loaded: any valid map will do
-        mk = mv = CUtensorMap{};
-    } else if ((e = map_of(&mk, k, n_k, kv_heads, head_dim, dtype)) != cudaSuccess ||
-               (e = map_of(&mv, v, n_k, kv_heads, head_dim, dtype)) != cudaSuccess) {
+    CUtensorMap mq, mk{}, mv{};
+    // without keys no key tile is ever loaded, and the maps are never read
+    if ((e = map_of(&mq, q, n_q, q_heads, head_dim, dtype, a.tile_tokens, a.tile_heads)) != cudaSuccess ||
+        (n_k && (e = map_of(&mk, k, n_k, kv_heads, head_dim, dtype, kKeys, 1)) != cudaSuccess) ||
+        (n_k && (e = map_of(&mv, v, n_k, kv_heads, head_dim, dtype, kKeys, 1)) != cudaSuccess))
         return e;
-    }
+    const uint32_t item_tokens = 2 * a.tile_tokens;
+    e = pk_launch(k_prompt_tiles, 1, kPlanThreads, s, q_off, k_off, R, n_q, n_k, item_tokens, a.chunks, a.tile_off,
+                  status);
+    if (e != cudaSuccess) return e;
+    // every request rounds its tokens up to whole items: at most one more each
+    const uint64_t items = (n_q / item_tokens + R) * a.chunks * kv_heads;
+    const unsigned grid = items < (uint64_t)sms ? (unsigned)items : (unsigned)sms;
     if (head_dim == 128)
-        e = dtype == PK_BF16 ? launch<128, PK_BF16>(a, grid, mk, mv, s) : launch<128, PK_FP16>(a, grid, mk, mv, s);
+        e = dtype == PK_BF16 ? launch<128, PK_BF16>(a, grid, mq, mk, mv, s) : launch<128, PK_FP16>(a, grid, mq, mk, mv, s);
     else
-        e = dtype == PK_BF16 ? launch<64, PK_BF16>(a, grid, mk, mv, s) : launch<64, PK_FP16>(a, grid, mk, mv, s);
+        e = dtype == PK_BF16 ? launch<64, PK_BF16>(a, grid, mq, mk, mv, s) : launch<64, PK_FP16>(a, grid, mq, mk, mv, s);
     return e != cudaSuccess ? e : cudaGetLastError();
 }

@@ -33,10 +33,12 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 // Waits for the phase of `parity` to complete; false: it gave up, after
 // seconds (a try suspends for a while in hardware before it answers).
 constexpr uint64_t kMbarLimitNs = 4000000000ull;
-static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity) {
     uint64_t t0, t1;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
+#pragma unroll 1
     do {
+#pragma unroll 1
         for (int i = 0; i < 64; ++i)
             if (mbar_try(bar, parity)) return true;
         asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));

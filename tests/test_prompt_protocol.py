@@ -1,5 +1,5 @@
-"""CPU model of the prompt-attention kernel's barriers: loader, matrix, cleaning and softmax warps of one CTA as
-coroutines under random interleavings, with the copies and the matrix pipe as asynchronous agents.  Checks that no
+"""CPU model of the prompt-attention kernel's barriers: loader, matrix, cleaning and softmax warps of one CTA, which
+walks over several items, as coroutines under random interleavings, with the copies and the matrix pipe as asynchronous agents.  Checks that no
 barrier gets an arrival its phase does not expect, that every product reads what it should, that nothing is overwritten
 while it is read, that all roles end, and that nothing asynchronous is left when they have."""
 import random
@@ -32,128 +32,175 @@ class Bar:
 
 
 class Cta:
-    def __init__(self, n_tiles, first_edge, stages, rng, rescale):
-        self.nt, self.n_all, self.fe, self.S, self.rng = n_tiles, max(n_tiles), first_edge, stages, rng
+    def __init__(self, items, stages, rng):
+        """items: (key tiles of tile 0, of tile 1, first edge tile) each."""
+        self.items, self.S, self.rng = items, stages, rng
         self.full = [Bar(2) for _ in range(stages)]
         self.empty = [Bar(1) for _ in range(stages)]
-        self.s_full, self.p_ready, self.o_done = ([Bar(c) for _ in range(2)] for c in (1, 4, 1))
-        self.q_ready, self.edge_v = Bar(8), [Bar(1) for _ in range(4)]
-        self.stage = [None] * stages      # content: ("K"|"V", j, clean)
+        self.q_full, self.q_empty, self.s_full, self.o_done = ([Bar(1) for _ in range(2)] for _ in range(4))
+        self.p_ready, self.edge_v = [Bar(4) for _ in range(2)], [Bar(1) for _ in range(4)]
+        self.stage, self.q = [None] * stages, [None, None]
         self.copies, self.pipe = [], []   # in flight; the pipe runs in order
-        self.sp = [None, None]            # S / P columns of a tile: ("S", j) or ("P", j)
-        self.o = [-1, -1]                 # last PV accumulated
-        self.rescale = rescale
+        self.sp, self.o = [None, None], [None, None]
+        self.epilogues, self.notes = [0] * 8, [None, None]
+        self.stored = [set(), set()]
         self.speed = rng.choice((0.5, 0.02)), rng.choice((0.5, 0.05))
+        self.rescale = rng.choice((0.0, 0.3))
 
     def loader(self):
-        n = 0
-        for j in range(self.n_all):
-            for kv in (0, 1):
-                st = n % self.S
-                dirty = kv and j >= self.fe
-                bar = self.edge_v[j - self.fe] if dirty else self.full[st]
-                if n >= self.S:
-                    while not self.empty[st].done((n // self.S + 1) & 1):
+        n, edges, nq = 0, 0, [0, 0]
+        for x, (n0, n1, fe) in enumerate(self.items):
+            for j in range(max(n0, n1)):
+                for kv in (0, 1):
+                    st = n % self.S
+                    dirty = kv and j >= fe
+                    bar = self.edge_v[edges & 3] if dirty else self.full[st]
+                    while n >= self.S and not self.empty[st].done((n // self.S + 1) & 1):
                         yield
-                yield
-                if not dirty:
-                    bar.arrive()
-                yield
-                bar.arrive(tx=1)
-                self.stage[st] = None
-                self.copies.append((st, ("KV"[kv], j, not dirty), bar))
-                n += 1
+                    if not dirty:
+                        bar.arrive()
+                    yield
+                    bar.arrive(tx=1)
+                    self.stage[st] = None
+                    self.copies.append((self.stage, st, ("KV"[kv], x, j, not dirty), bar))
+                    n, edges = n + 1, edges + dirty
+                    yield
+                for t in (0, 1) if j == 0 else ():
+                    if not (n0, n1)[t]:
+                        continue
+                    while nq[t] and not self.q_empty[t].done((nq[t] - 1) & 1):
+                        yield
+                    self.q_full[t].arrive(tx=1)
+                    self.q[t] = None
+                    self.copies.append((self.q, t, x, self.q_full[t]))
+                    nq[t] += 1
+                    yield
         for i in range(max(0, n - self.S), n):
             while not self.full[i % self.S].done((i // self.S) & 1):
                 yield
+        for t in (0, 1):
+            while nq[t] and not self.q_full[t].done((nq[t] - 1) & 1):
+                yield
 
     def mma(self):
+        base, ni, nq = 0, [0, 0], [0, 0]
+
         def wait_full(n):
             while not self.full[n % self.S].done((n // self.S) & 1):
                 yield
-        if not self.n_all:
-            return
-        while not self.q_ready.done(0):
-            yield
-        yield from wait_full(0)
-        for t in (0, 1):
-            if self.nt[t]:
-                self.pipe += [("QK", t, 0, 0), ("commit", self.s_full[t])]
-        self.pipe.append(("commit", self.empty[0]))
-        for j in range(self.n_all):
-            nv, nk = 2 * j + 1, 2 * j + 2
-            yield from wait_full(nv)
-            for t in (0, 1):
-                if j >= self.nt[t]:
-                    continue
-                while not self.p_ready[t].done(j & 1):
-                    yield
-                self.pipe += [("PV", t, j, nv % self.S), ("commit", self.o_done[t])]
-                yield
-                if j + 1 < self.nt[t]:
-                    yield from wait_full(nk)
-                    self.pipe += [("QK", t, j + 1, nk % self.S), ("commit", self.s_full[t])]
-                yield
-            self.pipe.append(("commit", self.empty[nv % self.S]))
-            if j + 1 < self.n_all:
-                self.pipe.append(("commit", self.empty[nk % self.S]))
 
-    def cleaner(self):
-        for j in range(self.fe, self.n_all):
-            st = (2 * j + 1) % self.S
-            while not self.edge_v[j - self.fe].done(0):
-                yield
-            yield
-            assert self.stage[st] and self.stage[st][:2] == ("V", j)
-            self.stage[st] = ("V", j, True)
-            yield
-            self.full[st].arrive()
+        def qk(x, t, j, n, last):
+            self.pipe += [("QK", t, x, j, n % self.S), ("commit", self.s_full[t])]
+            if last:
+                self.pipe.append(("commit", self.q_empty[t]))
 
-    def softmax(self, t, warp, shared):
-        self.q_ready.arrive()
-        for j in range(self.nt[t]):
-            while not self.s_full[t].done(j & 1):
-                yield
-            assert self.sp[t] == ("S", j)
+        for x, (n0, n1, _) in enumerate(self.items):
+            nt, n_all = (n0, n1), max(n0, n1)
+            if n_all:
+                yield from wait_full(base)
+                for t in (0, 1):
+                    if nt[t]:
+                        while not self.q_full[t].done(nq[t] & 1):
+                            yield
+                        nq[t] += 1
+                        qk(x, t, 0, base, nt[t] == 1)
+                self.pipe.append(("commit", self.empty[base % self.S]))
             yield
-            if j and self.rescale(t, j):
-                while not self.o_done[t].done((j - 1) & 1):
+            for j in range(n_all):
+                nv, nk = base + 2 * j + 1, base + 2 * j + 2
+                yield from wait_full(nv)
+                for t in (0, 1):
+                    if j >= nt[t]:
+                        continue
+                    while not self.p_ready[t].done(ni[t] & 1):
+                        yield
+                    ni[t] += 1
+                    self.pipe += [("PV", t, x, j, nv % self.S), ("commit", self.o_done[t])]
                     yield
-                assert self.o[t] == j - 1
+                    if j + 1 < nt[t]:
+                        yield from wait_full(nk)
+                        qk(x, t, j + 1, nk, j + 2 == nt[t])
+                    yield
+                self.pipe.append(("commit", self.empty[nv % self.S]))
+                if j + 1 < n_all:
+                    self.pipe.append(("commit", self.empty[nk % self.S]))
+            base += 2 * n_all
+
+    def cleaner(self, half):
+        base, edges = 0, 0
+        for x, (n0, n1, fe) in enumerate(self.items):
+            n_all = max(n0, n1)
+            if fe < n_all:
+                while x >= 2 and min(self.epilogues) < x - 1:
+                    yield
+                self.notes[x & 1] = x
                 yield
-            shared[t].add((warp, j))
-            if len([1 for w, i in shared[t] if i == j]) == 4:
-                self.sp[t] = ("P", j)
-            self.p_ready[t].arrive()
-        if self.nt[t]:
-            while not self.o_done[t].done((self.nt[t] - 1) & 1):
+            for j in range(fe, n_all):
+                st = (base + 2 * j + 1) % self.S
+                while not self.edge_v[edges & 3].done((edges >> 2) & 1):
+                    yield
+                edges += 1
                 yield
-            assert self.o[t] == self.nt[t] - 1
+                assert self.stage[st] and self.stage[st][:3] == ("V", x, j)
+                self.stage[st] = ("V", x, j, self.stage[st][3] + 1 if self.stage[st][3] else 1)
+                yield
+                self.full[st].arrive()
+            base += 2 * n_all
+
+    def softmax(self, t, warp):
+        ni = 0
+        for x, item in enumerate(self.items):
+            n_all, fe = max(item[:2]), item[2]
+            for j in range(item[t]):
+                while not self.s_full[t].done(ni & 1):
+                    yield
+                assert self.sp[t] == ("S", x, j)
+                yield
+                if j and self.rng.random() < self.rescale:
+                    while not self.o_done[t].done((ni - 1) & 1):
+                        yield
+                    assert self.o[t] == (x, j - 1)
+                    yield
+                self.stored[t].add((warp, x, j))
+                if all((w, x, j) in self.stored[t] for w in range(4)):
+                    self.sp[t] = ("P", x, j)
+                self.p_ready[t].arrive()
+                ni += 1
+            if item[t]:
+                while not self.o_done[t].done((ni - 1) & 1):
+                    yield
+                for _ in range(self.rng.choice((1, 1, 40))):
+                    assert self.o[t] == (x, item[t] - 1), "O overwritten before it was read"
+                    assert fe >= n_all or self.notes[x & 1] == x
+                    yield
+            self.epilogues[4 * t + warp] = x + 1
 
     def agents(self):
         if self.copies and self.rng.random() < self.speed[0]:
-            st, content, bar = self.copies.pop(self.rng.randrange(len(self.copies)))
-            self.stage[st] = content
+            where, at, content, bar = self.copies.pop(self.rng.randrange(len(self.copies)))
+            where[at] = content
             bar.landed(1)
         if self.pipe and self.rng.random() < self.speed[1]:
             op = self.pipe.pop(0)
             if op[0] == "commit":
                 op[1].arrive()
-            elif op[0] == "QK":
-                assert self.stage[op[3]] == ("K", op[2], True)
-                assert self.sp[op[1]] == (None if op[2] == 0 else ("P", op[2] - 1))
-                self.sp[op[1]] = ("S", op[2])
+                return
+            kind, t, x, j, st = op
+            if kind == "QK":
+                assert self.stage[st] == ("K", x, j, True) and self.q[t] == x
+                assert self.sp[t] is None or self.sp[t][0] == "P"
+                self.sp[t] = ("S", x, j)
             else:
-                assert self.stage[op[3]] == ("V", op[2], True)
-                assert self.sp[op[1]] == ("P", op[2]) and self.o[op[1]] == op[2] - 1
-                self.o[op[1]] = op[2]
+                v = self.stage[st]
+                assert v and v[:3] == ("V", x, j) and v[3] == (2 if j >= self.items[x][2] else True)
+                assert self.sp[t] == ("P", x, j) and (j == 0 or self.o[t] == (x, j - 1))
+                self.o[t] = (x, j)
 
     def run(self):
-        shared = [set(), set()]
-        roles = [self.loader(), self.mma(), self.cleaner(), self.cleaner()]
-        roles += [self.softmax(t, w, shared) for t in (0, 1) for w in range(4)]
+        roles = [self.loader(), self.mma(), self.cleaner(0), self.cleaner(1)]
+        roles += [self.softmax(t, w) for t in (0, 1) for w in range(4)]
         slow = {id(x): self.rng.choice((1.0, 0.3, 0.03)) for x in roles}
-        for _ in range(200000):
+        for _ in range(2000000):
             if not roles:
                 break
             x = self.rng.choice(roles)
@@ -171,8 +218,10 @@ class Cta:
 @pytest.mark.parametrize("stages", [4, 8])
 def test_every_interleaving_tried_is_sound(stages):
     rng = random.Random(7)
-    for _ in range(400):
-        n1 = rng.randint(0, 9)
-        n0 = rng.randint(max(0, n1 - 2), n1) if n1 else rng.randint(0, 9)
-        fe = max(0, max(n0, n1) - rng.randint(0, 3))
-        Cta((n0, n1), fe, stages, rng, lambda t, j: rng.random() < 0.3).run()
+    for _ in range(150):
+        items = []
+        for _ in range(rng.randint(1, 7)):
+            n1 = rng.choice((0, 0, 1, 1, 2, 5))
+            n0 = rng.randint(max(0, n1 - 2), n1) if n1 else rng.choice((0, 1, 1, 2, 4))
+            items.append((n0, n1, max(0, max(n0, n1) - rng.randint(0, 3))))
+        Cta(items, stages, rng).run()
