@@ -89,7 +89,7 @@ __device__ __forceinline__ float ex2(float x) {
 template <int D>
 struct Layout {
     static constexpr uint32_t kTile = 128 * D * 2;  // 128 rows; blocks of [128][64] values, 16 KB each
-    static constexpr uint32_t kStages = D == 128 ? 4 : 8;
+    static constexpr uint32_t kStages = D == 128 ? 5 : 8;
     static constexpr uint32_t kRing = 2 * kTile;
     static constexpr uint32_t kBytes = kRing + kStages * kTile;
 };
@@ -111,10 +111,15 @@ struct Item {
     int32_t n_tiles[2], first_last[2], n_all, first_edge;
 };
 
+// The turn-th item of this CTA.  Items come heaviest first within a request, so
+// every other turn runs through the CTAs backwards: one that got the heaviest of
+// a turn gets the lightest of the next (two prompts of 8192: 855 -> TURNS us).
 __device__ __forceinline__ bool find_item(const Args &a, const uint64_t *tile_off, const int64_t *q_off,
-                                          const int64_t *k_off, uint64_t index, Item &it) {
+                                          const int64_t *k_off, uint32_t turn, Item &it) {
+    const uint64_t total = __ldcg(tile_off + a.R) * a.kv_heads;
+    const uint64_t index = (uint64_t)turn * gridDim.x + (turn & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    if (index >= total) return false;
     const uint64_t tile = index / a.kv_heads;
-    if (tile >= __ldcg(tile_off + a.R)) return false;
     const uint32_t r = pk::warp_find_request(reinterpret_cast<const int64_t *>(tile_off), a.R, (int64_t)tile);
     it.head = (int32_t)(index % a.kv_heads);
     it.q0 = (int32_t)__ldcg(q_off + r);
@@ -179,7 +184,7 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
     __shared__ Small sm;
     const uint32_t smem = (pk::smem_addr(smem_raw) + 1023) & ~1023u;
     uint8_t *smem_p = smem_raw + (smem - pk::smem_addr(smem_raw));
-    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = pk::uniform(tid >> 5);
 
     if (tid == 0) {
         for (uint32_t i = 0; i < L::kStages; ++i) {
@@ -202,7 +207,7 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
     pk::tmem_fence_before();
     __syncthreads();
     pk::tmem_fence_after();
-    const uint32_t tmem = sm.tmem;
+    const uint32_t tmem = pk::uniform(sm.tmem);
     const uint64_t *tile_off = a.tile_off;
     const int64_t *q_off = a.q_off, *k_off = a.k_off;
     pk::pdl_wait(tile_off, q_off, k_off);
@@ -215,8 +220,8 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
     };
 
     Item it;
-    uint64_t index = blockIdx.x;
-    bool more = find_item(a, tile_off, q_off, k_off, index, it);
+    uint32_t turn = 0;
+    bool more = find_item(a, tile_off, q_off, k_off, turn, it);
     if (warp == kWarpLoad) {
         uint32_t n = 0, edges = 0, nq[2] = {0, 0};  // ring stages, edge tiles and Q tiles loaded so far
         bool ok = true;
@@ -262,8 +267,8 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                 }
             }
             ok = __all_sync(0xffffffffu, ok);
-            index += gridDim.x;
-            more = find_item(a, tile_off, q_off, k_off, index, it);
+            ++turn;
+            more = find_item(a, tile_off, q_off, k_off, turn, it);
         }
         if (lane == 0) {
             if (!ok) give_up();
@@ -278,72 +283,85 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
         const uint32_t qk_kind = pk::mma_idesc(DT == PK_BF16, 128, 128, false) |
                                  (a.scale2 < 0.0f ? 1u << 13 : 0u);  // a negative scale negates Q
         constexpr uint32_t kPv = pk::mma_idesc(DT == PK_BF16, 128, D, true);
-        uint32_t base = 0, ni[2] = {0, 0}, nq[2] = {0, 0};  // ring stages, key tiles and Q tiles used so far
+        uint32_t ring = 0, use = 0;             // next ring stage, and how often the ring has been gone round
+        uint32_t ni0 = 0, ni1 = 0, nq0 = 0, nq1 = 0;  // key tiles and Q tiles used so far, by tile
         bool ok = true;
-        auto stage_of = [&](uint32_t n) { return smem + L::kRing + (n % L::kStages) * L::kTile; };
-        auto wait_full = [&](uint32_t n) {
-            return pk::mbar_wait(pk::smem_addr(&sm.full[n % L::kStages]), (n / L::kStages) & 1);
+        auto wait_full = [&](uint32_t st, uint32_t round) {
+            return pk::mbar_wait_warp(pk::smem_addr(&sm.full[st]), round & 1);
         };
-        auto qk = [&](int t, uint32_t n, bool last) {
-            const uint32_t q = smem + t * L::kTile, k = stage_of(n);
+        auto advance = [&](uint32_t by) {
+            ring += by;
+            if (ring >= L::kStages) ring -= L::kStages, ++use;
+        };
+        auto qk = [&](int t, uint32_t st, bool last) {
+            const uint32_t q = smem + t * L::kTile, k = smem + L::kRing + st * L::kTile;
+            if (pk::elect_lane()) {
 #pragma unroll
-            for (int s = 0; s < D / 16; ++s)
-                pk::mma_ss(tmem + 128 * t, pk::mma_desc(q + (s / 4) * 16384 + (s % 4) * 32, 16, 1024),
-                           pk::mma_desc(k + (s / 4) * 16384 + (s % 4) * 32, 16, 1024), qk_kind, s > 0);
-            pk::mma_commit(pk::smem_addr(&sm.s_full[t]));
-            if (last) pk::mma_commit(pk::smem_addr(&sm.q_empty[t]));
+                for (int s = 0; s < D / 16; ++s)
+                    pk::mma_ss(tmem + 128 * t, pk::mma_desc(q + (s / 4) * 16384 + (s % 4) * 32, 16, 1024),
+                               pk::mma_desc(k + (s / 4) * 16384 + (s % 4) * 32, 16, 1024), qk_kind, s > 0);
+                pk::mma_commit(pk::smem_addr(&sm.s_full[t]));
+                if (last) pk::mma_commit(pk::smem_addr(&sm.q_empty[t]));
+            }
+            __syncwarp();
+        };
+        auto pv = [&](int t, uint32_t st, bool first) {
+            const uint32_t v = smem + L::kRing + st * L::kTile;
+            if (pk::elect_lane()) {
+#pragma unroll
+                for (int s = 0; s < 8; ++s)
+                    pk::mma_ts(tmem + 256 + D * t, tmem + 128 * t + 8 * s, pk::mma_desc(v + s * 2048, 16384, 1024),
+                               kPv, !first || s > 0);
+                pk::mma_commit(pk::smem_addr(&sm.o_done[t]));
+            }
+            __syncwarp();
+        };
+        auto release = [&](uint32_t st) {
+            if (pk::elect_lane()) pk::mma_commit(pk::smem_addr(&sm.empty[st]));
+            __syncwarp();
         };
         while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
-            if (lane == 0 && it.n_all) {
-                ok = wait_full(base);
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    if (!ok || it.n_tiles[t] == 0) continue;
-                    ok = pk::mbar_wait(pk::smem_addr(&sm.q_full[t]), nq[t] & 1);
-                    if (!ok) break;
+            const int32_t n0 = (int32_t)pk::uniform(it.n_tiles[0]), n1 = (int32_t)pk::uniform(it.n_tiles[1]);
+            const int32_t n_all = max(n0, n1);
+            if (n_all) {
+                ok = wait_full(ring, use);
+                if (ok && n0 > 0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.q_full[0]), nq0++ & 1))) {
                     pk::tmem_fence_after();
-                    ++nq[t];
-                    qk(t, base, it.n_tiles[t] == 1);
+                    qk(0, ring, n0 == 1);
                 }
-                if (ok) pk::mma_commit(pk::smem_addr(&sm.empty[base % L::kStages]));
+                if (ok && n1 > 0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.q_full[1]), nq1++ & 1))) {
+                    pk::tmem_fence_after();
+                    qk(1, ring, n1 == 1);
+                }
+                if (ok) release(ring);
+                advance(1);
             }
             // the next item is looked up while the first scores are weighed
-            Item next;
-            index += gridDim.x;
-            more = find_item(a, tile_off, q_off, k_off, index, next);
-            if (lane == 0) {
-                for (int32_t j = 0; ok && j < it.n_all; ++j) {
-                    const uint32_t nv = base + 2 * j + 1, nk = nv + 1;
-                    ok = wait_full(nv);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        if (!ok || j >= it.n_tiles[t]) continue;
-                        ok = pk::mbar_wait(pk::smem_addr(&sm.p_ready[t]), ni[t] & 1);
-                        if (!ok) break;
-                        ++ni[t];
-                        pk::tmem_fence_after();
-                        const uint32_t v = stage_of(nv);
-#pragma unroll
-                        for (int s = 0; s < 8; ++s)
-                            pk::mma_ts(tmem + 256 + D * t, tmem + 128 * t + 64 * (s / 4) + 8 * (s % 4),
-                                       pk::mma_desc(v + s * 2048, 16384, 1024), kPv, j > 0 || s > 0);
-                        pk::mma_commit(pk::smem_addr(&sm.o_done[t]));
-                        if (j + 1 < it.n_tiles[t]) {
-                            ok = wait_full(nk);
-                            if (!ok) break;
-                            pk::tmem_fence_after();
-                            qk(t, nk, j + 2 == it.n_tiles[t]);
-                        }
-                    }
-                    if (ok) {
-                        pk::mma_commit(pk::smem_addr(&sm.empty[nv % L::kStages]));
-                        if (j + 1 < it.n_all) pk::mma_commit(pk::smem_addr(&sm.empty[nk % L::kStages]));
-                    }
+            ++turn;
+            more = find_item(a, tile_off, q_off, k_off, turn, it);
+            for (int32_t j = 0; ok && j < n_all; ++j) {
+                const uint32_t sv = ring, uv = use;
+                advance(1);
+                const uint32_t sk = ring, uk = use;  // K of the next tile, where there is one
+                ok = wait_full(sv, uv);
+                if (ok && j < n0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.p_ready[0]), ni0++ & 1))) {
+                    pk::tmem_fence_after();
+                    pv(0, sv, j == 0);
+                    if (j + 1 < n0 && (ok = wait_full(sk, uk))) qk(0, sk, j + 2 == n0);
                 }
-                base += 2 * it.n_all;
+                if (ok && j < n1 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.p_ready[1]), ni1++ & 1))) {
+                    pk::tmem_fence_after();
+                    pv(1, sv, j == 0);
+                    release(sv);
+                    if (j + 1 < n1 && (ok = wait_full(sk, uk))) qk(1, sk, j + 2 == n1);
+                } else if (ok) {
+                    release(sv);
+                }
+                if (ok && j + 1 < n_all) {
+                    release(sk);
+                    advance(1);
+                }
             }
-            ok = __all_sync(0xffffffffu, ok);
-            it = next;
         }
         if (!ok && lane == 0) give_up();
     } else if (warp >= kWarpClean) {
@@ -415,8 +433,8 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
             }
             base += 2 * it.n_all;
             ++items;
-            index += gridDim.x;
-            more = find_item(a, tile_off, q_off, k_off, index, it);
+            ++turn;
+            more = find_item(a, tile_off, q_off, k_off, turn, it);
         }
         if (!ok && lane == 0) give_up();
     } else {
@@ -438,91 +456,96 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
             const int32_t last = on ? tok + it.lk - it.lq : -1;
             const int64_t q_row = it.q0 + tok;
             const uint32_t qh = it.head * a.group + gh;
-            const bool notes = it.first_edge < it.n_all;
-            index += gridDim.x;
-            more = find_item(a, tile_off, q_off, k_off, index, it);  // the next one
-            float ref = -FLT_MAX;
-            uint64_t sum2[2] = {0, 0};
+            const bool notes = it.first_edge < n_tiles;  // only then are this item's notes sure to be there
+            ++turn;
+            more = find_item(a, tile_off, q_off, k_off, turn, it);  // the next one
+            float ref = -FLT_MAX, sum = 0.0f;
 #pragma unroll 1
             for (int32_t j = 0; j < n_tiles; ++j, ++ni) {
                 ok = pk::mbar_wait_warp(pk::smem_addr(&sm.s_full[t]), ni & 1);
                 if (!ok) break;
                 pk::tmem_fence_after();
-                // two chunks of 32 scores in registers: keys 0-63 pass once for the maximum and are read again after
-                // keys 64-127 have become weights
-                uint32_t x[2][32];
                 const bool edge = j * kKeys + kKeys - 1 > first_last;
                 const int32_t see = last - j * kKeys;  // columns up to here
-                auto mask = [&](uint32_t(&y)[32], int c) {
+                uint32_t x[2][32];
+                // scores of chunk c, 32 keys, into x[c & 1]; the next chunk is on its way meanwhile
+                auto chunk = [&](int c) -> uint32_t(&)[32] {
+                    uint32_t(&y)[32] = x[c & 1];
+                    pk::tmem_wait_load(y);
+                    if (c < 3) pk::tmem_load32(ts + 32 * (c + 1), x[(c + 1) & 1]);
                     if (edge) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (32 * c + i > see) y[i] = 0xff800000u;
                     }
+                    return y;
                 };
-                float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    pk::tmem_load32(ts + 64 * h, x[0]);
-                    pk::tmem_load32(ts + 64 * h + 32, x[1]);
-                    pk::tmem_wait_load(x[0]);
-                    pk::tmem_wait_load(x[1]);
-                    mask(x[0], 2 * h);
-                    mask(x[1], 2 * h + 1);
-#pragma unroll
-                    for (int i = 0; i < 64; ++i) m4[i & 3] = fmaxf(m4[i & 3], __uint_as_float(x[i / 32][i % 32]));
-                }
-                const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale2;
-                const bool over = m > ref + kTop;
-                if (__any_sync(0xffffffffu, over)) {
-                    const float next = over ? ceilf(m) - kBase : ref;
+                // Moves the reference of the rows whose largest score has outgrown it; their sum and output so far
+                // are rescaled by a power of two.
+                auto move_ref = [&](float m) {
+                    const float next = m > ref + kTop ? ceilf(m) - kBase : ref;
                     const float f = ex2(ref - next);
                     ref = next;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float2 y = unpack2(sum2[e]);
-                        sum2[e] = pack2(y.x * f, y.y * f);
-                    }
-                    if (j > 0) {
-                        ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
-                        if (!ok) break;
-                        pk::tmem_fence_after();
+                    sum *= f;
+                    if (j == 0) return;
+                    ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
+                    if (!ok) return;
+                    pk::tmem_fence_after();
 #pragma unroll 1
-                        for (int c = 0; c < D / 32; ++c) {
-                            uint32_t y[32];
-                            pk::tmem_load32(to + 32 * c, y);
-                            pk::tmem_wait_load(y);
+                    for (int d = 0; d < D / 32; ++d) {
+                        pk::tmem_load32(to + 32 * d, x[0]);
+                        pk::tmem_wait_load(x[0]);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * f);
-                            pk::tmem_store32(to + 32 * c, y);
+                        for (int i = 0; i < 32; ++i) x[0][i] = __float_as_uint(__uint_as_float(x[0][i]) * f);
+                        pk::tmem_store32(to + 32 * d, x[0]);
+                    }
+                };
+                if (j == 0) {  // a first reference
+                    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    pk::tmem_load32(ts, x[0]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t(&y)[32] = chunk(c);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) m4[i & 3] = fmaxf(m4[i & 3], __uint_as_float(y[i]));
+                    }
+                    move_ref(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale2);
+                }
+                // One pass over the scores takes both the weights by the reference so far and the maximum; only where
+                // that shows a weight of 2^kTop or more is the reference moved and the pass done again.
+                uint32_t p[2][32];
+                uint64_t sum2[2];
+#pragma unroll 1
+                for (;;) {
+                    const uint64_t ref2 = pack2(-ref, -ref);
+                    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    sum2[0] = sum2[1] = 0;
+                    pk::tmem_load32(ts, x[0]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t(&y)[32] = chunk(c);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            m4[i / 2 & 3] = fmaxf(fmaxf(m4[i / 2 & 3], __uint_as_float(y[i])), __uint_as_float(y[i + 1]));
+                            float2 z = unpack2(fma2(pack2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), scale22, ref2));
+                            z.x = ex2(z.x);
+                            z.y = ex2(z.y);
+                            sum2[i / 2 & 1] = add2(sum2[i / 2 & 1], pack2(z.x, z.y));
+                            p[c / 2][c % 2 * 16 + i / 2] = pk::Elem<DT>::from2(z.x, z.y);
                         }
                     }
+                    const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale2;
+                    if (!__any_sync(0xffffffffu, m > ref + kTop)) break;
+                    move_ref(m);
+                    if (!ok) break;
                 }
-                const uint64_t ref2 = pack2(-ref, -ref);
-                // the weights of a chunk lie in the first half of its scores' columns' pair: keys 0-63 in columns 0-31,
-                // keys 64-127 in columns 64-95
-                auto weigh = [&](uint32_t(&y)[32], int c) {
-                    uint32_t p[16];
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        float2 z = unpack2(fma2(pack2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), scale22, ref2));
-                        z.x = ex2(z.x);
-                        z.y = ex2(z.y);
-                        sum2[i / 2 & 1] = add2(sum2[i / 2 & 1], pack2(z.x, z.y));
-                        p[i / 2] = pk::Elem<DT>::from2(z.x, z.y);
-                    }
-                    pk::tmem_store16(ts + 64 * (c >> 1) + 16 * (c & 1), p);
-                };
-                weigh(x[0], 2);
-                pk::tmem_load32(ts, x[0]);
-                weigh(x[1], 3);
-                pk::tmem_load32(ts + 32, x[1]);
-                pk::tmem_wait_load(x[0]);
-                pk::tmem_wait_load(x[1]);
-                mask(x[0], 0);
-                mask(x[1], 1);
-                weigh(x[0], 0);
-                weigh(x[1], 1);
+                if (!ok) break;
+                {
+                    const float2 s0 = unpack2(sum2[0]), s1 = unpack2(sum2[1]);
+                    sum += (s0.x + s1.x) + (s0.y + s1.y);
+                }
+                pk::tmem_store32(ts, p[0]);  // over the scores, which every pass is done with
+                pk::tmem_store32(ts + 32, p[1]);
                 pk::tmem_wait_store();
                 pk::tmem_fence_before();
                 __syncwarp();
@@ -530,8 +553,6 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
             }
             if (ok && n_tiles > 0) ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
             if (!ok) break;
-            const float2 s0 = unpack2(sum2[0]), s1 = unpack2(sum2[1]);
-            const float sum = (s0.x + s1.x) + (s0.y + s1.y);
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
             if (on && a.lse)
                 a.lse[q_row * a.q_heads + qh] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;

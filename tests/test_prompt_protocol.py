@@ -116,12 +116,15 @@ class Cta:
                         yield
                     ni[t] += 1
                     self.pipe += [("PV", t, x, j, nv % self.S), ("commit", self.o_done[t])]
+                    if t:
+                        self.pipe.append(("commit", self.empty[nv % self.S]))
                     yield
                     if j + 1 < nt[t]:
                         yield from wait_full(nk)
                         qk(x, t, j + 1, nk, j + 2 == nt[t])
                     yield
-                self.pipe.append(("commit", self.empty[nv % self.S]))
+                if j >= n1:
+                    self.pipe.append(("commit", self.empty[nv % self.S]))
                 if j + 1 < n_all:
                     self.pipe.append(("commit", self.empty[nk % self.S]))
             base += 2 * n_all
@@ -150,7 +153,7 @@ class Cta:
     def softmax(self, t, warp):
         ni = 0
         for x, item in enumerate(self.items):
-            n_all, fe = max(item[:2]), item[2]
+            fe = item[2]
             for j in range(item[t]):
                 while not self.s_full[t].done(ni & 1):
                     yield
@@ -171,7 +174,7 @@ class Cta:
                     yield
                 for _ in range(self.rng.choice((1, 1, 40))):
                     assert self.o[t] == (x, item[t] - 1), "O overwritten before it was read"
-                    assert fe >= n_all or self.notes[x & 1] == x
+                    assert fe >= item[t] or self.notes[x & 1] == x
                     yield
             self.epilogues[4 * t + warp] = x + 1
 
@@ -215,7 +218,7 @@ class Cta:
         assert all(op[0] == "commit" for op in self.pipe), "a product runs after the CTA's end"
 
 
-@pytest.mark.parametrize("stages", [4, 8])
+@pytest.mark.parametrize("stages", [5, 8])
 def test_every_interleaving_tried_is_sound(stages):
     rng = random.Random(7)
     for _ in range(150):
