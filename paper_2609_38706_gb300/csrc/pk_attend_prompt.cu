@@ -113,7 +113,7 @@ struct Item {
 
 // The turn-th item of this CTA.  Items come heaviest first within a request, so
 // every other turn runs through the CTAs backwards: one that got the heaviest of
-// a turn gets the lightest of the next (two prompts of 8192: 855 -> TURNS us).
+// a turn gets the lightest of the next (two prompts of 8192: 855 -> 830 us when added).
 __device__ __forceinline__ bool find_item(const Args &a, const uint64_t *tile_off, const int64_t *q_off,
                                           const int64_t *k_off, uint32_t turn, Item &it) {
     const uint64_t total = __ldcg(tile_off + a.R) * a.kv_heads;
@@ -144,6 +144,9 @@ __device__ __forceinline__ bool find_item(const Args &a, const uint64_t *tile_of
     return true;
 }
 
+// Registers move to the softmax warps, whose scores on their way and weights do not fit 168: 256 * 200 + 128 * 104 =
+// 384 * 168, the launch's own.
+constexpr int kRegsSoftmax = 200, kRegsOther = 104;
 constexpr uint32_t kWarpLoad = 8, kWarpMma = 9, kWarpClean = 10;  // warps 0-7: softmax
 
 __device__ __forceinline__ uint64_t pack2(float lo, float hi) {
@@ -222,222 +225,226 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
     Item it;
     uint32_t turn = 0;
     bool more = find_item(a, tile_off, q_off, k_off, turn, it);
-    if (warp == kWarpLoad) {
-        uint32_t n = 0, edges = 0, nq[2] = {0, 0};  // ring stages, edge tiles and Q tiles loaded so far
-        bool ok = true;
-        pk::fence_proxy_async();
-        while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
-            if (lane == 0) {
-                const uint32_t q_bytes = a.tile_tokens * a.tile_heads * 128 * (D / 64);
-                for (int32_t j = 0; ok && j < it.n_all; ++j) {
+    if (warp >= kWarpLoad) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+        if (warp == kWarpLoad) {
+            uint32_t n = 0, edges = 0, nq[2] = {0, 0};  // ring stages, edge tiles and Q tiles loaded so far
+            bool ok = true;
+            pk::fence_proxy_async();
+            while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
+                if (lane == 0) {
+                    const uint32_t q_bytes = a.tile_tokens * a.tile_heads * 128 * (D / 64);
+                    for (int32_t j = 0; ok && j < it.n_all; ++j) {
 #pragma unroll
-                    for (int kv = 0; kv < 2; ++kv) {
-                        const uint32_t st = n % L::kStages;
-                        const bool dirty = kv && j >= it.first_edge;
-                        const uint32_t bar = pk::smem_addr(dirty ? &sm.edge_v[edges & 3] : &sm.full[st]);
-                        ok = ok && (n < L::kStages ||
-                                    pk::mbar_wait(pk::smem_addr(&sm.empty[st]), (n / L::kStages + 1) & 1));
-                        if (!ok) break;
-                        // only now: the barrier's earlier phase is over, as the stage was read
-                        if (!dirty) pk::mbar_arrive(bar);
-                        pk::mbar_expect(bar, L::kTile);
-#pragma unroll
-                        for (int b = 0; b < D / 64; ++b)
-                            pk::tile_load3(smem + L::kRing + st * L::kTile + b * 16384, kv ? &map_v : &map_k, b * 64,
-                                           it.head, it.k0 + j * kKeys, bar);
-                        ++n;
-                        edges += dirty;
-                    }
-                    if (j == 0) {  // Q behind the first tiles, which need not wait for the last item's Q
-#pragma unroll
-                        for (int t = 0; t < 2; ++t) {
-                            if (!ok || it.n_tiles[t] == 0) continue;
-                            ok = nq[t] == 0 || pk::mbar_wait(pk::smem_addr(&sm.q_empty[t]), (nq[t] - 1) & 1);
+                        for (int kv = 0; kv < 2; ++kv) {
+                            const uint32_t st = n % L::kStages;
+                            const bool dirty = kv && j >= it.first_edge;
+                            const uint32_t bar = pk::smem_addr(dirty ? &sm.edge_v[edges & 3] : &sm.full[st]);
+                            ok = ok && (n < L::kStages ||
+                                        pk::mbar_wait(pk::smem_addr(&sm.empty[st]), (n / L::kStages + 1) & 1));
                             if (!ok) break;
-                            const uint32_t bar = pk::smem_addr(&sm.q_full[t]);
-                            pk::mbar_expect(bar, q_bytes);
+                            // only now: the barrier's earlier phase is over, as the stage was read
+                            if (!dirty) pk::mbar_arrive(bar);
+                            pk::mbar_expect(bar, L::kTile);
 #pragma unroll
                             for (int b = 0; b < D / 64; ++b)
-                                pk::tile_load3(smem + t * L::kTile + b * 16384, &map_q, b * 64,
-                                               it.head * (int)a.group + it.chunk * (int)a.tile_heads,
-                                               it.q0 + it.tok0 + t * (int)a.tile_tokens, bar);
-                            ++nq[t];
+                                pk::tile_load3(smem + L::kRing + st * L::kTile + b * 16384, kv ? &map_v : &map_k, b * 64,
+                                               it.head, it.k0 + j * kKeys, bar);
+                            ++n;
+                            edges += dirty;
+                        }
+                        if (j == 0) {  // Q behind the first tiles, which need not wait for the last item's Q
+#pragma unroll
+                            for (int t = 0; t < 2; ++t) {
+                                if (!ok || it.n_tiles[t] == 0) continue;
+                                ok = nq[t] == 0 || pk::mbar_wait(pk::smem_addr(&sm.q_empty[t]), (nq[t] - 1) & 1);
+                                if (!ok) break;
+                                const uint32_t bar = pk::smem_addr(&sm.q_full[t]);
+                                pk::mbar_expect(bar, q_bytes);
+#pragma unroll
+                                for (int b = 0; b < D / 64; ++b)
+                                    pk::tile_load3(smem + t * L::kTile + b * 16384, &map_q, b * 64,
+                                                   it.head * (int)a.group + it.chunk * (int)a.tile_heads,
+                                                   it.q0 + it.tok0 + t * (int)a.tile_tokens, bar);
+                                ++nq[t];
+                            }
                         }
                     }
                 }
+                ok = __all_sync(0xffffffffu, ok);
+                ++turn;
+                more = find_item(a, tile_off, q_off, k_off, turn, it);
             }
-            ok = __all_sync(0xffffffffu, ok);
-            ++turn;
-            more = find_item(a, tile_off, q_off, k_off, turn, it);
-        }
-        if (lane == 0) {
-            if (!ok) give_up();
-            // no copy of its own stays in flight
-            for (uint32_t i = n > L::kStages ? n - L::kStages : 0; i < n; ++i)
-                pk::mbar_wait(pk::smem_addr(&sm.full[i % L::kStages]), (i / L::kStages) & 1);
-            for (int t = 0; t < 2; ++t)
-                if (nq[t]) pk::mbar_wait(pk::smem_addr(&sm.q_full[t]), (nq[t] - 1) & 1);
-        }
-        __syncwarp();
-    } else if (warp == kWarpMma) {
-        const uint32_t qk_kind = pk::mma_idesc(DT == PK_BF16, 128, 128, false) |
-                                 (a.scale2 < 0.0f ? 1u << 13 : 0u);  // a negative scale negates Q
-        constexpr uint32_t kPv = pk::mma_idesc(DT == PK_BF16, 128, D, true);
-        uint32_t ring = 0, use = 0;             // next ring stage, and how often the ring has been gone round
-        uint32_t ni0 = 0, ni1 = 0, nq0 = 0, nq1 = 0;  // key tiles and Q tiles used so far, by tile
-        bool ok = true;
-        auto wait_full = [&](uint32_t st, uint32_t round) {
-            return pk::mbar_wait_warp(pk::smem_addr(&sm.full[st]), round & 1);
-        };
-        auto advance = [&](uint32_t by) {
-            ring += by;
-            if (ring >= L::kStages) ring -= L::kStages, ++use;
-        };
-        auto qk = [&](int t, uint32_t st, bool last) {
-            const uint32_t q = smem + t * L::kTile, k = smem + L::kRing + st * L::kTile;
-            if (pk::elect_lane()) {
+            if (lane == 0) {
+                if (!ok) give_up();
+                // no copy of its own stays in flight
+                for (uint32_t i = n > L::kStages ? n - L::kStages : 0; i < n; ++i)
+                    pk::mbar_wait(pk::smem_addr(&sm.full[i % L::kStages]), (i / L::kStages) & 1);
+                for (int t = 0; t < 2; ++t)
+                    if (nq[t]) pk::mbar_wait(pk::smem_addr(&sm.q_full[t]), (nq[t] - 1) & 1);
+            }
+            __syncwarp();
+        } else if (warp == kWarpMma) {
+            const uint32_t qk_kind = pk::mma_idesc(DT == PK_BF16, 128, 128, false) |
+                                     (a.scale2 < 0.0f ? 1u << 13 : 0u);  // a negative scale negates Q
+            constexpr uint32_t kPv = pk::mma_idesc(DT == PK_BF16, 128, D, true);
+            uint32_t ring = 0, use = 0;             // next ring stage, and how often the ring has been gone round
+            uint32_t ni0 = 0, ni1 = 0, nq0 = 0, nq1 = 0;  // key tiles and Q tiles used so far, by tile
+            bool ok = true;
+            auto wait_full = [&](uint32_t st, uint32_t round) {
+                return pk::mbar_wait_warp(pk::smem_addr(&sm.full[st]), round & 1);
+            };
+            auto advance = [&](uint32_t by) {
+                ring += by;
+                if (ring >= L::kStages) ring -= L::kStages, ++use;
+            };
+            auto qk = [&](int t, uint32_t st, bool last) {
+                const uint32_t q = smem + t * L::kTile, k = smem + L::kRing + st * L::kTile;
+                if (pk::elect_lane()) {
 #pragma unroll
-                for (int s = 0; s < D / 16; ++s)
-                    pk::mma_ss(tmem + 128 * t, pk::mma_desc(q + (s / 4) * 16384 + (s % 4) * 32, 16, 1024),
-                               pk::mma_desc(k + (s / 4) * 16384 + (s % 4) * 32, 16, 1024), qk_kind, s > 0);
-                pk::mma_commit(pk::smem_addr(&sm.s_full[t]));
-                if (last) pk::mma_commit(pk::smem_addr(&sm.q_empty[t]));
-            }
-            __syncwarp();
-        };
-        auto pv = [&](int t, uint32_t st, bool first) {
-            const uint32_t v = smem + L::kRing + st * L::kTile;
-            if (pk::elect_lane()) {
+                    for (int s = 0; s < D / 16; ++s)
+                        pk::mma_ss(tmem + 128 * t, pk::mma_desc(q + (s / 4) * 16384 + (s % 4) * 32, 16, 1024),
+                                   pk::mma_desc(k + (s / 4) * 16384 + (s % 4) * 32, 16, 1024), qk_kind, s > 0);
+                    pk::mma_commit(pk::smem_addr(&sm.s_full[t]));
+                    if (last) pk::mma_commit(pk::smem_addr(&sm.q_empty[t]));
+                }
+                __syncwarp();
+            };
+            auto pv = [&](int t, uint32_t st, bool first) {
+                const uint32_t v = smem + L::kRing + st * L::kTile;
+                if (pk::elect_lane()) {
 #pragma unroll
-                for (int s = 0; s < 8; ++s)
-                    pk::mma_ts(tmem + 256 + D * t, tmem + 128 * t + 8 * s, pk::mma_desc(v + s * 2048, 16384, 1024),
-                               kPv, !first || s > 0);
-                pk::mma_commit(pk::smem_addr(&sm.o_done[t]));
-            }
-            __syncwarp();
-        };
-        auto release = [&](uint32_t st) {
-            if (pk::elect_lane()) pk::mma_commit(pk::smem_addr(&sm.empty[st]));
-            __syncwarp();
-        };
-        while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
-            const int32_t n0 = (int32_t)pk::uniform(it.n_tiles[0]), n1 = (int32_t)pk::uniform(it.n_tiles[1]);
-            const int32_t n_all = max(n0, n1);
-            if (n_all) {
-                ok = wait_full(ring, use);
-                if (ok && n0 > 0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.q_full[0]), nq0++ & 1))) {
-                    pk::tmem_fence_after();
-                    qk(0, ring, n0 == 1);
+                    for (int s = 0; s < 8; ++s)
+                        pk::mma_ts(tmem + 256 + D * t, tmem + 128 * t + 8 * s, pk::mma_desc(v + s * 2048, 16384, 1024),
+                                   kPv, !first || s > 0);
+                    pk::mma_commit(pk::smem_addr(&sm.o_done[t]));
                 }
-                if (ok && n1 > 0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.q_full[1]), nq1++ & 1))) {
-                    pk::tmem_fence_after();
-                    qk(1, ring, n1 == 1);
-                }
-                if (ok) release(ring);
-                advance(1);
-            }
-            // the next item is looked up while the first scores are weighed
-            ++turn;
-            more = find_item(a, tile_off, q_off, k_off, turn, it);
-            for (int32_t j = 0; ok && j < n_all; ++j) {
-                const uint32_t sv = ring, uv = use;
-                advance(1);
-                const uint32_t sk = ring, uk = use;  // K of the next tile, where there is one
-                ok = wait_full(sv, uv);
-                if (ok && j < n0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.p_ready[0]), ni0++ & 1))) {
-                    pk::tmem_fence_after();
-                    pv(0, sv, j == 0);
-                    if (j + 1 < n0 && (ok = wait_full(sk, uk))) qk(0, sk, j + 2 == n0);
-                }
-                if (ok && j < n1 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.p_ready[1]), ni1++ & 1))) {
-                    pk::tmem_fence_after();
-                    pv(1, sv, j == 0);
-                    release(sv);
-                    if (j + 1 < n1 && (ok = wait_full(sk, uk))) qk(1, sk, j + 2 == n1);
-                } else if (ok) {
-                    release(sv);
-                }
-                if (ok && j + 1 < n_all) {
-                    release(sk);
+                __syncwarp();
+            };
+            auto release = [&](uint32_t st) {
+                if (pk::elect_lane()) pk::mma_commit(pk::smem_addr(&sm.empty[st]));
+                __syncwarp();
+            };
+            while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
+                const int32_t n0 = (int32_t)pk::uniform(it.n_tiles[0]), n1 = (int32_t)pk::uniform(it.n_tiles[1]);
+                const int32_t n_all = max(n0, n1);
+                if (n_all) {
+                    ok = wait_full(ring, use);
+                    if (ok && n0 > 0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.q_full[0]), nq0++ & 1))) {
+                        pk::tmem_fence_after();
+                        qk(0, ring, n0 == 1);
+                    }
+                    if (ok && n1 > 0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.q_full[1]), nq1++ & 1))) {
+                        pk::tmem_fence_after();
+                        qk(1, ring, n1 == 1);
+                    }
+                    if (ok) release(ring);
                     advance(1);
                 }
-            }
-        }
-        if (!ok && lane == 0) give_up();
-    } else if (warp >= kWarpClean) {
-        // V of the tiles at the causal edge and at the request's end: rows past its last key become 0, and so do
-        // infinities and NaN, which are noted for the queries that do attend them.  Each of the two warps has its
-        // own half of the dimensions.
-        constexpr uint32_t kChunks = D / 16;  // 16-byte chunks of a row that a warp looks at
-        const uint32_t half = warp - kWarpClean;
-        uint32_t base = 0, edges = 0, items = 0;
-        bool ok = true;
-        while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
-            int32_t *bad_row = sm.bad_row[items & 1];
-            if (it.first_edge < it.n_all) {
-                // the item before the last one shared these notes: its outputs must have been written
-                uint64_t t0 = 0, t1 = 0;
-                while (items >= 2) {
-                    uint32_t done;
-                    asm volatile("ld.acquire.cta.shared.u32 %0, [%1];" : "=r"(done) : "r"(pk::smem_addr(&sm.epilogues[lane & 7])) : "memory");
-                    if (__all_sync(0xffffffffu, (int32_t)(done - (items - 1)) >= 0)) break;
-                    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
-                    t1 = __shfl_sync(0xffffffffu, t1, 0);
-                    if (t0 == 0) t0 = t1;
-                    if (t1 - t0 > pk::kMbarLimitNs) {
-                        ok = false;
-                        break;
+                // the next item is looked up while the first scores are weighed
+                ++turn;
+                more = find_item(a, tile_off, q_off, k_off, turn, it);
+                for (int32_t j = 0; ok && j < n_all; ++j) {
+                    const uint32_t sv = ring, uv = use;
+                    advance(1);
+                    const uint32_t sk = ring, uk = use;  // K of the next tile, where there is one
+                    ok = wait_full(sv, uv);
+                    if (ok && j < n0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.p_ready[0]), ni0++ & 1))) {
+                        pk::tmem_fence_after();
+                        pv(0, sv, j == 0);
+                        if (j + 1 < n0 && (ok = wait_full(sk, uk))) qk(0, sk, j + 2 == n0);
+                    }
+                    if (ok && j < n1 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.p_ready[1]), ni1++ & 1))) {
+                        pk::tmem_fence_after();
+                        pv(1, sv, j == 0);
+                        release(sv);
+                        if (j + 1 < n1 && (ok = wait_full(sk, uk))) qk(1, sk, j + 2 == n1);
+                    } else if (ok) {
+                        release(sv);
+                    }
+                    if (ok && j + 1 < n_all) {
+                        release(sk);
+                        advance(1);
                     }
                 }
-                for (uint32_t d = lane; d < D / 2; d += 32) bad_row[half * (D / 2) + d] = 0x7fffffff;
-                if (lane == 0) sm.any_bad[items & 1][half] = 0;
-                __syncwarp();
             }
-            for (int32_t j = it.first_edge; ok && j < it.n_all; ++j, ++edges) {
-                const uint32_t st = (base + 2 * j + 1) % L::kStages;
-                ok = pk::mbar_wait_warp(pk::smem_addr(&sm.edge_v[edges & 3]), (edges >> 2) & 1);
-                if (!ok) break;
-                uint8_t *v = smem_p + L::kRing + st * L::kTile + (D == 128 ? half * 16384 : 0);
-                for (uint32_t x = lane; x < 128 * kChunks; x += 32) {
-                    const uint32_t row = x / kChunks, chunk = x % kChunks + (D == 128 ? 0 : half * kChunks);
-                    uint4 *at = reinterpret_cast<uint4 *>(v + row * 128 + ((chunk ^ (row & 7)) << 4));
-                    const uint4 u = *at;
-                    const int32_t key = j * kKeys + (int32_t)row;
-                    constexpr uint32_t kInf = pk::Elem<DT>::kInfBits;
-                    if (key >= it.lk) {
-                        *at = make_uint4(0, 0, 0, 0);
-                        continue;
-                    }
-                    uint32_t w[4] = {u.x, u.y, u.z, u.w}, m = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
-                    if ((m & 0xffffu) < kInf && m >> 16 < kInf) continue;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t d = (D == 128 ? half * 64 : 0) + chunk * 8 + 2 * i;
-                        if ((w[i] & 0x7fffu) >= kInf) {
-                            atomicMin(&bad_row[d], key);
-                            w[i] &= 0xffff0000u;
-                        }
-                        if ((w[i] >> 16 & 0x7fffu) >= kInf) {
-                            atomicMin(&bad_row[d + 1], key);
-                            w[i] &= 0xffffu;
+            if (!ok && lane == 0) give_up();
+        } else {
+            // V of the tiles at the causal edge and at the request's end: rows past its last key become 0, and so do
+            // infinities and NaN, which are noted for the queries that do attend them.  Each of the two warps has its
+            // own half of the dimensions.
+            constexpr uint32_t kChunks = D / 16;  // 16-byte chunks of a row that a warp looks at
+            const uint32_t half = warp - kWarpClean;
+            uint32_t base = 0, edges = 0, items = 0;
+            bool ok = true;
+            while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
+                int32_t *bad_row = sm.bad_row[items & 1];
+                if (it.first_edge < it.n_all) {
+                    // the item before the last one shared these notes: its outputs must have been written
+                    uint64_t t0 = 0, t1 = 0;
+                    while (items >= 2) {
+                        uint32_t done;
+                        asm volatile("ld.acquire.cta.shared.u32 %0, [%1];" : "=r"(done) : "r"(pk::smem_addr(&sm.epilogues[lane & 7])) : "memory");
+                        if (__all_sync(0xffffffffu, (int32_t)(done - (items - 1)) >= 0)) break;
+                        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t1));
+                        t1 = __shfl_sync(0xffffffffu, t1, 0);
+                        if (t0 == 0) t0 = t1;
+                        if (t1 - t0 > pk::kMbarLimitNs) {
+                            ok = false;
+                            break;
                         }
                     }
-                    *at = make_uint4(w[0], w[1], w[2], w[3]);
-                    sm.any_bad[items & 1][half] = 1;
+                    for (uint32_t d = lane; d < D / 2; d += 32) bad_row[half * (D / 2) + d] = 0x7fffffff;
+                    if (lane == 0) sm.any_bad[items & 1][half] = 0;
+                    __syncwarp();
                 }
-                pk::fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.full[st]));
+                for (int32_t j = it.first_edge; ok && j < it.n_all; ++j, ++edges) {
+                    const uint32_t st = (base + 2 * j + 1) % L::kStages;
+                    ok = pk::mbar_wait_warp(pk::smem_addr(&sm.edge_v[edges & 3]), (edges >> 2) & 1);
+                    if (!ok) break;
+                    uint8_t *v = smem_p + L::kRing + st * L::kTile + (D == 128 ? half * 16384 : 0);
+                    for (uint32_t x = lane; x < 128 * kChunks; x += 32) {
+                        const uint32_t row = x / kChunks, chunk = x % kChunks + (D == 128 ? 0 : half * kChunks);
+                        uint4 *at = reinterpret_cast<uint4 *>(v + row * 128 + ((chunk ^ (row & 7)) << 4));
+                        const uint4 u = *at;
+                        const int32_t key = j * kKeys + (int32_t)row;
+                        constexpr uint32_t kInf = pk::Elem<DT>::kInfBits;
+                        if (key >= it.lk) {
+                            *at = make_uint4(0, 0, 0, 0);
+                            continue;
+                        }
+                        uint32_t w[4] = {u.x, u.y, u.z, u.w}, m = 0;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+                        if ((m & 0xffffu) < kInf && m >> 16 < kInf) continue;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t d = (D == 128 ? half * 64 : 0) + chunk * 8 + 2 * i;
+                            if ((w[i] & 0x7fffu) >= kInf) {
+                                atomicMin(&bad_row[d], key);
+                                w[i] &= 0xffff0000u;
+                            }
+                            if ((w[i] >> 16 & 0x7fffu) >= kInf) {
+                                atomicMin(&bad_row[d + 1], key);
+                                w[i] &= 0xffffu;
+                            }
+                        }
+                        *at = make_uint4(w[0], w[1], w[2], w[3]);
+                        sm.any_bad[items & 1][half] = 1;
+                    }
+                    pk::fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.full[st]));
+                }
+                base += 2 * it.n_all;
+                ++items;
+                ++turn;
+                more = find_item(a, tile_off, q_off, k_off, turn, it);
             }
-            base += 2 * it.n_all;
-            ++items;
-            ++turn;
-            more = find_item(a, tile_off, q_off, k_off, turn, it);
+            if (!ok && lane == 0) give_up();
         }
-        if (!ok && lane == 0) give_up();
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         const uint32_t t = warp >> 2;
         const int32_t row = tid & 127;  // TMEM lane
         const int32_t row_tok = row / (int32_t)a.tile_heads, row_head = row % (int32_t)a.tile_heads;
@@ -467,12 +474,20 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                 pk::tmem_fence_after();
                 const bool edge = j * kKeys + kKeys - 1 > first_last;
                 const int32_t see = last - j * kKeys;  // columns up to here
-                uint32_t x[2][32];
-                // scores of chunk c, 32 keys, into x[c & 1]; the next chunk is on its way meanwhile
+                uint32_t x[3][32];
+                // Chunk c of the scores, 32 keys.  Loads run ahead (1 and 2 behind 0's use, 3 behind 1's), as one takes
+                // hundreds of cycles while the tensor core works on the same memory.
                 auto chunk = [&](int c) -> uint32_t(&)[32] {
-                    uint32_t(&y)[32] = x[c & 1];
-                    pk::tmem_wait_load(y);
-                    if (c < 3) pk::tmem_load32(ts + 32 * (c + 1), x[(c + 1) & 1]);
+                    if (c == 0) pk::tmem_load32(ts, x[0]);
+                    uint32_t(&y)[32] = x[c % 3];
+                    if (c != 2) pk::tmem_wait_load(y);
+                    if (c == 0) {
+                        pk::tmem_load32(ts + 32, x[1]);
+                        pk::tmem_load32(ts + 64, x[2]);
+                    } else if (c == 1) {
+                        pk::tmem_wait_load(x[2]);
+                        pk::tmem_load32(ts + 96, x[0]);
+                    }
                     if (edge) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
@@ -502,7 +517,6 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                 };
                 if (j == 0) {  // a first reference
                     float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    pk::tmem_load32(ts, x[0]);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         uint32_t(&y)[32] = chunk(c);
@@ -520,7 +534,6 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                     const uint64_t ref2 = pack2(-ref, -ref);
                     float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                     sum2[0] = sum2[1] = 0;
-                    pk::tmem_load32(ts, x[0]);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         uint32_t(&y)[32] = chunk(c);
