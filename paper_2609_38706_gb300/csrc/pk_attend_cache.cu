@@ -20,6 +20,9 @@
 #include <cuda_runtime.h>
 #include <float.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "pk_device.cuh"
 #include "pk_internal.h"
 #include "pk_kv.cuh"
@@ -27,9 +30,13 @@
 
 namespace {
 
-constexpr int kWarps = 8;
+// Four warps a CTA and four CTAs an SM: against eight and two, the start and the
+// end of one CTA are covered by three others (16 x 131072 cached tokens: 343 ->
+// 324 us; 128 x 2048: 69 -> 65 us).
+constexpr int kWarps = 4;
+constexpr uint32_t kSlots = 152 * 16 / kWarps;  // CTAs that the GPU holds
 constexpr int kThreads = 32 * kWarps;
-constexpr int kStages = 4;
+constexpr int kFinishWarps = 8, kFinishThreads = 32 * kFinishWarps;
 constexpr float kTop = 15.0f;   // p stays below 2^kTop (half: 2^16)
 constexpr float kBase = 8.0f;   // the largest p when ref moves: 2^kBase, so 22 bits of range lie below it
 
@@ -92,15 +99,31 @@ __device__ __forceinline__ int32_t length_of(const int32_t *kv_len, uint64_t r, 
     return len < 0 || (uint64_t)len > most ? 0 : len;
 }
 
+// How a variant is cut: columns (8 query rows each), granules that a warp takes
+// at once, stages of its ring, CTAs an SM.  Two granules share the waiting, the
+// look for a new reference and the loop around them (338 instructions a granule
+// one by one); with 16 rows of 128 dimensions the accumulators leave room for one.
+template <int D, int NT>
+struct Shape {
+    static constexpr int kGrans = D == 128 && NT == 2 ? 1 : 2;
+    static constexpr int kStages = kGrans == 2 ? 3 : 4;
+    static constexpr uint32_t kStage = kGrans * pk::Granule<D>::kBytes;
+    static constexpr uint32_t kRing = kStages * kStage;  // a warp's; holds its [8 NT][D] outputs at the end
+    static_assert(kRing >= 8 * NT * D * 4, "outputs fit the ring");
+};
+
 // One CTA: one request, KV head, tile of 8 NT query rows and split of the
-// tokens.  Warp w takes the split's granules w, w + 8, ...  Lane = 4 g + c.
+// tokens.  Warp w takes the split's steps w, w + kWarps, ... of kGrans granules.
+// Lane = 4 g + c.
 template <int D, int NT, uint32_t DT, bool kWeigh>
-__global__ void __launch_bounds__(kThreads, 2) k_attend_cache(const Args a) {
+__global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Args a) {
     using G = pk::Granule<D>;
+    using S = Shape<D, NT>;
+    constexpr int TG = S::kGrans;
     constexpr int kSteps = D / 16;  // k16 steps of QK, m16 tiles of PV
     constexpr int kRows = 8 * NT;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t bars[kWarps][kStages];
+    __shared__ __align__(8) uint64_t bars[kWarps][S::kStages];
     __shared__ float s_ref[kWarps][kRows], s_sum[kWarps][kRows];
 
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
@@ -112,10 +135,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_cache(const Args a) {
     const uint32_t head = id % a.kv_heads;
     const uint32_t r = id / a.kv_heads;
 
-    uint8_t *ring = smem + warp * (kStages * G::kBytes);
+    uint8_t *ring = smem + warp * S::kRing;
     const uint32_t ring_s = pk::smem_addr(ring), bar_s = pk::smem_addr(&bars[warp][0]);
     if (lane == 0) {
-        for (int i = 0; i < kStages; ++i) pk::mbar_init(bar_s + 8 * i, 1);
+        for (int i = 0; i < S::kStages; ++i) pk::mbar_init(bar_s + 8 * i, 1);
         pk::mbar_fence_init();
     }
     __syncwarp();
@@ -133,49 +156,50 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_cache(const Args a) {
     const uint32_t n_gran = ((uint32_t)len + 15) / 16;
     const uint32_t g0 = split * a.split_grans, g1 = min(g0 + a.split_grans, n_gran);
     if (a.splits > 1 && g0 >= n_gran) return;  // no partial result: the combination counts the splits itself
-    const uint32_t mine = g0 + warp < g1 ? (g1 - g0 - warp + kWarps - 1) / kWarps : 0;
+    const uint32_t steps = g0 < g1 ? (g1 - g0 + TG - 1) / TG : 0;
+    const uint32_t mine = warp < steps ? (steps - warp + kWarps - 1) / kWarps : 0;
 
     pages += (uint64_t)r * a.page_stride;
     const uint32_t slot_shift = 31 - __clz(a.page_grans);
     const bool pow2 = (a.page_grans & (a.page_grans - 1)) == 0;
-    // lane l holds the slot (checked) of granule slot_base + l of this warp
-    uint32_t slot_base = 0, slot_reg = 0;
-    auto load_slots = [&](uint32_t k) {
-        slot_base = k;
-        slot_reg = 0;
-        if (k + lane < mine) {
-            const uint32_t gr = g0 + warp + (k + lane) * kWarps;
-            slot_reg = __ldcg(pages + (pow2 ? gr >> slot_shift : gr / a.page_grans));
-            if (slot_reg >= a.n_slots) {
+    // lane l holds where the warp's granule ahead * TG + l lies; a slot out of range is reported and read as slot 0
+    uint32_t ahead = 0;
+    uint64_t where = 0;
+    auto find_granules = [&](uint32_t k) {
+        ahead = k;
+        const uint32_t gr = g0 + (warp + (k + lane / TG) * kWarps) * TG + lane % TG;
+        if (gr < g1) {
+            const uint32_t page = pow2 ? gr >> slot_shift : gr / a.page_grans;
+            uint64_t slot = __ldcg(pages + page);
+            if (slot >= a.n_slots) {
                 pk::set_status(a.status, PK_ERR_ARG);
-                slot_reg = 0;
+                slot = 0;
             }
+            where = reinterpret_cast<uint64_t>(pool) + slot * a.page_bytes +
+                    ((uint64_t)head * a.page_grans + (gr - page * a.page_grans)) * G::kBytes;
         }
     };
     auto issue = [&](uint32_t k) {
         if (k >= mine) return;  // uniform
-        if (k >= slot_base + 32) load_slots(k);
-        const uint64_t slot = __shfl_sync(0xffffffffu, slot_reg, k - slot_base);
-        if (lane == 0) {
-            const uint32_t gr = g0 + warp + k * kWarps;
-            const uint32_t in_page = pow2 ? gr & (a.page_grans - 1) : gr % a.page_grans;
-            const uint32_t st = k % kStages;
-            pk::mbar_expect(bar_s + 8 * st, G::kBytes);
-            pk::bulk_load(ring_s + st * G::kBytes,
-                          pool + slot * a.page_bytes + ((uint64_t)head * a.page_grans + in_page) * G::kBytes,
-                          G::kBytes, bar_s + 8 * st);
-        }
+        if (k >= ahead + 32 / TG) find_granules(k);
+        const uint64_t src = __shfl_sync(0xffffffffu, where, (k - ahead) * TG + lane % TG);
+        const uint32_t st = k % S::kStages;
+        const uint32_t n = min(g1 - (g0 + (warp + k * kWarps) * TG), (uint32_t)TG);
+        if (lane == 0) pk::mbar_expect(bar_s + 8 * st, n * G::kBytes);
+        __syncwarp();
+        if (lane < n)  // a lane a granule
+            pk::bulk_load(ring_s + st * S::kStage + lane * G::kBytes, reinterpret_cast<const void *>(src), G::kBytes,
+                          bar_s + 8 * st);
     };
-    load_slots(0);
+    find_granules(0);
 #pragma unroll
-    for (int k = 0; k < kStages; ++k) issue(k);
+    for (int k = 0; k < S::kStages; ++k) issue(k);
 
     // Q: column n = g of tile nt, dimensions c D/4 + 4 s + {0..3} at step s; scaled by a power of two that
     // brings the row's largest value to [2^7, 2^8), so that a half holds any 16-bit row.
     uint32_t qf[NT][kSteps][2];
     float mul[NT][2];   // for columns 2c, 2c + 1
     int32_t last[NT][2];
-    uint32_t col_row[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const uint32_t row = tile * kRows + nt * 8 + g;
@@ -211,7 +235,6 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_cache(const Args a) {
         for (int j = 0; j < 2; ++j) {
             mul[nt][j] = a.scale2 * __shfl_sync(0xffffffffu, down, 4 * (2 * c + j));
             const uint32_t cr = tile * kRows + nt * 8 + 2 * c + j;
-            col_row[nt][j] = cr;
             last[nt][j] = len - (int32_t)a.n_q + (int32_t)(cr < a.rows ? cr / a.group : a.n_q - 1);
         }
     }
@@ -225,46 +248,44 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_cache(const Args a) {
         sum[nt][0] = sum[nt][1] = 0.0f;
     }
     const int32_t all_see = len - (int32_t)a.n_q;  // positions up to here are seen by every query
-    const uint64_t gran_row0 = ((uint64_t)(r * a.kv_heads + head) * a.row_tiles + tile) * a.gran_stride;
+    // where this lane's granule sums of the first step go: lanes of g = 0..3 write, column 2c + (g & 1) of granule
+    // g >> 1 (of tile nt: + 8 nt)
+    float2 *gran_at = nullptr;
+    if (kWeigh)
+        gran_at = a.gran_ml + ((((uint64_t)(r * a.kv_heads + head) * a.row_tiles + tile) * a.gran_stride + g0 +
+                                warp * TG + (g >> 1)) * a.gran_rows + 2 * c + (g & 1));
     bool gave_up = false;
 
-#pragma unroll 1
-    for (uint32_t k = 0; k < mine; ++k) {
-        const uint32_t st = k % kStages;
-        if (!pk::mbar_wait_warp(bar_s + 8 * st, (k / kStages) & 1)) {
-            gave_up = true;
-            for (uint32_t i = k + 1; i < min(k + kStages, mine); ++i)  // no copy of its own stays in flight
-                pk::mbar_wait(bar_s + 8 * (i % kStages), (i / kStages) & 1);
-            break;
-        }
-        const uint8_t *gr = ring + st * G::kBytes;
-        const uint32_t gi = g0 + warp + k * kWarps;
-        const int32_t pos0 = (int32_t)(gi * 16);
-        const bool edge = pos0 + 15 > all_see;  // some query does not see some token
+    // One step: TG granules in stage `st`.  kEdge: some query does not see some token of them.
+    auto step = [&](uint32_t k, uint32_t st, auto edge) {
+        constexpr bool kEdge = decltype(edge)::value;
+        const uint8_t *gr = ring + st * S::kStage;
+        const int32_t pos0 = (int32_t)((g0 + (warp + k * kWarps) * TG) * 16);
 
-        // S^T = K Q^T: rows g and g + 8 are tokens
-        float s[NT][4];
+        // S^T = K Q^T: rows g and g + 8 of a granule's 16 are tokens
+        float s[TG][NT][4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.0f;
-        {
+        for (int h = 0; h < TG; ++h) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) s[h][nt][0] = s[h][nt][1] = s[h][nt][2] = s[h][nt][3] = 0.0f;
             uint32_t w[2][D / 32];   // this lane's code words of tokens g and g + 8
             uint32_t sc[2][D / 64];  // their scales, twice in a half2
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const uint8_t *row = gr + G::kK + (g + 8 * t) * G::kRow + c * (D / 8);
-                const uint8_t *ss = gr + G::kKs + (g + 8 * t) * G::kScales + c * (D / 64);
-                uint32_t h;
+                const uint8_t *row = gr + h * G::kBytes + G::kK + (g + 8 * t) * G::kRow + c * (D / 8);
+                const uint8_t *ss = gr + h * G::kBytes + G::kKs + (g + 8 * t) * G::kScales + c * (D / 64);
+                uint32_t z;
                 if (D == 128) {
                     const uint4 u = *reinterpret_cast<const uint4 *>(row);
                     w[t][0] = u.x, w[t][1] = u.y, w[t][D == 128 ? 2 : 0] = u.z, w[t][D == 128 ? 3 : 1] = u.w;
-                    h = pk::e4m3_to_half2(*reinterpret_cast<const uint16_t *>(ss));
-                    sc[t][D == 128 ? 1 : 0] = __byte_perm(h, h, 0x3232);
+                    z = pk::e4m3_to_half2(*reinterpret_cast<const uint16_t *>(ss));
+                    sc[t][D == 128 ? 1 : 0] = __byte_perm(z, z, 0x3232);
                 } else {
                     const uint2 u = *reinterpret_cast<const uint2 *>(row);
                     w[t][0] = u.x, w[t][1] = u.y;
-                    h = pk::e4m3_to_half2(*ss);
+                    z = pk::e4m3_to_half2(*ss);
                 }
-                sc[t][0] = __byte_perm(h, h, 0x1010);
+                sc[t][0] = __byte_perm(z, z, 0x1010);
             }
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) {
@@ -278,32 +299,45 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_cache(const Args a) {
                 }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    mma(s[nt], h0[0], h1[0], h0[1], h1[1], qf[nt][2 * j][0], qf[nt][2 * j][1]);
-                    mma(s[nt], h0[2], h1[2], h0[3], h1[3], qf[nt][2 * j + 1][0], qf[nt][2 * j + 1][1]);
+                    mma(s[h][nt], h0[0], h1[0], h0[1], h1[1], qf[nt][2 * j][0], qf[nt][2 * j][1]);
+                    mma(s[h][nt], h0[2], h1[2], h0[3], h1[3], qf[nt][2 * j + 1][0], qf[nt][2 * j + 1][1]);
                 }
             }
         }
 
-        // p = 2^(s - ref); s: [0] (token g, column 2c) [1] (g, 2c + 1) [2] (g + 8, 2c) [3] (g + 8, 2c + 1)
-        bool over = false;
+        // p = 2^x, x = s * mul - ref: [0] (token g, column 2c) [1] (g, 2c + 1) [2] (g + 8, 2c) [3] (g + 8, 2c + 1)
+        float x[TG][NT][4];
+        auto exponents = [&]() {
+            float top = -INFINITY;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+            for (int h = 0; h < TG; ++h)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[nt][e] *= mul[nt][e & 1];
-                if (edge && pos0 + (int32_t)(g + 8 * (e >> 1)) > last[nt][e & 1]) s[nt][e] = -INFINITY;
-                over |= s[nt][e] > ref[nt][e & 1] + kTop;
-            }
-        if (__any_sync(0xffffffffu, over)) {
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float &y = x[h][nt][e];
+                        y = fmaf(s[h][nt][e], mul[nt][e & 1], -ref[nt][e & 1]);
+                        if (kEdge && pos0 + 16 * h + (int32_t)(g + 8 * (e >> 1)) > last[nt][e & 1]) y = -INFINITY;
+                        top = fmaxf(top, y);
+                    }
+            return top > kTop;
+        };
+        if (__any_sync(0xffffffffu, exponents())) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    float m = fmaxf(s[nt][j], s[nt][j + 2]);
+                    // the column's largest score, from the scores that it sees
+                    float m = -INFINITY;
+#pragma unroll
+                    for (int h = 0; h < TG; ++h)
+#pragma unroll
+                        for (int e = j; e < 4; e += 2)
+                            m = fmaxf(m, x[h][nt][e] == -INFINITY ? -INFINITY : s[h][nt][e] * mul[nt][j]);
                     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                    if (m > ref[nt][j] + kTop) {
+                    if (m - ref[nt][j] > kTop) {
                         const float to = ceilf(m) - kBase;
                         const float f = ex2(ref[nt][j] - to);
                         ref[nt][j] = to;
@@ -312,52 +346,59 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_cache(const Args a) {
                         for (int i = 0; i < kSteps; ++i) o[nt][i][j] *= f, o[nt][i][j + 2] *= f;
                     }
                 }
+            exponents();
         }
-        uint32_t pf[NT][2];
+        uint32_t pf[TG][NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float p[4];
+            float t[TG][2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] = ex2(s[nt][e] - ref[nt][e & 1]);
-            const float t0 = p[0] + p[2], t1 = p[1] + p[3];
-            sum[nt][0] += t0;
-            sum[nt][1] += t1;
-            if (kWeigh) {
-                float x0 = t0, x1 = t1;
+            for (int h = 0; h < TG; ++h) {
+                float p[4];
 #pragma unroll
-                for (int d = 4; d < 32; d *= 2) {
-                    x0 += __shfl_xor_sync(0xffffffffu, x0, d);
-                    x1 += __shfl_xor_sync(0xffffffffu, x1, d);
-                }
-                if (g < 2) {  // lanes of g = 0 write column 2c, of g = 1 column 2c + 1
-                    const uint32_t col = nt * 8 + 2 * c + g;
-                    if (col < a.gran_rows && col_row[nt][0] + g < a.rows)
-                        a.gran_ml[(gran_row0 + gi) * a.gran_rows + col] =
-                            g ? make_float2(x1, ref[nt][1]) : make_float2(x0, ref[nt][0]);
-                }
+                for (int e = 0; e < 4; ++e) p[e] = ex2(x[h][nt][e]);
+                t[h][0] = p[0] + p[2];
+                t[h][1] = p[1] + p[3];
+                sum[nt][0] += t[h][0];
+                sum[nt][1] += t[h][1];
+                // rounded to halves for the product with V; the sums keep 32 bits
+                pf[h][nt][0] = transpose8x8(half2_of(p[0], p[1]));
+                pf[h][nt][1] = transpose8x8(half2_of(p[2], p[3]));
             }
-            // rounded to halves for the product with V; the sums keep 32 bits
-            pf[nt][0] = transpose8x8(half2_of(p[0], p[1]));
-            pf[nt][1] = transpose8x8(half2_of(p[2], p[3]));
+            if (kWeigh) {
+                // over a granule's 16 tokens: lanes keep column 2c + (g & 1) of granule (g >> 1) & 1
+                const bool odd = g & 1, second = g & 2;
+                float u[TG];
+#pragma unroll
+                for (int h = 0; h < TG; ++h)
+                    u[h] = (odd ? t[h][1] : t[h][0]) + __shfl_xor_sync(0xffffffffu, odd ? t[h][0] : t[h][1], 4);
+                float v = TG == 2 ? (second ? u[TG - 1] : u[0]) + __shfl_xor_sync(0xffffffffu, second ? u[0] : u[TG - 1], 8)
+                                  : u[0] + __shfl_xor_sync(0xffffffffu, u[0], 8);
+                v += __shfl_xor_sync(0xffffffffu, v, 16);
+                const uint32_t col = nt * 8 + 2 * c + (g & 1);
+                if (g < 2 * TG && tile * kRows + col < a.rows && (!kEdge || pos0 + 16 * (int32_t)(g >> 1) < len))
+                    gran_at[(uint64_t)k * (kWarps * TG) * a.gran_rows + nt * 8] =
+                        make_float2(v, odd ? ref[nt][1] : ref[nt][0]);
+            }
         }
 
         // O^T += V^T P^T: this lane's tokens 2c, 2c + 1, 2c + 8, 2c + 9, dimensions g D/8 ..
-        uint32_t v[4][D / 64], vs[2];
-        {
-            uint32_t b[4];
+#pragma unroll
+        for (int h = 0; h < TG; ++h) {
+            uint32_t v[4][D / 64], vs[2], b[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const uint32_t tok = 2 * c + (t & 1) + 8 * (t >> 1);
-                const uint8_t *row = gr + G::kV + tok * G::kRow + g * (D / 16);
+                const uint8_t *row = gr + h * G::kBytes + G::kV + tok * G::kRow + g * (D / 16);
                 if (D == 128) {
                     const uint2 u = *reinterpret_cast<const uint2 *>(row);
                     v[t][0] = u.x, v[t][D == 128 ? 1 : 0] = u.y;
                 } else {
                     v[t][0] = *reinterpret_cast<const uint32_t *>(row);
                 }
-                b[t] = gr[G::kVs + tok * G::kScales + (D == 128 ? g : g / 2)];
+                b[t] = gr[h * G::kBytes + G::kVs + tok * G::kScales + (D == 128 ? g : g / 2)];
             }
-            if (edge) {
+            if (kEdge) {
                 // A token that some query does not see has p = 0 there, which must not meet a NaN; a token that
                 // none sees is stale bytes.  Blocks marked NaN count as 0, and the queries that do see them get
                 // their NaN by hand.
@@ -365,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_cache(const Args a) {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     const uint32_t tok = 2 * c + (t & 1) + 8 * (t >> 1);
-                    if (pos0 + (int32_t)tok >= len) {
+                    if (pos0 + 16 * h + (int32_t)tok >= len) {
                         b[t] = 0;
                     } else if ((b[t] & 0x7f) == 0x7f) {
                         b[t] = 0;
@@ -379,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_cache(const Args a) {
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
-                            const int32_t see = last[nt][j] - pos0 + 1;  // tokens of this granule that it sees
+                            const int32_t see = last[nt][j] - (pos0 + 16 * h) + 1;  // tokens here that it sees
                             const uint32_t m = see <= 0 ? 0u : see >= 16 ? 0xffffu : (1u << see) - 1;
                             if (bad & m) {
 #pragma unroll
@@ -391,27 +432,45 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_cache(const Args a) {
             }
             vs[0] = pk::e4m3_to_half2(b[0] | b[1] << 8);
             vs[1] = pk::e4m3_to_half2(b[2] | b[3] << 8);
-        }
-        __syncwarp();  // every lane has read the stage
-        issue(k + kStages);
-#pragma unroll
-        for (int j = 0; j < D / 64; ++j) {
-            // byte i of a word: dimensions 2i (low half) and 2i + 1; pair up the tokens of one dimension
-            uint32_t lo[2][4], hi[2][4];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const uint32_t x = v[2 * t][j], y = v[2 * t + 1][j];
-                pk::e2m1x8_to_half2((x & 0x0f0f0f0fu) | ((y << 4) & 0xf0f0f0f0u), lo[t]);
-                pk::e2m1x8_to_half2(((x >> 4) & 0x0f0f0f0fu) | (y & 0xf0f0f0f0u), hi[t]);
+            if (h == TG - 1) {
+                __syncwarp();  // every lane has read the stage
+                issue(k + S::kStages);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t a0 = hmul2(lo[0][i], vs[0]), a1 = hmul2(hi[0][i], vs[0]);
-                const uint32_t a2 = hmul2(lo[1][i], vs[1]), a3 = hmul2(hi[1][i], vs[1]);
+            for (int j = 0; j < D / 64; ++j) {
+                // byte i of a word: dimensions 2i (low half) and 2i + 1; pair up the tokens of one dimension
+                uint32_t lo[2][4], hi[2][4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma(o[nt][4 * j + i], a0, a1, a2, a3, pf[nt][0], pf[nt][1]);
+                for (int t = 0; t < 2; ++t) {
+                    const uint32_t y = v[2 * t][j], z = v[2 * t + 1][j];
+                    pk::e2m1x8_to_half2((y & 0x0f0f0f0fu) | ((z << 4) & 0xf0f0f0f0u), lo[t]);
+                    pk::e2m1x8_to_half2(((y >> 4) & 0x0f0f0f0fu) | (z & 0xf0f0f0f0u), hi[t]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t a0 = hmul2(lo[0][i], vs[0]), a1 = hmul2(hi[0][i], vs[0]);
+                    const uint32_t a2 = hmul2(lo[1][i], vs[1]), a3 = hmul2(hi[1][i], vs[1]);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma(o[nt][4 * j + i], a0, a1, a2, a3, pf[h][nt][0], pf[h][nt][1]);
+                }
             }
         }
+    };
+
+    uint32_t st = 0, turn = 0;
+#pragma unroll 1
+    for (uint32_t k = 0; k < mine; ++k) {
+        if (!pk::mbar_wait_warp(bar_s + 8 * st, turn & 1)) {
+            gave_up = true;
+            for (uint32_t i = k + 1; i < min(k + S::kStages, mine); ++i)  // no copy of its own stays in flight
+                pk::mbar_wait(bar_s + 8 * (i % S::kStages), (i / S::kStages) & 1);
+            break;
+        }
+        if ((int32_t)((g0 + (warp + k * kWarps) * TG) * 16) + 16 * TG - 1 > all_see)
+            step(k, st, std::true_type{});
+        else
+            step(k, st, std::false_type{});
+        if (++st == S::kStages) st = 0, ++turn;
     }
     if (gave_up && lane == 0) pk::set_status(a.status, PK_ERR_TIMEOUT);
     pk::pdl_launch_dependents();
@@ -445,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_attend_cache(const Args a) {
         for (int w = 0; w < kWarps; ++w) {
             const float f = ex2(s_ref[w][q] - m);
             const float2 y = *reinterpret_cast<const float2 *>(
-                reinterpret_cast<const float *>(smem + w * (kStages * G::kBytes)) + q * D + d);
+                reinterpret_cast<const float *>(smem + w * S::kRing) + q * D + d);
             l += f * s_sum[w][q];
             o0 += f * y.x;
             o1 += f * y.y;
@@ -471,81 +530,80 @@ __device__ __forceinline__ uint32_t live_splits(const Args &a, int32_t len) {
     return (n_gran + a.split_grans - 1) / a.split_grans;
 }
 
-// Joins the splits of one query row: a warp a row.
-template <int D, uint32_t DT>
-__global__ void __launch_bounds__(kThreads) k_cache_combine(const Args a, uint32_t tile_rows) {
-    const uint32_t lane = threadIdx.x & 31;
-    const uint64_t id = ((uint64_t)blockIdx.x * kThreads + threadIdx.x) >> 5;
-    const int32_t *kv_len = a.kv_len;
-    const float *part_o = a.part_o;
-    const float2 *part_ml = a.part_ml;
-    pk::pdl_wait(kv_len, part_o, part_ml);
-    pk::pdl_launch_dependents();
-    const uint64_t heads = (uint64_t)a.R * a.kv_heads;
-    if (id >= heads * a.rows) return;
-    const uint64_t rh = id / a.rows;
-    const uint32_t row = (uint32_t)(id % a.rows);
-    const uint32_t r = (uint32_t)(rh / a.kv_heads), head = (uint32_t)(rh % a.kv_heads);
-    const uint32_t n = live_splits(a, length_of(kv_len, r, a.page_stride * a.page_tokens));
-    const uint64_t first = (rh * a.row_tiles + row / tile_rows) * a.splits * tile_rows + row % tile_rows;
-    float m = -FLT_MAX;
-    for (uint32_t s = lane; s < n; s += 32) m = fmaxf(m, __ldcg(part_ml + first + (uint64_t)s * tile_rows).x);
-#pragma unroll
-    for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    constexpr int kPer = D / 32;
-    float l = 0.0f, o[kPer] = {};
-#pragma unroll 4
-    for (uint32_t s = 0; s < n; ++s) {
-        const uint64_t at = first + (uint64_t)s * tile_rows;
-        const float2 ml = __ldcg(part_ml + at);
-        const float f = ex2(ml.x - m);
-        l += f * ml.y;
-#pragma unroll
-        for (int i = 0; i < kPer; i += 2) {
-            const float2 y = __ldcg(reinterpret_cast<const float2 *>(part_o + at * D + lane * kPer + i));
-            o[i] += f * y.x;
-            o[i + 1] += f * y.y;
-        }
-    }
-    const uint32_t i = row / a.group, qh = head * a.group + row - i * a.group;
-    const float inv = l == 0.0f ? 0.0f : a.v_scale / l;
-    const int64_t t = (int64_t)r * a.n_q + i;
-#pragma unroll
-    for (int x = 0; x < kPer; x += 2)
-        *reinterpret_cast<uint32_t *>(a.out + t * a.o_ts + (int64_t)qh * a.o_hs + lane * kPer + x) =
-            pk::Elem<DT>::from2(o[x] * inv, o[x + 1] * inv);
-    if (lane == 0 && a.lse)
-        a.lse[t * (a.kv_heads * a.group) + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
-}
-
 constexpr uint32_t kStatRows = 512;
 
-// page_weight[r][j] += sum over heads, rows and granules of the page of
-// (granule's sum of p) * 2^(its ref - ref) / sum: a warp a page, lanes over
-// (head, row), in an order that depends on the sizes alone.
-__global__ void __launch_bounds__(kThreads) k_page_weights(const Args a, uint32_t tile_rows) {
+// The rest of a call, by block: the first ones join the splits of the query
+// rows (a warp a row), the others add to the pages' weights
+//     page_weight[r][j] += sum over heads, rows and granules of the page of
+//                          (granule's sum of p) * 2^(its ref - ref) / sum,
+// a warp a page, lanes over (head, row), in an order that depends on the sizes
+// alone.  Both need a row's final reference and sum over the splits; the
+// weighing blocks find them again, which costs less than waiting for a launch.
+template <int D, uint32_t DT>
+__global__ void __launch_bounds__(kFinishThreads) k_cache_finish(const Args a, uint32_t tile_rows, uint32_t join_blocks) {
     __shared__ float2 stat[kStatRows];  // (ref, 1 / sum) of (head, row)
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t blocks = (uint32_t)((a.page_stride + kWarps - 1) / kWarps);
-    const uint32_t r = blockIdx.x / blocks, page = (blockIdx.x % blocks) * kWarps + warp;
     const int32_t *kv_len = a.kv_len;
+    const float *part_o = a.part_o;
     const float2 *part_ml = a.part_ml, *gran_ml = a.gran_ml;
     float *weight = a.page_weight;
-    pk::pdl_wait(kv_len, part_ml, gran_ml, weight);
+    pk::pdl_wait(kv_len, part_o, part_ml, gran_ml, weight);
     pk::pdl_launch_dependents();
-    const int32_t len = length_of(kv_len, r, a.page_stride * a.page_tokens);
+    const uint64_t most = a.page_stride * a.page_tokens;
+    if (blockIdx.x < join_blocks) {
+        const uint64_t id = (uint64_t)blockIdx.x * kFinishWarps + warp;
+        if (id >= (uint64_t)a.R * a.kv_heads * a.rows) return;
+        const uint64_t rh = id / a.rows;
+        const uint32_t row = (uint32_t)(id % a.rows);
+        const uint32_t r = (uint32_t)(rh / a.kv_heads), head = (uint32_t)(rh % a.kv_heads);
+        const uint32_t n = live_splits(a, length_of(kv_len, r, most));
+        const uint64_t first = (rh * a.row_tiles + row / tile_rows) * a.splits * tile_rows + row % tile_rows;
+        float m = -FLT_MAX;
+        for (uint32_t s = lane; s < n; s += 32) m = fmaxf(m, __ldcg(part_ml + first + (uint64_t)s * tile_rows).x);
+#pragma unroll
+        for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        constexpr int kPer = D / 32;
+        float l = 0.0f, o[kPer] = {};
+#pragma unroll 4
+        for (uint32_t s = 0; s < n; ++s) {
+            const uint64_t at = first + (uint64_t)s * tile_rows;
+            const float2 ml = __ldcg(part_ml + at);
+            const float f = ex2(ml.x - m);
+            l += f * ml.y;
+#pragma unroll
+            for (int i = 0; i < kPer; i += 2) {
+                const float2 y = __ldcg(reinterpret_cast<const float2 *>(part_o + at * D + lane * kPer + i));
+                o[i] += f * y.x;
+                o[i + 1] += f * y.y;
+            }
+        }
+        const uint32_t i = row / a.group, qh = head * a.group + row - i * a.group;
+        const float inv = l == 0.0f ? 0.0f : a.v_scale / l;
+        const int64_t t = (int64_t)r * a.n_q + i;
+#pragma unroll
+        for (int x = 0; x < kPer; x += 2)
+            *reinterpret_cast<uint32_t *>(a.out + t * a.o_ts + (int64_t)qh * a.o_hs + lane * kPer + x) =
+                pk::Elem<DT>::from2(o[x] * inv, o[x + 1] * inv);
+        if (lane == 0 && a.lse)
+            a.lse[t * (a.kv_heads * a.group) + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+        return;
+    }
+    const uint32_t blocks = (uint32_t)((a.page_stride + kFinishWarps - 1) / kFinishWarps);
+    const uint32_t id = blockIdx.x - join_blocks, r = id / blocks, page0 = id % blocks * kFinishWarps;
+    const int32_t len = length_of(kv_len, r, most);
     const uint32_t n = live_splits(a, len), n_gran = ((uint32_t)len + 15) / 16;
-    if ((blockIdx.x % blocks) * kWarps * a.page_grans >= n_gran) return;  // uniform: no token in these pages
+    if ((uint64_t)page0 * a.page_grans >= n_gran) return;  // uniform: no token in these pages
     const uint32_t total = a.kv_heads * a.rows;
-    const uint32_t gr0 = page * a.page_grans, gr1 = min(gr0 + a.page_grans, n_gran);
+    const uint32_t page = page0 + warp, gr0 = page * a.page_grans, gr1 = min(gr0 + a.page_grans, n_gran);
     float acc = 0.0f;
     for (uint32_t base = 0; base < total; base += kStatRows) {
         __syncthreads();
-        for (uint32_t x = tid; x < kStatRows && base + x < total; x += kThreads) {
+        for (uint32_t x = tid; x < kStatRows && base + x < total; x += kFinishThreads) {
             const uint32_t head = (base + x) / a.rows, row = (base + x) % a.rows;
             const uint64_t first = (((uint64_t)r * a.kv_heads + head) * a.row_tiles + row / tile_rows) * a.splits *
                                        tile_rows + row % tile_rows;
             float m = -FLT_MAX, l = 0.0f;
+#pragma unroll 8
             for (uint32_t s = 0; s < n; ++s) {
                 const float2 ml = __ldcg(part_ml + first + (uint64_t)s * tile_rows);
                 const float to = fmaxf(m, ml.x);
@@ -560,7 +618,7 @@ __global__ void __launch_bounds__(kThreads) k_page_weights(const Args a, uint32_
             const float2 st = stat[x];
             const float2 *src = gran_ml + (((uint64_t)r * a.kv_heads + head) * a.row_tiles + row / tile_rows) *
                                               a.gran_stride * a.gran_rows + row % tile_rows;
-#pragma unroll 4
+#pragma unroll 8
             for (uint32_t gr = gr0; gr < gr1; ++gr) {
                 const float2 y = __ldcg(src + (uint64_t)gr * a.gran_rows);
                 acc += y.x * ex2(y.y - st.x) * st.y;
@@ -569,7 +627,7 @@ __global__ void __launch_bounds__(kThreads) k_page_weights(const Args a, uint32_
     }
 #pragma unroll
     for (int d = 16; d; d /= 2) acc += __shfl_xor_sync(0xffffffffu, acc, d);
-    if (lane == 0 && gr0 < gr1) weight[(uint64_t)r * a.page_stride + page] += acc;
+    if (lane == 0 && gr0 < n_gran) weight[(uint64_t)r * a.page_stride + page] += acc;
 }
 
 struct Plan {
@@ -581,8 +639,12 @@ uint64_t up16(uint64_t x) { return (x + 15) & ~15ull; }
 
 // How the call is cut.  Tiles of 8 query rows, or 16 where there are more: a
 // second column of tiles uses the dequantised values again.  Splits: enough
-// CTAs to fill 152 SMs twice over with two resident each, of at least two
-// granules a warp.
+// CTAs for kWaves rounds, so that requests of different lengths even out, but of
+// kMinGrans granules at least: below that a split's start and the join cost more
+// than it gives (128 x 2048 tokens, by least granules of a split: 32 74 us, 64
+// 67 us, 128 65 us).  Where that leaves places free, shorter ones down to
+// kLeastGrans fill them: the call then lasts as long as one split.
+constexpr uint64_t kWaves = 6, kMinGrans = 128, kLeastGrans = 32;
 Plan plan_of(const pk_kv_cache &kv, uint32_t R, uint32_t n_q, uint32_t q_heads, uint64_t page_stride, bool weigh) {
     Plan p;
     p.rows = q_heads / kv.kv_heads * n_q;
@@ -590,13 +652,13 @@ Plan plan_of(const pk_kv_cache &kv, uint32_t R, uint32_t n_q, uint32_t q_heads, 
     p.row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
     p.max_grans = (uint32_t)(page_stride * kv.page_tokens / 16);
     const uint64_t units = (uint64_t)R * kv.kv_heads * p.row_tiles;
-    const uint64_t want = units ? (152 * 4 + units - 1) / units : 1;
-    const uint64_t most = (p.max_grans + 2 * kWarps - 1) / (2 * kWarps);
-    uint64_t n = want < most ? want : most;
+    auto up = [](uint64_t x, uint64_t by) { return by ? (x + by - 1) / by : 1; };
+    uint64_t n = std::min(up(kSlots * kWaves, units), up(p.max_grans, kMinGrans));
+    if (units * n < kSlots) n = std::max(n, std::min(up(kSlots, units), up(p.max_grans, kLeastGrans)));
     if (n < 1) n = 1;
     p.split_grans = (uint32_t)((p.max_grans + n - 1) / n);
-    p.split_grans = (p.split_grans + kWarps - 1) / kWarps * kWarps;
-    if (p.split_grans == 0) p.split_grans = kWarps;
+    p.split_grans = (p.split_grans + 2 * kWarps - 1) / (2 * kWarps) * (2 * kWarps);  // whole steps of all warps
+    if (p.split_grans == 0) p.split_grans = 2 * kWarps;
     p.splits = p.max_grans ? (p.max_grans + p.split_grans - 1) / p.split_grans : 1;
     p.part_rows = units * p.splits * p.tile_rows;
     p.o_bytes = p.splits > 1 ? up16(p.part_rows * kv.head_dim * 4) : 0;
@@ -609,21 +671,17 @@ Plan plan_of(const pk_kv_cache &kv, uint32_t R, uint32_t n_q, uint32_t q_heads, 
 template <int D, int NT, uint32_t DT>
 cudaError_t launch(const Args &a, const Plan &p, cudaStream_t s) {
     void (*const kern)(Args) = a.page_weight ? k_attend_cache<D, NT, DT, true> : k_attend_cache<D, NT, DT, false>;
-    constexpr size_t smem = (size_t)kWarps * kStages * pk::Granule<D>::kBytes;
+    constexpr size_t smem = (size_t)kWarps * Shape<D, NT>::kRing;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     const uint64_t units = (uint64_t)a.R * a.kv_heads * p.row_tiles;
     if (units * p.splits > 0x7fffffffull) return cudaErrorInvalidValue;
     e = pk_launch_smem(kern, (unsigned)(units * p.splits), kThreads, smem, s, a);
-    if (e == cudaSuccess && p.splits > 1) {
-        const uint64_t blocks = ((uint64_t)a.R * a.kv_heads * p.rows + kWarps - 1) / kWarps;
-        e = pk_launch(k_cache_combine<D, DT>, (unsigned)blocks, kThreads, s, a, p.tile_rows);
-    }
-    if (e == cudaSuccess && a.page_weight && a.page_stride) {
-        const uint64_t blocks = (a.page_stride + kWarps - 1) / kWarps * a.R;
-        if (blocks > 0x7fffffffull) return cudaErrorInvalidValue;
-        e = pk_launch(k_page_weights, (unsigned)blocks, kThreads, s, a, p.tile_rows);
-    }
+    const uint64_t join = p.splits > 1 ? ((uint64_t)a.R * a.kv_heads * p.rows + kFinishWarps - 1) / kFinishWarps : 0;
+    const uint64_t weigh = a.page_weight ? (a.page_stride + kFinishWarps - 1) / kFinishWarps * a.R : 0;
+    if (join + weigh > 0x7fffffffull) return cudaErrorInvalidValue;
+    if (e == cudaSuccess && join + weigh)
+        e = pk_launch(k_cache_finish<D, DT>, (unsigned)(join + weigh), kFinishThreads, s, a, p.tile_rows, (uint32_t)join);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
