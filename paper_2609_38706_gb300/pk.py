@@ -489,64 +489,94 @@ def pk_table_load(ctx: int, src: torch.Tensor, stream=None) -> None:
     _check(lib().pk_table_load(ctx, _p(src), src.numel() * src.element_size(), _s(stream)), "pk_table_load")
 
 
+# -- KV pages ---------------------------------------------------------------------------------------------------------
+# A decode step makes several of these calls, so their marshalling is kept short: tensors are looked at once, and texts
+# of errors are made only when they are raised.
 _KV_DTYPES = {torch.bfloat16: PK_BF16, torch.float16: PK_FP16}
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _dtype(*tensors) -> int:
-    d = tensors[0].dtype
-    if d not in _KV_DTYPES or any(t.dtype != d for t in tensors):
-        raise PKError(PK_ERR_ARG, "16-bit tensors of one type (bfloat16 or float16)")
-    return _KV_DTYPES[d]
+def _stream_of(stream, t: torch.Tensor) -> Optional[int]:
+    """Handle of `stream`, or of the current stream of t's device."""
+    if stream is None and _raw_stream is not None and t.is_cuda:
+        return _raw_stream(t.device.index)
+    return _s(stream)
 
 
-def _heads(t: torch.Tensor) -> pk_heads:
-    """[tokens, heads, head_dim] (leading dimensions flattened by the caller), last dimension contiguous."""
-    if t.dim() == 3 and t.numel() == 0:
+def _refuse(where: str, what: str):
+    raise PKError(PK_ERR_ARG, f"{where}: {what}")
+
+
+def _ints(t: torch.Tensor, dtype, n: int, where: str, what: str) -> Optional[int]:
+    """Pointer of a contiguous array of n entries."""
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        _refuse(where, what)
+    return t.data_ptr() if n else None
+
+
+def _heads(t: torch.Tensor, where: str):
+    """pk_heads of [tokens, heads, head_dim], or [R, n, heads, head_dim] whose first two dimensions run on as one; the
+    last dimension contiguous."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 4:
+        a, b = stride[0], stride[1]
+        if shape[0] > 1 and shape[1] > 1 and a != shape[1] * b:
+            _refuse(where, "the first two dimensions do not run on as one")
+        n, ts = shape[0] * shape[1], b if shape[1] > 1 else a
+    elif len(shape) == 3:
+        n, ts = shape[0], stride[0]
+    else:
+        _refuse(where, "a [tokens, heads, head_dim] tensor")
+    if t.numel() == 0:
         return pk_heads(None, 0, 0)
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise PKError(PK_ERR_ARG, "a [tokens, heads, head_dim] tensor with contiguous rows")
-    ts, hs = t.stride(0), t.stride(1)
-    return pk_heads(_p(t), ts if t.shape[0] > 1 else 0, hs if t.shape[1] > 1 else 0)
+    if stride[-1] != 1 and shape[-1] > 1:
+        _refuse(where, "rows are not contiguous")
+    return pk_heads(t.data_ptr(), ts if n > 1 else 0, stride[-2] if shape[-2] > 1 else 0)
 
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise PKError(PK_ERR_ARG, what)
-
-
-def _i(t: torch.Tensor, dtype, n: int, what: str) -> Optional[int]:
-    """Pointer of a contiguous index array of n entries."""
-    _need(t.dtype == dtype and t.numel() == n and t.is_contiguous(), what)
-    return _p(t)
+def _dtype(where: str, first: torch.Tensor, *others) -> int:
+    d = first.dtype
+    for t in others:
+        if t.dtype is not d:
+            _refuse(where, "tensors of one type")
+    code = _KV_DTYPES.get(d)
+    if code is None:
+        _refuse(where, "16-bit tensors (bfloat16 or float16)")
+    return code
 
 
 def pk_kv_page_bytes(page_tokens: int, kv_heads: int, head_dim: int) -> int:
     return int(lib().pk_kv_page_bytes(page_tokens, kv_heads, head_dim))
 
 
-def _kv_move(fn: str, kv: pk_kv_cache, k, v, tok_off, start, pages, status, stream) -> None:
+def _kv_move(fn: str, call, kv: pk_kv_cache, k, v, tok_off, start, pages, status, stream) -> None:
     R = start.numel()
-    _need(k.shape == v.shape and k.dim() == 3 and tuple(k.shape[1:]) == (kv.kv_heads, kv.head_dim),
-          f"{fn}: k and v are [tokens, kv_heads, head_dim]")
-    _need(pages.dim() == 2 and pages.shape[0] == R, f"{fn}: pages is [R, page_stride]")
-    _check(getattr(lib(), fn)(ctypes.byref(kv), _dtype(k, v), ctypes.byref(_heads(k)), ctypes.byref(_heads(v)),
-                              k.shape[0], _i(tok_off, torch.int64, R + 1, f"{fn}: tok_off is int64[R+1]"),
-                              _i(start, torch.int32, R, f"{fn}: start is int32[R]"), R,
-                              _i(pages, torch.int32, pages.numel(), f"{fn}: pages is contiguous int32"),
-                              pages.shape[1], _p(status), _s(stream)), fn)
+    shape = k.shape
+    if v.shape != shape or len(shape) != 3 or shape[1] != kv.kv_heads or shape[2] != kv.head_dim:
+        _refuse(fn, "k and v are [tokens, kv_heads, head_dim]")
+    if pages.dim() != 2 or pages.shape[0] != R:
+        _refuse(fn, "pages is [R, page_stride]")
+    width = pages.shape[1]
+    rc = call(ctypes.byref(kv), _dtype(fn, k, v), ctypes.byref(_heads(k, fn)), ctypes.byref(_heads(v, fn)), shape[0],
+              _ints(tok_off, torch.int64, R + 1, fn, "tok_off is contiguous int64[R+1]"),
+              _ints(start, torch.int32, R, fn, "start is contiguous int32[R]"), R,
+              _ints(pages, torch.int32, R * width, fn, "pages is contiguous int32"), width, _p(status),
+              _stream_of(stream, k))
+    if rc:
+        _check(rc, fn)
 
 
 def pk_kv_write(kv: pk_kv_cache, k: torch.Tensor, v: torch.Tensor, tok_off: torch.Tensor, start: torch.Tensor,
                 pages: torch.Tensor, status: torch.Tensor, stream=None) -> None:
     """k, v: [tokens, kv_heads, head_dim] bf16 / fp16 (strided); tok_off: int64[R+1]; start: int32[R]; pages:
     int32 [R, page_stride] holding uint32 slots."""
-    _kv_move("pk_kv_write", kv, k, v, tok_off, start, pages, status, stream)
+    _kv_move("pk_kv_write", lib().pk_kv_write, kv, k, v, tok_off, start, pages, status, stream)
 
 
 def pk_kv_read(kv: pk_kv_cache, k: torch.Tensor, v: torch.Tensor, tok_off: torch.Tensor, start: torch.Tensor,
                pages: torch.Tensor, status: torch.Tensor, stream=None) -> None:
     """k, v: outputs; the other arguments as pk_kv_write."""
-    _kv_move("pk_kv_read", kv, k, v, tok_off, start, pages, status, stream)
+    _kv_move("pk_kv_read", lib().pk_kv_read, kv, k, v, tok_off, start, pages, status, stream)
 
 
 def pk_attend_prompt_scratch_bytes(R: int) -> int:
@@ -557,18 +587,21 @@ def pk_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: tor
                      lse: Optional[torch.Tensor], q_off: torch.Tensor, k_off: torch.Tensor, scale: float,
                      scratch: torch.Tensor, status: torch.Tensor, stream=None) -> None:
     """q, out: [n_q, q_heads, D]; k, v: [n_k, kv_heads, D]; q_off, k_off: int64[R+1]; lse: float32 [n_q, q_heads]."""
+    fn = "pk_attend_prompt"
     R = q_off.numel() - 1
-    _need(q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and q.shape == out.shape and q.shape[2] == k.shape[2],
-          "pk_attend_prompt: q, out [n_q, q_heads, D], k, v [n_k, kv_heads, D]")
-    _need(R >= 0, "pk_attend_prompt: q_off is int64[R+1]")
-    _need(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == tuple(q.shape[:2])),
-          "pk_attend_prompt: lse is contiguous float32 [n_q, q_heads]")
-    _check(lib().pk_attend_prompt(_dtype(q, k, v, out), ctypes.byref(_heads(q)), ctypes.byref(_heads(k)),
-                                  ctypes.byref(_heads(v)), ctypes.byref(_heads(out)), _p(lse), q.shape[0], k.shape[0],
-                                  _i(q_off, torch.int64, R + 1, "pk_attend_prompt: q_off is int64[R+1]"),
-                                  _i(k_off, torch.int64, R + 1, "pk_attend_prompt: k_off is int64[R+1]"), R,
-                                  q.shape[1], k.shape[1], q.shape[2], scale, _p(scratch), scratch.numel(), _p(status),
-                                  _s(stream)), "pk_attend_prompt")
+    qs, ks = q.shape, k.shape
+    if len(qs) != 3 or len(ks) != 3 or v.shape != ks or out.shape != qs or qs[2] != ks[2]:
+        _refuse(fn, "q, out [n_q, q_heads, D], k, v [n_k, kv_heads, D]")
+    if R < 0:
+        _refuse(fn, "q_off is int64[R+1]")
+    z = None if lse is None else _ints(lse, torch.float32, qs[0] * qs[1], fn, "lse is contiguous float32 [n_q, q_heads]")
+    rc = lib().pk_attend_prompt(_dtype(fn, q, k, v, out), ctypes.byref(_heads(q, fn)), ctypes.byref(_heads(k, fn)),
+                                ctypes.byref(_heads(v, fn)), ctypes.byref(_heads(out, fn)), z, qs[0], ks[0],
+                                _ints(q_off, torch.int64, R + 1, fn, "q_off is contiguous int64[R+1]"),
+                                _ints(k_off, torch.int64, R + 1, fn, "k_off is contiguous int64[R+1]"), R, qs[1],
+                                ks[1], qs[2], scale, _p(scratch), scratch.numel(), _p(status), _stream_of(stream, q))
+    if rc:
+        _check(rc, fn)
 
 
 def pk_attend_cache_scratch_bytes(kv: pk_kv_cache, R: int, n_q: int, q_heads: int, page_stride: int,
@@ -579,23 +612,29 @@ def pk_attend_cache_scratch_bytes(kv: pk_kv_cache, R: int, n_q: int, q_heads: in
 def pk_attend_cache(kv: pk_kv_cache, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor], n_q: int,
                     kv_len: torch.Tensor, pages: torch.Tensor, scale: float, page_weight: Optional[torch.Tensor],
                     scratch: torch.Tensor, status: torch.Tensor, stream=None) -> None:
-    """q, out: [R * n_q, q_heads, D]; lse: float32 [R * n_q, q_heads]; kv_len: int32[R]; pages: int32 and page_weight:
-    float32 [R, page_stride]."""
+    """q, out: [R * n_q, q_heads, D] or [R, n_q, q_heads, D]; lse: float32, R * n_q * q_heads; kv_len: int32[R]; pages:
+    int32 and page_weight: float32 [R, page_stride]."""
+    fn = "pk_attend_cache"
     R = kv_len.numel()
-    _need(q.dim() == 3 and q.shape == out.shape and q.shape[0] == R * n_q and q.shape[2] == kv.head_dim,
-          "pk_attend_cache: q, out [R * n_q, q_heads, head_dim]")
-    _need(pages.dim() == 2 and pages.shape[0] == R, "pk_attend_cache: pages is [R, page_stride]")
-    _need(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == tuple(q.shape[:2])),
-          "pk_attend_cache: lse is contiguous float32 [R * n_q, q_heads]")
-    _need(page_weight is None or (page_weight.dtype == torch.float32 and page_weight.is_contiguous() and
-                                  page_weight.shape == pages.shape),
-          "pk_attend_cache: page_weight is contiguous float32 [R, page_stride]")
-    _check(lib().pk_attend_cache(ctypes.byref(kv), _dtype(q, out), ctypes.byref(_heads(q)), ctypes.byref(_heads(out)),
-                                 _p(lse), R, n_q, q.shape[1], scale,
-                                 _i(kv_len, torch.int32, R, "pk_attend_cache: kv_len is int32[R]"),
-                                 _i(pages, torch.int32, pages.numel(), "pk_attend_cache: pages is contiguous int32"),
-                                 pages.shape[1], _p(page_weight), _p(scratch), scratch.numel(), _p(status),
-                                 _s(stream)), "pk_attend_cache")
+    qs = q.shape
+    if out.shape != qs or len(qs) not in (3, 4) or q.numel() != R * n_q * qs[-2] * qs[-1] or qs[-1] != kv.head_dim:
+        _refuse(fn, "q, out are [R * n_q, q_heads, head_dim]")
+    if pages.dim() != 2 or pages.shape[0] != R:
+        _refuse(fn, "pages is [R, page_stride]")
+    width = pages.shape[1]
+    z = None if lse is None else _ints(lse, torch.float32, R * n_q * qs[-2], fn, "lse is contiguous float32, R * n_q * q_heads")
+    w = None
+    if page_weight is not None:
+        if page_weight.shape != pages.shape:
+            _refuse(fn, "page_weight is [R, page_stride]")
+        w = _ints(page_weight, torch.float32, R * width, fn, "page_weight is contiguous float32")
+    rc = lib().pk_attend_cache(ctypes.byref(kv), _dtype(fn, q, out), ctypes.byref(_heads(q, fn)),
+                               ctypes.byref(_heads(out, fn)), z, R, n_q, qs[-2], scale,
+                               _ints(kv_len, torch.int32, R, fn, "kv_len is contiguous int32[R]"),
+                               _ints(pages, torch.int32, R * width, fn, "pages is contiguous int32"), width, w,
+                               _p(scratch), scratch.numel(), _p(status), _stream_of(stream, q))
+    if rc:
+        _check(rc, fn)
 
 
 def pk_evict_pages(pages: torch.Tensor, weight: torch.Tensor, kv_len: torch.Tensor, page_tokens: int, budget: int,
@@ -604,21 +643,26 @@ def pk_evict_pages(pages: torch.Tensor, weight: torch.Tensor, kv_len: torch.Tens
                    stream=None) -> None:
     """pages: int32 and weight: float32 [R, page_stride]; kv_len, kv_len_out: int32[R]; pages_out: int32 and
     weight_out: float32 [R, budget]; evicted: int32 [R, page_stride] or None."""
+    fn = "pk_evict_pages"
     R = kv_len.numel()
-    where = "pk_evict_pages"
-    _need(pages.dim() == 2 and pages.shape[0] == R and weight.shape == pages.shape and
-          (evicted is None or evicted.shape == pages.shape), f"{where}: pages, weight, evicted are [R, page_stride]")
-    _need(min(page_tokens, budget, sinks, recent) >= 0, f"{where}: counts are not negative")
-    _check(lib().pk_evict_pages(_i(pages, torch.int32, pages.numel(), f"{where}: pages is contiguous int32"),
-                                _i(weight, torch.float32, pages.numel(), f"{where}: weight is contiguous float32"),
-                                _i(kv_len, torch.int32, R, f"{where}: kv_len is int32[R]"), R, pages.shape[1],
-                                page_tokens, budget, sinks, recent,
-                                _i(pages_out, torch.int32, R * budget, f"{where}: pages_out is int32[R, budget]"),
-                                _i(weight_out, torch.float32, R * budget, f"{where}: weight_out is float32[R, budget]"),
-                                _i(kv_len_out, torch.int32, R, f"{where}: kv_len_out is int32[R]"),
-                                None if evicted is None else
-                                _i(evicted, torch.int32, pages.numel(), f"{where}: evicted is int32[R, page_stride]"),
-                                _p(status), _s(stream)), where)
+    if pages.dim() != 2 or pages.shape[0] != R or weight.shape != pages.shape:
+        _refuse(fn, "pages, weight are [R, page_stride]")
+    if page_tokens < 0 or budget < 0 or sinks < 0 or recent < 0:
+        _refuse(fn, "counts are not negative")
+    width = pages.shape[1]
+    n = R * width
+    rc = lib().pk_evict_pages(_ints(pages, torch.int32, n, fn, "pages is contiguous int32"),
+                              _ints(weight, torch.float32, n, fn, "weight is contiguous float32"),
+                              _ints(kv_len, torch.int32, R, fn, "kv_len is contiguous int32[R]"), R, width,
+                              page_tokens, budget, sinks, recent,
+                              _ints(pages_out, torch.int32, R * budget, fn, "pages_out is int32[R, budget]"),
+                              _ints(weight_out, torch.float32, R * budget, fn, "weight_out is float32[R, budget]"),
+                              _ints(kv_len_out, torch.int32, R, fn, "kv_len_out is int32[R]"),
+                              None if evicted is None else
+                              _ints(evicted, torch.int32, n, fn, "evicted is int32[R, page_stride]"), _p(status),
+                              _stream_of(stream, pages))
+    if rc:
+        _check(rc, fn)
 
 
 def pk_store_noalloc(table: torch.Tensor, capacity_log2: int, keys: torch.Tensor, slots: torch.Tensor,

@@ -9,7 +9,6 @@ per-batch buffers, all allocated with PyTorch, every step run by libpk.
 """
 from __future__ import annotations
 
-import contextlib
 from typing import Optional
 
 import numpy as np
@@ -32,10 +31,14 @@ def _dev(x, dtype, device) -> torch.Tensor:
     return torch.from_numpy(a).to(device=device)
 
 
-def _on(stream):
-    """Buffers made inside belong to `stream` (None: the current one), so that one freed while its kernel still runs
-    is only given out again to later work of that stream."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+def _empty(like: torch.Tensor, stream, *wanted) -> list:
+    """Buffers (shape, dtype) on like's device that belong to `stream` (None: the current one), so that one freed while
+    its kernel still runs is only given out again to later work of that stream."""
+    device = like.device
+    if stream is None:
+        return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
+    with torch.cuda.stream(stream):
+        return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
 
 
 class KeyTable:
@@ -251,6 +254,7 @@ class KVPages:
             raise pk.PKError(pk.PK_ERR_ARG, "KVPages: pool is contiguous uint8 [n_slots, pk_kv_page_bytes]")
         self.pool, self.device = pool, pool.device
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._scratch_bytes: dict = {}
         self.kv = pk.pk_kv_cache(pool.data_ptr(), n_slots, page_tokens, kv_heads, head_dim, k_scale, v_scale)
 
     @property
@@ -265,10 +269,10 @@ class KVPages:
 
     def read(self, tok_off, start, pages, n_tokens: int, dtype=torch.bfloat16):
         """(k, v) [n_tokens, kv_heads, head_dim]; rows that belong to no request are unspecified."""
-        with _on(self.stream):
-            kv = torch.empty((2, n_tokens, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
-        pk.pk_kv_read(self.kv, kv[0], kv[1], tok_off, start, pages, self.status, self.stream)
-        return kv[0], kv[1]
+        shape = (n_tokens, self.kv_heads, self.head_dim)
+        k, v = _empty(self.pool, self.stream, (shape, dtype), (shape, dtype))
+        pk.pk_kv_read(self.kv, k, v, tok_off, start, pages, self.status, self.stream)
+        return k, v
 
     def attend(self, q, kv_len, pages, scale: Optional[float] = None, weight: Optional[torch.Tensor] = None):
         """q [R, n_q, q_heads, head_dim] over the pages: (out like q, lse float32 [R, n_q, q_heads]).  weight
@@ -276,14 +280,16 @@ class KVPages:
         if q.dim() != 4:
             raise pk.PKError(pk.PK_ERR_ARG, "KVPages.attend: q is [R, n_q, q_heads, head_dim]")
         R, n_q, heads, D = q.shape
-        nbytes = pk.pk_attend_cache_scratch_bytes(self.kv, R, n_q, heads, pages.shape[-1], weight is not None)
-        with _on(self.stream):
-            out = torch.empty((R, n_q, heads, D), dtype=q.dtype, device=q.device)
-            lse = torch.empty((R, n_q, heads), dtype=torch.float32, device=q.device)
-            scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-        pk.pk_attend_cache(self.kv, q.flatten(0, 1), out.view(R * n_q, heads, D), lse.view(R * n_q, heads), n_q,
-                           kv_len, pages, D ** -0.5 if scale is None else scale, weight, scratch, self.status,
-                           self.stream)
+        key = (R, n_q, heads, pages.shape[-1], weight is not None)
+        nbytes = self._scratch_bytes.get(key)
+        if nbytes is None:
+            if len(self._scratch_bytes) >= 4096:
+                self._scratch_bytes.clear()
+            nbytes = self._scratch_bytes[key] = pk.pk_attend_cache_scratch_bytes(self.kv, *key)
+        out, lse, scratch = _empty(q, self.stream, (q.shape, q.dtype), (q.shape[:3], torch.float32),
+                                   ((nbytes,), torch.uint8))
+        pk.pk_attend_cache(self.kv, q, out, lse, n_q, kv_len, pages, D ** -0.5 if scale is None else scale, weight,
+                           scratch, self.status, self.stream)
         return out, lse
 
 
@@ -292,10 +298,7 @@ def attend_prompt(q, k, v, q_off, k_off, scale: Optional[float] = None, status: 
     """Causal attention over packed prompts (pk_attend_prompt): (out like q, lse float32 [n_q, q_heads]).  Without
     ``status`` a device-reported error leaves the outputs unspecified and is not reported."""
     nbytes = pk.pk_attend_prompt_scratch_bytes(max(q_off.numel() - 1, 0))
-    with _on(stream):
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-        scratch = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    out, lse, scratch = _empty(q, stream, (q.shape, q.dtype), (q.shape[:2], torch.float32), ((nbytes,), torch.uint8))
     pk.pk_attend_prompt(q, k, v, out, lse, q_off, k_off, q.shape[-1] ** -0.5 if scale is None else scale, scratch,
                         status, stream)
     return out, lse
@@ -305,12 +308,9 @@ def evict_pages(pages, weight, kv_len, page_tokens: int, budget: int, sinks: int
                 status: Optional[torch.Tensor] = None, stream=None):
     """Cut each request to `budget` pages by accumulated attention weight (pk_evict_pages): (pages [R, budget],
     weight [R, budget], kv_len [R], evicted slots like pages), unused places PK_NO_SLOT (-1) and 0."""
-    R = pages.shape[0]
-    with _on(stream):
-        pages_out = torch.empty((R, max(budget, 0)), dtype=torch.int32, device=pages.device)
-        weight_out = torch.empty((R, max(budget, 0)), dtype=torch.float32, device=pages.device)
-        kv_len_out = torch.empty(R, dtype=torch.int32, device=pages.device)
-        evicted = torch.empty(pages.shape, dtype=torch.int32, device=pages.device)
+    kept = (pages.shape[0], max(budget, 0))
+    pages_out, weight_out, kv_len_out, evicted = _empty(
+        pages, stream, (kept, torch.int32), (kept, torch.float32), (kept[:1], torch.int32), (pages.shape, torch.int32))
     pk.pk_evict_pages(pages, weight, kv_len, page_tokens, budget, sinks, recent, pages_out, weight_out, kv_len_out,
                       evicted, status, stream)
     return pages_out, weight_out, kv_len_out, evicted
