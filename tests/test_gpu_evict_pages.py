@@ -60,7 +60,8 @@ def weights(kind, shape, rng):
 @pytest.mark.parametrize("R,stride,C,budget,sinks,recent", [
     (1, 1, 16, 1, 0, 1), (3, 5, 16, 3, 1, 1), (7, 33, 48, 8, 0, 8), (5, 300, 16, 100, 4, 17), (4, 1024, 16, 1023, 1, 1),
     (6, 1025, 256, 512, 4, 32), (3, 5000, 16, 700, 0, 1), (2, 9001, 16, 9000, 3, 5), (3, 70, 16, 90, 2, 3),
-    (2, 40000, 16, 20001, 4, 64),
+    (2, 40000, 16, 20001, 4, 64), (3, 4096, 16, 1000, 1, 7), (3, 4097, 16, 4000, 0, 1), (2, 8192, 32, 4, 2, 2),
+    (2, 8193, 16, 77, 1, 1), (5, 1024, 16, 6, 3, 3),
 ])
 def test_matches_the_rule(kind, R, stride, C, budget, sinks, recent):
     rng = np.random.default_rng(31)
