@@ -515,8 +515,9 @@ size_t pk_kv_page_bytes(uint32_t page_tokens, uint32_t kv_heads, uint32_t head_d
  * scale, in 32-bit arithmetic: s = e4m3(min(a * fl(1/6) / g, 448)), code =
  * e2m1(x / (s * g)), both to nearest even and saturating (0 where s = 0).
  * Only the bytes of the named positions are written; two tokens given the
- * same place in one call leave either's bytes.  Device errors: offsets,
- * start, or a slot out of range (PK_ERR_ARG; that token is not written). */
+ * same place in one call leave either's bytes.  Positions are below 2^31 and
+ * page_stride * page_tokens.  Device errors: offsets, start, or a slot out of
+ * range (PK_ERR_ARG; that token is not written). */
 int pk_kv_write(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *k, const pk_heads *v, uint64_t n_tokens,
                 const int64_t *tok_off_dev, const int32_t *start_dev, uint32_t R, const uint32_t *pages_dev,
                 uint64_t page_stride, int32_t *status_dev, pk_stream stream);

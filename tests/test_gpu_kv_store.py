@@ -120,6 +120,17 @@ def test_strided_inputs_and_another_stream():
     again.write(head_major, x[1].cuda(), *args)
     assert torch.equal(kv.pool, again.pool)
     assert torch.equal(k, kv.read(*args, t)[0])
+    # rows that start on 16 bytes but not on 32
+    odd = torch.zeros(t * H * D + 16, dtype=x.dtype, device="cuda")[8:-8].view(t, H, D)
+    odd.copy_(x[0])
+    third = KVPages(kv.pool.shape[0], C, H, D, pool=torch.full_like(kv.pool, 0xA5))
+    third.write(odd, x[1].cuda(), *args)
+    assert torch.equal(kv.pool, third.pool)
+    from paper_2609_38706_gb300 import pk
+    v2 = torch.empty_like(k)
+    odd.zero_()
+    pk.pk_kv_read(kv.kv, odd, v2, *args, kv.status)
+    assert torch.equal(odd, k) and torch.equal(v2, v)
     kv.check(), other.check(), again.check()
 
 
