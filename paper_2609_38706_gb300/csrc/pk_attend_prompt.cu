@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <float.h>
 
+#include <type_traits>
+
 #include "pk_device.cuh"
 #include "pk_internal.h"
 #include "pk_kv.cuh"
@@ -15,8 +17,8 @@ namespace {
 constexpr int kRows = 128;      // (query token, head of the group) rows of a tile; an item is two tiles
 constexpr int kKeys = 128;      // keys of a tile
 constexpr int kThreads = 384;
-constexpr float kTop = 15.0f;   // p stays below 2^kTop (half: 2^16)
-constexpr float kBase = 8.0f;   // the largest p when the reference moves: 2^kBase
+constexpr float kTop = 32768.0f;  // a tile's weights of a row sum to no more, so each fits a half (65504)
+constexpr float kBase = 4.0f;     // the largest weight when the reference moves: 2^kBase, so a tile's 128 stay below 2^11
 constexpr int kPlanThreads = 1024;
 
 struct Args {
@@ -475,9 +477,9 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                 const bool edge = j * kKeys + kKeys - 1 > first_last;
                 const int32_t see = last - j * kKeys;  // columns up to here
                 uint32_t x[3][32];
-                // Chunk c of the scores, 32 keys.  Loads run ahead (1 and 2 behind 0's use, 3 behind 1's), as one takes
-                // hundreds of cycles while the tensor core works on the same memory.
-                auto chunk = [&](int c) -> uint32_t(&)[32] {
+                // Chunk c of the scores, 32 keys.  Loads run ahead (1 and 2 behind 0's use, 3 behind 1's).  Masked or
+                // not is known at compile time: as a branch around the masking it cost 170 of 1010 cycles a tile.
+                auto chunk = [&](int c, auto masked) -> uint32_t(&)[32] {
                     if (c == 0) pk::tmem_load32(ts, x[0]);
                     uint32_t(&y)[32] = x[c % 3];
                     if (c != 2) pk::tmem_wait_load(y);
@@ -488,17 +490,48 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                         pk::tmem_wait_load(x[2]);
                         pk::tmem_load32(ts + 96, x[0]);
                     }
-                    if (edge) {
+                    if (decltype(masked)::value) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             if (32 * c + i > see) y[i] = 0xff800000u;
                     }
                     return y;
                 };
-                // Moves the reference of the rows whose largest score has outgrown it; their sum and output so far
-                // are rescaled by a power of two.
-                auto move_ref = [&](float m) {
-                    const float next = m > ref + kTop ? ceilf(m) - kBase : ref;
+                auto largest = [&](auto masked) {
+                    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t(&y)[32] = chunk(c, masked);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) m4[i & 3] = fmaxf(m4[i & 3], __uint_as_float(y[i]));
+                    }
+                    return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale2;
+                };
+                // The weights by the reference so far, and their sum.
+                uint32_t p[2][32];
+                auto weigh = [&](auto masked) {
+                    const uint64_t ref2 = pack2(-ref, -ref);
+                    uint64_t sum2[2] = {0, 0};
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t(&y)[32] = chunk(c, masked);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            float2 z = unpack2(fma2(pack2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), scale22, ref2));
+                            z.x = ex2(z.x);
+                            z.y = ex2(z.y);
+                            sum2[i / 2 & 1] = add2(sum2[i / 2 & 1], pack2(z.x, z.y));
+                            p[c / 2][c % 2 * 16 + i / 2] = pk::Elem<DT>::from2(z.x, z.y);
+                        }
+                    }
+                    const float2 s0 = unpack2(sum2[0]), s1 = unpack2(sum2[1]);
+                    return (s0.x + s1.x) + (s0.y + s1.y);
+                };
+                // Moves the reference of the rows that `over` names to their largest score; their sum and output so
+                // far are rescaled by a power of two.
+                auto move_ref = [&](bool over) {
+                    const float m = edge ? largest(std::true_type{}) : largest(std::false_type{});
+                    const float next = over && m > -INFINITY ? ceilf(m) - kBase : ref;
                     const float f = ex2(ref - next);
                     ref = next;
                     sum *= f;
@@ -515,48 +548,18 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                         pk::tmem_store32(to + 32 * d, x[0]);
                     }
                 };
-                if (j == 0) {  // a first reference
-                    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t(&y)[32] = chunk(c);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) m4[i & 3] = fmaxf(m4[i & 3], __uint_as_float(y[i]));
-                    }
-                    move_ref(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale2);
-                }
-                // One pass over the scores takes both the weights by the reference so far and the maximum; only where
-                // that shows a weight of 2^kTop or more is the reference moved and the pass done again.
-                uint32_t p[2][32];
-                uint64_t sum2[2];
-#pragma unroll 1
-                for (;;) {
-                    const uint64_t ref2 = pack2(-ref, -ref);
-                    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    sum2[0] = sum2[1] = 0;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t(&y)[32] = chunk(c);
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            m4[i / 2 & 3] = fmaxf(fmaxf(m4[i / 2 & 3], __uint_as_float(y[i])), __uint_as_float(y[i + 1]));
-                            float2 z = unpack2(fma2(pack2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), scale22, ref2));
-                            z.x = ex2(z.x);
-                            z.y = ex2(z.y);
-                            sum2[i / 2 & 1] = add2(sum2[i / 2 & 1], pack2(z.x, z.y));
-                            p[c / 2][c % 2 * 16 + i / 2] = pk::Elem<DT>::from2(z.x, z.y);
-                        }
-                    }
-                    const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale2;
-                    if (!__any_sync(0xffffffffu, m > ref + kTop)) break;
-                    move_ref(m);
+                if (j == 0) move_ref(true);
+                // One pass over the scores takes the weights by the reference so far, with no look at the scores
+                // first: a weight that has outgrown it shows in the sum, and only then the reference is moved and
+                // the pass done again.
+                float part = edge ? weigh(std::true_type{}) : weigh(std::false_type{});
+                while (__any_sync(0xffffffffu, part > kTop)) {
+                    move_ref(part > kTop);
                     if (!ok) break;
+                    part = edge ? weigh(std::true_type{}) : weigh(std::false_type{});
                 }
                 if (!ok) break;
-                {
-                    const float2 s0 = unpack2(sum2[0]), s1 = unpack2(sum2[1]);
-                    sum += (s0.x + s1.x) + (s0.y + s1.y);
-                }
+                sum += part;
                 pk::tmem_store32(ts, p[0]);  // over the scores, which every pass is done with
                 pk::tmem_store32(ts + 32, p[1]);
                 pk::tmem_wait_store();
