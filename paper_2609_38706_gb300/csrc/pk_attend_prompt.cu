@@ -26,12 +26,23 @@ struct Args {
     int64_t o_ts, o_hs;
     float *lse;
     const int64_t *q_off, *k_off;
-    uint64_t *tile_off;  // [R + 1]: items of one KV head in the requests before r
+    uint64_t *tile_off;  // [R + 1]: items of one KV head in the requests before r; NULL for up to 32 requests
     uint32_t R, q_heads, kv_heads, group;
+    uint64_t n_q, n_k;
     uint32_t tile_tokens, tile_heads, chunks;  // of a tile; tiles that it takes for a group's heads
     float scale2;  // scale * log2 e
     int32_t *status;
 };
+
+__device__ __forceinline__ bool bad_offsets(int64_t qa, int64_t qb, int64_t ka, int64_t kb, uint64_t n_q,
+                                            uint64_t n_k) {
+    return qa < 0 || qb < qa || (uint64_t)qb > n_q || ka < 0 || kb < ka || (uint64_t)kb > n_k;
+}
+
+// Items of one KV head in a request of n queries.
+__device__ __forceinline__ uint32_t items_of(int64_t n, uint32_t item_tokens, uint32_t chunks) {
+    return ((uint32_t)n + item_tokens - 1) / item_tokens * chunks;
+}
 
 // tile_off: how many items of one KV head the requests before each one have;
 // all zero where an offset is out of order or range.
@@ -52,10 +63,10 @@ k_prompt_tiles(const int64_t *q_off, const int64_t *k_off, uint32_t R, uint64_t 
         if (r < R) {
             const int64_t a = __ldcg(q_off + r), b = __ldcg(q_off + r + 1);
             const int64_t e = __ldcg(k_off + r), f = __ldcg(k_off + r + 1);
-            if (a < 0 || b < a || (uint64_t)b > n_q || e < 0 || f < e || (uint64_t)f > n_k)
+            if (bad_offsets(a, b, e, f, n_q, n_k))
                 bad = 1;
             else
-                n = ((uint64_t)(b - a) + item_tokens - 1) / item_tokens * chunks;
+                n = items_of(b - a, item_tokens, chunks);
         }
         uint64_t scan = n;
 #pragma unroll
@@ -87,7 +98,7 @@ __device__ __forceinline__ float ex2(float x) {
     return r;
 }
 
-// Shared memory of a CTA, from a 1024-byte boundary: Q (two tiles), then the ring of K and V tiles.
+// Shared memory of a CTA, from a 1024-byte boundary: Q (two tiles), the ring of K and V tiles, then Small.
 template <int D>
 struct Layout {
     static constexpr uint32_t kTile = 128 * D * 2;  // 128 rows; blocks of [128][64] values, 16 KB each
@@ -102,10 +113,38 @@ struct Small {
     uint64_t s_full[2], p_ready[2], o_done[2];
     uint64_t edge_v[4];            // an edge tile's V loaded, by edge tile
     uint32_t tmem, abort;
+    int32_t work[8][2];            // by item with keys: key tiles of its two tiles, for the matrix warp; 0, 0 ends it
     uint32_t epilogues[8];         // by softmax warp: items whose outputs it has written
     uint32_t any_bad[2][2];        // by item parity and half of the dimensions: bad_row holds something
     int32_t bad_row[2][128];       // first key of an edge tile whose V is not finite, by dimension
+    uint64_t item_end[32];         // up to 32 requests: items of one KV head in those up to each, and where they lie
+    int32_t q_start[32], k_start[32], q_len[32], k_len[32];
 };
+
+// Up to 32 requests every CTA counts the items itself, a lane a request, and keeps
+// the list in shared memory: no launch of k_prompt_tiles, and no loads to wait for
+// at each item.
+__device__ __forceinline__ void count_items(const Args &a, Small &sm, const int64_t *q_off, const int64_t *k_off) {
+    const uint32_t lane = threadIdx.x & 31;
+    int64_t qa = 0, qb = 0, ka = 0, kb = 0;
+    if (lane < a.R) {
+        qa = __ldcg(q_off + lane), qb = __ldcg(q_off + lane + 1);
+        ka = __ldcg(k_off + lane), kb = __ldcg(k_off + lane + 1);
+    }
+    const bool bad = __any_sync(0xffffffffu, bad_offsets(qa, qb, ka, kb, a.n_q, a.n_k));
+    if (bad && lane == 0) pk::set_status(a.status, PK_ERR_ARG);
+    uint64_t scan = bad ? 0 : items_of(qb - qa, 2 * a.tile_tokens, a.chunks);
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const uint64_t o = __shfl_up_sync(0xffffffffu, scan, d);
+        if (lane >= (uint32_t)d) scan += o;
+    }
+    sm.item_end[lane] = scan;
+    sm.q_start[lane] = (int32_t)qa;
+    sm.k_start[lane] = (int32_t)ka;
+    sm.q_len[lane] = (int32_t)(qb - qa);
+    sm.k_len[lane] = (int32_t)(kb - ka);
+}
 
 // One item: 2 tiles of `tokens` query tokens times `heads` heads of one group.
 struct Item {
@@ -116,20 +155,31 @@ struct Item {
 // The turn-th item of this CTA.  Items come heaviest first within a request, so
 // every other turn runs through the CTAs backwards: one that got the heaviest of
 // a turn gets the lightest of the next (two prompts of 8192: 855 -> 830 us when added).
-__device__ __forceinline__ bool find_item(const Args &a, const uint64_t *tile_off, const int64_t *q_off,
+__device__ __forceinline__ bool find_item(const Args &a, const Small &sm, const uint64_t *tile_off, const int64_t *q_off,
                                           const int64_t *k_off, uint32_t turn, Item &it) {
-    const uint64_t total = __ldcg(tile_off + a.R) * a.kv_heads;
     const uint64_t index = (uint64_t)turn * gridDim.x + (turn & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-    if (index >= total) return false;
     const uint64_t tile = index / a.kv_heads;
-    const uint32_t r = pk::warp_find_request(reinterpret_cast<const int64_t *>(tile_off), a.R, (int64_t)tile);
-    it.head = (int32_t)(index % a.kv_heads);
-    it.q0 = (int32_t)__ldcg(q_off + r);
-    it.k0 = (int32_t)__ldcg(k_off + r);
-    it.lq = (int32_t)__ldcg(q_off + r + 1) - it.q0;
-    it.lk = (int32_t)__ldcg(k_off + r + 1) - it.k0;
+    it.head = (int32_t)(index - tile * a.kv_heads);
+    uint64_t x;  // which of the request's items
+    if (tile_off) {
+        if (tile >= __ldcg(tile_off + a.R)) return false;
+        const uint32_t r = pk::warp_find_request(reinterpret_cast<const int64_t *>(tile_off), a.R, (int64_t)tile);
+        it.q0 = (int32_t)__ldcg(q_off + r);
+        it.k0 = (int32_t)__ldcg(k_off + r);
+        it.lq = (int32_t)__ldcg(q_off + r + 1) - it.q0;
+        it.lk = (int32_t)__ldcg(k_off + r + 1) - it.k0;
+        x = __ldcg(tile_off + r + 1) - 1 - tile;
+    } else {
+        const uint32_t lane = threadIdx.x & 31;
+        const uint32_t r = __popc(__ballot_sync(0xffffffffu, sm.item_end[lane] <= tile));
+        if (r >= 32) return false;  // (requests past R repeat the total)
+        it.q0 = sm.q_start[r];
+        it.k0 = sm.k_start[r];
+        it.lq = sm.q_len[r];
+        it.lk = sm.k_len[r];
+        x = sm.item_end[r] - 1 - tile;
+    }
     // the last queries first: they have the most keys
-    const uint64_t x = __ldcg(tile_off + r + 1) - 1 - tile;
     it.chunk = (int32_t)(x % a.chunks);
     it.tok0 = (int32_t)(x / a.chunks) * 2 * (int32_t)a.tile_tokens;
 #pragma unroll
@@ -185,11 +235,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                 const __grid_constant__ CUtensorMap map_v) {
     using L = Layout<D>;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ Small sm;
-    const uint32_t smem = (pk::smem_addr(smem_raw) + 1023) & ~1023u;
-    uint8_t *smem_p = smem_raw + (smem - pk::smem_addr(smem_raw));
+    // all the shared memory that the kernel has, so that it starts on the swizzle's 1024 bytes
+    extern __shared__ __align__(1024) uint8_t smem_p[];
+    Small &sm = *reinterpret_cast<Small *>(smem_p + L::kBytes);
+    const uint32_t smem = pk::smem_addr(smem_p);
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = pk::uniform(tid >> 5);
+    if (smem & 1023) {
+        if (tid == 0) pk::set_status(a.status, PK_ERR_CUDA);
+        return;
+    }
 
     if (tid == 0) {
         for (uint32_t i = 0; i < L::kStages; ++i) {
@@ -209,14 +263,15 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
         for (int i = 0; i < 8; ++i) sm.epilogues[i] = 0;
     }
     if (warp == kWarpMma) pk::tmem_alloc(pk::smem_addr(&sm.tmem), 512);
-    pk::tmem_fence_before();
-    __syncthreads();
-    pk::tmem_fence_after();
-    const uint32_t tmem = pk::uniform(sm.tmem);
     const uint64_t *tile_off = a.tile_off;
     const int64_t *q_off = a.q_off, *k_off = a.k_off;
     pk::pdl_wait(tile_off, q_off, k_off);
     pk::pdl_launch_dependents();
+    if (warp == kWarpLoad && !tile_off) count_items(a, sm, q_off, k_off);
+    pk::tmem_fence_before();
+    __syncthreads();
+    pk::tmem_fence_after();
+    const uint32_t tmem = pk::uniform(sm.tmem);
 
     volatile uint32_t *abort = &sm.abort;
     auto give_up = [&]() {
@@ -226,15 +281,19 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
 
     Item it;
     uint32_t turn = 0;
-    bool more = find_item(a, tile_off, q_off, k_off, turn, it);
+    bool more = find_item(a, sm, tile_off, q_off, k_off, turn, it);
     if (warp >= kWarpLoad) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
         if (warp == kWarpLoad) {
-            uint32_t n = 0, edges = 0, nq[2] = {0, 0};  // ring stages, edge tiles and Q tiles loaded so far
+            uint32_t n = 0, edges = 0, nq[2] = {0, 0}, items = 0;  // ring stages, edge tiles, Q tiles, items so far
             bool ok = true;
             pk::fence_proxy_async();
             while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
-                if (lane == 0) {
+                if (lane == 0 && it.n_all > 0) {
+                    // its reader, at most four items behind, sees it by way of the first K tile's barrier
+                    sm.work[items & 7][0] = it.n_tiles[0];
+                    sm.work[items & 7][1] = it.n_tiles[1];
+                    ++items;
                     const uint32_t q_bytes = a.tile_tokens * a.tile_heads * 128 * (D / 64);
                     for (int32_t j = 0; ok && j < it.n_all; ++j) {
 #pragma unroll
@@ -275,9 +334,18 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                 }
                 ok = __all_sync(0xffffffffu, ok);
                 ++turn;
-                more = find_item(a, tile_off, q_off, k_off, turn, it);
+                more = find_item(a, sm, tile_off, q_off, k_off, turn, it);
             }
             if (lane == 0) {
+                const uint32_t st = n % L::kStages;
+                ok = ok && (n < L::kStages ||
+                            pk::mbar_wait(pk::smem_addr(&sm.empty[st]), (n / L::kStages + 1) & 1));
+                if (ok) {  // the matrix warp's end: a stage without a tile
+                    sm.work[items & 7][0] = sm.work[items & 7][1] = 0;
+                    pk::mbar_arrive(pk::smem_addr(&sm.full[st]));
+                    pk::mbar_arrive(pk::smem_addr(&sm.full[st]));
+                    ++n;
+                }
                 if (!ok) give_up();
                 // no copy of its own stays in flight
                 for (uint32_t i = n > L::kStages ? n - L::kStages : 0; i < n; ++i)
@@ -327,25 +395,23 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                 if (pk::elect_lane()) pk::mma_commit(pk::smem_addr(&sm.empty[st]));
                 __syncwarp();
             };
-            while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
-                const int32_t n0 = (int32_t)pk::uniform(it.n_tiles[0]), n1 = (int32_t)pk::uniform(it.n_tiles[1]);
+            for (uint32_t items = 0; ok && !__any_sync(0xffffffffu, *abort != 0); ++items) {
+                ok = wait_full(ring, use);
+                if (!ok) break;
+                const int32_t n0 = (int32_t)pk::uniform(sm.work[items & 7][0]);
+                const int32_t n1 = (int32_t)pk::uniform(sm.work[items & 7][1]);
                 const int32_t n_all = max(n0, n1);
-                if (n_all) {
-                    ok = wait_full(ring, use);
-                    if (ok && n0 > 0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.q_full[0]), nq0++ & 1))) {
-                        pk::tmem_fence_after();
-                        qk(0, ring, n0 == 1);
-                    }
-                    if (ok && n1 > 0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.q_full[1]), nq1++ & 1))) {
-                        pk::tmem_fence_after();
-                        qk(1, ring, n1 == 1);
-                    }
-                    if (ok) release(ring);
-                    advance(1);
+                if (n_all == 0) break;
+                if (n0 > 0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.q_full[0]), nq0++ & 1))) {
+                    pk::tmem_fence_after();
+                    qk(0, ring, n0 == 1);
                 }
-                // the next item is looked up while the first scores are weighed
-                ++turn;
-                more = find_item(a, tile_off, q_off, k_off, turn, it);
+                if (ok && n1 > 0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.q_full[1]), nq1++ & 1))) {
+                    pk::tmem_fence_after();
+                    qk(1, ring, n1 == 1);
+                }
+                if (ok) release(ring);
+                advance(1);
                 for (int32_t j = 0; ok && j < n_all; ++j) {
                     const uint32_t sv = ring, uv = use;
                     advance(1);
@@ -441,7 +507,7 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                 base += 2 * it.n_all;
                 ++items;
                 ++turn;
-                more = find_item(a, tile_off, q_off, k_off, turn, it);
+                more = find_item(a, sm, tile_off, q_off, k_off, turn, it);
             }
             if (!ok && lane == 0) give_up();
         }
@@ -467,7 +533,7 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
             const uint32_t qh = it.head * a.group + gh;
             const bool notes = it.first_edge < n_tiles;  // only then are this item's notes sure to be there
             ++turn;
-            more = find_item(a, tile_off, q_off, k_off, turn, it);  // the next one
+            more = find_item(a, sm, tile_off, q_off, k_off, turn, it);  // the next one
             float ref = -FLT_MAX, sum = 0.0f;
 #pragma unroll 1
             for (int32_t j = 0; j < n_tiles; ++j, ++ni) {
@@ -648,7 +714,8 @@ cudaError_t map_of(CUtensorMap *map, const pk_heads &h, uint64_t n, uint32_t hea
 template <int D, uint32_t DT>
 cudaError_t launch(const Args &a, unsigned grid, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv,
                    cudaStream_t s) {
-    constexpr size_t smem = Layout<D>::kBytes + 1024;
+    constexpr size_t smem = Layout<D>::kBytes + sizeof(Small);
+    static_assert(smem <= 227 * 1024, "shared memory of a block");
     const cudaError_t e = cudaFuncSetAttribute(k_attend_prompt<D, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     return e != cudaSuccess ? e : pk_launch_smem(k_attend_prompt<D, DT>, grid, kThreads, smem, s, a, mq, mk, mv);
 }
@@ -665,8 +732,10 @@ cudaError_t pk_launch_attend_prompt(uint32_t dtype, const pk_heads &q, const pk_
     a.lse = lse;
     a.q_off = q_off;
     a.k_off = k_off;
-    a.tile_off = static_cast<uint64_t *>(scratch);
+    a.tile_off = R > 32 ? static_cast<uint64_t *>(scratch) : nullptr;
     a.R = R;
+    a.n_q = n_q;
+    a.n_k = n_k;
     a.q_heads = q_heads;
     a.kv_heads = kv_heads;
     a.group = q_heads / kv_heads;
@@ -687,8 +756,9 @@ cudaError_t pk_launch_attend_prompt(uint32_t dtype, const pk_heads &q, const pk_
         (n_k && (e = map_of(&mv, v, n_k, kv_heads, head_dim, dtype, kKeys, 1)) != cudaSuccess))
         return e;
     const uint32_t item_tokens = 2 * a.tile_tokens;
-    e = pk_launch(k_prompt_tiles, 1, kPlanThreads, s, q_off, k_off, R, n_q, n_k, item_tokens, a.chunks, a.tile_off,
-                  status);
+    if (a.tile_off)
+        e = pk_launch(k_prompt_tiles, 1, kPlanThreads, s, q_off, k_off, R, n_q, n_k, item_tokens, a.chunks,
+                      a.tile_off, status);
     if (e != cudaSuccess) return e;
     // every request rounds its tokens up to whole items: at most one more each
     const uint64_t items = (n_q / item_tokens + R) * a.chunks * kv_heads;

@@ -65,6 +65,8 @@ CASES = [
     ([3], [130], 1, 129, 64, "bf16"),              # a group larger than a tile's rows
     ([0], [0], 1, 1, 64, "bf16"),
     ([300] * 7, [300] * 7, 2, 2, 128, "bf16"),
+    ([3, 0, 40] * 11, [5, 2, 90] * 11, 2, 3, 64, "fp16"),  # more requests than a warp has lanes
+    ([2] * 32, [9] * 32, 1, 1, 128, "bf16"),
 ]
 
 
@@ -133,6 +135,17 @@ def test_strided_tensors():
     assert torch.all(whole[:, :, D:] == 7.0) and int(status.item()) == 0
 
 
+def test_keys_broadcast_over_heads():
+    """One head's keys and values for every KV head, as expanded tensors (stride 0)."""
+    from paper_2609_38706_gb300 import service
+    lq = [70, 33]
+    q, k, v = (x.cuda() for x in inputs(lq, lq, 1, 6, 64, "bf16", 20))
+    off = dev(offs(lq))
+    one, _ = service.attend_prompt(q, k, v, off, off)
+    three, _ = service.attend_prompt(q, k.expand(-1, 3, -1), v.expand(-1, 3, -1), off, off)
+    assert torch.equal(one, three)
+
+
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
 @pytest.mark.parametrize("D,G", [(64, 1), (128, 4)])
 def test_masked_places_do_not_leak(value, D, G):
@@ -175,21 +188,23 @@ def test_outputs_repeat_and_other_rows_stay():
     assert torch.all(outs[0][0][154:] == 3.0) and torch.all(outs[0][1][154:] == 3.0)
 
 
+@pytest.mark.parametrize("many_requests", [0, 50])
 @pytest.mark.parametrize("what", ["q order", "k range", "k negative"])
-def test_bad_offsets_write_nothing(what):
+def test_bad_offsets_write_nothing(what, many_requests):
     from paper_2609_38706_gb300 import pk, service
     lq = [30, 30]
     q, k, v = (x.cuda() for x in inputs(lq, lq, 1, 1, 64, "fp16", 17))
-    qo, ko = offs(lq), offs(lq)
+    many = np.full(many_requests, 60, np.int64)  # empty requests behind the two
+    qo, ko = np.concatenate((offs(lq), many)), np.concatenate((offs(lq), many))
     if what == "q order":
         qo[1] = 70
     elif what == "k range":
-        ko[2] = 61
+        ko[2:] = 61
     else:
         ko[0] = -1
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     out = torch.full_like(q, 5.0)
-    scratch = torch.empty(pk.pk_attend_prompt_scratch_bytes(2), dtype=torch.uint8, device="cuda")
+    scratch = torch.empty(pk.pk_attend_prompt_scratch_bytes(len(qo) - 1), dtype=torch.uint8, device="cuda")
     pk.pk_attend_prompt(q, k, v, out, None, dev(qo), dev(ko), 1.0, scratch, status)
     assert int(status.item()) == pk.PK_ERR_ARG and torch.all(out == 5.0)
 

@@ -42,14 +42,19 @@ class Cta:
         self.stage, self.q = [None] * stages, [None, None]
         self.copies, self.pipe = [], []   # in flight; the pipe runs in order
         self.sp, self.o = [None, None], [None, None]
+        self.work = [None] * 8
         self.epilogues, self.notes = [0] * 8, [None, None]
         self.stored = [set(), set()]
         self.speed = rng.choice((0.5, 0.02)), rng.choice((0.5, 0.05))
         self.rescale = rng.choice((0.0, 0.3))
 
     def loader(self):
-        n, edges, nq = 0, 0, [0, 0]
+        n, edges, nq, sent = 0, 0, [0, 0], 0
         for x, (n0, n1, fe) in enumerate(self.items):
+            if max(n0, n1):
+                assert self.work[sent & 7] is None, "an item's note overwritten before it was read"
+                self.work[sent & 7] = x
+                sent += 1
             for j in range(max(n0, n1)):
                 for kv in (0, 1):
                     st = n % self.S
@@ -75,6 +80,14 @@ class Cta:
                     self.copies.append((self.q, t, x, self.q_full[t]))
                     nq[t] += 1
                     yield
+        st = n % self.S
+        while n >= self.S and not self.empty[st].done((n // self.S + 1) & 1):
+            yield
+        self.work[sent & 7] = "end"
+        for _ in range(2):
+            self.full[st].arrive()
+            yield
+        n += 1
         for i in range(max(0, n - self.S), n):
             while not self.full[i % self.S].done((i // self.S) & 1):
                 yield
@@ -94,17 +107,23 @@ class Cta:
             if last:
                 self.pipe.append(("commit", self.q_empty[t]))
 
-        for x, (n0, n1, _) in enumerate(self.items):
+        taken = 0
+        while True:
+            yield from wait_full(base)
+            x = self.work[taken & 7]
+            self.work[taken & 7] = None
+            taken += 1
+            if x == "end":
+                return
+            n0, n1, _ = self.items[x]
             nt, n_all = (n0, n1), max(n0, n1)
-            if n_all:
-                yield from wait_full(base)
-                for t in (0, 1):
-                    if nt[t]:
-                        while not self.q_full[t].done(nq[t] & 1):
-                            yield
-                        nq[t] += 1
-                        qk(x, t, 0, base, nt[t] == 1)
-                self.pipe.append(("commit", self.empty[base % self.S]))
+            for t in (0, 1):
+                if nt[t]:
+                    while not self.q_full[t].done(nq[t] & 1):
+                        yield
+                    nq[t] += 1
+                    qk(x, t, 0, base, nt[t] == 1)
+            self.pipe.append(("commit", self.empty[base % self.S]))
             yield
             for j in range(n_all):
                 nv, nk = base + 2 * j + 1, base + 2 * j + 2
