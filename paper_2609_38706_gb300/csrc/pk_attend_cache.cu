@@ -672,7 +672,8 @@ template <int D, int NT, uint32_t DT>
 cudaError_t launch(const Args &a, const Plan &p, cudaStream_t s) {
     void (*const kern)(Args) = a.page_weight ? k_attend_cache<D, NT, DT, true> : k_attend_cache<D, NT, DT, false>;
     constexpr size_t smem = (size_t)kWarps * Shape<D, NT>::kRing;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static std::atomic<uint64_t> seen[2] = {};
+    cudaError_t e = pk_allow_smem(kern, smem, seen[a.page_weight != nullptr]);
     if (e != cudaSuccess) return e;
     const uint64_t units = (uint64_t)a.R * a.kv_heads * p.row_tiles;
     if (units * p.splits > 0x7fffffffull) return cudaErrorInvalidValue;

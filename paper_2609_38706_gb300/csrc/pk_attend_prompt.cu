@@ -24,11 +24,13 @@ constexpr int kPlanThreads = 1024;
 struct Args {
     uint16_t *out;
     int64_t o_ts, o_hs;
+    bool wide_out;  // every 16 values of out start on 32 bytes
     float *lse;
     const int64_t *q_off, *k_off;
     uint64_t *tile_off;  // [R + 1]: items of one KV head in the requests before r; NULL for up to 32 requests
     uint32_t R, q_heads, kv_heads, group;
     uint64_t n_q, n_k;
+    uint32_t most_items;  // no call has more
     uint32_t tile_tokens, tile_heads, chunks;  // of a tile; tiles that it takes for a group's heads
     float scale2;  // scale * log2 e
     int32_t *status;
@@ -117,7 +119,7 @@ struct Small {
     uint32_t epilogues[8];         // by softmax warp: items whose outputs it has written
     uint32_t any_bad[2][2];        // by item parity and half of the dimensions: bad_row holds something
     int32_t bad_row[2][128];       // first key of an edge tile whose V is not finite, by dimension
-    uint64_t item_end[32];         // up to 32 requests: items of one KV head in those up to each, and where they lie
+    uint32_t item_end[32];         // up to 32 requests: items of one KV head in those up to each, and where they lie
     int32_t q_start[32], k_start[32], q_len[32], k_len[32];
 };
 
@@ -133,10 +135,10 @@ __device__ __forceinline__ void count_items(const Args &a, Small &sm, const int6
     }
     const bool bad = __any_sync(0xffffffffu, bad_offsets(qa, qb, ka, kb, a.n_q, a.n_k));
     if (bad && lane == 0) pk::set_status(a.status, PK_ERR_ARG);
-    uint64_t scan = bad ? 0 : items_of(qb - qa, 2 * a.tile_tokens, a.chunks);
+    uint32_t scan = bad ? 0 : items_of(qb - qa, 2 * a.tile_tokens, a.chunks);
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-        const uint64_t o = __shfl_up_sync(0xffffffffu, scan, d);
+        const uint32_t o = __shfl_up_sync(0xffffffffu, scan, d);
         if (lane >= (uint32_t)d) scan += o;
     }
     sm.item_end[lane] = scan;
@@ -157,10 +159,11 @@ struct Item {
 // a turn gets the lightest of the next (two prompts of 8192: 855 -> 830 us when added).
 __device__ __forceinline__ bool find_item(const Args &a, const Small &sm, const uint64_t *tile_off, const int64_t *q_off,
                                           const int64_t *k_off, uint32_t turn, Item &it) {
-    const uint64_t index = (uint64_t)turn * gridDim.x + (turn & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-    const uint64_t tile = index / a.kv_heads;
+    const uint64_t wide = (uint64_t)turn * gridDim.x + (turn & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    if (wide >= a.most_items) return false;  // less than 2^31: 32 bits do from here
+    const uint32_t index = (uint32_t)wide, tile = index / a.kv_heads;
     it.head = (int32_t)(index - tile * a.kv_heads);
-    uint64_t x;  // which of the request's items
+    uint32_t x;  // which of the request's items
     if (tile_off) {
         if (tile >= __ldcg(tile_off + a.R)) return false;
         const uint32_t r = pk::warp_find_request(reinterpret_cast<const int64_t *>(tile_off), a.R, (int64_t)tile);
@@ -168,7 +171,7 @@ __device__ __forceinline__ bool find_item(const Args &a, const Small &sm, const 
         it.k0 = (int32_t)__ldcg(k_off + r);
         it.lq = (int32_t)__ldcg(q_off + r + 1) - it.q0;
         it.lk = (int32_t)__ldcg(k_off + r + 1) - it.k0;
-        x = __ldcg(tile_off + r + 1) - 1 - tile;
+        x = (uint32_t)__ldcg(tile_off + r + 1) - 1 - tile;
     } else {
         const uint32_t lane = threadIdx.x & 31;
         const uint32_t r = __popc(__ballot_sync(0xffffffffu, sm.item_end[lane] <= tile));
@@ -471,34 +474,55 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                     ok = pk::mbar_wait_warp(pk::smem_addr(&sm.edge_v[edges & 3]), (edges >> 2) & 1);
                     if (!ok) break;
                     uint8_t *v = smem_p + L::kRing + st * L::kTile + (D == 128 ? half * 16384 : 0);
-                    for (uint32_t x = lane; x < 128 * kChunks; x += 32) {
+                    // eight 16-byte pieces of a lane at once: mostly there is nothing to do
+                    auto piece = [&](uint32_t x) {
                         const uint32_t row = x / kChunks, chunk = x % kChunks + (D == 128 ? 0 : half * kChunks);
-                        uint4 *at = reinterpret_cast<uint4 *>(v + row * 128 + ((chunk ^ (row & 7)) << 4));
-                        const uint4 u = *at;
-                        const int32_t key = j * kKeys + (int32_t)row;
-                        constexpr uint32_t kInf = pk::Elem<DT>::kInfBits;
-                        if (key >= it.lk) {
-                            *at = make_uint4(0, 0, 0, 0);
-                            continue;
-                        }
-                        uint32_t w[4] = {u.x, u.y, u.z, u.w}, m = 0;
+                        return reinterpret_cast<uint4 *>(v + row * 128 + ((chunk ^ (row & 7)) << 4));
+                    };
+                    constexpr uint32_t kInf = pk::Elem<DT>::kInfBits;
+#pragma unroll 1
+                    for (uint32_t x0 = lane; x0 < 128 * kChunks; x0 += 256) {
+                        uint4 u[8];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
-                        if ((m & 0xffffu) < kInf && m >> 16 < kInf) continue;
+                        for (int i = 0; i < 8; ++i) u[i] = *piece(x0 + 32 * i);
+                        uint32_t m = 0;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t d = (D == 128 ? half * 64 : 0) + chunk * 8 + 2 * i;
-                            if ((w[i] & 0x7fffu) >= kInf) {
-                                atomicMin(&bad_row[d], key);
-                                w[i] &= 0xffff0000u;
+                        for (int i = 0; i < 8; ++i) {
+                            m = __vmaxu2(m, __vmaxu2(u[i].x & 0x7fff7fffu, u[i].y & 0x7fff7fffu));
+                            m = __vmaxu2(m, __vmaxu2(u[i].z & 0x7fff7fffu, u[i].w & 0x7fff7fffu));
+                        }
+                        const bool past = j * kKeys + (int32_t)((x0 + 224) / kChunks) >= it.lk;
+                        if (!past && (m & 0xffffu) < kInf && m >> 16 < kInf) continue;
+#pragma unroll 1
+                        for (uint32_t x = x0; x < x0 + 256; x += 32) {
+                            const uint32_t row = x / kChunks, chunk = x % kChunks + (D == 128 ? 0 : half * kChunks);
+                            const int32_t key = j * kKeys + (int32_t)row;
+                            if (key >= it.lk) {
+                                *piece(x) = make_uint4(0, 0, 0, 0);
+                                continue;
                             }
-                            if ((w[i] >> 16 & 0x7fffu) >= kInf) {
-                                atomicMin(&bad_row[d + 1], key);
-                                w[i] &= 0xffffu;
+                            const uint4 y = *piece(x);
+                            uint32_t w[4] = {y.x, y.y, y.z, y.w};
+                            bool found = false;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t d = (D == 128 ? half * 64 : 0) + chunk * 8 + 2 * i;
+                                if ((w[i] & 0x7fffu) >= kInf) {
+                                    atomicMin(&bad_row[d], key);
+                                    w[i] &= 0xffff0000u;
+                                    found = true;
+                                }
+                                if ((w[i] >> 16 & 0x7fffu) >= kInf) {
+                                    atomicMin(&bad_row[d + 1], key);
+                                    w[i] &= 0xffffu;
+                                    found = true;
+                                }
+                            }
+                            if (found) {
+                                *piece(x) = make_uint4(w[0], w[1], w[2], w[3]);
+                                sm.any_bad[items & 1][half] = 1;
                             }
                         }
-                        *at = make_uint4(w[0], w[1], w[2], w[3]);
-                        sm.any_bad[items & 1][half] = 1;
                     }
                     pk::fence_proxy_async();
                     __syncwarp();
@@ -641,30 +665,34 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
             uint16_t *dst = a.out + q_row * a.o_ts + (int64_t)qh * a.o_hs;
             const bool bad = notes && (sm.any_bad[items & 1][0] | sm.any_bad[items & 1][1]) != 0;
             pk::tmem_fence_after();
-#pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-                uint32_t y[32];
-                __syncwarp();
+            // 16 columns of the output, the next ones on their way meanwhile
+            uint32_t y[2][16];
+            if (n_tiles > 0) pk::tmem_load16(to, y[0]);
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {  // no load is left in flight over a loop's end
+                uint32_t(&z)[16] = y[c & 1];
                 if (n_tiles > 0) {  // else O was never written
-                    pk::tmem_load32(to + 32 * c, y);
-                    pk::tmem_wait_load(y);
+                    __syncwarp();
+                    pk::tmem_wait_load(z);
+                    if (c + 1 < D / 16) pk::tmem_load16(to + 16 * (c + 1), y[(c + 1) & 1]);
                 }
-                if (on) {
+                if (!on) continue;
+                uint32_t w[8];
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        float z = n_tiles > 0 && inv != 0.0f ? __uint_as_float(y[i]) * inv : 0.0f;
-                        if (bad && sm.bad_row[items & 1][32 * c + i] <= last) z = __int_as_float(0x7fffffff);
-                        y[i] = __float_as_uint(z);
-                    }
+                for (int i = 0; i < 16; i += 2) {
+                    float f0 = __uint_as_float(z[i]) * inv, f1 = __uint_as_float(z[i + 1]) * inv;
+                    if (n_tiles == 0 || inv == 0.0f) f0 = f1 = 0.0f;
+                    w[i / 2] = pk::Elem<DT>::from2(f0, f1);
+                }
+                if (bad) {
+                    const int32_t *row = sm.bad_row[items & 1] + 16 * c;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t w[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            w[e] = pk::Elem<DT>::from2(__uint_as_float(y[8 * i + 2 * e]), __uint_as_float(y[8 * i + 2 * e + 1]));
-                        reinterpret_cast<uint4 *>(dst + 32 * c)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                    for (int i = 0; i < 16; i += 2) {
+                        if (row[i] <= last) w[i / 2] |= 0x7fffu;
+                        if (row[i + 1] <= last) w[i / 2] |= 0x7fff0000u;
                     }
                 }
+                pk::store32(dst + 16 * c, a.wide_out, w);
             }
             __syncwarp();
             ++items;
@@ -716,7 +744,8 @@ cudaError_t launch(const Args &a, unsigned grid, const CUtensorMap &mq, const CU
                    cudaStream_t s) {
     constexpr size_t smem = Layout<D>::kBytes + sizeof(Small);
     static_assert(smem <= 227 * 1024, "shared memory of a block");
-    const cudaError_t e = cudaFuncSetAttribute(k_attend_prompt<D, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static std::atomic<uint64_t> seen{0};
+    const cudaError_t e = pk_allow_smem(k_attend_prompt<D, DT>, smem, seen);
     return e != cudaSuccess ? e : pk_launch_smem(k_attend_prompt<D, DT>, grid, kThreads, smem, s, a, mq, mk, mv);
 }
 
@@ -729,6 +758,7 @@ cudaError_t pk_launch_attend_prompt(uint32_t dtype, const pk_heads &q, const pk_
     Args a;
     a.out = static_cast<uint16_t *>(out.p);
     a.o_ts = out.tok_stride, a.o_hs = out.head_stride;
+    a.wide_out = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && a.o_ts % 16 == 0 && a.o_hs % 16 == 0;
     a.lse = lse;
     a.q_off = q_off;
     a.k_off = k_off;
@@ -762,6 +792,8 @@ cudaError_t pk_launch_attend_prompt(uint32_t dtype, const pk_heads &q, const pk_
     if (e != cudaSuccess) return e;
     // every request rounds its tokens up to whole items: at most one more each
     const uint64_t items = (n_q / item_tokens + R) * a.chunks * kv_heads;
+    if (items > 0x7fffffffull) return cudaErrorInvalidValue;
+    a.most_items = (uint32_t)items;
     const unsigned grid = items < (uint64_t)sms ? (unsigned)items : (unsigned)sms;
     if (head_dim == 128)
         e = dtype == PK_BF16 ? launch<128, PK_BF16>(a, grid, mq, mk, mv, s) : launch<128, PK_FP16>(a, grid, mq, mk, mv, s);

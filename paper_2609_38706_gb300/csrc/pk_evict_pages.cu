@@ -16,7 +16,6 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;  // -inf -> 0x007fffff: above NaN
 }
 
-constexpr int kPer = 16;  // pages a thread of the resident kernel holds
 constexpr uint32_t kFew = 512;  // keys that one warp goes on with
 
 // One CTA per request whose row fits its registers, kPer consecutive pages a
@@ -28,7 +27,7 @@ constexpr uint32_t kFew = 512;  // keys that one warp goes on with
 // of the steps that the key's 32 bits would, and a step is kPer compares a
 // thread and one barrier.  Kept and dropped pages are put in order in shared
 // memory and leave in whole lines.  Bound by the issue of those steps.
-template <int kThreads>
+template <int kThreads, int kPer>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
 k_evict_resident(const uint32_t *pages, const float *weight, const int32_t *kv_len, uint32_t stride,
                  uint32_t page_tokens, uint32_t budget, uint32_t sinks, uint32_t recent, uint32_t *pages_out,
@@ -398,14 +397,15 @@ cudaError_t pk_launch_evict_pages(const uint32_t *pages, const float *weight, co
                               (uint32_t)page_stride, page_tokens, budget, sinks, recent, pages_out, weight_out,
                               kv_len_out, evicted, status);
     };
-    // Rows that a CTA's registers hold, by the fewest threads that do (512 rows of 8192 pages, 1024 to keep: 21 us
-    // against 92 us by histogram); longer ones by histogram, whose passes read the row again.
-    if (page_stride <= 64 * kPer)
-        e = resident(k_evict_resident<64>, 64);
-    else if (page_stride <= 256 * kPer)
-        e = resident(k_evict_resident<256>, 256);
-    else if (page_stride <= 512 * kPer)
-        e = resident(k_evict_resident<512>, 512);
+    // Rows that a CTA's registers hold, by the smallest shape that does (512 rows of 8192 pages, 1024 to keep: 34 us
+    // against 92 us by histogram; 64 rows of 128 pages, 4 a thread against 16: 5 against 8 us); longer ones by
+    // histogram, whose passes read the row again.
+    if (page_stride <= 256 * 4)
+        e = resident(k_evict_resident<256, 4>, 256);
+    else if (page_stride <= 256 * 16)
+        e = resident(k_evict_resident<256, 16>, 256);
+    else if (page_stride <= 512 * 16)
+        e = resident(k_evict_resident<512, 16>, 512);
     else
         e = pk_launch(k_evict_pages<1024>, R, 1024, s, pages, weight, kv_len, page_stride, page_tokens, budget, sinks,
                       recent, pages_out, weight_out, kv_len_out, evicted, status);

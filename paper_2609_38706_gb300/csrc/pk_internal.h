@@ -108,7 +108,21 @@ cudaError_t pk_launch_evict_pages(const uint32_t *pages, const float *weight, co
                                   uint32_t *evicted, int32_t *status, cudaStream_t s);
 
 #if defined(__CUDACC__)
+#include <atomic>
 #include <utility>
+// Lets `kernel` have `bytes` of dynamic shared memory; asked for once a kernel
+// and device (a bit of `seen`), as the call costs a small launch's share.
+template <typename K>
+static inline cudaError_t pk_allow_smem(K kernel, size_t bytes, std::atomic<uint64_t> &seen) {
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    if (seen.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess) seen.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 // Launch with programmatic stream serialization (see pk_device.cuh).
 template <typename... KArgs, typename... Args>
 static inline cudaError_t pk_launch(void (*kernel)(KArgs...), unsigned grid, unsigned block, cudaStream_t s,

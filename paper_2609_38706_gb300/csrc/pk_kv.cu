@@ -82,32 +82,6 @@ __device__ __forceinline__ void quantise16(const uint4 (&v)[2], float g, uint2 *
     *scale = s;
 }
 
-// A block's 32 bytes, in one access where they start on a 32-byte boundary (two
-// halves of a sector by separate instructions cost the L2 two requests: reading
-// 64 x 2048 tokens back 119 -> 93 us).
-__device__ __forceinline__ void load32(const uint16_t *p, bool wide, uint4 (&v)[2]) {
-    if (wide) {
-        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                     : "=r"(v[0].x), "=r"(v[0].y), "=r"(v[0].z), "=r"(v[0].w), "=r"(v[1].x), "=r"(v[1].y),
-                       "=r"(v[1].z), "=r"(v[1].w)
-                     : "l"(p)
-                     : "memory");
-    } else {
-        v[0] = __ldcg(reinterpret_cast<const uint4 *>(p));
-        v[1] = __ldcg(reinterpret_cast<const uint4 *>(p) + 1);
-    }
-}
-__device__ __forceinline__ void store32(uint16_t *p, bool wide, const uint32_t (&w)[8]) {
-    if (wide) {
-        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]),
-                     "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                     : "memory");
-    } else {
-        reinterpret_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        reinterpret_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-    }
-}
-
 // D/16 lanes hold one token (16 dimensions each), so a warp takes 512/D tokens
 // at a time and walks over heads_per_warp heads: the search for the tokens'
 // requests is paid once.  Codes of a token are D/2 consecutive bytes and
@@ -178,7 +152,7 @@ __global__ void __launch_bounds__(kMoveThreads) k_kv_move(const Move a) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 if (kWrite) {
-                    load32((j ? xv : xk) + t * a.ts[j] + (int64_t)(h + i) * a.hs[j] + block * 16, a.wide, x[i][j]);
+                    pk::load32((j ? xv : xk) + t * a.ts[j] + (int64_t)(h + i) * a.hs[j] + block * 16, a.wide, x[i][j]);
                 } else {
                     c[i][j] = __ldcg(reinterpret_cast<const uint2 *>(gran[i] + (j ? G::kV : G::kK) + tok * G::kRow + block * 8));
                     sc[i][j] = __ldcg(gran[i] + (j ? G::kVs : G::kKs) + tok * G::kScales + block);
@@ -204,7 +178,7 @@ __global__ void __launch_bounds__(kMoveThreads) k_kv_move(const Move a) {
                         const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&half[k]));
                         w[k] = pk::Elem<DT>::from2(__fmul_rn(f.x, den), __fmul_rn(f.y, den));
                     }
-                    store32((j ? xv : xk) + t * a.ts[j] + (int64_t)(h + i) * a.hs[j] + block * 16, a.wide, w);
+                    pk::store32((j ? xv : xk) + t * a.ts[j] + (int64_t)(h + i) * a.hs[j] + block * 16, a.wide, w);
                 }
             }
         }
