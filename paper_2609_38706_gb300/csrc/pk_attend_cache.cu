@@ -5,9 +5,10 @@
 // pass over the tokens, o = v_scale * sum p_j V_j / sum p_j: the format's
 // tensor scales leave the loop, and what is left of a value, code * scale, has
 // six significant bits, so it is exact in a half and every product of the QK
-// step is exact in 32 bits.  `ref` is a running integer near the maximum; it
-// moves only when a p would pass 2^15 (a warp vote), so the sums are rescaled
-// by exact powers of two, and rarely.
+// step is exact in 32 bits.  `ref` is a running score near the maximum; it moves
+// only when a p would pass 2^15 (a warp vote), so rescaling is rare, and to the
+// maximum itself, so that the heaviest p is a power of two, which its rounding to
+// a half leaves as it is: a row with one key gets that key's value exactly.
 //
 // The work is reading the pages once: 1.125 D bytes a token and KV head.  A
 // granule (16 tokens of one head) is one contiguous bulk copy; every warp has
@@ -338,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
                     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
                     if (m - ref[nt][j] > kTop) {
-                        const float to = ceilf(m) - kBase;
+                        const float to = m - kBase;
                         const float f = ex2(ref[nt][j] - to);
                         ref[nt][j] = to;
                         sum[nt][j] *= f;

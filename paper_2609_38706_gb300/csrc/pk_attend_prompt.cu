@@ -618,10 +618,11 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                     return (s0.x + s1.x) + (s0.y + s1.y);
                 };
                 // Moves the reference of the rows that `over` names to their largest score; their sum and output so
-                // far are rescaled by a power of two.
+                // far are rescaled.  That score's weight is then a power of two, which rounding leaves as it is: a
+                // row with one key, or one that outweighs the others, gets its value of V and no more error.
                 auto move_ref = [&](bool over) {
                     const float m = edge ? largest(std::true_type{}) : largest(std::false_type{});
-                    const float next = over && m > -INFINITY ? ceilf(m) - kBase : ref;
+                    const float next = over && m > -INFINITY ? m - kBase : ref;
                     const float f = ex2(ref - next);
                     ref = next;
                     sum *= f;
