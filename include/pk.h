@@ -548,7 +548,8 @@ int pk_kv_read(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *k, const p
  * last one never reach its outputs, whatever they hold.  A query that attends
  * a value of V that is infinite or NaN gets a non-finite output in that
  * dimension.  Rows of q that belong to no request are not written.
- * head_dim: 64 or 128; q_heads a multiple of kv_heads; scale finite.
+ * head_dim: 64 or 128; q_heads a multiple of kv_heads; scale finite; n_q and
+ * n_k at most 0x7fff0000; strides of q, k and v below 2^39.
  * scratch_dev: pk_attend_prompt_scratch_bytes(R) bytes, 16-byte aligned.
  * Device errors: offsets out of order or range (PK_ERR_ARG; nothing is
  * written); PK_ERR_TIMEOUT. */

@@ -18,7 +18,7 @@ constexpr int kRows = 128;      // (query token, head of the group) rows of a ti
 constexpr int kKeys = 128;      // keys of a tile
 constexpr int kThreads = 384;
 constexpr float kTop = 32768.0f;  // a tile's weights of a row sum to no more, so each fits a half (65504)
-constexpr float kBase = 4.0f;     // the largest weight when the reference moves: 2^kBase, so a tile's 128 stay below 2^11
+constexpr float kBase = 4.0f;     // the largest weight when the reference moves: 2^kBase, so 128 stay below 2^11
 constexpr int kPlanThreads = 1024;
 
 struct Args {

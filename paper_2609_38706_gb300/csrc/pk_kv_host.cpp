@@ -90,10 +90,12 @@ int pk_attend_prompt(uint32_t dtype, const pk_heads *q, const pk_heads *k, const
                      void *scratch_dev, size_t scratch_bytes, int32_t *status_dev, pk_stream stream) {
     if (dtype > PK_FP16 || (head_dim != 64 && head_dim != 128) || !std::isfinite(scale)) return PK_ERR_ARG;
     if (kv_heads == 0 || q_heads == 0 || q_heads % kv_heads || q_heads > 65536) return PK_ERR_ARG;
-    if (n_q >= 1ull << 31 || n_k >= 1ull << 31) return PK_ERR_ARG;
+    if (n_q > 0x7fff0000ull || n_k > 0x7fff0000ull) return PK_ERR_ARG;  // a tile's end still fits 31 bits
     if (!good_heads(q, n_q, q_heads) || !good_heads(k, n_k, kv_heads) || !good_heads(v, n_k, kv_heads) ||
         !good_out(out, n_q, q_heads, head_dim))
         return PK_ERR_ARG;
+    for (const pk_heads *h : {q, k, v})  // what a tensor map takes: less than 2^40 bytes
+        if (h->tok_stride >= (int64_t)1 << 39 || h->head_stride >= (int64_t)1 << 39) return PK_ERR_ARG;
     if (!aligned(lse_dev, 4) || !aligned(q_off_dev, 8) || !aligned(k_off_dev, 8) || !aligned(scratch_dev, 16) ||
         !aligned(status_dev, 4))
         return PK_ERR_ARG;

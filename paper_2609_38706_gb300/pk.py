@@ -508,9 +508,9 @@ def _refuse(where: str, what: str):
 
 
 def _ints(t: torch.Tensor, dtype, n: int, where: str, what: str) -> Optional[int]:
-    """Pointer of a contiguous array of n entries."""
-    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
-        _refuse(where, what)
+    """Pointer of a contiguous array of n entries on the device."""
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        _refuse(where, what + ", on the device")
     return t.data_ptr() if n else None
 
 
@@ -529,9 +529,18 @@ def _heads(t: torch.Tensor, where: str):
         _refuse(where, "a [tokens, heads, head_dim] tensor")
     if t.numel() == 0:
         return pk_heads(None, 0, 0)
-    if stride[-1] != 1 and shape[-1] > 1:
-        _refuse(where, "rows are not contiguous")
+    if (stride[-1] != 1 and shape[-1] > 1) or not t.is_cuda:
+        _refuse(where, "rows are contiguous, on the device")
     return pk_heads(t.data_ptr(), ts if n > 1 else 0, stride[-2] if shape[-2] > 1 else 0)
+
+
+def _buffer(t: Optional[torch.Tensor], where: str) -> Optional[int]:
+    """Pointer of a status word or scratch (None for None)."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        _refuse(where, "status and scratch are on the device")
+    return t.data_ptr() if t.numel() else None
 
 
 def _dtype(where: str, first: torch.Tensor, *others) -> int:
@@ -560,7 +569,7 @@ def _kv_move(fn: str, call, kv: pk_kv_cache, k, v, tok_off, start, pages, status
     rc = call(ctypes.byref(kv), _dtype(fn, k, v), ctypes.byref(_heads(k, fn)), ctypes.byref(_heads(v, fn)), shape[0],
               _ints(tok_off, torch.int64, R + 1, fn, "tok_off is contiguous int64[R+1]"),
               _ints(start, torch.int32, R, fn, "start is contiguous int32[R]"), R,
-              _ints(pages, torch.int32, R * width, fn, "pages is contiguous int32"), width, _p(status),
+              _ints(pages, torch.int32, R * width, fn, "pages is contiguous int32"), width, _buffer(status, fn),
               _stream_of(stream, k))
     if rc:
         _check(rc, fn)
@@ -594,12 +603,15 @@ def pk_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: tor
         _refuse(fn, "q, out [n_q, q_heads, D], k, v [n_k, kv_heads, D]")
     if R < 0:
         _refuse(fn, "q_off is int64[R+1]")
-    z = None if lse is None else _ints(lse, torch.float32, qs[0] * qs[1], fn, "lse is contiguous float32 [n_q, q_heads]")
+    z = lse
+    if lse is not None:
+        z = _ints(lse, torch.float32, qs[0] * qs[1], fn, "lse is contiguous float32 [n_q, q_heads]")
     rc = lib().pk_attend_prompt(_dtype(fn, q, k, v, out), ctypes.byref(_heads(q, fn)), ctypes.byref(_heads(k, fn)),
                                 ctypes.byref(_heads(v, fn)), ctypes.byref(_heads(out, fn)), z, qs[0], ks[0],
                                 _ints(q_off, torch.int64, R + 1, fn, "q_off is contiguous int64[R+1]"),
                                 _ints(k_off, torch.int64, R + 1, fn, "k_off is contiguous int64[R+1]"), R, qs[1],
-                                ks[1], qs[2], scale, _p(scratch), scratch.numel(), _p(status), _stream_of(stream, q))
+                                ks[1], qs[2], scale, _buffer(scratch, fn), scratch.numel(), _buffer(status, fn),
+                                _stream_of(stream, q))
     if rc:
         _check(rc, fn)
 
@@ -622,8 +634,9 @@ def pk_attend_cache(kv: pk_kv_cache, q: torch.Tensor, out: torch.Tensor, lse: Op
     if pages.dim() != 2 or pages.shape[0] != R:
         _refuse(fn, "pages is [R, page_stride]")
     width = pages.shape[1]
-    z = None if lse is None else _ints(lse, torch.float32, R * n_q * qs[-2], fn, "lse is contiguous float32, R * n_q * q_heads")
-    w = None
+    z = w = None
+    if lse is not None:
+        z = _ints(lse, torch.float32, R * n_q * qs[-2], fn, "lse is contiguous float32, R * n_q * q_heads")
     if page_weight is not None:
         if page_weight.shape != pages.shape:
             _refuse(fn, "page_weight is [R, page_stride]")
@@ -632,7 +645,8 @@ def pk_attend_cache(kv: pk_kv_cache, q: torch.Tensor, out: torch.Tensor, lse: Op
                                ctypes.byref(_heads(out, fn)), z, R, n_q, qs[-2], scale,
                                _ints(kv_len, torch.int32, R, fn, "kv_len is contiguous int32[R]"),
                                _ints(pages, torch.int32, R * width, fn, "pages is contiguous int32"), width, w,
-                               _p(scratch), scratch.numel(), _p(status), _stream_of(stream, q))
+                               _buffer(scratch, fn), scratch.numel(), _buffer(status, fn),
+                                _stream_of(stream, q))
     if rc:
         _check(rc, fn)
 
@@ -659,8 +673,8 @@ def pk_evict_pages(pages: torch.Tensor, weight: torch.Tensor, kv_len: torch.Tens
                               _ints(weight_out, torch.float32, R * budget, fn, "weight_out is float32[R, budget]"),
                               _ints(kv_len_out, torch.int32, R, fn, "kv_len_out is int32[R]"),
                               None if evicted is None else
-                              _ints(evicted, torch.int32, n, fn, "evicted is int32[R, page_stride]"), _p(status),
-                              _stream_of(stream, pages))
+                              _ints(evicted, torch.int32, n, fn, "evicted is int32[R, page_stride]"),
+                              _buffer(status, fn), _stream_of(stream, pages))
     if rc:
         _check(rc, fn)
 

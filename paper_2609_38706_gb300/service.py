@@ -250,8 +250,8 @@ class KVPages:
             raise pk.PKError(pk.PK_ERR_ARG, "KVPages")
         if pool is None:
             pool = torch.zeros((n_slots, nbytes), dtype=torch.uint8, device=device)
-        if pool.dtype != torch.uint8 or not pool.is_contiguous() or pool.numel() != n_slots * nbytes:
-            raise pk.PKError(pk.PK_ERR_ARG, "KVPages: pool is contiguous uint8 [n_slots, pk_kv_page_bytes]")
+        if pool.dtype != torch.uint8 or not pool.is_contiguous() or pool.numel() != n_slots * nbytes or not pool.is_cuda:
+            raise pk.PKError(pk.PK_ERR_ARG, "KVPages: pool is contiguous uint8 [n_slots, pk_kv_page_bytes] on the device")
         self.pool, self.device = pool, pool.device
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._scratch_bytes: dict = {}

@@ -64,6 +64,7 @@ CASES = [
     ([40], [41], 1, 16, 128, "fp16"),
     ([3], [130], 1, 129, 64, "bf16"),              # a group larger than a tile's rows
     ([0], [0], 1, 1, 64, "bf16"),
+    ([3, 2], [0, 0], 2, 2, 128, "fp16"),           # no key at all
     ([300] * 7, [300] * 7, 2, 2, 128, "bf16"),
     ([3, 0, 40] * 11, [5, 2, 90] * 11, 2, 3, 64, "fp16"),  # more requests than a warp has lanes
     ([2] * 32, [9] * 32, 1, 1, 128, "bf16"),
@@ -217,6 +218,10 @@ def test_refusals():
               (q, k[:, :, ::2], v[:, :, ::2])):
         with pytest.raises(pk.PKError):
             service.attend_prompt(*a, off, off)
+    with pytest.raises(pk.PKError):
+        service.attend_prompt(q, k, v, off.cpu(), off)
+    with pytest.raises(pk.PKError):
+        service.attend_prompt(q, k.cpu(), v, off, off)
     with pytest.raises(pk.PKError):
         service.attend_prompt(q, k, v, off, off, float("nan"))
     with pytest.raises(pk.PKError):

@@ -51,7 +51,7 @@ def test_bad_cache_refused_everywhere(pk, change):
 
 
 @pytest.mark.parametrize("h", [(0, 128, 64), (FAKE + 2, 128, 64), (FAKE, 127, 64), (FAKE, 128, 60), (FAKE, -128, 64),
-                               (FAKE, 128, -64), (FAKE, 1 << 60, 64)])
+                               (FAKE, 128, -64), (FAKE, 1 << 60, 64)])  # and, for prompts, what a tensor map does not take
 def test_bad_strides_refused(pk, h):
     kv, ok = good(pk)
     bad = pk.pk_heads(*h)
@@ -82,6 +82,9 @@ def test_attention_arguments_refused(pk):
         return L.pk_attend_prompt(dtype, b(h), b(h), b(h), b(h), None, n_q, 4, off, off, R, qh, kh, D, scale, scratch,
                                   nbytes, None, None)
 
+    far = pk.pk_heads(FAKE, 1 << 39, 64)
+    assert L.pk_attend_prompt(0, b(far), b(h), b(h), b(h), None, 4, 4, FAKE, FAKE, 1, 2, 2, 64, 1.0, FAKE, 1 << 20, None,
+                              None) == pk.PK_ERR_ARG
     for kw in (dict(dtype=2), dict(qh=3), dict(kh=0), dict(qh=0), dict(D=96), dict(scale=float("nan")), dict(scratch=None),
                dict(scratch=FAKE + 8), dict(nbytes=8), dict(off=None), dict(off=FAKE + 4), dict(n_q=1 << 31)):
         assert prompt(**kw) == pk.PK_ERR_ARG, kw
