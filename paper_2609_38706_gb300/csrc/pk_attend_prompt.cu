@@ -19,6 +19,8 @@ constexpr int kKeys = 128;      // keys of a tile
 constexpr int kThreads = 384;
 constexpr float kTop = 32768.0f;  // a tile's weights of a row sum to no more, so each fits a half (65504)
 constexpr float kBase = 4.0f;     // the largest weight when the reference moves: 2^kBase, so 128 stay below 2^11
+constexpr float kFar = 16777216.0f;  // scores (times log2 e) from here on are further apart than a weight's exponents:
+                                     // one 32-bit reference cannot lie kBase below one
 constexpr int kPlanThreads = 1024;
 
 struct Args {
@@ -558,7 +560,8 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
             const bool notes = it.first_edge < n_tiles;  // only then are this item's notes sure to be there
             ++turn;
             more = find_item(a, sm, tile_off, q_off, k_off, turn, it);  // the next one
-            float ref = -FLT_MAX, sum = 0.0f;
+            // a weight is 2^(score - ref + fine), and fine is 0 but for a reference of kFar and more
+            float ref = -FLT_MAX, fine = 0.0f, sum = 0.0f;
 #pragma unroll 1
             for (int32_t j = 0; j < n_tiles; ++j, ++ni) {
                 ok = pk::mbar_wait_warp(pk::smem_addr(&sm.s_full[t]), ni & 1);
@@ -595,7 +598,7 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
 #pragma unroll
                         for (int i = 0; i < 32; ++i) m4[i & 3] = fmaxf(m4[i & 3], __uint_as_float(y[i]));
                     }
-                    return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * scale2;
+                    return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
                 };
                 // The weights by the reference so far, and their sum.
                 uint32_t p[2][32];
@@ -617,14 +620,45 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                     const float2 s0 = unpack2(sum2[0]), s1 = unpack2(sum2[1]);
                     return (s0.x + s1.x) + (s0.y + s1.y);
                 };
+                // The same where a row of the warp has a far reference, which few calls have: by 16 scores, with `fine`.
+                auto weigh_far = [&]() {
+                    float s = 0.0f;
+                    uint32_t(&y)[16] = reinterpret_cast<uint32_t(&)[16]>(x[0]);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        pk::tmem_load16(ts + 16 * c, y);
+                        pk::tmem_wait_load(y);
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            float w[2];
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const bool masked = edge && 16 * c + i + h > see;
+                                w[h] = masked ? 0.0f : ex2(fmaf(__uint_as_float(y[i + h]), scale2, -ref) + fine);
+                                s += w[h];
+                            }
+                            p[c / 4][c % 4 * 8 + i / 2] = pk::Elem<DT>::from2(w[0], w[1]);
+                        }
+                    }
+                    return s;
+                };
+                auto weigh_any = [&]() {
+                    if (__any_sync(0xffffffffu, fine != 0.0f)) return weigh_far();
+                    return edge ? weigh(std::true_type{}) : weigh(std::false_type{});
+                };
                 // Moves the reference of the rows that `over` names to their largest score; their sum and output so
                 // far are rescaled.  That score's weight is then a power of two, which rounding leaves as it is: a
                 // row with one key, or one that outweighs the others, gets its value of V and no more error.
                 auto move_ref = [&](bool over) {
-                    const float m = edge ? largest(std::true_type{}) : largest(std::false_type{});
-                    const float next = over && m > -INFINITY ? m - kBase : ref;
-                    const float f = ex2(ref - next);
+                    const float top = edge ? largest(std::true_type{}) : largest(std::false_type{}), m = top * scale2;
+                    const bool moves = over && m > -INFINITY, far = moves && fabsf(m) >= kFar;
+                    const float next = !moves ? ref : far ? m : m - kBase;
+                    // far: what m's rounding lost comes off again, so the largest weight is 2^kBase or, where kBase
+                    // is lost beside that, 1; not a number where m overflowed
+                    const float next_fine = !moves ? fine : far ? kBase - fmaf(top, scale2, -m) : 0.0f;
+                    const float f = ex2((ref - next) + (next_fine - fine));
                     ref = next;
+                    fine = next_fine;
                     sum *= f;
                     if (j == 0) return;
                     ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
@@ -639,15 +673,17 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                         pk::tmem_store32(to + 32 * d, x[0]);
                     }
                 };
-                if (j == 0) move_ref(true);
+                if (j == 0) move_ref(on);
                 // One pass over the scores takes the weights by the reference so far, with no look at the scores
                 // first: a weight that has outgrown it shows in the sum, and only then the reference is moved and
                 // the pass done again.
-                float part = edge ? weigh(std::true_type{}) : weigh(std::false_type{});
-                while (__any_sync(0xffffffffu, part > kTop)) {
-                    move_ref(part > kTop);
+                // Once does: behind a move no weight is above 2^(kBase + 2).  Rows without a query, of a tile's unused
+                // rows too, which hold anything, have no say.
+                float part = weigh_any();
+                if (__any_sync(0xffffffffu, on && part > kTop)) {
+                    move_ref(on && part > kTop);
                     if (!ok) break;
-                    part = edge ? weigh(std::true_type{}) : weigh(std::false_type{});
+                    part = weigh_any();
                 }
                 if (!ok) break;
                 sum += part;
@@ -662,7 +698,7 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
             if (!ok) break;
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
             if (on && a.lse)
-                a.lse[q_row * a.q_heads + qh] = sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+                a.lse[q_row * a.q_heads + qh] = sum == 0.0f ? -INFINITY : (ref - fine + log2f(sum)) * 0.69314718055994531f;
             uint16_t *dst = a.out + q_row * a.o_ts + (int64_t)qh * a.o_hs;
             const bool bad = notes && (sm.any_bad[items & 1][0] | sm.any_bad[items & 1][1]) != 0;
             pk::tmem_fence_after();

@@ -228,3 +228,47 @@ def test_refusals():
         service.attend_prompt(q, k, v, off.int(), off)
     with pytest.raises(pk.PKError):
         service.attend_prompt(q, k, v, off, dev(offs([4, 4])))
+
+
+@pytest.mark.parametrize("D,G", [(64, 3), (128, 1), (128, 7)])
+def test_scores_beyond_a_weights_exponents(D, G):
+    """Scores 2^24 and more apart from each other, up to near the top of their type: 32 bits hold them exactly here
+    (one nonzero value a key, powers of two), so the softmax is exact: the heaviest keys share the weight."""
+    from paper_2609_38706_gb300 import service
+    H, lq, lk = 2, [70, 5], [200, 133]
+    rng = np.random.default_rng(2)
+    q = np.zeros((sum(lq), H * G, D), np.float32)
+    q[..., 0] = 2.0 ** rng.choice((0, 20, 30, 45, 60), q.shape[:2])
+    k = np.zeros((sum(lk), H, D), np.float32)
+    k[..., 0] = rng.choice((-1, 1, 1.0078125, 2.0 ** 20, 2.0 ** 40, -2.0 ** 40), k.shape[:2])
+    v = rng.standard_normal(k.shape).astype(np.float32)
+    q, k, v = (torch.from_numpy(x).to(torch.bfloat16) for x in (q, k, v))
+    out, lse = service.attend_prompt(q.cuda(), k.cuda(), v.cuda(), dev(offs(lq)), dev(offs(lk)), 0.37)
+    qd, kd, vd = (x.double().numpy() for x in (q, k, v))
+    qo, ko = offs(lq), offs(lk)
+    for r in range(2):
+        for h in range(H * G):
+            kk, vv = kd[ko[r]:ko[r + 1], h // G, 0], vd[ko[r]:ko[r + 1], h // G]
+            for i in range(lq[r]):
+                n = i + lk[r] - lq[r] + 1
+                s = qd[qo[r] + i, h, 0] * kk[:n]
+                w = np.exp(0.37 * (s - s.max()))
+                ref = w @ vv[:n] / w.sum()
+                # the scale's log2 e rounds to 32 bits, and the scores' distances with it
+                err = np.minimum(0.37 * (s.max() - s), 40.0) * 2.0 ** -22
+                rel = 2 * np.expm1(err.max()) + 2.0 ** -8 + n * 2.0 ** -24
+                assert np.all(np.abs(out[qo[r] + i, h].double().cpu().numpy() - ref) <= rel * (np.abs(vv[:n]).max() + np.abs(ref)))
+                assert abs(float(lse[qo[r] + i, h]) - (0.37 * s.max() + np.log(w.sum()))) <= 2.0 ** -21 * abs(0.37 * s.max()) + 2.0 ** -18
+
+
+def test_unused_rows_of_a_tile_may_hold_anything():
+    """Groups of 3 and 7 leave rows of a 128-row tile without a query: what shared memory holds there (here the values
+    of an earlier call, up to the type's top) does not matter, and keeps no warp."""
+    from paper_2609_38706_gb300 import service
+    big = torch.full((300, 8, 64), 3e38, dtype=torch.bfloat16, device="cuda")
+    service.attend_prompt(big, big[:, :2].contiguous(), big[:, :2].contiguous(), dev(offs([300])), dev(offs([300])))
+    for G in (3, 7):
+        lq, lk = [300, 40], [300, 90]
+        q, k, v = inputs(lq, lk, 2, G, 64, "bf16", G)
+        out, lse = service.attend_prompt(q.cuda(), k.cuda(), v.cuda(), dev(offs(lq)), dev(offs(lk)), 0.125)
+        check(q, k, v, lq, lk, out, lse, "bf16", 0.125)
