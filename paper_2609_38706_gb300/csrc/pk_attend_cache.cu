@@ -39,6 +39,9 @@ constexpr uint32_t kSlots = 152 * 16 / kWarps;  // CTAs that the GPU holds
 constexpr int kThreads = 32 * kWarps;
 constexpr int kFinishWarps = 8, kFinishThreads = 32 * kFinishWarps;
 constexpr float kTop = 15.0f;   // p stays below 2^kTop (half: 2^16)
+// Scores (times log2 e) from here on are further apart than a half's exponents, and so is a product from its rounding:
+// a reference that far is met with rounded products, by which the heaviest score is kBase or nothing above it.
+constexpr float kFar = 16777216.0f;
 constexpr float kBase = 8.0f;   // the largest p when ref moves: 2^kBase, so 22 bits of range lie below it
 
 struct Args {
@@ -255,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
     if (kWeigh)
         gran_at = a.gran_ml + ((((uint64_t)(r * a.kv_heads + head) * a.row_tiles + tile) * a.gran_stride + g0 +
                                 warp * TG + (g >> 1)) * a.gran_rows + 2 * c + (g & 1));
-    bool gave_up = false;
+    bool gave_up = false, far = false;  // far: a reference of the warp's is
 
     // One step: TG granules in stage `st`.  kEdge: some query does not see some token of them.
     auto step = [&](uint32_t k, uint32_t st, auto edge) {
@@ -308,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
 
         // p = 2^x, x = s * mul - ref: [0] (token g, column 2c) [1] (g, 2c + 1) [2] (g + 8, 2c) [3] (g + 8, 2c + 1)
         float x[TG][NT][4];
-        auto exponents = [&]() {
+        auto exponents_by = [&](auto rounded) {
             float top = -INFINITY;
 #pragma unroll
             for (int h = 0; h < TG; ++h)
@@ -317,12 +320,16 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         float &y = x[h][nt][e];
-                        y = fmaf(s[h][nt][e], mul[nt][e & 1], -ref[nt][e & 1]);
+                        if (decltype(rounded)::value)
+                            y = __fmul_rn(s[h][nt][e], mul[nt][e & 1]) - ref[nt][e & 1];
+                        else
+                            y = fmaf(s[h][nt][e], mul[nt][e & 1], -ref[nt][e & 1]);
                         if (kEdge && pos0 + 16 * h + (int32_t)(g + 8 * (e >> 1)) > last[nt][e & 1]) y = -INFINITY;
                         top = fmaxf(top, y);
                     }
             return top > kTop;
         };
+        auto exponents = [&]() { return far ? exponents_by(std::true_type{}) : exponents_by(std::false_type{}); };
         if (__any_sync(0xffffffffu, exponents())) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -334,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
                     for (int h = 0; h < TG; ++h)
 #pragma unroll
                         for (int e = j; e < 4; e += 2)
-                            m = fmaxf(m, x[h][nt][e] == -INFINITY ? -INFINITY : s[h][nt][e] * mul[nt][j]);
+                            m = fmaxf(m, x[h][nt][e] == -INFINITY ? -INFINITY : __fmul_rn(s[h][nt][e], mul[nt][j]));
                     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                     m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
@@ -346,7 +353,9 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
 #pragma unroll
                         for (int i = 0; i < kSteps; ++i) o[nt][i][j] *= f, o[nt][i][j + 2] *= f;
                     }
+                    far |= fabsf(ref[nt][j]) >= kFar && ref[nt][j] != -FLT_MAX;
                 }
+            far = __any_sync(0xffffffffu, far);
             exponents();
         }
         uint32_t pf[TG][NT][2];

@@ -124,6 +124,48 @@ def test_wide_range_of_scores_moves_the_reference():
     kv.check()
 
 
+@pytest.mark.parametrize("D,G,n_q", [(64, 3, 1), (128, 8, 2)])
+def test_scores_beyond_a_weights_exponents(D, G, n_q):
+    """Scores 2^24 and more apart: keys and queries with one nonzero value of few bits each, so that 32 bits hold the
+    scores exactly: the heaviest keys, several alike, share the weight."""
+    C, H, lens = 16, 2, [700, 33]
+    rng = np.random.default_rng(5)
+    n_pages = [-(-n // C) for n in lens]
+    pages = np.arange(2 * max(n_pages), dtype=np.int32).reshape(2, -1)
+    pool = random_pool(pages.size, C, H, D, rng).reshape(pages.size, H, -1)
+    pool[..., : 8 * D] = 0
+    pool[..., 0: 8 * D: D // 2] = rng.choice((2, 4, 7, 10, 15), pool[..., 0: 8 * D: D // 2].shape)  # 1, 2, 6, -1, -6
+    pool[..., 16 * D: 17 * D] = 0x38  # 1.0
+    pool = pool.reshape(pages.size, -1)
+    kv = cache(pool, C, H, D)
+    q = np.zeros((2, n_q, H * G, D), np.float32)
+    q[..., 0] = 2.0 ** rng.choice((3, 20, 30, 45, 90), q.shape[:3])
+    scale = 0.37
+    qt = torch.from_numpy(q).to(torch.bfloat16)
+    weight = torch.zeros(pages.shape, dtype=torch.float32, device="cuda")
+    out, lse = kv.attend(qt.cuda(), dev(np.array(lens, np.int32)), dev(pages), scale, weight)
+    kv.check()
+    got_w = weight.double().cpu().numpy()
+    for r, n in enumerate(lens):
+        k, v = R.get_tokens(pool, pages[r, : n_pages[r]], n, C, H, D)
+        total = 0.0
+        for h in range(H * G):
+            for i in range(n_q):
+                m = n - n_q + i + 1
+                s = float(q[r, i, h, 0]) * k[:m, h // G, 0]
+                w = np.exp(scale * (s - s.max()))
+                ref = w @ v[:m, h // G] / w.sum()
+                err = (np.minimum(scale * (s.max() - s), 40.0) * 2.0 ** -21).max()
+                rel = 2 * np.expm1(err) + 2.0 ** -8 + m * 2.0 ** -24
+                got = out[r, i, h].double().cpu().numpy()
+                assert np.all(np.abs(got - ref) <= rel * (np.abs(v[:m, h // G]).max() + np.abs(ref)))
+                want = scale * s.max() + np.log(w.sum())
+                assert abs(float(lse[r, i, h]) - want) <= 2.0 ** -21 * abs(want) + 2.0 ** -18
+                total += 1.0
+        # every query's weights add up to 1 over the pages
+        assert abs(got_w[r].sum() - total) <= total * (n * 2.0 ** -22 + 2.0 ** -18)
+
+
 def poison(pool, slot, tok, head, C, D, what):
     """Marks one scale byte of a token NaN: block 1 of its K or V."""
     gb = 16 * (D + D // 8)
