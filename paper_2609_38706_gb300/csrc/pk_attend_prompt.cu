@@ -1,5 +1,29 @@
 // pk_attend_prompt.cu -- causal attention over packed prompts with grouped
 // heads (pk_attend_prompt).
+//
+// out = sum_j p_j v_j / sum_j p_j over the keys j that a query sees, p_j =
+// 2^(s_j - ref), s_j = scale log2(e) q . k_j.  Any ref gives the same quotient:
+// it stays as long as a tile's weights of a row sum to 2^15 at most, which is
+// looked at after the weights are taken, not before.  So most tiles cost one
+// pass over the scores and no rescaling of the output; lse = ln 2 (ref + log2 of
+// the sum).  Scores, sums and outputs are 32 bits; the weights round to the
+// operands' type for the second product, which takes no other.
+//
+// Arithmetic: 4 D products a (query, key, head) on the tensor pipe, one 2^x on a
+// unit of 32 a clock.  A 128 x 128 tile of D = 128 is 1024 clocks of the first
+// and 512 of the second; at D = 64 the two are even.  So both have to run at
+// once: an item is two tiles, one's weights are taken while the other's products
+// run.  Rows of a tile are (token, head of the group), so K and V are read once
+// for a group.  Two tiles, because their scores (256 columns) and outputs
+// (2 D) fill the TMEM at D = 128.  At D = 64 a third buffer of scores, made
+// ahead, changed nothing (128 | 128 us), nor did halves of a tile to two
+// warpgroups (675 | 776 us at D = 128, two prompts of 8192).
+//
+// Two prompts of 8192 (32 heads over 8, D = 128, bf16): 605 us, 1.5 PFLOP/s,
+// tensor pipe 70% busy at 1.8 GHz under the power limit.  12 of 1500 behind 2048
+// keys (12 over 4, D = 64): 118 us, 0.79 PFLOP/s: a tile's chain (scores, 2^x,
+// product) and five items an SM.  8 of 512: 31 us, 3 short items an SM: the
+// chain's latency.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <float.h>
@@ -22,6 +46,7 @@ constexpr float kBase = 4.0f;     // the largest weight when the reference moves
 constexpr float kFar = 16777216.0f;  // scores (times log2 e) from here on are further apart than a weight's exponents:
                                      // one 32-bit reference cannot lie kBase below one
 constexpr int kPlanThreads = 1024;
+constexpr uint64_t kLongKeys = 1280;  // keys a request, on average, from which blocks take their items as they come
 
 struct Args {
     uint16_t *out;
@@ -116,6 +141,8 @@ struct Small {
     uint64_t q_full[2], q_empty[2];
     uint64_t s_full[2], p_ready[2], o_done[2];
     uint64_t edge_v[4];            // an edge tile's V loaded, by edge tile
+    uint64_t next_full[4], next_empty[4];  // an answer on the next item is there; its readers have it
+    alignas(16) uint64_t next[4][2];       // the answers
     uint32_t tmem, abort;
     int32_t work[8][2];            // by item with keys: key tiles of its two tiles, for the matrix warp; 0, 0 ends it
     uint32_t epilogues[8];         // by softmax warp: items whose outputs it has written
@@ -156,33 +183,32 @@ struct Item {
     int32_t n_tiles[2], first_last[2], n_all, first_edge;
 };
 
-// The turn-th item of this CTA.  Items come heaviest first within a request, so
-// every other turn runs through the CTAs backwards: one that got the heaviest of
-// a turn gets the lightest of the next (two prompts of 8192: 855 -> 830 us when added).
+// Item `index` of the call's; false: there are not so many, or an offset is out of range.
 __device__ __forceinline__ bool find_item(const Args &a, const Small &sm, const uint64_t *tile_off, const int64_t *q_off,
-                                          const int64_t *k_off, uint32_t turn, Item &it) {
-    const uint64_t wide = (uint64_t)turn * gridDim.x + (turn & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-    if (wide >= a.most_items) return false;  // less than 2^31: 32 bits do from here
-    const uint32_t index = (uint32_t)wide, tile = index / a.kv_heads;
+                                          const int64_t *k_off, uint32_t index, Item &it) {
+    const uint32_t tile = index / a.kv_heads;
     it.head = (int32_t)(index - tile * a.kv_heads);
-    uint32_t x;  // which of the request's items
+    it.q0 = it.k0 = it.lq = it.lk = 0;
+    uint32_t x = 0;  // which of the request's items
     if (tile_off) {
-        if (tile >= __ldcg(tile_off + a.R)) return false;
-        const uint32_t r = pk::warp_find_request(reinterpret_cast<const int64_t *>(tile_off), a.R, (int64_t)tile);
-        it.q0 = (int32_t)__ldcg(q_off + r);
-        it.k0 = (int32_t)__ldcg(k_off + r);
-        it.lq = (int32_t)__ldcg(q_off + r + 1) - it.q0;
-        it.lk = (int32_t)__ldcg(k_off + r + 1) - it.k0;
-        x = (uint32_t)__ldcg(tile_off + r + 1) - 1 - tile;
+        if (tile < __ldcg(tile_off + a.R)) {
+            const uint32_t r = pk::warp_find_request(reinterpret_cast<const int64_t *>(tile_off), a.R, (int64_t)tile);
+            it.q0 = (int32_t)__ldcg(q_off + r);
+            it.k0 = (int32_t)__ldcg(k_off + r);
+            it.lq = (int32_t)__ldcg(q_off + r + 1) - it.q0;
+            it.lk = (int32_t)__ldcg(k_off + r + 1) - it.k0;
+            x = (uint32_t)__ldcg(tile_off + r + 1) - 1 - tile;
+        }
     } else {
         const uint32_t lane = threadIdx.x & 31;
         const uint32_t r = __popc(__ballot_sync(0xffffffffu, sm.item_end[lane] <= tile));
-        if (r >= 32) return false;  // (requests past R repeat the total)
-        it.q0 = sm.q_start[r];
-        it.k0 = sm.k_start[r];
-        it.lq = sm.q_len[r];
-        it.lk = sm.k_len[r];
-        x = sm.item_end[r] - 1 - tile;
+        if (r < 32) {  // (requests past R repeat the total)
+            it.q0 = sm.q_start[r];
+            it.k0 = sm.k_start[r];
+            it.lq = sm.q_len[r];
+            it.lk = sm.k_len[r];
+            x = sm.item_end[r] - 1 - tile;
+        }
     }
     // the last queries first: they have the most keys
     it.chunk = (int32_t)(x % a.chunks);
@@ -198,7 +224,43 @@ __device__ __forceinline__ bool find_item(const Args &a, const Small &sm, const 
     // From this key tile on, some query does not see some key: p = 0 there, which must not meet an infinity or NaN
     // of V.  At most three tiles, as an item has at most 256 queries.
     it.first_edge = it.first_last[0] + 1 >= kKeys ? (it.first_last[0] + 1) / kKeys : 0;
-    return true;
+    return it.lq > 0;
+}
+
+// How a block gets to its next item.
+// Fixed: the grid has a block an SM, and every other turn runs through the blocks backwards: one that got the heaviest
+// item of a turn gets the lightest of the next.
+// Else the grid has a block for every item, and a running one takes the place of the next that has not started, until
+// none is left: the SM that is done first gets the next item.  Item n + 1 is asked for near the end of item n's loads.
+// It evens out what is left over at the end, but the next block number takes time to come, a block that waits for it
+// cannot look for its item early, and the next kernel starts later.  Fixed | taken, D = 128: 32 prompts of 512 103 |
+// 117 us, 8 of 2048 105 | 94, two of 8192 616 | 604; D = 64: 40 of 700 behind 300 keys 89 | 100, 12 of 1500 behind 2048
+// 130 | 118.  So the keys per request decide (kLongKeys).
+__device__ __forceinline__ void ask_next(uint32_t answer, uint32_t bar) {
+    pk::mbar_expect(bar, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(answer),
+                 "r"(bar)
+                 : "memory");
+}
+// n-th answer; false: no block was left.  ok turns false when none came.
+__device__ __forceinline__ bool next_taken(Small &sm, uint32_t n, bool reader, uint32_t &index, bool &ok) {
+    ok = pk::mbar_wait_warp(pk::smem_addr(&sm.next_full[n & 3]), n >> 2 & 1);
+    if (!ok) return false;
+    const volatile uint64_t *answer = sm.next[n & 3];
+    const uint64_t lo = answer[0], hi = answer[1];
+    uint32_t got;
+    asm volatile(
+        "{\n .reg .pred p;\n .reg .b128 r;\n mov.b128 r, {%2, %3};\n"
+        " clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n selp.u32 %0, 1, 0, p;\n mov.u32 %1, 0;\n"
+        " @p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n}"
+        : "=r"(got), "=r"(index)
+        : "l"(lo), "l"(hi));
+    if (reader) {
+        pk::fence_proxy_async();  // the slot's next answer comes by the async proxy
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) pk::mbar_arrive(pk::smem_addr(&sm.next_empty[n & 3]));
+    }
+    return got != 0;
 }
 
 // Registers move to the softmax warps, whose scores on their way and weights do not fit 168: 256 * 200 + 128 * 104 =
@@ -227,7 +289,7 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     return r;
 }
 
-// One CTA an SM walks over items.  Warp roles: one loads Q, K and V by TMA,
+// One CTA an SM takes one item after another.  Warp roles: one loads Q, K and V by TMA,
 // one issues the matrix products, two look after V at the causal edge, and
 // two warpgroups of four turn scores into weights, a thread a row, for one of
 // the item's two tiles each: while one tile's scores are weighed the other's
@@ -235,7 +297,7 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 // to a column, take the place of scores that have been read), then their outputs
 // (D columns each).  Every counter of a barrier's use runs on over the items, so
 // the next item's loads and first products run under this one's end.
-template <int D, uint32_t DT>
+template <int D, uint32_t DT, bool kFixed>
 __global__ void __launch_bounds__(kThreads, 1)
 k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                 const __grid_constant__ CUtensorMap map_v) {
@@ -262,7 +324,11 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
             pk::mbar_init(pk::smem_addr(&sm.p_ready[t]), 4);
             pk::mbar_init(pk::smem_addr(&sm.o_done[t]), 1);
         }
-        for (int i = 0; i < 4; ++i) pk::mbar_init(pk::smem_addr(&sm.edge_v[i]), 1);
+        for (int i = 0; i < 4; ++i) {
+            pk::mbar_init(pk::smem_addr(&sm.edge_v[i]), 1);
+            pk::mbar_init(pk::smem_addr(&sm.next_full[i]), 1);
+            pk::mbar_init(pk::smem_addr(&sm.next_empty[i]), 10);  // cleaning and softmax warps
+        }
         pk::mbar_fence_init();
         sm.abort = 0;
         for (int i = 0; i < 8; ++i) sm.epilogues[i] = 0;
@@ -285,15 +351,27 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
     };
 
     Item it;
-    uint32_t turn = 0;
-    bool more = find_item(a, sm, tile_off, q_off, k_off, turn, it);
+    uint32_t turn = 0, index = blockIdx.x;  // items before the present one; its number
+    auto next_index = [&](uint32_t n, bool reader, uint32_t &index, bool &ok) {
+        if (!kFixed) return next_taken(sm, n, reader, index, ok);
+        const uint64_t next = (uint64_t)(n + 1) * gridDim.x + (n & 1 ? blockIdx.x : gridDim.x - 1 - blockIdx.x);
+        index = (uint32_t)next;  // less than 2^31 if it is one
+        return next < a.most_items;
+    };
+    bool more = find_item(a, sm, tile_off, q_off, k_off, index, it);
     if (warp >= kWarpLoad) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
         if (warp == kWarpLoad) {
             uint32_t n = 0, edges = 0, nq[2] = {0, 0}, items = 0;  // ring stages, edge tiles, Q tiles, items so far
+            uint32_t asked = 0;
             bool ok = true;
             pk::fence_proxy_async();
             while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
+                auto ask = [&]() {  // by lane 0, once an item
+                    ok = ok && (turn < 4 || pk::mbar_wait(pk::smem_addr(&sm.next_empty[turn & 3]), (turn / 4 + 1) & 1));
+                    if (ok) ask_next(pk::smem_addr(sm.next[turn & 3]), pk::smem_addr(&sm.next_full[turn & 3])), ++asked;
+                };
+                if (lane == 0 && !kFixed && it.n_all <= 3) ask();
                 if (lane == 0 && it.n_all > 0) {
                     // its reader, at most four items behind, sees it by way of the first K tile's barrier
                     sm.work[items & 7][0] = it.n_tiles[0];
@@ -335,11 +413,14 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                                 ++nq[t];
                             }
                         }
+                        if (!kFixed && it.n_all > 3 && j == it.n_all - 3) ask();
                     }
                 }
                 ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                more = next_index(turn, false, index, ok);
                 ++turn;
-                more = find_item(a, sm, tile_off, q_off, k_off, turn, it);
+                if (more) more = find_item(a, sm, tile_off, q_off, k_off, index, it);
             }
             if (lane == 0) {
                 const uint32_t st = n % L::kStages;
@@ -352,7 +433,8 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                     ++n;
                 }
                 if (!ok) give_up();
-                // no copy of its own stays in flight
+                // no copy of its own stays in flight, and no answer on its way
+                if (asked > turn) pk::mbar_wait(pk::smem_addr(&sm.next_full[turn & 3]), turn >> 2 & 1);
                 for (uint32_t i = n > L::kStages ? n - L::kStages : 0; i < n; ++i)
                     pk::mbar_wait(pk::smem_addr(&sm.full[i % L::kStages]), (i / L::kStages) & 1);
                 for (int t = 0; t < 2; ++t)
@@ -532,8 +614,10 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                 }
                 base += 2 * it.n_all;
                 ++items;
+                if (!ok) break;
+                more = next_index(turn, true, index, ok);
                 ++turn;
-                more = find_item(a, sm, tile_off, q_off, k_off, turn, it);
+                if (more) more = find_item(a, sm, tile_off, q_off, k_off, index, it);
             }
             if (!ok && lane == 0) give_up();
         }
@@ -558,12 +642,16 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
             const int64_t q_row = it.q0 + tok;
             const uint32_t qh = it.head * a.group + gh;
             const bool notes = it.first_edge < n_tiles;  // only then are this item's notes sure to be there
-            ++turn;
-            more = find_item(a, sm, tile_off, q_off, k_off, turn, it);  // the next one
+            auto take_next = [&]() {
+                if (ok) more = next_index(turn, true, index, ok);
+                ++turn;
+                if (more) more = find_item(a, sm, tile_off, q_off, k_off, index, it);
+            };
+            if (kFixed) take_next();
             // a weight is 2^(score - ref + fine), and fine is 0 but for a reference of kFar and more
             float ref = -FLT_MAX, fine = 0.0f, sum = 0.0f;
 #pragma unroll 1
-            for (int32_t j = 0; j < n_tiles; ++j, ++ni) {
+            for (int32_t j = 0; ok && j < n_tiles; ++j, ++ni) {
                 ok = pk::mbar_wait_warp(pk::smem_addr(&sm.s_full[t]), ni & 1);
                 if (!ok) break;
                 pk::tmem_fence_after();
@@ -694,6 +782,7 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                 __syncwarp();
                 if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.p_ready[t]));
             }
+            if (!kFixed) take_next();  // while the last product runs
             if (ok && n_tiles > 0) ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
             if (!ok) break;
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -776,14 +865,20 @@ cudaError_t map_of(CUtensorMap *map, const pk_heads &h, uint64_t n, uint32_t hea
     return e == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <int D, uint32_t DT>
-cudaError_t launch(const Args &a, unsigned grid, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv,
+template <int D, uint32_t DT, bool kFixed>
+cudaError_t launch_as(const Args &a, unsigned grid, const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv,
                    cudaStream_t s) {
     constexpr size_t smem = Layout<D>::kBytes + sizeof(Small);
     static_assert(smem <= 227 * 1024, "shared memory of a block");
     static std::atomic<uint64_t> seen{0};
-    const cudaError_t e = pk_allow_smem(k_attend_prompt<D, DT>, smem, seen);
-    return e != cudaSuccess ? e : pk_launch_smem(k_attend_prompt<D, DT>, grid, kThreads, smem, s, a, mq, mk, mv);
+    const cudaError_t e = pk_allow_smem(k_attend_prompt<D, DT, kFixed>, smem, seen);
+    return e != cudaSuccess ? e : pk_launch_smem(k_attend_prompt<D, DT, kFixed>, grid, kThreads, smem, s, a, mq, mk, mv);
+}
+
+template <int D, uint32_t DT>
+cudaError_t launch(const Args &a, bool fixed, unsigned grid, const CUtensorMap &mq, const CUtensorMap &mk,
+                   const CUtensorMap &mv, cudaStream_t s) {
+    return fixed ? launch_as<D, DT, true>(a, grid, mq, mk, mv, s) : launch_as<D, DT, false>(a, grid, mq, mk, mv, s);
 }
 
 }  // namespace
@@ -831,10 +926,11 @@ cudaError_t pk_launch_attend_prompt(uint32_t dtype, const pk_heads &q, const pk_
     const uint64_t items = (n_q / item_tokens + R) * a.chunks * kv_heads;
     if (items > 0x7fffffffull) return cudaErrorInvalidValue;
     a.most_items = (uint32_t)items;
-    const unsigned grid = items < (uint64_t)sms ? (unsigned)items : (unsigned)sms;
+    const bool fixed = items <= (uint64_t)sms || n_k < kLongKeys * R;
+    const unsigned grid = fixed && items > (uint64_t)sms ? (unsigned)sms : (unsigned)items;
     if (head_dim == 128)
-        e = dtype == PK_BF16 ? launch<128, PK_BF16>(a, grid, mq, mk, mv, s) : launch<128, PK_FP16>(a, grid, mq, mk, mv, s);
+        e = dtype == PK_BF16 ? launch<128, PK_BF16>(a, fixed, grid, mq, mk, mv, s) : launch<128, PK_FP16>(a, fixed, grid, mq, mk, mv, s);
     else
-        e = dtype == PK_BF16 ? launch<64, PK_BF16>(a, grid, mq, mk, mv, s) : launch<64, PK_FP16>(a, grid, mq, mk, mv, s);
+        e = dtype == PK_BF16 ? launch<64, PK_BF16>(a, fixed, grid, mq, mk, mv, s) : launch<64, PK_FP16>(a, fixed, grid, mq, mk, mv, s);
     return e != cudaSuccess ? e : cudaGetLastError();
 }

@@ -106,6 +106,31 @@ def test_many_more_blocks_than_the_gpu_holds(H, G, D, dtype):
     check(q, k, v, lq, lk, *res[0], dtype, D ** -0.5, rows=np.array([0, 31, 64, 200, 255, 256, 300, 511]))
 
 
+@pytest.mark.parametrize("R,H,G,D,dtype", [(7, 8, 4, 128, "bf16"), (41, 4, 3, 64, "fp16"), (1, 4, 128, 64, "bf16")])
+def test_blocks_take_items_as_they_come(R, H, G, D, dtype):
+    """More items than SMs and many keys a request: a block's next item is the next that has not started.  Requests
+    without queries or keys among them, calls back to back and on two streams: the same bits each time."""
+    from paper_2609_38706_gb300 import service
+    rng = np.random.default_rng(R)
+    lq = [int(x) for x in rng.integers(60, 400 if R < 32 else 90, R)]
+    lk = [n + int(x) for n, x in zip(lq, rng.integers(1300, 2400, R))]
+    if R > 1:
+        lq[3], lk[5] = 0, 0
+    q, k, v = inputs(lq, lk, H, G, D, dtype, 23)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    args = q.cuda(), k.cuda(), v.cuda(), dev(offs(lq)), dev(offs(lk))
+    res = [service.attend_prompt(*args, status=status) for _ in range(4)]
+    torch.cuda.synchronize()
+    for s in [torch.cuda.Stream() for _ in range(2)]:
+        with torch.cuda.stream(s):
+            res.append(service.attend_prompt(*args, status=status))
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    for out, lse in res[1:]:
+        assert torch.equal(out, res[0][0]) and torch.equal(lse, res[0][1])
+    check(q, k, v, lq, lk, *res[0], dtype, D ** -0.5, rows=np.array([0, 41, 84, 300]))
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
 def test_scales_and_peaked_rows(scale):
     """A scale of 0 weighs all keys alike; a large one is decided by the maximum, which moves as keys come."""

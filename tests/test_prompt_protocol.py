@@ -1,5 +1,6 @@
 """CPU model of the prompt-attention kernel's barriers: loader, matrix, cleaning and softmax warps of one CTA, which
-walks over several items, as coroutines under random interleavings, with the copies and the matrix pipe as asynchronous agents.  Checks that no
+takes one item after another, as coroutines under random interleavings, with the copies, the answers on the next item
+and the matrix pipe as asynchronous agents.  Checks that no
 barrier gets an arrival its phase does not expect, that every product reads what it should, that nothing is overwritten
 while it is read, that all roles end, and that nothing asynchronous is left when they have."""
 import random
@@ -46,11 +47,48 @@ class Cta:
         self.epilogues, self.notes = [0] * 8, [None, None]
         self.stored = [set(), set()]
         self.speed = rng.choice((0.5, 0.02)), rng.choice((0.5, 0.05))
+        self.next, self.given = [None] * 4, 1  # answers; items given out
+        self.next_full, self.next_empty = [Bar(1) for _ in range(4)], [Bar(10) for _ in range(4)]
         self.rescale = rng.choice((0.0, 0.3))
 
+    def ask(self, turn):
+        while turn >= 4 and not self.next_empty[turn & 3].done((turn // 4 + 1) & 1):
+            yield
+        self.next_full[turn & 3].arrive(tx=1)
+        self.next[turn & 3] = None
+        self.copies.append((self.next, turn & 3, "next", self.next_full[turn & 3]))
+
+    def read(self, turn, reader=True):
+        while not self.next_full[turn & 3].done(turn >> 2 & 1):
+            yield
+        x = self.next[turn & 3]
+        assert x is not None
+        yield
+        if reader:
+            self.next_empty[turn & 3].arrive()
+        return x
+
+    def walk(self):
+        """The items that a cleaning or softmax warp goes through, read as the kernel does; None: not there yet."""
+        turn, x = 0, 0
+        while x != "end":
+            yield x
+            step = self.read(turn)
+            while True:
+                try:
+                    next(step)
+                except StopIteration as e:
+                    x = e.value
+                    break
+                yield None
+            turn += 1
+
     def loader(self):
-        n, edges, nq, sent = 0, 0, [0, 0], 0
-        for x, (n0, n1, fe) in enumerate(self.items):
+        n, edges, nq, sent, x, turn = 0, 0, [0, 0], 0, 0, 0
+        while x != "end":
+            n0, n1, fe = self.items[x]
+            if max(n0, n1) <= 3:
+                yield from self.ask(turn)
             if max(n0, n1):
                 assert self.work[sent & 7] is None, "an item's note overwritten before it was read"
                 self.work[sent & 7] = x
@@ -80,6 +118,10 @@ class Cta:
                     self.copies.append((self.q, t, x, self.q_full[t]))
                     nq[t] += 1
                     yield
+                if max(n0, n1) > 3 and j == max(n0, n1) - 3:
+                    yield from self.ask(turn)
+            x = yield from self.read(turn, False)
+            turn += 1
         st = n % self.S
         while n >= self.S and not self.empty[st].done((n // self.S + 1) & 1):
             yield
@@ -150,7 +192,11 @@ class Cta:
 
     def cleaner(self, half):
         base, edges = 0, 0
-        for x, (n0, n1, fe) in enumerate(self.items):
+        for x in self.walk():
+            if x is None:
+                yield
+                continue
+            n0, n1, fe = self.items[x]
             n_all = max(n0, n1)
             if fe < n_all:
                 while x >= 2 and min(self.epilogues) < x - 1:
@@ -171,7 +217,9 @@ class Cta:
 
     def softmax(self, t, warp):
         ni = 0
-        for x, item in enumerate(self.items):
+        turn, x = 0, 0
+        while x != "end":
+            item = self.items[x]
             fe = item[2]
             for j in range(item[t]):
                 while not self.s_full[t].done(ni & 1):
@@ -188,18 +236,22 @@ class Cta:
                     self.sp[t] = ("P", x, j)
                 self.p_ready[t].arrive()
                 ni += 1
+            here, x = x, (yield from self.read(turn))
+            turn += 1
             if item[t]:
                 while not self.o_done[t].done((ni - 1) & 1):
                     yield
                 for _ in range(self.rng.choice((1, 1, 40))):
-                    assert self.o[t] == (x, item[t] - 1), "O overwritten before it was read"
-                    assert fe >= item[t] or self.notes[x & 1] == x
+                    assert self.o[t] == (here, item[t] - 1), "O overwritten before it was read"
+                    assert fe >= item[t] or self.notes[here & 1] == here
                     yield
-            self.epilogues[4 * t + warp] = x + 1
+            self.epilogues[4 * t + warp] = here + 1
 
     def agents(self):
         if self.copies and self.rng.random() < self.speed[0]:
             where, at, content, bar = self.copies.pop(self.rng.randrange(len(self.copies)))
+            if content == "next":
+                content, self.given = (self.given if self.given < len(self.items) else "end"), self.given + 1
             where[at] = content
             bar.landed(1)
         if self.pipe and self.rng.random() < self.speed[1]:
