@@ -1,5 +1,14 @@
 // pk_kv.cu -- the 4-bit page store: quantise new K/V into their pages
 // (pk_kv_write) and read pages back as 16-bit rows (pk_kv_read).
+//
+// A value is code * scale * k_scale (v_scale): per block of 16 dimensions the
+// scale is e4m3(max|x| / 6 / k_scale) and a code e2m1(x / (scale * k_scale)).
+// A lane has a whole block, so nothing is exchanged between lanes, and each byte
+// moves once: 4 D bytes a token and head of rows, 1.125 D of pages.  64 prompts
+// of 1024 to 2048 tokens (8 heads, D = 128, 511 MB either way): write 109 us, 4.7
+// TB/s, held by the issue of the conversions (62% of the slots); read 89 us, 5.7
+// TB/s.  Small calls are a chain of latencies: request, page, row, 4 us for one
+// token a request.
 #include <cuda_runtime.h>
 
 #include "pk_device.cuh"
@@ -87,8 +96,6 @@ __device__ __forceinline__ void quantise16(const uint4 (&v)[2], float g, uint2 *
 // requests is paid once.  Codes of a token are D/2 consecutive bytes and
 // consecutive tokens of a granule follow each other, so whole 32-byte sectors
 // are written where four tokens (two for D = 64's codes) lie together.
-// Bound by memory: 4 D bytes of K and V against 1.125 D bytes of pages a token
-// and head.
 template <int D, uint32_t DT, bool kWrite>
 __global__ void __launch_bounds__(kMoveThreads) k_kv_move(const Move a) {
     constexpr uint32_t kLanes = D / 16, kTokens = 32 / kLanes;
