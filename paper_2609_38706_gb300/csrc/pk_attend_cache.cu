@@ -22,7 +22,7 @@
 // 16 requests of up to 131072 tokens (8 KV heads, groups of 8, D = 128): 326 us
 // for both launches, 5.4 TB/s of pages, the attention itself 302 us with 77% of
 // the memory's cycles and 65% of the issue slots taken (dequantising is 58% of
-// the ALU's).  128 requests of up to 2048: 66 us (57 + 9): 1024 CTAs of unequal
+// the ALU's).  128 requests of up to 2048: 64 us (55 + 9): 1024 CTAs of unequal
 // lengths for 608 places.  Short caches: two launches, 8 us.
 #include <cuda_runtime.h>
 #include <float.h>
@@ -43,6 +43,7 @@ namespace {
 constexpr int kWarps = 4;
 constexpr uint32_t kSlots = 152 * 16 / kWarps;  // CTAs that the GPU holds
 constexpr int kThreads = 32 * kWarps;
+constexpr uint32_t kRanked = 256, kRankedGrans = 64;  // requests that are ranked by length: most of them, least size
 constexpr int kFinishWarps = 8, kFinishThreads = 32 * kFinishWarps;
 constexpr float kTop = 15.0f;   // p stays below 2^kTop (half: 2^16)
 // Scores (times log2 e) from here on are further apart than a half's exponents, and so is a product from its rounding:
@@ -55,6 +56,7 @@ struct Args {
     uint64_t page_bytes, n_slots;
     uint32_t page_tokens, page_grans, kv_heads, group, n_q, rows, row_tiles, R;
     uint32_t splits, split_grans;  // granules of one split
+    bool by_length;                // the longest requests' blocks come first
     float scale2, v_scale;         // scale2 = scale * k_scale * log2 e
     const uint16_t *q;
     int64_t q_ts, q_hs;
@@ -125,6 +127,45 @@ struct Shape {
 // One CTA: one request, KV head, tile of 8 NT query rows and split of the
 // tokens.  Warp w takes the split's steps w, w + kWarps, ... of kGrans granules.
 // Lane = 4 g + c.
+// The n-th request by length, longest first, in 64 steps of the longest; within a step by number.  By every warp for
+// itself: a search over the steps that counts by votes.
+__device__ __forceinline__ uint32_t nth_longest(const int32_t *kv_len, uint32_t R, uint32_t n) {
+    constexpr int kPer = kRanked / 32;
+    const uint32_t lane = threadIdx.x & 31;
+    int32_t x[kPer], most = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        x[k] = 32 * k + lane < R ? max(__ldcg(kv_len + 32 * k + lane), 0) : -1;
+        most = max(most, x[k]);
+    }
+    const int shift = max(26 - __clz(__reduce_max_sync(0xffffffffu, most)), 0);
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) x[k] >>= shift;  // 0..63; -1 stays
+    int32_t step = 0;  // the largest that more than n requests reach
+    uint32_t above = 0;
+#pragma unroll
+    for (int bit = 32; bit; bit /= 2) {
+        uint32_t reach = 0;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k)
+            if (32 * k < R) reach += __popc(__ballot_sync(0xffffffffu, x[k] >= step + bit));
+        if (reach > n)
+            step += bit;
+        else
+            above = reach;  // fewer as `step + bit` falls: in the end those above `step`
+    }
+    uint32_t m = n - above, r = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const bool in = x[k] == step;
+        const uint32_t all = __ballot_sync(0xffffffffu, in), before = __popc(all & ((1u << lane) - 1));
+        const uint32_t hit = __ballot_sync(0xffffffffu, in && before == m);
+        if (hit) r = 32 * k + __ffs(hit) - 1;
+        m -= __popc(all);  // past the request's own: wraps, and nothing is hit
+    }
+    return r;
+}
+
 template <int D, int NT, uint32_t DT, bool kWeigh>
 __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Args a) {
     using G = pk::Granule<D>;
@@ -143,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
     const uint32_t tile = id % a.row_tiles;
     id /= a.row_tiles;
     const uint32_t head = id % a.kv_heads;
-    const uint32_t r = id / a.kv_heads;
+    uint32_t r = id / a.kv_heads;
 
     uint8_t *ring = smem + warp * S::kRing;
     const uint32_t ring_s = pk::smem_addr(ring), bar_s = pk::smem_addr(&bars[warp][0]);
@@ -159,6 +200,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
     const uint32_t *pages = a.pages;
     pk::pdl_wait(pool, qp, kv_len, pages);
     pk::fence_proxy_async();  // pages written by an earlier kernel are read by the async proxy
+    if (a.by_length) r = nth_longest(kv_len, a.R, r);
 
     const uint64_t most = a.page_stride * a.page_tokens;
     const int32_t len = length_of(kv_len, r, most);
@@ -729,6 +771,11 @@ cudaError_t pk_launch_attend_cache(const pk_kv_cache &kv, uint32_t dtype, const 
     a.R = R;
     a.splits = p.splits;
     a.split_grans = p.split_grans;
+    // One CTA a request and head, and more of them than the GPU holds: the longest first, so that the last to start are
+    // the shortest (128 x 2048 tokens: 65.6 -> 63.5 us; 100 x 1500, D = 64: 36.9 -> 35.2).  The search costs short
+    // ones more than it gives (250 x 300: 31.7 -> 38.4 us).
+    a.by_length = p.splits == 1 && R > 1 && R <= kRanked && p.max_grans >= kRankedGrans &&
+                  (uint64_t)R * kv.kv_heads * p.row_tiles > kSlots;
     a.scale2 = (float)((double)scale * kv.k_scale * 1.4426950408889634);
     a.v_scale = kv.v_scale;
     a.q = static_cast<const uint16_t *>(q.p);

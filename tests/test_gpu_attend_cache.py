@@ -109,6 +109,36 @@ def test_matches_reference(lens, n_q, C, H, G, D, dtype, k_scale, v_scale, weigh
         assert np.all(np.abs(got - w0 - rw) <= bound + 1e-9)
 
 
+@pytest.mark.parametrize("weigh", [False, True])
+def test_more_requests_than_places_longest_first(weigh):
+    """Long and short requests, equal and empty ones, in more blocks than the GPU holds: each gets its own answer."""
+    rng = np.random.default_rng(31)
+    lens = [int(x) for x in rng.integers(1, 200, 90)]
+    lens[3], lens[17], lens[40], lens[41], lens[89] = 1100, 0, 1039, 1040, 700
+    lens[50:60] = [64] * 10
+    C, H, G, D = 16, 8, 2, 64
+    pages = np.zeros((90, 69), np.int32)
+    slots = 0
+    for r, n in enumerate(lens):
+        k = -(-n // C)
+        pages[r, :k] = slots + np.arange(k)
+        slots += k
+    pool = random_pool(slots, C, H, D, rng)
+    kv = cache(pool, C, H, D)
+    q = torch.from_numpy(rng.standard_normal((90, 1, H * G, D))).to(torch.bfloat16)
+    weight = torch.zeros(pages.shape, dtype=torch.float32, device="cuda") if weigh else None
+    out, lse = kv.attend(q.cuda(), dev(np.array(lens, np.int32)), dev(pages), 0.125, weight)
+    kv.check()
+    ref, rl, rw, mag, err = reference(pool, pages, lens, q.double().numpy(), C, H, D, 0.125)
+    assert np.all(np.abs(out.double().cpu().numpy() - ref) <= R.out_bound(ref, mag, R.U["fp16"], R.U["bf16"], err, 1100))
+    gl, none = lse.double().cpu().numpy(), np.isneginf(rl)
+    assert np.array_equal(none, np.isneginf(gl))
+    assert np.all(np.abs(gl[~none] - rl[~none]) <= R.lse_bound(rl, err, 1100)[~none])
+    if weigh:
+        got = weight.double().cpu().numpy()
+        assert np.all(np.abs(got - rw) <= (2 * np.expm1(err) + 1300 * 2.0 ** -24) * rw + 2.0 ** -23 * rw + 1e-9)
+
+
 def test_wide_range_of_scores_moves_the_reference():
     """Scores that grow by hundreds along the tokens, and queries far outside a half's range."""
     lens, C, H, G, D = [900], 16, 1, 4, 128
