@@ -22,7 +22,7 @@
 // 16 requests of up to 131072 tokens (8 KV heads, groups of 8, D = 128): 326 us
 // for both launches, 5.4 TB/s of pages, the attention itself 302 us with 77% of
 // the memory's cycles and 65% of the issue slots taken (dequantising is 58% of
-// the ALU's).  128 requests of up to 2048: 64 us (55 + 9): 1024 CTAs of unequal
+// the ALU's).  128 requests of up to 2048: 60 us (55 + 5): 1024 CTAs of unequal
 // lengths for 608 places.  Short caches: two launches, 8 us.
 #include <cuda_runtime.h>
 #include <float.h>
@@ -590,6 +590,10 @@ __device__ __forceinline__ uint32_t live_splits(const Args &a, int32_t len) {
 
 constexpr uint32_t kStatRows = 512;
 
+// Pages that a warp of k_cache_finish weighs: short ones by several, four granules at once (pages of 16 tokens, 128 x
+// 2048 tokens, by one | four: 63.5 | 60.4 us).
+__host__ __device__ constexpr uint32_t pages_a_warp(uint32_t page_grans) { return page_grans < 4 ? 4 / page_grans : 1; }
+
 // The rest of a call, by block: the first ones join the splits of the query
 // rows (a warp a row), the others add to the pages' weights
 //     page_weight[r][j] += sum over heads, rows and granules of the page of
@@ -646,14 +650,15 @@ __global__ void __launch_bounds__(kFinishThreads) k_cache_finish(const Args a, u
             a.lse[t * (a.kv_heads * a.group) + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
         return;
     }
-    const uint32_t blocks = (uint32_t)((a.page_stride + kFinishWarps - 1) / kFinishWarps);
-    const uint32_t id = blockIdx.x - join_blocks, r = id / blocks, page0 = id % blocks * kFinishWarps;
+    const uint32_t per = pages_a_warp(a.page_grans), block_pages = kFinishWarps * per;
+    const uint32_t blocks = (uint32_t)((a.page_stride + block_pages - 1) / block_pages);
+    const uint32_t id = blockIdx.x - join_blocks, r = id / blocks, page0 = id % blocks * block_pages;
     const int32_t len = length_of(kv_len, r, most);
     const uint32_t n = live_splits(a, len), n_gran = ((uint32_t)len + 15) / 16;
     if ((uint64_t)page0 * a.page_grans >= n_gran) return;  // uniform: no token in these pages
     const uint32_t total = a.kv_heads * a.rows;
-    const uint32_t page = page0 + warp, gr0 = page * a.page_grans, gr1 = min(gr0 + a.page_grans, n_gran);
-    float acc = 0.0f;
+    const uint32_t page = page0 + warp * per, gr0 = page * a.page_grans, gr1 = min(gr0 + per * a.page_grans, n_gran);
+    float acc[4] = {};  // of the granules gr0 + i mod 4
     for (uint32_t base = 0; base < total; base += kStatRows) {
         __syncthreads();
         for (uint32_t x = tid; x < kStatRows && base + x < total; x += kFinishThreads) {
@@ -676,16 +681,30 @@ __global__ void __launch_bounds__(kFinishThreads) k_cache_finish(const Args a, u
             const float2 st = stat[x];
             const float2 *src = gran_ml + (((uint64_t)r * a.kv_heads + head) * a.row_tiles + row / tile_rows) *
                                               a.gran_stride * a.gran_rows + row % tile_rows;
-#pragma unroll 8
-            for (uint32_t gr = gr0; gr < gr1; ++gr) {
-                const float2 y = __ldcg(src + (uint64_t)gr * a.gran_rows);
-                acc += y.x * ex2(y.y - st.x) * st.y;
+#pragma unroll 2
+            for (uint32_t gr = gr0; gr < gr1; gr += 4) {
+                float2 y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    y[i] = gr + i < gr1 ? __ldcg(src + (uint64_t)(gr + i) * a.gran_rows) : make_float2(0.0f, -FLT_MAX);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (gr + i < gr1) acc[i] += y[i].x * ex2(y[i].y - st.x) * st.y;
             }
         }
     }
 #pragma unroll
-    for (int d = 16; d; d /= 2) acc += __shfl_xor_sync(0xffffffffu, acc, d);
-    if (lane == 0 && gr0 < n_gran) weight[(uint64_t)r * a.page_stride + page] += acc;
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int d = 16; d; d /= 2) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], d);
+    // lane p adds to page p of the warp's
+    if (lane < per && gr0 + lane * a.page_grans < gr1) {
+        float sum = per == 1 ? (acc[0] + acc[1]) + (acc[2] + acc[3]) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (per > 1 && i / a.page_grans == lane) sum += acc[i];
+        weight[(uint64_t)r * a.page_stride + page + lane] += sum;
+    }
 }
 
 struct Plan {
@@ -737,7 +756,8 @@ cudaError_t launch(const Args &a, const Plan &p, cudaStream_t s) {
     if (units * p.splits > 0x7fffffffull) return cudaErrorInvalidValue;
     e = pk_launch_smem(kern, (unsigned)(units * p.splits), kThreads, smem, s, a);
     const uint64_t join = p.splits > 1 ? ((uint64_t)a.R * a.kv_heads * p.rows + kFinishWarps - 1) / kFinishWarps : 0;
-    const uint64_t weigh = a.page_weight ? (a.page_stride + kFinishWarps - 1) / kFinishWarps * a.R : 0;
+    const uint64_t block_pages = kFinishWarps * pages_a_warp(a.page_grans);
+    const uint64_t weigh = a.page_weight ? (a.page_stride + block_pages - 1) / block_pages * a.R : 0;
     if (join + weigh > 0x7fffffffull) return cudaErrorInvalidValue;
     if (e == cudaSuccess && join + weigh)
         e = pk_launch(k_cache_finish<D, DT>, (unsigned)(join + weigh), kFinishThreads, s, a, p.tile_rows, (uint32_t)join);
