@@ -131,6 +131,24 @@ def test_blocks_take_items_as_they_come(R, H, G, D, dtype):
     check(q, k, v, lq, lk, *res[0], dtype, D ** -0.5, rows=np.array([0, 41, 84, 300]))
 
 
+@pytest.mark.parametrize("R,n,prefix,H,G,D", [(8, 300, 1700, 8, 4, 128), (40, 100, 1400, 4, 3, 64), (8, 300, 0, 8, 4, 128)])
+def test_captured_calls_replay_the_same(R, n, prefix, H, G, D):
+    """Two calls behind each other in a CUDA graph, replayed: the bits of a plain call, either way of giving out items."""
+    from paper_2609_38706_gb300 import service
+    q, k, v = (x.cuda() for x in inputs([n] * R, [n + prefix] * R, H, G, D, "bf16", 29))
+    qo, ko = dev(offs([n] * R)), dev(offs([n + prefix] * R))
+    want = service.attend_prompt(q, k, v, qo, ko)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = [service.attend_prompt(q, k, v, qo, ko) for _ in range(2)]
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    for out, lse in got:
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
 def test_scales_and_peaked_rows(scale):
     """A scale of 0 weighs all keys alike; a large one is decided by the maximum, which moves as keys come."""
