@@ -52,8 +52,10 @@ __device__ __forceinline__ float divide(float x, float den, float inv) {
 // also finds an infinity or NaN.  den = s * g and the true division x / den
 // are the format's definition (pk.h): a tie between two codes is then decided
 // by the values, not by a reciprocal's rounding.  A quotient below 2^-3 is code
-// 0 however it is rounded, so only den bounds where divide() holds; outside it
-// (no calibrated scale is there) the plain division is called.
+// 0 however it is rounded, so divide() holds while den and the largest quotient,
+// a / den, are far from the ends of the range.  Elsewhere (no calibrated scale is
+// there) the plain division is called: past the top, divide() would take an
+// infinity from an infinity.
 template <uint32_t DT>
 __device__ __forceinline__ void quantise16(const uint4 (&v)[2], float g, uint2 *codes, uint32_t *scale) {
     const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
@@ -66,7 +68,7 @@ __device__ __forceinline__ void quantise16(const uint4 (&v)[2], float g, uint2 *
     const uint32_t s = finite ? pk::e4m3_byte(fminf(__fdiv_rn(a * (1.0f / 6.0f), g), 448.0f)) : 0x7fu;
     const float den = __fmul_rn(pk::e4m3_to_float(s), g);
     uint32_t out[2] = {0, 0};
-    if (finite && den > 0x1p-60f && den < 0x1p60f) {
+    if (finite && den > 0x1p-60f && den < 0x1p60f && a < den * 0x1p60f) {
         const float inv = __frcp_rn(den);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
