@@ -4,8 +4,9 @@
 // With s_j = scale * k_scale * (q . K_j), p_j = 2^(s_j log2 e - ref) and one
 // pass over the tokens, o = v_scale * sum p_j V_j / sum p_j: the format's
 // tensor scales leave the loop, and what is left of a value, code * scale, has
-// six significant bits, so it is exact in a half and every product of the QK
-// step is exact in 32 bits.  `ref` is a running score near the maximum; it moves
+// six significant bits, so it is exact in a half; so are the values of q, scaled
+// by a power of two (small ones beside a large one in two halves), and every
+// product of the QK step is exact in 32 bits.  `ref` is a running score near the maximum; it moves
 // only when a p would pass 2^15 (a warp vote), so rescaling is rare, and to the
 // maximum itself, so that the heaviest p is a power of two, which its rounding to
 // a half leaves as it is: a row with one key gets that key's value exactly.
@@ -248,8 +249,11 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
     for (int k = 0; k < S::kStages; ++k) issue(k);
 
     // Q: column n = g of tile nt, dimensions c D/4 + 4 s + {0..3} at step s; scaled by a power of two that
-    // brings the row's largest value to [2^7, 2^8), so that a half holds any 16-bit row.
+    // brings the row's largest value to [2^7, 2^8).  A half then holds all 8 or 11 bits of what is above 2^-14 or
+    // so; where a row has nonzero values below (`wide`), their rest goes through a second product (see step()).
     uint32_t qf[NT][kSteps][2];
+    bool wide = false;
+    uint32_t up_bits[NT];  // that power of two
     float mul[NT][2];   // for columns 2c, 2c + 1
     int32_t last[NT][2];
 #pragma unroll
@@ -278,10 +282,18 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
         e = top == 0.0f || e == 128 ? 7 : max(e, -110);
         const float up = __uint_as_float((uint32_t)(7 - e + 127) << 23);
         const float down = __uint_as_float((uint32_t)(e - 7 + 127) << 23);
+        up_bits[nt] = __float_as_uint(up);
+        uint32_t least = 0xffffffffu;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             qf[nt][s][0] = half2_of(x[4 * s] * up, x[4 * s + 1] * up);
             qf[nt][s][1] = half2_of(x[4 * s + 2] * up, x[4 * s + 3] * up);
+            least = __vminu2(least, __vminu2(qf[nt][s][0] & 0x7c007c00u, qf[nt][s][1] & 0x7c007c00u));
+        }
+        // only a half without an exponent can have lost something
+        if ((least & 0xffffu) == 0 || least >> 16 == 0) {
+#pragma unroll
+            for (int i = 0; i < D / 4; ++i) wide |= __half2float(__float2half_rn(x[i] * up)) != x[i] * up;
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -290,6 +302,8 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
             last[nt][j] = len - (int32_t)a.n_q + (int32_t)(cr < a.rows ? cr / a.group : a.n_q - 1);
         }
     }
+
+    wide = __any_sync(0xffffffffu, wide);
 
     float o[NT][kSteps][4], ref[NT][2], sum[NT][2];
 #pragma unroll
@@ -308,9 +322,11 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
                                 warp * TG + (g >> 1)) * a.gran_rows + 2 * c + (g & 1));
     bool gave_up = false, far = false;  // far: a reference of the warp's is
 
-    // One step: TG granules in stage `st`.  kEdge: some query does not see some token of them.
-    auto step = [&](uint32_t k, uint32_t st, auto edge) {
-        constexpr bool kEdge = decltype(edge)::value;
+    // One step: TG granules in stage `st`.  kEdge: some query does not see some token of them.  kWide: what the halves
+    // of Q lost of a small value beside a large one, times 2^38 a half again, has its own product with K (exact down
+    // to 2^-62 of the row's largest value); such rows are rare, so it is read from Q again at each step.
+    auto step = [&](uint32_t k, uint32_t st, auto edge, auto with_rest) {
+        constexpr bool kEdge = decltype(edge)::value, kWide = decltype(with_rest)::value;
         const uint8_t *gr = ring + st * S::kStage;
         const int32_t pos0 = (int32_t)((g0 + (warp + k * kWarps) * TG) * 16);
 
@@ -353,6 +369,46 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
                 for (int nt = 0; nt < NT; ++nt) {
                     mma(s[h][nt], h0[0], h1[0], h0[1], h1[1], qf[nt][2 * j][0], qf[nt][2 * j][1]);
                     mma(s[h][nt], h0[2], h1[2], h0[3], h1[3], qf[nt][2 * j + 1][0], qf[nt][2 * j + 1][1]);
+                }
+            }
+            if (kWide) {
+#pragma unroll 1
+                for (int nt = 0; nt < NT; ++nt) {
+                    const uint32_t row = tile * kRows + nt * 8 + g, i = row / a.group;
+                    const uint16_t *src = qp + ((int64_t)r * a.n_q + i) * a.q_ts +
+                                          (int64_t)(head * a.group + (row - i * a.group)) * a.q_hs + c * (D / 4);
+                    const float up = __uint_as_float(NT == 2 && nt ? up_bits[NT - 1] : up_bits[0]);
+                    float rest[4] = {};
+#pragma unroll 1
+                    for (int j = 0; j < D / 32; ++j) {
+                        const uint4 u = row < a.rows ? __ldcg(reinterpret_cast<const uint4 *>(src + 8 * j))
+                                                     : make_uint4(0, 0, 0, 0);
+                        const uint32_t y[4] = {u.x, u.y, u.z, u.w};
+                        uint32_t b[4], kf[2][4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float2 f = pk::Elem<DT>::to2(y[i]);
+                            const float lo = f.x * up, hi = f.y * up;
+                            const __half2 had = __floats2half2_rn(lo, hi);
+                            b[i] = half2_of((lo - __low2float(had)) * 0x1p38f, (hi - __high2float(had)) * 0x1p38f);
+                        }
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            const uint8_t *tok = gr + h * G::kBytes + G::kK + (g + 8 * t) * G::kRow + c * (D / 8) + 4 * j;
+                            const uint8_t *ss = gr + h * G::kBytes + G::kKs + (g + 8 * t) * G::kScales + c * (D / 64) + j / 2;
+                            const uint32_t z = pk::e4m3_to_half2(*ss);
+                            pk::e2m1x8_to_half2(*reinterpret_cast<const uint32_t *>(tok), kf[t]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) kf[t][i] = hmul2(kf[t][i], __byte_perm(z, z, 0x1010));
+                        }
+                        mma(rest, kf[0][0], kf[1][0], kf[0][1], kf[1][1], b[0], b[1]);
+                        mma(rest, kf[0][2], kf[1][2], kf[0][3], kf[1][3], b[2], b[3]);
+                    }
+#pragma unroll
+                    for (int n2 = 0; n2 < NT; ++n2)
+                        if (n2 == nt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[h][n2][e] = fmaf(rest[e], 0x1p-38f, s[h][n2][e]);
                 }
             }
         }
@@ -515,21 +571,27 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
         }
     };
 
-    uint32_t st = 0, turn = 0;
+    auto walk = [&](auto with_rest) {
+        uint32_t st = 0, turn = 0;
 #pragma unroll 1
-    for (uint32_t k = 0; k < mine; ++k) {
-        if (!pk::mbar_wait_warp(bar_s + 8 * st, turn & 1)) {
-            gave_up = true;
-            for (uint32_t i = k + 1; i < min(k + S::kStages, mine); ++i)  // no copy of its own stays in flight
-                pk::mbar_wait(bar_s + 8 * (i % S::kStages), (i / S::kStages) & 1);
-            break;
+        for (uint32_t k = 0; k < mine; ++k) {
+            if (!pk::mbar_wait_warp(bar_s + 8 * st, turn & 1)) {
+                gave_up = true;
+                for (uint32_t i = k + 1; i < min(k + S::kStages, mine); ++i)  // no copy of its own stays in flight
+                    pk::mbar_wait(bar_s + 8 * (i % S::kStages), (i / S::kStages) & 1);
+                break;
+            }
+            if (decltype(with_rest)::value || (int32_t)((g0 + (warp + k * kWarps) * TG) * 16) + 16 * TG - 1 > all_see)
+                step(k, st, std::true_type{}, with_rest);
+            else
+                step(k, st, std::false_type{}, with_rest);
+            if (++st == S::kStages) st = 0, ++turn;
         }
-        if ((int32_t)((g0 + (warp + k * kWarps) * TG) * 16) + 16 * TG - 1 > all_see)
-            step(k, st, std::true_type{});
-        else
-            step(k, st, std::false_type{});
-        if (++st == S::kStages) st = 0, ++turn;
-    }
+    };
+    if (wide)
+        walk(std::true_type{});
+    else
+        walk(std::false_type{});
     if (gave_up && lane == 0) pk::set_status(a.status, PK_ERR_TIMEOUT);
     pk::pdl_launch_dependents();
 
