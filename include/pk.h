@@ -573,7 +573,10 @@ int pk_attend_prompt(uint32_t dtype, const pk_heads *q, const pk_heads *k, const
  * past kv_len are never used.  q_heads a multiple of kv_heads, at most 65536;
  * n_q >= 1.
  * scratch_dev: pk_attend_cache_scratch_bytes(...) bytes for the same
- * arguments, 16-byte aligned (weigh: page_weight_dev given).  Device errors: kv_len or a slot out of range (PK_ERR_ARG). */
+ * arguments, 16-byte aligned (weigh: page_weight_dev given).  Device errors
+ * (PK_ERR_ARG): a kv_len out of range counts as 0; a slot out of range below
+ * kv_len makes all of that request's out and lse NaN, and nothing is added to
+ * its page weights. */
 size_t pk_attend_cache_scratch_bytes(const pk_kv_cache *kv, uint32_t R, uint32_t n_q, uint32_t q_heads,
                                      uint64_t page_stride, int weigh);
 int pk_attend_cache(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, const pk_heads *out, float *lse_dev,

@@ -106,6 +106,17 @@ __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+// Stands for the sum of a row that a slot out of range has a part in: its request's outputs are NaN, and its pages'
+// weights stay.  Sums are not negative.
+constexpr float kLost = -1.0f;
+// What a row's weighted values are multiplied with, and ln of its sum by the reference m, of a sum l.
+__device__ __forceinline__ float inverse(const Args &a, float l, bool gone) {
+    return gone ? __int_as_float(0x7fffffff) : l == 0.0f ? 0.0f : a.v_scale / l;
+}
+__device__ __forceinline__ float log_sum(float m, float l, bool gone) {
+    return gone ? __int_as_float(0x7fffffff) : l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
 // The length of request r, 0 when it is out of range.
 __device__ __forceinline__ int32_t length_of(const int32_t *kv_len, uint64_t r, uint64_t most) {
     const int32_t len = __ldcg(kv_len + r);
@@ -215,8 +226,10 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
     pages += (uint64_t)r * a.page_stride;
     const uint32_t slot_shift = 31 - __clz(a.page_grans);
     const bool pow2 = (a.page_grans & (a.page_grans - 1)) == 0;
-    // lane l holds where the warp's granule ahead * TG + l lies; a slot out of range is reported and read as slot 0
+    // lane l holds where the warp's granule ahead * TG + l lies.  A slot out of range is reported; slot 0's bytes stand
+    // in for what it should hold, and `lost` keeps all that is made of them from the outputs.
     uint32_t ahead = 0;
+    bool lost = false;
     uint64_t where = 0;
     auto find_granules = [&](uint32_t k) {
         ahead = k;
@@ -227,6 +240,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
             if (slot >= a.n_slots) {
                 pk::set_status(a.status, PK_ERR_ARG);
                 slot = 0;
+                lost = true;
             }
             where = reinterpret_cast<uint64_t>(pool) + slot * a.page_bytes +
                     ((uint64_t)head * a.page_grans + (gr - page * a.page_grans)) * G::kBytes;
@@ -595,6 +609,8 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
     if (gave_up && lane == 0) pk::set_status(a.status, PK_ERR_TIMEOUT);
     pk::pdl_launch_dependents();
 
+    lost = __any_sync(0xffffffffu, lost);
+
     // join the warps: O of each goes to its own ring, [row][D]
     float *ow = reinterpret_cast<float *>(ring);
 #pragma unroll
@@ -605,7 +621,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
 #pragma unroll
             for (int d = 4; d < 32; d *= 2) x += __shfl_xor_sync(0xffffffffu, x, d);
             const uint32_t q = nt * 8 + 2 * c + j;
-            if (g == 0) s_ref[warp][q] = ref[nt][j], s_sum[warp][q] = x;
+            if (g == 0) s_ref[warp][q] = ref[nt][j], s_sum[warp][q] = lost ? kLost : x;
 #pragma unroll
             for (int i = 0; i < kSteps; ++i)  // tile i, rows g and g + 8: dimensions g D/8 + 2i, + 1
                 *reinterpret_cast<float2 *>(ow + q * D + g * (D / 8) + 2 * i) =
@@ -618,8 +634,9 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
         const uint32_t q = x / D, d = x % D, row = tile * kRows + q;
         if (row >= a.rows) break;  // rows only grow from here
         float m = -FLT_MAX, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+        bool gone = false;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) m = fmaxf(m, s_ref[w][q]);
+        for (int w = 0; w < kWarps; ++w) m = fmaxf(m, s_ref[w][q]), gone |= s_sum[w][q] == kLost;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             const float f = ex2(s_ref[w][q] - m);
@@ -629,17 +646,16 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
             o0 += f * y.x;
             o1 += f * y.y;
         }
-        if (d == 0 && a.part_ml) a.part_ml[part + q] = make_float2(m, l);
+        if (d == 0 && a.part_ml) a.part_ml[part + q] = make_float2(m, gone ? kLost : l);
         if (a.splits > 1) {
             *reinterpret_cast<float2 *>(a.part_o + (part + q) * D + d) = make_float2(o0, o1);
         } else {
             const uint32_t i = row / a.group, qh = head * a.group + row - i * a.group;
-            const float inv = l == 0.0f ? 0.0f : a.v_scale / l;
+            const float inv = inverse(a, l, gone);
             const int64_t t = (int64_t)r * a.n_q + i;
             *reinterpret_cast<uint32_t *>(a.out + t * a.o_ts + (int64_t)qh * a.o_hs + d) =
                 pk::Elem<DT>::from2(o0 * inv, o1 * inv);
-            if (d == 0 && a.lse)
-                a.lse[t * (a.kv_heads * a.group) + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+            if (d == 0 && a.lse) a.lse[t * (a.kv_heads * a.group) + qh] = log_sum(m, l, gone);
         }
     }
 }
@@ -688,11 +704,13 @@ __global__ void __launch_bounds__(kFinishThreads) k_cache_finish(const Args a, u
         for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
         constexpr int kPer = D / 32;
         float l = 0.0f, o[kPer] = {};
+        bool gone = false;
 #pragma unroll 4
         for (uint32_t s = 0; s < n; ++s) {
             const uint64_t at = first + (uint64_t)s * tile_rows;
             const float2 ml = __ldcg(part_ml + at);
             const float f = ex2(ml.x - m);
+            gone |= ml.y == kLost;
             l += f * ml.y;
 #pragma unroll
             for (int i = 0; i < kPer; i += 2) {
@@ -702,14 +720,13 @@ __global__ void __launch_bounds__(kFinishThreads) k_cache_finish(const Args a, u
             }
         }
         const uint32_t i = row / a.group, qh = head * a.group + row - i * a.group;
-        const float inv = l == 0.0f ? 0.0f : a.v_scale / l;
+        const float inv = inverse(a, l, gone);
         const int64_t t = (int64_t)r * a.n_q + i;
 #pragma unroll
         for (int x = 0; x < kPer; x += 2)
             *reinterpret_cast<uint32_t *>(a.out + t * a.o_ts + (int64_t)qh * a.o_hs + lane * kPer + x) =
                 pk::Elem<DT>::from2(o[x] * inv, o[x + 1] * inv);
-        if (lane == 0 && a.lse)
-            a.lse[t * (a.kv_heads * a.group) + qh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+        if (lane == 0 && a.lse) a.lse[t * (a.kv_heads * a.group) + qh] = log_sum(m, l, gone);
         return;
     }
     const uint32_t per = pages_a_warp(a.page_grans), block_pages = kFinishWarps * per;
@@ -728,19 +745,22 @@ __global__ void __launch_bounds__(kFinishThreads) k_cache_finish(const Args a, u
             const uint64_t first = (((uint64_t)r * a.kv_heads + head) * a.row_tiles + row / tile_rows) * a.splits *
                                        tile_rows + row % tile_rows;
             float m = -FLT_MAX, l = 0.0f;
+            bool gone = false;
 #pragma unroll 8
             for (uint32_t s = 0; s < n; ++s) {
                 const float2 ml = __ldcg(part_ml + first + (uint64_t)s * tile_rows);
                 const float to = fmaxf(m, ml.x);
                 l = l * ex2(m - to) + ml.y * ex2(ml.x - to);
                 m = to;
+                gone |= ml.y == kLost;
             }
-            stat[x] = make_float2(m, l == 0.0f ? 0.0f : 1.0f / l);
+            stat[x] = make_float2(m, l == 0.0f || gone ? 0.0f : 1.0f / l);
         }
         __syncthreads();
         for (uint32_t x = lane; x < kStatRows && base + x < total; x += 32) {
             const uint32_t head = (base + x) / a.rows, row = (base + x) % a.rows;
             const float2 st = stat[x];
+            if (st.y == 0.0f) continue;  // no key, or a slot out of range: nothing is added, whatever the sums hold
             const float2 *src = gran_ml + (((uint64_t)r * a.kv_heads + head) * a.row_tiles + row / tile_rows) *
                                               a.gran_stride * a.gran_rows + row % tile_rows;
 #pragma unroll 2
