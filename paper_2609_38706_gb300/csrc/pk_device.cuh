@@ -64,14 +64,15 @@ __device__ __forceinline__ uint32_t lane_request(const int64_t *key_off, uint32_
 // and a search over those 32 values by shuffles (non-decreasing key_off: r = r0
 // + the count of them <= g, one of 33 outcomes: 6 halvings).  A lane whose item
 // lies past those 32 requests (only after runs of empty requests) falls back to
-// find_request_in.
+// find_request_in.  Whatever key_off and total hold, the result lies in [0, R) and
+// no load past key_off[R].
 __device__ __forceinline__ uint32_t lane_request_window(const int64_t *key_off, uint32_t R, int64_t g0,
                                                         int64_t total, int64_t g) {
     const uint32_t lane = threadIdx.x & 31;
     const uint32_t r0 = warp_find_request(key_off, R, g0);
     const uint64_t p = (uint64_t)r0 + 1 + lane;
     const int64_t v = p <= R ? __ldcg(key_off + p) : INT64_MAX;
-    const int64_t gg = g < total ? g : total - 1;
+    const int64_t gg = g < total ? g : max(total, (int64_t)(INT64_MIN + 1)) - 1;
     int lo = 0, hi = 32;  // the first j with key_off[r0 + 1 + j] > gg lies in [lo, hi] (32: none of the 32)
 #pragma unroll
     for (int it = 0; it < 6; ++it) {
@@ -81,8 +82,8 @@ __device__ __forceinline__ uint32_t lane_request_window(const int64_t *key_off, 
             if (vm <= gg) lo = mid + 1; else hi = mid;
         }
     }
-    if (lo < 32) return r0 + (uint32_t)lo;
-    return find_request_in(key_off, r0 + 32, R, gg);
+    if (lo < 32) return min(r0 + (uint32_t)lo, R - 1);
+    return r0 + 32 < R ? find_request_in(key_off, r0 + 32, R, gg) : R - 1;
 }
 
 // Same result again, for batches of about equal requests: a guess from the mean

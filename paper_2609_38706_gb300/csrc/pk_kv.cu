@@ -127,10 +127,10 @@ __global__ void __launch_bounds__(kMoveThreads) k_kv_move(const Move a) {
     const int64_t t0 = (int64_t)(group * kTokens);
     const int64_t t = t0 + lane / kLanes;
     const uint32_t r = pk::lane_request_window(tok_off, a.R, t0, __ldcg(tok_off + a.R), t);
-    const int64_t first = __ldcg(tok_off + r);
-    const int64_t pos = (int64_t)__ldcg(start + r) + (t - first);
-    bool on = (uint64_t)t < a.n_tokens && t >= first && t < __ldcg(tok_off + r + 1) && pos >= t - first &&
-              (uint64_t)pos < a.positions;
+    const int64_t first = __ldcg(tok_off + r), next = __ldcg(tok_off + r + 1);
+    const bool mine = first >= 0 && t >= first && t < next && (uint64_t)next <= a.n_tokens;
+    const int64_t pos = mine ? (int64_t)__ldcg(start + r) + (t - first) : -1;
+    bool on = mine && pos >= t - first && (uint64_t)pos < a.positions;
     uint32_t slot = 0;
     const uint32_t page = on ? (uint32_t)pos / a.page_tokens : 0;
     if (on) {
