@@ -141,6 +141,7 @@ struct Small {
     uint64_t q_full[2], q_empty[2];
     uint64_t s_full[2], p_ready[2], o_done[2];
     uint64_t edge_v[4];            // an edge tile's V loaded, by edge tile
+    uint64_t over;                 // every product that was issued is done (a matrix warp that gave up)
     uint64_t next_full[4], next_empty[4];  // an answer on the next item is there; its readers have it
     alignas(16) uint64_t next[4][2];       // the answers
     uint32_t tmem, abort;
@@ -329,6 +330,7 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
             pk::mbar_init(pk::smem_addr(&sm.next_full[i]), 1);
             pk::mbar_init(pk::smem_addr(&sm.next_empty[i]), 10);  // cleaning and softmax warps
         }
+        pk::mbar_init(pk::smem_addr(&sm.over), 1);
         pk::mbar_fence_init();
         sm.abort = 0;
         for (int i = 0; i < 8; ++i) sm.epilogues[i] = 0;
@@ -363,7 +365,7 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
         if (warp == kWarpLoad) {
             uint32_t n = 0, edges = 0, nq[2] = {0, 0}, items = 0;  // ring stages, edge tiles, Q tiles, items so far
-            uint32_t asked = 0;
+            uint32_t asked = 0, dirty_last = 0;  // dirty_last: bit i is 1 where the stage i before the next one is an edge tile's
             bool ok = true;
             pk::fence_proxy_async();
             while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
@@ -396,6 +398,7 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                                                it.head, it.k0 + j * kKeys, bar);
                             ++n;
                             edges += dirty;
+                            dirty_last = dirty_last << 1 | (uint32_t)dirty;
                         }
                         if (j == 0) {  // Q behind the first tiles, which need not wait for the last item's Q
 #pragma unroll
@@ -431,12 +434,17 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                     pk::mbar_arrive(pk::smem_addr(&sm.full[st]));
                     pk::mbar_arrive(pk::smem_addr(&sm.full[st]));
                     ++n;
+                    dirty_last <<= 1;
                 }
                 if (!ok) give_up();
-                // no copy of its own stays in flight, and no answer on its way
+                // no copy of its own stays in flight, and no answer on its way; each by the barrier that its own
+                // arrivals complete, so that no wait depends on a warp that gave up
                 if (asked > turn) pk::mbar_wait(pk::smem_addr(&sm.next_full[turn & 3]), turn >> 2 & 1);
                 for (uint32_t i = n > L::kStages ? n - L::kStages : 0; i < n; ++i)
-                    pk::mbar_wait(pk::smem_addr(&sm.full[i % L::kStages]), (i / L::kStages) & 1);
+                    if (!(dirty_last >> (n - 1 - i) & 1))
+                        pk::mbar_wait(pk::smem_addr(&sm.full[i % L::kStages]), (i / L::kStages) & 1);
+                for (uint32_t i = edges > 4 ? edges - 4 : 0; i < edges; ++i)
+                    pk::mbar_wait(pk::smem_addr(&sm.edge_v[i & 3]), (i >> 2) & 1);
                 for (int t = 0; t < 2; ++t)
                     if (nq[t]) pk::mbar_wait(pk::smem_addr(&sm.q_full[t]), (nq[t] - 1) & 1);
             }
@@ -522,6 +530,27 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                         advance(1);
                     }
                 }
+            }
+            // The commits' arrivals come by themselves: none may be left to find the shared memory in another block's
+            // hands, nor a product the TMEM.  So the last one on every barrier is waited for: a stage, two tiles' scores
+            // and outputs, and their Q, were given back once a use.
+            auto last_commit = [&](const uint64_t &bar, uint32_t commits) {
+                if (commits) ok = pk::mbar_wait_warp(pk::smem_addr(&bar), (commits - 1) & 1) && ok;
+            };
+            if (ok) {
+                const uint32_t freed = use * L::kStages + ring;
+                for (uint32_t i = freed > L::kStages ? freed - L::kStages : 0; i < freed; ++i)
+                    last_commit(sm.empty[i % L::kStages], i / L::kStages + 1);
+                last_commit(sm.s_full[0], ni0);
+                last_commit(sm.s_full[1], ni1);
+                last_commit(sm.o_done[0], ni0);
+                last_commit(sm.o_done[1], ni1);
+                last_commit(sm.q_empty[0], nq0);
+                last_commit(sm.q_empty[1], nq1);
+            } else {  // it left somewhere between: behind this one all products are done
+                if (pk::elect_lane()) pk::mma_commit(pk::smem_addr(&sm.over));
+                __syncwarp();
+                last_commit(sm.over, 1);
             }
             if (!ok && lane == 0) give_up();
         } else {
