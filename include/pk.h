@@ -490,7 +490,9 @@ typedef struct {
 
 /* A strided [tokens][heads][head_dim] array of 16-bit values: strides in
  * elements, the last dimension contiguous.  p 16-byte aligned, strides
- * multiples of 8 (every row starts on a 16-byte boundary), not negative. */
+ * multiples of 8 (every row starts on a 16-byte boundary), not negative.  An
+ * output's rows must lie apart: one stride at least head_dim, the other at
+ * least what the rows along the first one span. */
 typedef struct {
     void *p;
     int64_t tok_stride;

@@ -33,11 +33,13 @@ bool good_heads(const pk_heads *h, uint64_t rows, uint32_t heads) {
            h->head_stride <= lim / ((int64_t)heads + 1);
 }
 
-// An output must not write one row twice.
+// An output must not write one value twice: one stride steps over a row, the other over all that the first one spans.
 bool good_out(const pk_heads *h, uint64_t rows, uint32_t heads, uint32_t head_dim) {
     if (!good_heads(h, rows, heads)) return false;
-    return rows == 0 || ((heads == 1 || h->head_stride >= (int64_t)head_dim) &&
-                         (rows == 1 || h->tok_stride >= (int64_t)head_dim));
+    if (rows == 0) return true;
+    const int64_t d = head_dim, ts = h->tok_stride, hs = h->head_stride;
+    if ((heads > 1 && hs < d) || (rows > 1 && ts < d)) return false;
+    return heads == 1 || rows == 1 || ts >= hs * ((int64_t)heads - 1) + d || hs >= ts * ((int64_t)rows - 1) + d;
 }
 
 int kv_move(bool write, const pk_kv_cache *kv, uint32_t dtype, const pk_heads *k, const pk_heads *v,
