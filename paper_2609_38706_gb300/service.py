@@ -9,6 +9,7 @@ per-batch buffers, all allocated with PyTorch, every step run by libpk.
 """
 from __future__ import annotations
 
+import contextlib
 from typing import Optional
 
 import numpy as np
@@ -31,13 +32,21 @@ def _dev(x, dtype, device) -> torch.Tensor:
     return torch.from_numpy(a).to(device=device)
 
 
+def _on(stream):
+    """Context in which PyTorch's work and allocations belong to `stream` (a torch stream or a raw handle; None: the
+    current one)."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+
+
 def _empty(like: torch.Tensor, stream, *wanted) -> list:
     """Buffers (shape, dtype) on like's device that belong to `stream` (None: the current one), so that one freed while
     its kernel still runs is only given out again to later work of that stream."""
     device = like.device
     if stream is None:
         return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
-    with torch.cuda.stream(stream):
+    with _on(stream):
         return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
 
 
@@ -51,8 +60,9 @@ class KeyTable:
         nbytes = pk.pk_table_bytes(capacity_log2)
         if nbytes == 0:
             raise pk.PKError(pk.PK_ERR_CAPACITY, "KeyTable")
-        self.table = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        with _on(stream):
+            self.table = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.ctx = pk.pk_init(self.table, chunk_tokens, capacity_log2, max_probe, stream)
 
     # -- lifecycle ---------------------------------------------------------
@@ -82,9 +92,10 @@ class KeyTable:
         pk.pk_table_load(self.ctx, src, self.stream)
 
     def take_status(self) -> int:
-        """Read and clear the device status word (synchronises)."""
-        v = int(self.status.item())
-        self.status.zero_()
+        """Read and clear the device status word, behind all that was enqueued on its stream so far (synchronises)."""
+        with _on(self.stream):
+            v = int(self.status.item())
+            self.status.zero_()
         return v
 
     def check(self, where: str = "device") -> None:
@@ -238,7 +249,8 @@ class KVPages:
         out, lse = kv.attend(q, kv_len, pages, scale, weight=weight)
         pages, weight, kv_len, _ = evict_pages(pages, weight, kv_len, kv.page_tokens, budget, sinks, recent)
 
-    Bind ``kv.kv_format`` in the descriptors of what is stored here."""
+    Bind ``kv.kv_format`` in the descriptors of what is stored here.  With ``stream`` the pool's zero fill, every call and
+    the status word belong to that stream; tensors that the caller passes, ``pool`` among them, the caller orders."""
 
     def __init__(self, n_slots: int, page_tokens: int, kv_heads: int, head_dim: int, k_scale: float = 1.0,
                  v_scale: float = 1.0, device="cuda", stream: Optional[torch.cuda.Stream] = None,
@@ -249,11 +261,13 @@ class KVPages:
         if nbytes == 0 or n_slots < 1:
             raise pk.PKError(pk.PK_ERR_ARG, "KVPages")
         if pool is None:
-            pool = torch.zeros((n_slots, nbytes), dtype=torch.uint8, device=device)
+            with _on(stream):
+                pool = torch.zeros((n_slots, nbytes), dtype=torch.uint8, device=device)
         if pool.dtype != torch.uint8 or not pool.is_contiguous() or pool.numel() != n_slots * nbytes or not pool.is_cuda:
             raise pk.PKError(pk.PK_ERR_ARG, "KVPages: pool is contiguous uint8 [n_slots, pk_kv_page_bytes] on the device")
         self.pool, self.device = pool, pool.device
-        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        with _on(stream):
+            self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._scratch_bytes: dict = {}
         self.kv = pk.pk_kv_cache(pool.data_ptr(), n_slots, page_tokens, kv_heads, head_dim, k_scale, v_scale)
 
