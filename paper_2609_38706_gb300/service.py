@@ -6,6 +6,9 @@ per-batch buffers, all allocated with PyTorch, every step run by libpk.
     key_off, keys = kt.derive(tokens, tok_off, desc_idx, d)      # a1 + a2
     hit, slots = kt.lookup(keys, key_off)                        # a3
     result, slot_out = kt.store(keys, new_slots, key_off, hit)   # a4 (the misses)
+
+A table or pool made with a stream runs on it, with the buffers that it makes;
+device tensors that a caller passes, and reads of what it gets, the caller orders.
 """
 from __future__ import annotations
 
@@ -21,23 +24,34 @@ from . import pk
 _NP_SIGNED = {torch.int32: np.int32, torch.int64: np.int64, torch.uint8: np.uint8}
 
 
-def _dev(x, dtype, device) -> torch.Tensor:
-    """Host array or tensor -> contiguous device tensor of ``dtype``; unsigned
-    host arrays of the same width are reinterpreted, not converted."""
-    if isinstance(x, torch.Tensor):
-        return x.to(device=device, dtype=dtype).contiguous()
-    a = np.ascontiguousarray(x)
-    want = np.dtype(_NP_SIGNED[dtype])
-    a = a.view(want) if a.dtype.itemsize == want.itemsize and a.dtype.kind in "ui" else a.astype(want)
-    return torch.from_numpy(a).to(device=device)
+def _stream(stream):
+    """The torch stream of `stream`, a torch stream or a raw handle."""
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
 
 
 def _on(stream):
-    """Context in which PyTorch's work and allocations belong to `stream` (a torch stream or a raw handle; None: the
-    current one)."""
-    if stream is None:
-        return contextlib.nullcontext()
-    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+    """Context in which PyTorch's work and allocations belong to `stream` (None: the current one)."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(_stream(stream))
+
+
+def _dev(x, dtype, device, stream=None) -> torch.Tensor:
+    """Host array or tensor -> contiguous device tensor of ``dtype``; unsigned
+    host arrays of the same width are reinterpreted, not converted.  The copy is
+    made on the current stream (one from the host is over when this returns);
+    ``stream``, whose kernels will read it, is ordered behind it, and the copy's
+    memory is not given out again before those have run."""
+    if isinstance(x, torch.Tensor):
+        t = x.to(device=device, dtype=dtype).contiguous()
+    else:
+        a = np.ascontiguousarray(x)
+        want = np.dtype(_NP_SIGNED[dtype])
+        a = a.view(want) if a.dtype.itemsize == want.itemsize and a.dtype.kind in "ui" else a.astype(want)
+        t = torch.from_numpy(a).to(device=device)
+    if stream is not None and t is not x:
+        if isinstance(x, torch.Tensor) and x.is_cuda:
+            _stream(stream).wait_stream(torch.cuda.current_stream(t.device))
+        t.record_stream(_stream(stream))
+    return t
 
 
 def _empty(like: torch.Tensor, stream, *wanted) -> list:
@@ -81,10 +95,15 @@ class KeyTable:
     def entries(self) -> int:
         return pk.pk_entries(self.ctx, self.stream)
 
+    def _new(self, shape, dtype, zero: bool = False) -> torch.Tensor:
+        """A buffer that belongs to the table's stream."""
+        with _on(self.stream):
+            return (torch.zeros if zero else torch.empty)(shape, dtype=dtype, device=self.device)
+
     def save(self, dst: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Checkpoint the table (device tensor unless ``dst`` is given)."""
         if dst is None:
-            dst = torch.empty(self.table.numel() + 64, dtype=torch.uint8, device=self.device)
+            dst = self._new(self.table.numel() + 64, torch.uint8)
         pk.pk_table_save(self.ctx, dst, self.stream)
         return dst
 
@@ -107,20 +126,20 @@ class KeyTable:
     def digests(self, descriptors) -> torch.Tensor:
         enc, off = pk.pk_descriptors_encode(descriptors)
         D = off.size - 1
-        enc_d = _dev(enc if enc.size else np.zeros(1, np.uint8), torch.uint8, self.device)
-        off_d = _dev(off, torch.int64, self.device)
-        out = torch.zeros((max(D, 1), 32), dtype=torch.uint8, device=self.device)
+        enc_d = _dev(enc if enc.size else np.zeros(1, np.uint8), torch.uint8, self.device, self.stream)
+        off_d = _dev(off, torch.int64, self.device, self.stream)
+        out = self._new((max(D, 1), 32), torch.uint8, zero=True)
         pk.pk_digest_descriptors(self.ctx, enc_d[: enc.size], off_d, out, self.status, self.stream)
         return out[:D]
 
     def derive(self, tokens, tok_off, desc_idx, digests):
-        tokens = _dev(tokens, torch.int32, self.device)
-        tok_off = _dev(tok_off, torch.int64, self.device)
-        desc_idx = _dev(desc_idx, torch.int32, self.device)
+        tokens = _dev(tokens, torch.int32, self.device, self.stream)
+        tok_off = _dev(tok_off, torch.int64, self.device, self.stream)
+        desc_idx = _dev(desc_idx, torch.int32, self.device, self.stream)
         R = tok_off.numel() - 1
         cap = tokens.numel() // self.chunk_tokens
-        key_off = torch.empty(R + 1, dtype=torch.int64, device=self.device)
-        keys = torch.empty((max(cap, 0), 32), dtype=torch.uint8, device=self.device)
+        key_off = self._new(R + 1, torch.int64)
+        keys = self._new((max(cap, 0), 32), torch.uint8)
         pk.pk_derive_keys(self.ctx, tokens, tok_off, desc_idx, digests, key_off, keys, self.status, self.stream)
         return key_off, keys
 
@@ -128,40 +147,42 @@ class KeyTable:
         """Descriptor digests and keys in one call (pk_derive_keys_enc)."""
         enc, off = pk.pk_descriptors_encode(descriptors)
         D = off.size - 1
-        enc_d = _dev(enc if enc.size else np.zeros(1, np.uint8), torch.uint8, self.device)[: enc.size]
-        off_d = _dev(off, torch.int64, self.device)
-        digests = torch.zeros((max(D, 1), 32), dtype=torch.uint8, device=self.device)[:D]
-        tokens = _dev(tokens, torch.int32, self.device)
-        tok_off = _dev(tok_off, torch.int64, self.device)
-        desc_idx = _dev(desc_idx, torch.int32, self.device)
+        enc_d = _dev(enc if enc.size else np.zeros(1, np.uint8), torch.uint8, self.device, self.stream)[: enc.size]
+        off_d = _dev(off, torch.int64, self.device, self.stream)
+        digests = self._new((max(D, 1), 32), torch.uint8, zero=True)[:D]
+        tokens = _dev(tokens, torch.int32, self.device, self.stream)
+        tok_off = _dev(tok_off, torch.int64, self.device, self.stream)
+        desc_idx = _dev(desc_idx, torch.int32, self.device, self.stream)
         R = tok_off.numel() - 1
         cap = tokens.numel() // self.chunk_tokens
-        key_off = torch.empty(R + 1, dtype=torch.int64, device=self.device)
-        keys = torch.empty((max(cap, 0), 32), dtype=torch.uint8, device=self.device)
+        key_off = self._new(R + 1, torch.int64)
+        keys = self._new((max(cap, 0), 32), torch.uint8)
         pk.pk_derive_keys_enc(self.ctx, tokens, tok_off, desc_idx, enc_d, off_d, digests, key_off, keys,
                               self.status, self.stream)
         return digests, key_off, keys
 
     def lookup(self, keys, key_off):
         R = key_off.numel() - 1
-        hit = torch.empty(R, dtype=torch.int32, device=self.device)
-        slots = torch.empty(keys.shape[0], dtype=torch.int32, device=self.device)
+        hit = self._new(R, torch.int32)
+        slots = self._new(keys.shape[0], torch.int32)
         pk.pk_lookup(self.ctx, keys, key_off, hit, slots, self.status, self.stream)
         return hit, slots
 
     def store(self, keys, slots, key_off=None, hit=None):
         """List mode (key_off is None) or miss-range mode (key_off and hit)."""
         if keys.shape[1] == 16:  # widen 16-byte prefixes to the 32-byte key stride
-            k = torch.zeros((keys.shape[0], 32), dtype=torch.uint8, device=self.device)
-            k[:, :16] = _dev(keys, torch.uint8, self.device)
+            k = self._new((keys.shape[0], 32), torch.uint8, zero=True)
+            narrow = _dev(keys, torch.uint8, self.device, self.stream)
+            with _on(self.stream):
+                k[:, :16] = narrow
             keys = k
         else:
-            keys = _dev(keys, torch.uint8, self.device)
+            keys = _dev(keys, torch.uint8, self.device, self.stream)
         slots = _dev(slots if isinstance(slots, torch.Tensor) else np.asarray(slots, np.uint32), torch.int32,
-                     self.device)
+                     self.device, self.stream)
         n = keys.shape[0]
-        result = torch.empty(n, dtype=torch.int32, device=self.device)
-        slot_out = torch.empty(n, dtype=torch.int32, device=self.device)
+        result = self._new(n, torch.int32)
+        slot_out = self._new(n, torch.int32)
         pk.pk_store(self.ctx, keys, slots, result, slot_out, self.status, key_off, hit, self.stream)
         return result, slot_out
 
@@ -171,11 +192,11 @@ class KeyTable:
         R = key_off.numel() - 1
         n = keys.shape[0]
         new_slots = _dev(new_slots if isinstance(new_slots, torch.Tensor) else np.asarray(new_slots, np.uint32),
-                         torch.int32, self.device)
-        hit = torch.empty(R, dtype=torch.int32, device=self.device)
-        slots = torch.empty(n, dtype=torch.int32, device=self.device)
-        result = torch.empty(n, dtype=torch.int32, device=self.device)
-        slot_out = torch.empty(n, dtype=torch.int32, device=self.device)
+                         torch.int32, self.device, self.stream)
+        hit = self._new(R, torch.int32)
+        slots = self._new(n, torch.int32)
+        result = self._new(n, torch.int32)
+        slot_out = self._new(n, torch.int32)
         pk.pk_lookup_store(self.ctx, keys, new_slots, key_off, hit, slots, result, slot_out, self.status,
                            self.stream)
         return hit, slots, result, slot_out
@@ -185,22 +206,22 @@ class KeyTable:
         (digests, key_off, keys, hit, slots, result, slot_out)."""
         enc, off = pk.pk_descriptors_encode(descriptors)
         D = off.size - 1
-        enc_d = _dev(enc if enc.size else np.zeros(1, np.uint8), torch.uint8, self.device)[: enc.size]
-        off_d = _dev(off, torch.int64, self.device)
-        digests = torch.zeros((max(D, 1), 32), dtype=torch.uint8, device=self.device)[:D]
-        tokens = _dev(tokens, torch.int32, self.device)
-        tok_off = _dev(tok_off, torch.int64, self.device)
-        desc_idx = _dev(desc_idx, torch.int32, self.device)
+        enc_d = _dev(enc if enc.size else np.zeros(1, np.uint8), torch.uint8, self.device, self.stream)[: enc.size]
+        off_d = _dev(off, torch.int64, self.device, self.stream)
+        digests = self._new((max(D, 1), 32), torch.uint8, zero=True)[:D]
+        tokens = _dev(tokens, torch.int32, self.device, self.stream)
+        tok_off = _dev(tok_off, torch.int64, self.device, self.stream)
+        desc_idx = _dev(desc_idx, torch.int32, self.device, self.stream)
         R = tok_off.numel() - 1
         cap = tokens.numel() // self.chunk_tokens
-        key_off = torch.empty(R + 1, dtype=torch.int64, device=self.device)
-        keys = torch.empty((max(cap, 0), 32), dtype=torch.uint8, device=self.device)
+        key_off = self._new(R + 1, torch.int64)
+        keys = self._new((max(cap, 0), 32), torch.uint8)
         new_slots = _dev(new_slots if isinstance(new_slots, torch.Tensor) else np.asarray(new_slots, np.uint32),
-                         torch.int32, self.device)
-        hit = torch.empty(R, dtype=torch.int32, device=self.device)
-        slots = torch.empty(max(cap, 0), dtype=torch.int32, device=self.device)
-        result = torch.empty(max(cap, 0), dtype=torch.int32, device=self.device)
-        slot_out = torch.empty(max(cap, 0), dtype=torch.int32, device=self.device)
+                         torch.int32, self.device, self.stream)
+        hit = self._new(R, torch.int32)
+        slots = self._new(max(cap, 0), torch.int32)
+        result = self._new(max(cap, 0), torch.int32)
+        slot_out = self._new(max(cap, 0), torch.int32)
         pk.pk_derive_lookup_store(self.ctx, tokens, tok_off, desc_idx, enc_d, off_d, digests, key_off, keys, new_slots,
                                   hit, slots, result, slot_out, self.status, self.stream)
         return digests, key_off, keys, hit, slots, result, slot_out
@@ -210,12 +231,11 @@ class KeyTable:
         """Turn budget mode on: a zeroed last-use stamp per entry, and the
         scratch and output buffers of evict()."""
         cap = 1 << self.capacity_log2
-        self.stamps = torch.empty(pk.pk_stamps_bytes(self.capacity_log2) // 8, dtype=torch.int64, device=self.device)
+        self.stamps = self._new(pk.pk_stamps_bytes(self.capacity_log2) // 8, torch.int64)
         pk.pk_attach_stamps(self.ctx, self.stamps, self.stream)
-        self.evict_scratch = torch.empty(pk.pk_evict_scratch_bytes(self.capacity_log2), dtype=torch.uint8,
-                                         device=self.device)
-        self.evicted = torch.empty(cap, dtype=torch.int32, device=self.device)
-        self.n_evicted = torch.zeros(1, dtype=torch.int64, device=self.device)
+        self.evict_scratch = self._new(pk.pk_evict_scratch_bytes(self.capacity_log2), torch.uint8)
+        self.evicted = self._new(cap, torch.int32)
+        self.n_evicted = self._new(1, torch.int64, zero=True)
         return self.stamps
 
     def evict(self, budget: int, keep: int):
