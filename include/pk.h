@@ -24,7 +24,8 @@
  *   - Returns PK_OK (0) or a negative PK_ERR_* code.  A host-detected error
  *     returns before anything is enqueued and leaves the table unchanged.
  *   - "_dev" pointers are device memory owned by the caller; the library
- *     allocates no device memory except a small fixed block in pk_init.
+ *     allocates no device memory except a small fixed block in pk_init.  That
+ *     memory, the stream and the context belong to the current device.
  *   - All device work is enqueued asynchronously on the given stream
  *     (NULL = legacy default stream).  Errors found on the device are written
  *     to the caller's int32 status word *status_dev (first error wins; the

@@ -67,6 +67,7 @@ class pk_kv_cache(ctypes.Structure):
     _fields_ = [("pool_dev", ctypes.c_void_p), ("n_slots", ctypes.c_uint64), ("page_tokens", ctypes.c_uint32),
                 ("kv_heads", ctypes.c_uint32), ("head_dim", ctypes.c_uint32), ("k_scale", ctypes.c_float),
                 ("v_scale", ctypes.c_float)]
+    device: Optional[int] = None  # index of the pool's device, where known
 
 
 class pk_heads(ctypes.Structure):
@@ -153,11 +154,22 @@ def _check(rc: int, where: str) -> None:
         raise PKError(rc, where)
 
 
+if hasattr(torch._C, "_cuda_getDevice"):  # without what a public call adds to it, as every call asks
+
+    def _current_device() -> int:
+        """Index of the device that kernels are launched on.  Only asked where CUDA is in use."""
+        return torch._C._cuda_getDevice()
+else:
+    _current_device = torch.cuda.current_device
+
+
 def _p(t) -> Optional[int]:
-    """Raw pointer of a tensor / ndarray (None for None)."""
+    """Raw pointer of a tensor / ndarray (None for None).  A device tensor is on the current device."""
     if t is None:
         return None
     if isinstance(t, torch.Tensor):
+        if t.is_cuda and t.get_device() != _current_device():
+            raise PKError(PK_ERR_ARG, "a tensor is on another device than the current one")
         return t.data_ptr() if t.numel() else None
     if isinstance(t, np.ndarray):
         return t.ctypes.data if t.size else None
@@ -482,7 +494,9 @@ def pk_key_strings(keys: torch.Tensor, prefix: bytes, width: int, out: torch.Ten
 
 
 def pk_table_save(ctx: int, dst: torch.Tensor, stream=None) -> None:
-    _check(lib().pk_table_save(ctx, _p(dst), dst.numel() * dst.element_size(), _s(stream)), "pk_table_save")
+    """dst: host or device memory, on any device."""
+    at = dst.data_ptr() if dst.numel() else None
+    _check(lib().pk_table_save(ctx, at, dst.numel() * dst.element_size(), _s(stream)), "pk_table_save")
 
 
 def pk_table_load(ctx: int, src: torch.Tensor, stream=None) -> None:
@@ -507,14 +521,25 @@ def _refuse(where: str, what: str):
     raise PKError(PK_ERR_ARG, f"{where}: {what}")
 
 
-def _ints(t: torch.Tensor, dtype, n: int, where: str, what: str) -> Optional[int]:
-    """Pointer of a contiguous array of n entries on the device."""
-    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
-        _refuse(where, what + ", on the device")
+def _here(where: str, kv: Optional[pk_kv_cache] = None) -> int:
+    """The current device, on which a call's kernels run and all its tensors have to be, the pool among them."""
+    try:
+        dev = _current_device()
+    except RuntimeError:  # no GPU
+        dev = -2  # no tensor's: on the host it is -1
+    if kv is not None and kv.device is not None and kv.device != dev:
+        _refuse(where, "the pool is on another device than the current one")
+    return dev
+
+
+def _ints(t: torch.Tensor, dtype, n: int, dev: int, where: str, what: str) -> Optional[int]:
+    """Pointer of a contiguous array of n entries on device `dev`."""
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
+        _refuse(where, what + ", on the current device")
     return t.data_ptr() if n else None
 
 
-def _heads(t: torch.Tensor, where: str):
+def _heads(t: torch.Tensor, dev: int, where: str):
     """pk_heads of [tokens, heads, head_dim], or [R, n, heads, head_dim] whose first two dimensions run on as one; the
     last dimension contiguous."""
     shape, stride = t.shape, t.stride()
@@ -529,17 +554,17 @@ def _heads(t: torch.Tensor, where: str):
         _refuse(where, "a [tokens, heads, head_dim] tensor")
     if t.numel() == 0:
         return pk_heads(None, 0, 0)
-    if (stride[-1] != 1 and shape[-1] > 1) or not t.is_cuda:
-        _refuse(where, "rows are contiguous, on the device")
+    if (stride[-1] != 1 and shape[-1] > 1) or t.get_device() != dev:
+        _refuse(where, "rows are contiguous, on the current device")
     return pk_heads(t.data_ptr(), ts if n > 1 else 0, stride[-2] if shape[-2] > 1 else 0)
 
 
-def _buffer(t: Optional[torch.Tensor], where: str) -> Optional[int]:
+def _buffer(t: Optional[torch.Tensor], dev: int, where: str) -> Optional[int]:
     """Pointer of a status word or scratch (None for None)."""
     if t is None:
         return None
-    if not t.is_cuda:
-        _refuse(where, "status and scratch are on the device")
+    if t.get_device() != dev:
+        _refuse(where, "status and scratch are on the current device")
     return t.data_ptr() if t.numel() else None
 
 
@@ -559,6 +584,7 @@ def pk_kv_page_bytes(page_tokens: int, kv_heads: int, head_dim: int) -> int:
 
 
 def _kv_move(fn: str, call, kv: pk_kv_cache, k, v, tok_off, start, pages, status, stream) -> None:
+    dev = _here(fn, kv)
     R = start.numel()
     shape = k.shape
     if v.shape != shape or len(shape) != 3 or shape[1] != kv.kv_heads or shape[2] != kv.head_dim:
@@ -566,10 +592,10 @@ def _kv_move(fn: str, call, kv: pk_kv_cache, k, v, tok_off, start, pages, status
     if pages.dim() != 2 or pages.shape[0] != R:
         _refuse(fn, "pages is [R, page_stride]")
     width = pages.shape[1]
-    rc = call(ctypes.byref(kv), _dtype(fn, k, v), ctypes.byref(_heads(k, fn)), ctypes.byref(_heads(v, fn)), shape[0],
-              _ints(tok_off, torch.int64, R + 1, fn, "tok_off is contiguous int64[R+1]"),
-              _ints(start, torch.int32, R, fn, "start is contiguous int32[R]"), R,
-              _ints(pages, torch.int32, R * width, fn, "pages is contiguous int32"), width, _buffer(status, fn),
+    rc = call(ctypes.byref(kv), _dtype(fn, k, v), ctypes.byref(_heads(k, dev, fn)), ctypes.byref(_heads(v, dev, fn)), shape[0],
+              _ints(tok_off, torch.int64, R + 1, dev, fn, "tok_off is contiguous int64[R+1]"),
+              _ints(start, torch.int32, R, dev, fn, "start is contiguous int32[R]"), R,
+              _ints(pages, torch.int32, R * width, dev, fn, "pages is contiguous int32"), width, _buffer(status, dev, fn),
               _stream_of(stream, k))
     if rc:
         _check(rc, fn)
@@ -597,6 +623,7 @@ def pk_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: tor
                      scratch: torch.Tensor, status: torch.Tensor, stream=None) -> None:
     """q, out: [n_q, q_heads, D]; k, v: [n_k, kv_heads, D]; q_off, k_off: int64[R+1]; lse: float32 [n_q, q_heads]."""
     fn = "pk_attend_prompt"
+    dev = _here(fn)
     R = q_off.numel() - 1
     qs, ks = q.shape, k.shape
     if len(qs) != 3 or len(ks) != 3 or v.shape != ks or out.shape != qs or qs[2] != ks[2]:
@@ -605,12 +632,12 @@ def pk_attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: tor
         _refuse(fn, "q_off is int64[R+1]")
     z = lse
     if lse is not None:
-        z = _ints(lse, torch.float32, qs[0] * qs[1], fn, "lse is contiguous float32 [n_q, q_heads]")
-    rc = lib().pk_attend_prompt(_dtype(fn, q, k, v, out), ctypes.byref(_heads(q, fn)), ctypes.byref(_heads(k, fn)),
-                                ctypes.byref(_heads(v, fn)), ctypes.byref(_heads(out, fn)), z, qs[0], ks[0],
-                                _ints(q_off, torch.int64, R + 1, fn, "q_off is contiguous int64[R+1]"),
-                                _ints(k_off, torch.int64, R + 1, fn, "k_off is contiguous int64[R+1]"), R, qs[1],
-                                ks[1], qs[2], scale, _buffer(scratch, fn), scratch.numel(), _buffer(status, fn),
+        z = _ints(lse, torch.float32, qs[0] * qs[1], dev, fn, "lse is contiguous float32 [n_q, q_heads]")
+    rc = lib().pk_attend_prompt(_dtype(fn, q, k, v, out), ctypes.byref(_heads(q, dev, fn)), ctypes.byref(_heads(k, dev, fn)),
+                                ctypes.byref(_heads(v, dev, fn)), ctypes.byref(_heads(out, dev, fn)), z, qs[0], ks[0],
+                                _ints(q_off, torch.int64, R + 1, dev, fn, "q_off is contiguous int64[R+1]"),
+                                _ints(k_off, torch.int64, R + 1, dev, fn, "k_off is contiguous int64[R+1]"), R, qs[1],
+                                ks[1], qs[2], scale, _buffer(scratch, dev, fn), scratch.numel(), _buffer(status, dev, fn),
                                 _stream_of(stream, q))
     if rc:
         _check(rc, fn)
@@ -627,6 +654,7 @@ def pk_attend_cache(kv: pk_kv_cache, q: torch.Tensor, out: torch.Tensor, lse: Op
     """q, out: [R * n_q, q_heads, D] or [R, n_q, q_heads, D]; lse: float32, R * n_q * q_heads; kv_len: int32[R]; pages:
     int32 and page_weight: float32 [R, page_stride]."""
     fn = "pk_attend_cache"
+    dev = _here(fn, kv)
     R = kv_len.numel()
     qs = q.shape
     if out.shape != qs or len(qs) not in (3, 4) or q.numel() != R * n_q * qs[-2] * qs[-1] or qs[-1] != kv.head_dim:
@@ -636,16 +664,16 @@ def pk_attend_cache(kv: pk_kv_cache, q: torch.Tensor, out: torch.Tensor, lse: Op
     width = pages.shape[1]
     z = w = None
     if lse is not None:
-        z = _ints(lse, torch.float32, R * n_q * qs[-2], fn, "lse is contiguous float32, R * n_q * q_heads")
+        z = _ints(lse, torch.float32, R * n_q * qs[-2], dev, fn, "lse is contiguous float32, R * n_q * q_heads")
     if page_weight is not None:
         if page_weight.shape != pages.shape:
             _refuse(fn, "page_weight is [R, page_stride]")
-        w = _ints(page_weight, torch.float32, R * width, fn, "page_weight is contiguous float32")
-    rc = lib().pk_attend_cache(ctypes.byref(kv), _dtype(fn, q, out), ctypes.byref(_heads(q, fn)),
-                               ctypes.byref(_heads(out, fn)), z, R, n_q, qs[-2], scale,
-                               _ints(kv_len, torch.int32, R, fn, "kv_len is contiguous int32[R]"),
-                               _ints(pages, torch.int32, R * width, fn, "pages is contiguous int32"), width, w,
-                               _buffer(scratch, fn), scratch.numel(), _buffer(status, fn),
+        w = _ints(page_weight, torch.float32, R * width, dev, fn, "page_weight is contiguous float32")
+    rc = lib().pk_attend_cache(ctypes.byref(kv), _dtype(fn, q, out), ctypes.byref(_heads(q, dev, fn)),
+                               ctypes.byref(_heads(out, dev, fn)), z, R, n_q, qs[-2], scale,
+                               _ints(kv_len, torch.int32, R, dev, fn, "kv_len is contiguous int32[R]"),
+                               _ints(pages, torch.int32, R * width, dev, fn, "pages is contiguous int32"), width, w,
+                               _buffer(scratch, dev, fn), scratch.numel(), _buffer(status, dev, fn),
                                 _stream_of(stream, q))
     if rc:
         _check(rc, fn)
@@ -658,6 +686,7 @@ def pk_evict_pages(pages: torch.Tensor, weight: torch.Tensor, kv_len: torch.Tens
     """pages: int32 and weight: float32 [R, page_stride]; kv_len, kv_len_out: int32[R]; pages_out: int32 and
     weight_out: float32 [R, budget]; evicted: int32 [R, page_stride] or None."""
     fn = "pk_evict_pages"
+    dev = _here(fn)
     R = kv_len.numel()
     if pages.dim() != 2 or pages.shape[0] != R or weight.shape != pages.shape:
         _refuse(fn, "pages, weight are [R, page_stride]")
@@ -665,16 +694,16 @@ def pk_evict_pages(pages: torch.Tensor, weight: torch.Tensor, kv_len: torch.Tens
         _refuse(fn, "counts are not negative")
     width = pages.shape[1]
     n = R * width
-    rc = lib().pk_evict_pages(_ints(pages, torch.int32, n, fn, "pages is contiguous int32"),
-                              _ints(weight, torch.float32, n, fn, "weight is contiguous float32"),
-                              _ints(kv_len, torch.int32, R, fn, "kv_len is contiguous int32[R]"), R, width,
+    rc = lib().pk_evict_pages(_ints(pages, torch.int32, n, dev, fn, "pages is contiguous int32"),
+                              _ints(weight, torch.float32, n, dev, fn, "weight is contiguous float32"),
+                              _ints(kv_len, torch.int32, R, dev, fn, "kv_len is contiguous int32[R]"), R, width,
                               page_tokens, budget, sinks, recent,
-                              _ints(pages_out, torch.int32, R * budget, fn, "pages_out is int32[R, budget]"),
-                              _ints(weight_out, torch.float32, R * budget, fn, "weight_out is float32[R, budget]"),
-                              _ints(kv_len_out, torch.int32, R, fn, "kv_len_out is int32[R]"),
+                              _ints(pages_out, torch.int32, R * budget, dev, fn, "pages_out is int32[R, budget]"),
+                              _ints(weight_out, torch.float32, R * budget, dev, fn, "weight_out is float32[R, budget]"),
+                              _ints(kv_len_out, torch.int32, R, dev, fn, "kv_len_out is int32[R]"),
                               None if evicted is None else
-                              _ints(evicted, torch.int32, n, fn, "evicted is int32[R, page_stride]"),
-                              _buffer(status, fn), _stream_of(stream, pages))
+                              _ints(evicted, torch.int32, n, dev, fn, "evicted is int32[R, page_stride]"),
+                              _buffer(status, dev, fn), _stream_of(stream, pages))
     if rc:
         _check(rc, fn)
 

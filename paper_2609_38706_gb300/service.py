@@ -290,6 +290,7 @@ class KVPages:
             self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._scratch_bytes: dict = {}
         self.kv = pk.pk_kv_cache(pool.data_ptr(), n_slots, page_tokens, kv_heads, head_dim, k_scale, v_scale)
+        self.kv.device = self.device.index
 
     @property
     def kv_format(self) -> str:
