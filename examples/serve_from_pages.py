@@ -18,7 +18,7 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
-from paper_2609_38706_gb300.service import KeyTable, KVPages, attend_prompt, evict_pages  # noqa: E402
+from paper_2609_38706_gb300.service import KeyTable, KVPages  # noqa: E402
 
 CHUNK, VOCAB, WIDTH, Q_HEADS, KV_HEADS, D = 16, 1000, 256, 8, 2, 64
 
@@ -85,7 +85,7 @@ class Server:
         olds, news = np.cumsum([0] + start), np.cumsum([0] + new)
         k, v = (torch.cat([p for r in range(R) for p in (old[olds[r]: olds[r + 1]], fresh_[news[r]: news[r + 1]])])
                 for old, fresh_ in ((k_old, k_new), (v_old, v_new)))
-        out, _ = attend_prompt(q, k, v, off(new), off(lens), status=self.kv.status)
+        out, _ = self.kv.attend_prompt(q, k, v, off(new), off(lens))
 
         # only what no page holds yet: the missed chunks and the tail (a fully hit prompt's last token is there)
         first = [max(s, min(h * CHUNK, x)) for s, h, x in zip(start, hit, lens)]
@@ -119,8 +119,7 @@ def main(steps: int = 24, budget: int = 8, quiet: bool = False):
         for step in range(2 * steps):
             if step == steps:  # only the pages that attention has weighed most go on
                 full = table.shape[1]
-                table, weight, kv_len, gone = evict_pages(table, weight, kv_len, CHUNK, budget, sinks=1, recent=2,
-                                                          status=server.kv.status)
+                table, weight, kv_len, gone = server.kv.evict(table, weight, kv_len, budget, sinks=1, recent=2)
                 # room again for what is decoded: the pages that were dropped by this request alone are free
                 more = torch.tensor([[server.free.pop() for _ in range(full - budget)] for _ in batch],
                                     dtype=torch.int32, device="cuda")

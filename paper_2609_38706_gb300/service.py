@@ -265,9 +265,11 @@ class KVPages:
 
         kv = KVPages(n_slots, page_tokens=kt.chunk_tokens, kv_heads=8, head_dim=128)
         kv.write(k, v, tok_off, start, pages)          # the misses' chunks, or a decode step's tokens
-        k, v = kv.read(tok_off, start, pages, n)       # a hit's prefix, for attend_prompt
+        k, v = kv.read(tok_off, start, pages, n)       # a hit's prefix
+        out, lse = kv.attend_prompt(q, k, v, q_off, k_off)
         out, lse = kv.attend(q, kv_len, pages, scale, weight=weight)
-        pages, weight, kv_len, _ = evict_pages(pages, weight, kv_len, kv.page_tokens, budget, sinks, recent)
+        pages, weight, kv_len, _ = kv.evict(pages, weight, kv_len, budget, sinks, recent)
+        kv.check()                                     # any call's device error
 
     Bind ``kv.kv_format`` in the descriptors of what is stored here.  With ``stream`` the pool's zero fill, every call and
     the status word belong to that stream; tensors that the caller passes, ``pool`` among them, the caller orders."""
@@ -327,11 +329,20 @@ class KVPages:
                            scratch, self.status, self.stream)
         return out, lse
 
+    def attend_prompt(self, q, k, v, q_off, k_off, scale: Optional[float] = None):
+        """attend_prompt on the pool's stream, its device errors in the pool's status word."""
+        return attend_prompt(q, k, v, q_off, k_off, scale, self.status, self.stream)
+
+    def evict(self, pages, weight, kv_len, budget: int, sinks: int, recent: int):
+        """evict_pages for pages of this pool, on its stream, its device errors in the pool's status word."""
+        return evict_pages(pages, weight, kv_len, self.page_tokens, budget, sinks, recent, self.status, self.stream)
+
 
 def attend_prompt(q, k, v, q_off, k_off, scale: Optional[float] = None, status: Optional[torch.Tensor] = None,
                   stream=None):
-    """Causal attention over packed prompts (pk_attend_prompt): (out like q, lse float32 [n_q, q_heads]).  Without
-    ``status`` a device-reported error leaves the outputs unspecified and is not reported."""
+    """Causal attention over packed prompts (pk_attend_prompt): (out like q, lse float32 [n_q, q_heads]).  Device errors
+    go to ``status`` (int32, zeroed by the caller; KVPages.attend_prompt passes the pool's); without one the caller
+    answers for the offsets: what is wrong with them leaves the outputs unspecified and is not reported."""
     nbytes = pk.pk_attend_prompt_scratch_bytes(max(q_off.numel() - 1, 0))
     out, lse, scratch = _empty(q, stream, (q.shape, q.dtype), (q.shape[:2], torch.float32), ((nbytes,), torch.uint8))
     pk.pk_attend_prompt(q, k, v, out, lse, q_off, k_off, q.shape[-1] ** -0.5 if scale is None else scale, scratch,
@@ -342,7 +353,8 @@ def attend_prompt(q, k, v, q_off, k_off, scale: Optional[float] = None, status: 
 def evict_pages(pages, weight, kv_len, page_tokens: int, budget: int, sinks: int, recent: int,
                 status: Optional[torch.Tensor] = None, stream=None):
     """Cut each request to `budget` pages by accumulated attention weight (pk_evict_pages): (pages [R, budget],
-    weight [R, budget], kv_len [R], evicted slots like pages), unused places PK_NO_SLOT (-1) and 0."""
+    weight [R, budget], kv_len [R], evicted slots like pages), unused places PK_NO_SLOT (-1) and 0.  ``status`` as in
+    attend_prompt (KVPages.evict passes the pool's)."""
     kept = (pages.shape[0], max(budget, 0))
     pages_out, weight_out, kv_len_out, evicted = _empty(
         pages, stream, (kept, torch.int32), (kept, torch.float32), (kept[:1], torch.int32), (pages.shape, torch.int32))
