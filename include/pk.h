@@ -465,7 +465,8 @@ int pk_store_noalloc(const pk_config *cfg, const uint8_t *keys_dev, const uint32
 /* KV pages: what lies behind a slot, and what a serving step does with it.
  * The paper keeps page payloads opaque (Sec. 2.1: a hit loads stored KV state
  * and skips that prefill, a miss computes and writes new state); these calls
- * are one such payload, held in 4 bits, with the attention that reads it.
+ * are one such payload, held in 4 bits, with the attention that reads it.  They
+ * serve: none has a backward pass.
  *
  * A page holds page_tokens tokens of every KV head:
  *     page    = [kv_heads][page_tokens / 16] granules

@@ -556,6 +556,8 @@ def _heads(t: torch.Tensor, dev: int, where: str):
         return pk_heads(None, 0, 0)
     if (stride[-1] != 1 and shape[-1] > 1) or t.get_device() != dev:
         _refuse(where, "rows are contiguous, on the current device")
+    if t.requires_grad and torch.is_grad_enabled():
+        _refuse(where, "no gradient is computed: detach, or call under torch.no_grad()")
     return pk_heads(t.data_ptr(), ts if n > 1 else 0, stride[-2] if shape[-2] > 1 else 0)
 
 
