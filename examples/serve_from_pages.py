@@ -44,6 +44,7 @@ class Layer:
 class Server:
     def __init__(self, layer: Layer, slots: int = 512):
         self.layer, self.free = layer, list(range(slots))
+        self.private = set()  # slots that one request has to itself: no key of the table leads to them
         self.kt = KeyTable(CHUNK, 12)
         self.kv = KVPages(slots, CHUNK, KV_HEADS, D)
         self.descriptors = [{"model_id": "example/one-layer", "weight_precision": "bf16", "weight_version": "1",
@@ -67,10 +68,12 @@ class Server:
 
         # page tables: the chunks' slots, then private pages for the rest of the prompt and what is decoded
         stride = max(-(-(x + room) // CHUNK) for x in lens)
-        table = torch.full((R, stride), 0, dtype=torch.int32)
+        table = torch.full((R, stride), -1, dtype=torch.int32)
         for r in range(R):
             row = used[key_off[r]: key_off[r + 1]]
-            row += [self.free.pop() for _ in range(-(-(lens[r] + room) // CHUNK) - len(row))]
+            own = [self.free.pop() for _ in range(-(-(lens[r] + room) // CHUNK) - len(row))]
+            self.private.update(own)
+            row += own
             table[r, : len(row)] = torch.tensor(row, dtype=torch.int32)
         table = table.cuda()
 
@@ -105,6 +108,42 @@ class Server:
         return self.layer.logits(out), kv_len
 
 
+    def evict(self, table, weight, kv_len, budget: int):
+        """Cuts each request to the pages that attention has weighed most; the rest of its room follows them."""
+        stride = table.shape[1]
+        held = (kv_len + CHUNK - 1) // CHUNK
+        kept, kept_weight, kv_len, gone = self.kv.evict(table, weight, kv_len, budget, sinks=1, recent=2)
+        left = (kv_len + CHUNK - 1) // CHUNK
+        at = torch.arange(stride, device="cuda").view(1, -1)
+        room = at + (held - left).view(-1, 1)  # where a place behind the kept pages was before
+        moved = torch.where(room < stride, table.gather(1, room.clamp(max=stride - 1)), -1)
+        kept, kept_weight = (torch.nn.functional.pad(x, (0, max(0, stride - budget)))[:, :stride] for x in (kept, kept_weight))
+        table = torch.where(at < left.view(-1, 1), kept, moved).to(torch.int32).contiguous()
+        self.release(gone)
+        return table, kept_weight.contiguous(), kv_len
+
+    def release(self, slots):
+        """Gives back what of `slots` no key leads to: a chunk's page may be another request's, now or later."""
+        mine = self.private.intersection(slots.flatten().tolist())
+        self.private -= mine
+        self.free += sorted(mine)
+
+    def serve(self, batch, steps: int, budget: int):
+        """Answers of 2 * steps tokens a request, cut to `budget` pages after the first half; a report."""
+        logits, table, kv_len, hit = self.prefill(batch, room=2 * steps)
+        weight = torch.zeros(table.shape, dtype=torch.float32, device="cuda")
+        answers = []
+        for step in range(2 * steps):
+            if step == steps:
+                table, weight, kv_len = self.evict(table, weight, kv_len, budget)
+            token = logits.argmax(-1).to(torch.int32)
+            answers.append(token)
+            logits, kv_len = self.decode(token, table, kv_len, weight)
+        self.kv.check("decode")
+        self.release(table)
+        return dict(hit=hit, kv_len=kv_len.tolist(), answers=torch.stack(answers).T.tolist(), weight=weight.sum(1).tolist())
+
+
 def main(steps: int = 24, budget: int = 8, quiet: bool = False):
     rng = np.random.default_rng(0)
     server = Server(Layer(0))
@@ -113,30 +152,9 @@ def main(steps: int = 24, budget: int = 8, quiet: bool = False):
     second = [document + rng.integers(0, VOCAB, 60).tolist(), first[0], rng.integers(0, VOCAB, 5).tolist()]
     report = {}
     for name, batch in (("first", first), ("second", second)):
-        logits, table, kv_len, hit = server.prefill(batch, room=2 * steps)
-        weight = torch.zeros(table.shape, dtype=torch.float32, device="cuda")
-        answers = []
-        for step in range(2 * steps):
-            if step == steps:  # only the pages that attention has weighed most go on
-                full = table.shape[1]
-                table, weight, kv_len, gone = server.kv.evict(table, weight, kv_len, budget, sinks=1, recent=2)
-                # room again for what is decoded: the pages that were dropped by this request alone are free
-                more = torch.tensor([[server.free.pop() for _ in range(full - budget)] for _ in batch],
-                                    dtype=torch.int32, device="cuda")
-                pages = ((kv_len + CHUNK - 1) // CHUNK).view(-1, 1)
-                at = torch.arange(full, device="cuda").view(1, -1)
-                table = torch.where(at < pages, torch.nn.functional.pad(table, (0, full - budget)),
-                                    more.gather(1, (at - pages).clamp(0, full - budget - 1)))
-                weight = torch.nn.functional.pad(weight, (0, full - budget)).contiguous()
-                table = table.to(torch.int32).contiguous()
-            token = logits.argmax(-1).to(torch.int32)
-            answers.append(token)
-            logits, kv_len = server.decode(token, table, kv_len, weight)
-        server.kv.check("decode")
-        report[name] = dict(hit=hit, kv_len=kv_len.tolist(), answers=torch.stack(answers).T.tolist(),
-                            weight=weight.sum(1).tolist())
+        report[name] = server.serve(batch, steps, budget)
         if not quiet:
-            print(f"{name} batch: hit chunks {hit}, positions held {kv_len.tolist()}, "
+            print(f"{name} batch: hit chunks {report[name]['hit']}, positions held {report[name]['kv_len']}, "
                   f"first answers {[a[:6] for a in report[name]['answers']]}")
     server.kt.close()
     return report
