@@ -792,6 +792,7 @@ __global__ void __launch_bounds__(kFinishThreads) k_cache_finish(const Args a, u
 struct Plan {
     uint32_t rows, tile_rows, row_tiles, splits, split_grans, max_grans;
     uint64_t part_rows, o_bytes, ml_bytes, gran_bytes;
+    uint64_t blocks, join, weigh;  // of k_attend_cache; of k_cache_finish
 };
 
 uint64_t up16(uint64_t x) { return (x + 15) & ~15ull; }
@@ -824,6 +825,10 @@ Plan plan_of(const pk_kv_cache &kv, uint32_t R, uint32_t n_q, uint32_t q_heads, 
     p.ml_bytes = p.splits > 1 || weigh ? up16(p.part_rows * 8) : 0;
     const uint64_t gran_rows = p.rows < p.tile_rows ? p.rows : p.tile_rows;
     p.gran_bytes = weigh ? up16(units * p.max_grans * gran_rows * 8) : 0;
+    p.blocks = units * p.splits;
+    p.join = p.splits > 1 ? ((uint64_t)R * kv.kv_heads * p.rows + kFinishWarps - 1) / kFinishWarps : 0;
+    const uint64_t block_pages = kFinishWarps * pages_a_warp(kv.page_tokens / 16);
+    p.weigh = weigh ? (page_stride + block_pages - 1) / block_pages * R : 0;
     return p;
 }
 
@@ -834,15 +839,9 @@ cudaError_t launch(const Args &a, const Plan &p, cudaStream_t s) {
     static std::atomic<uint64_t> seen[2] = {};
     cudaError_t e = pk_allow_smem(kern, smem, seen[a.page_weight != nullptr]);
     if (e != cudaSuccess) return e;
-    const uint64_t units = (uint64_t)a.R * a.kv_heads * p.row_tiles;
-    if (units * p.splits > 0x7fffffffull) return cudaErrorInvalidValue;
-    e = pk_launch_smem(kern, (unsigned)(units * p.splits), kThreads, smem, s, a);
-    const uint64_t join = p.splits > 1 ? ((uint64_t)a.R * a.kv_heads * p.rows + kFinishWarps - 1) / kFinishWarps : 0;
-    const uint64_t block_pages = kFinishWarps * pages_a_warp(a.page_grans);
-    const uint64_t weigh = a.page_weight ? (a.page_stride + block_pages - 1) / block_pages * a.R : 0;
-    if (join + weigh > 0x7fffffffull) return cudaErrorInvalidValue;
-    if (e == cudaSuccess && join + weigh)
-        e = pk_launch(k_cache_finish<D, DT>, (unsigned)(join + weigh), kFinishThreads, s, a, p.tile_rows, (uint32_t)join);
+    e = pk_launch_smem(kern, (unsigned)p.blocks, kThreads, smem, s, a);
+    if (e == cudaSuccess && p.join + p.weigh)
+        e = pk_launch(k_cache_finish<D, DT>, (unsigned)(p.join + p.weigh), kFinishThreads, s, a, p.tile_rows, (uint32_t)p.join);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
@@ -851,6 +850,7 @@ cudaError_t launch(const Args &a, const Plan &p, cudaStream_t s) {
 uint64_t pk_attend_cache_scratch_bytes_impl(const pk_kv_cache &kv, uint32_t R, uint32_t n_q, uint32_t q_heads,
                                             uint64_t page_stride, bool weigh) {
     const Plan p = plan_of(kv, R, n_q, q_heads, page_stride, weigh);
+    if (p.blocks > 0x7fffffffull || p.join + p.weigh > 0x7fffffffull) return UINT64_MAX;
     return p.o_bytes + p.ml_bytes + p.gran_bytes;
 }
 

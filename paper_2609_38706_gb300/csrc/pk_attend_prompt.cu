@@ -912,6 +912,15 @@ cudaError_t launch(const Args &a, bool fixed, unsigned grid, const CUtensorMap &
 
 }  // namespace
 
+// A tile: all heads of the group for as many tokens as fit 128 rows, or 128 heads of one token.
+static uint32_t tile_heads_of(uint32_t group) { return group < (uint32_t)kRows ? group : kRows; }
+
+// Every request rounds its tokens up to whole items: at most one more each.
+uint64_t pk_attend_prompt_items(uint64_t n_q, uint32_t R, uint32_t q_heads, uint32_t kv_heads) {
+    const uint32_t group = q_heads / kv_heads, heads = tile_heads_of(group);
+    return (n_q / (2 * (kRows / heads)) + R) * ((group + heads - 1) / heads) * kv_heads;
+}
+
 cudaError_t pk_launch_attend_prompt(uint32_t dtype, const pk_heads &q, const pk_heads &k, const pk_heads &v,
                                     const pk_heads &out, float *lse, uint64_t n_q, uint64_t n_k, const int64_t *q_off,
                                     const int64_t *k_off, uint32_t R, uint32_t q_heads, uint32_t kv_heads,
@@ -930,8 +939,7 @@ cudaError_t pk_launch_attend_prompt(uint32_t dtype, const pk_heads &q, const pk_
     a.q_heads = q_heads;
     a.kv_heads = kv_heads;
     a.group = q_heads / kv_heads;
-    // a tile: all heads of the group for as many tokens as fit 128 rows, or 128 heads of one token
-    a.tile_heads = a.group < kRows ? a.group : kRows;
+    a.tile_heads = tile_heads_of(a.group);
     a.tile_tokens = kRows / a.tile_heads;
     a.chunks = (a.group + a.tile_heads - 1) / a.tile_heads;
     a.scale2 = (float)((double)scale * 1.4426950408889634);
@@ -951,9 +959,7 @@ cudaError_t pk_launch_attend_prompt(uint32_t dtype, const pk_heads &q, const pk_
         e = pk_launch(k_prompt_tiles, 1, kPlanThreads, s, q_off, k_off, R, n_q, n_k, item_tokens, a.chunks,
                       a.tile_off, status);
     if (e != cudaSuccess) return e;
-    // every request rounds its tokens up to whole items: at most one more each
-    const uint64_t items = (n_q / item_tokens + R) * a.chunks * kv_heads;
-    if (items > 0x7fffffffull) return cudaErrorInvalidValue;
+    const uint64_t items = pk_attend_prompt_items(n_q, R, q_heads, kv_heads);  // fewer than 2^31, looked at before
     a.most_items = (uint32_t)items;
     const bool fixed = items <= (uint64_t)sms || n_k < kLongKeys * R;
     const unsigned grid = fixed && items > (uint64_t)sms ? (unsigned)sms : (unsigned)items;

@@ -92,10 +92,12 @@ cudaError_t pk_launch_lookup_store(const pk_ctx *ctx, unsigned long long epoch, 
 cudaError_t pk_launch_kv_move(bool write, const pk_kv_cache &kv, uint32_t dtype, const pk_heads &k, const pk_heads &v,
                               uint64_t n_tokens, const int64_t *tok_off, const int32_t *start, uint32_t R,
                               const uint32_t *pages, uint64_t page_stride, int32_t *status, cudaStream_t s);
+uint64_t pk_attend_prompt_items(uint64_t n_q, uint32_t R, uint32_t q_heads, uint32_t kv_heads);  // blocks of a launch at most
 cudaError_t pk_launch_attend_prompt(uint32_t dtype, const pk_heads &q, const pk_heads &k, const pk_heads &v,
                                     const pk_heads &out, float *lse, uint64_t n_q, uint64_t n_k, const int64_t *q_off,
                                     const int64_t *k_off, uint32_t R, uint32_t q_heads, uint32_t kv_heads,
                                     uint32_t head_dim, float scale, void *scratch, int32_t *status, cudaStream_t s);
+// UINT64_MAX where a launch would need 2^31 blocks and more.
 uint64_t pk_attend_cache_scratch_bytes_impl(const pk_kv_cache &kv, uint32_t R, uint32_t n_q, uint32_t q_heads,
                                             uint64_t page_stride, bool weigh);
 cudaError_t pk_launch_attend_cache(const pk_kv_cache &kv, uint32_t dtype, const pk_heads &q, const pk_heads &out,

@@ -102,7 +102,8 @@ int pk_attend_prompt(uint32_t dtype, const pk_heads *q, const pk_heads *k, const
         !aligned(status_dev, 4))
         return PK_ERR_ARG;
     if (R == 0 || n_q == 0) return PK_OK;
-    if (!q_off_dev || !k_off_dev || !scratch_dev || scratch_bytes < pk_attend_prompt_scratch_bytes(R))
+    if (!q_off_dev || !k_off_dev || !scratch_dev || scratch_bytes < pk_attend_prompt_scratch_bytes(R) ||
+        pk_attend_prompt_items(n_q, R, q_heads, kv_heads) > 0x7fffffffull)
         return PK_ERR_ARG;
     return cuda_rc(pk_launch_attend_prompt(dtype, *q, *k, *v, *out, lse_dev, n_q, n_k, q_off_dev, k_off_dev, R,
                                            q_heads, kv_heads, head_dim, scale, scratch_dev, status_dev,
@@ -120,7 +121,8 @@ static bool good_attend(const pk_kv_cache *kv, uint32_t R, uint32_t n_q, uint32_
 size_t pk_attend_cache_scratch_bytes(const pk_kv_cache *kv, uint32_t R, uint32_t n_q, uint32_t q_heads,
                                      uint64_t page_stride, int weigh) {
     if (!good_attend(kv, R, n_q, q_heads, page_stride)) return 0;
-    return (size_t)pk_attend_cache_scratch_bytes_impl(*kv, R, n_q, q_heads, page_stride, weigh != 0);
+    const uint64_t need = pk_attend_cache_scratch_bytes_impl(*kv, R, n_q, q_heads, page_stride, weigh != 0);
+    return need == UINT64_MAX ? 0 : (size_t)need;
 }
 
 int pk_attend_cache(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, const pk_heads *out, float *lse_dev,
@@ -137,7 +139,7 @@ int pk_attend_cache(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, co
     if (R == 0) return PK_OK;
     if (!kv_len_dev || (page_stride && !pages_dev)) return PK_ERR_ARG;
     const uint64_t need = pk_attend_cache_scratch_bytes_impl(*kv, R, n_q, q_heads, page_stride, page_weight_dev);
-    if (scratch_bytes < need || (need && !scratch_dev)) return PK_ERR_ARG;
+    if (need == UINT64_MAX || scratch_bytes < need || (need && !scratch_dev)) return PK_ERR_ARG;
     return cuda_rc(pk_launch_attend_cache(*kv, dtype, *q, *out, lse_dev, R, n_q, q_heads, scale, kv_len_dev,
                                           pages_dev, page_stride, page_weight_dev, scratch_dev, status_dev,
                                           reinterpret_cast<cudaStream_t>(stream)));
