@@ -55,7 +55,7 @@ extern "C" {
 #define PK_ERR_RESERVED_KEY (-7)   /* key prefix is all zero (the empty marker), p = 2^-128 */
 #define PK_ERR_CUDA (-8)           /* a CUDA runtime call or launch failed */
 #define PK_ERR_TOO_LARGE (-9)      /* n above PK_NOALLOC_MAX_ENTRIES (pk_store_noalloc only) */
-#define PK_ERR_TIMEOUT (-10)       /* a bounded device-wide wait gave up (pk_evict); table unspecified */
+#define PK_ERR_TIMEOUT (-10)       /* a bounded device-wide wait gave up (pk_evict; table unspecified), or a copy's (attention) */
 
 /* Per-entry store results (int32). Negative values are the error codes above. */
 #define PK_STORE_SKIPPED 0         /* not in a miss range (range mode) */
@@ -580,7 +580,7 @@ int pk_attend_prompt(uint32_t dtype, const pk_heads *q, const pk_heads *k, const
  * arguments, 16-byte aligned (weigh: page_weight_dev given).  Device errors
  * (PK_ERR_ARG): a kv_len out of range counts as 0; a slot out of range below
  * kv_len makes all of that request's out and lse NaN, and nothing is added to
- * its page weights. */
+ * its page weights.  PK_ERR_TIMEOUT: likewise for the rows concerned. */
 size_t pk_attend_cache_scratch_bytes(const pk_kv_cache *kv, uint32_t R, uint32_t n_q, uint32_t q_heads,
                                      uint64_t page_stride, int weigh);
 int pk_attend_cache(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, const pk_heads *out, float *lse_dev,

@@ -136,9 +136,6 @@ struct Shape {
     static_assert(kRing >= 8 * NT * D * 4, "outputs fit the ring");
 };
 
-// One CTA: one request, KV head, tile of 8 NT query rows and split of the
-// tokens.  Warp w takes the split's steps w, w + kWarps, ... of kGrans granules.
-// Lane = 4 g + c.
 // The n-th request by length, longest first, in 64 steps of the longest; within a step by number.  By every warp for
 // itself: a search over the steps that counts by votes.
 __device__ __forceinline__ uint32_t nth_longest(const int32_t *kv_len, uint32_t R, uint32_t n) {
@@ -178,6 +175,9 @@ __device__ __forceinline__ uint32_t nth_longest(const int32_t *kv_len, uint32_t 
     return r;
 }
 
+// One CTA: one request, KV head, tile of 8 NT query rows and split of the
+// tokens.  Warp w takes the split's steps w, w + kWarps, ... of kGrans granules.
+// Lane = 4 g + c.
 template <int D, int NT, uint32_t DT, bool kWeigh>
 __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Args a) {
     using G = pk::Granule<D>;
@@ -609,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
     if (gave_up && lane == 0) pk::set_status(a.status, PK_ERR_TIMEOUT);
     pk::pdl_launch_dependents();
 
-    lost = __any_sync(0xffffffffu, lost);
+    lost = __any_sync(0xffffffffu, lost) || gave_up;
 
     // join the warps: O of each goes to its own ring, [row][D]
     float *ow = reinterpret_cast<float *>(ring);
