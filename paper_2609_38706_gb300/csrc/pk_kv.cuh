@@ -87,8 +87,6 @@ template <uint32_t DT>
 struct Elem;
 template <>
 struct Elem<PK_BF16> {
-    using T = __nv_bfloat16;
-    using T2 = __nv_bfloat162;
     static constexpr uint32_t kInfBits = 0x7f80;
     static __device__ __forceinline__ float2 to2(uint32_t w) {
         return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w));
@@ -103,8 +101,6 @@ struct Elem<PK_BF16> {
 };
 template <>
 struct Elem<PK_FP16> {
-    using T = __half;
-    using T2 = __half2;
     static constexpr uint32_t kInfBits = 0x7c00;
     static __device__ __forceinline__ float2 to2(uint32_t w) {
         return __half22float2(*reinterpret_cast<const __half2 *>(&w));
