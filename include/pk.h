@@ -552,7 +552,7 @@ int pk_kv_read(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *k, const p
  * last one never reach its outputs, whatever they hold.  A query that attends
  * a value of V that is infinite or NaN gets a non-finite output in that
  * dimension.  Rows of q that belong to no request are not written.
- * head_dim: 64 or 128; q_heads a multiple of kv_heads; scale finite; n_q and
+ * head_dim: 64 or 128; q_heads a multiple of kv_heads; |scale| at most 2.3e38; n_q and
  * n_k at most 0x7fff0000; strides of q, k and v below 2^39.
  * scratch_dev: pk_attend_prompt_scratch_bytes(R) bytes, 16-byte aligned.
  * Device errors: offsets out of order or range (PK_ERR_ARG; nothing is
@@ -575,7 +575,7 @@ int pk_attend_prompt(uint32_t dtype, const pk_heads *q, const pk_heads *k, const
  *            queries (what pk_evict_pages ranks by).  Deterministic.
  * A query before position 0 gives 0 and -infinity.  Bytes of positions at or
  * past kv_len are never used.  q_heads a multiple of kv_heads, at most 65536;
- * n_q >= 1.
+ * n_q >= 1; |scale * k_scale| at most 2.3e38.
  * scratch_dev: pk_attend_cache_scratch_bytes(...) bytes for the same
  * arguments, 16-byte aligned (weigh: page_weight_dev given).  Device errors
  * (PK_ERR_ARG): a kv_len out of range counts as 0; a slot out of range below

@@ -3,6 +3,7 @@
 // pk_evict_pages.cu.
 #include <cuda_runtime_api.h>
 
+#include <cfloat>
 #include <cmath>
 #include <initializer_list>
 
@@ -16,6 +17,9 @@ int cuda_rc(cudaError_t e) { return e == cudaSuccess ? PK_OK : PK_ERR_CUDA; }
 
 // A scale that multiplies values: finite and positive.
 bool good_scale(float x) { return std::isfinite(x) && x > 0.0f; }
+
+// A factor of scores whose exponents are taken to base 2, in 32 bits.
+bool good_score_scale(double x) { return std::fabs(x * 1.4426950408889634) <= FLT_MAX; }  // false for NaN
 
 bool good_cache(const pk_kv_cache *kv) {
     return kv && kv->pool_dev && aligned(kv->pool_dev, 16) && kv->n_slots >= 1 && kv->n_slots <= 0xffffffffull &&
@@ -90,7 +94,7 @@ int pk_attend_prompt(uint32_t dtype, const pk_heads *q, const pk_heads *k, const
                      float *lse_dev, uint64_t n_q, uint64_t n_k, const int64_t *q_off_dev, const int64_t *k_off_dev,
                      uint32_t R, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, float scale,
                      void *scratch_dev, size_t scratch_bytes, int32_t *status_dev, pk_stream stream) {
-    if (dtype > PK_FP16 || (head_dim != 64 && head_dim != 128) || !std::isfinite(scale)) return PK_ERR_ARG;
+    if (dtype > PK_FP16 || (head_dim != 64 && head_dim != 128) || !good_score_scale(scale)) return PK_ERR_ARG;
     if (kv_heads == 0 || q_heads == 0 || q_heads % kv_heads || q_heads > 65536) return PK_ERR_ARG;
     if (n_q > 0x7fff0000ull || n_k > 0x7fff0000ull) return PK_ERR_ARG;  // a tile's end still fits 31 bits
     if (!good_heads(q, n_q, q_heads) || !good_heads(k, n_k, kv_heads) || !good_heads(v, n_k, kv_heads) ||
@@ -129,7 +133,7 @@ int pk_attend_cache(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, co
                     uint32_t R, uint32_t n_q, uint32_t q_heads, float scale, const int32_t *kv_len_dev,
                     const uint32_t *pages_dev, uint64_t page_stride, float *page_weight_dev, void *scratch_dev,
                     size_t scratch_bytes, int32_t *status_dev, pk_stream stream) {
-    if (!good_cache(kv) || dtype > PK_FP16 || !std::isfinite(scale)) return PK_ERR_ARG;
+    if (!good_cache(kv) || dtype > PK_FP16 || !good_score_scale((double)scale * kv->k_scale)) return PK_ERR_ARG;
     if (!good_attend(kv, R, n_q, q_heads, page_stride)) return PK_ERR_ARG;
     const uint64_t rows = (uint64_t)R * n_q;
     if (!good_heads(q, rows, q_heads) || !good_out(out, rows, q_heads, kv->head_dim)) return PK_ERR_ARG;
