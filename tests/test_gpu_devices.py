@@ -69,14 +69,14 @@ def test_table_calls(elsewhere):
     tokens, off, idx = dev(np.arange(64, dtype=np.int32)), dev(np.array([0, 64])), dev(np.zeros(1, np.int32))
     key_off, keys = kt.derive(tokens, off, idx, d)
     slots = dev(np.arange(4, dtype=np.int32))
-    saved = kt.save()
+    saved = kt.save(torch.zeros(kt.table.numel() + 64, dtype=torch.uint8, device="cuda"))
     calls = [lambda: kt.derive(tokens, off, idx, d), lambda: kt.lookup(keys, key_off), lambda: kt.store(keys, slots),
              lambda: kt.lookup_store(keys, key_off, slots), lambda: kt.load(saved),
              lambda: pk.pk_init(kt.table, 16, 10)]
     for call in calls[:-1]:
         call()
     kt.check()
-    on_host = torch.empty(saved.numel(), dtype=torch.uint8)
+    on_host = torch.zeros(saved.numel(), dtype=torch.uint8)
     elsewhere()
     for call in calls:
         with pytest.raises(pk.PKError):
