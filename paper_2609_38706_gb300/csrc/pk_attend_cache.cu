@@ -20,11 +20,11 @@
 // mma.sync suits these 8-column products, whose operands never lie in shared
 // memory as 16-bit values (tcgen05 would need them there).
 //
-// 16 requests of up to 131072 tokens (8 KV heads, groups of 8, D = 128): 326 us
-// for both launches, 5.4 TB/s of pages, the attention itself 302 us with 77% of
-// the memory's cycles and 65% of the issue slots taken (dequantising is 58% of
-// the ALU's).  128 requests of up to 2048: 60 us (55 + 5): 1024 CTAs of unequal
-// lengths for 608 places.  Short caches: two launches, 8 us.
+// 16 requests of up to 131072 tokens (8 KV heads, groups of 8, D = 128): 328 us
+// for both launches, 25 of it the join, 5.4 TB/s of pages; the attention takes 76%
+// of the memory's cycles and 65% of the issue slots (dequantising is 58% of the
+// ALU's).  128 requests of up to 2048: 62.5 us, 5 of it the page weights: 1024 CTAs
+// of unequal lengths for 608 places.  Short caches: two launches, 8 us.
 #include <cuda_runtime.h>
 #include <float.h>
 

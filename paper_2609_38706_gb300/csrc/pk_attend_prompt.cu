@@ -19,10 +19,10 @@
 // ahead, changed nothing (128 | 128 us), nor did halves of a tile to two
 // warpgroups (675 | 776 us at D = 128, two prompts of 8192).
 //
-// Two prompts of 8192 (32 heads over 8, D = 128, bf16): 605 us, 1.5 PFLOP/s,
+// Two prompts of 8192 (32 heads over 8, D = 128, bf16): 604 us, 1.5 PFLOP/s,
 // tensor pipe 70% busy at 1.8 GHz under the power limit.  12 of 1500 behind 2048
-// keys (12 over 4, D = 64): 118 us, 0.79 PFLOP/s: a tile's chain (scores, 2^x,
-// product) and five items an SM.  8 of 512: 31 us, 3 short items an SM: the
+// keys (12 over 4, D = 64): 121 us, 0.77 PFLOP/s: a tile's chain (scores, 2^x,
+// product) and five items an SM.  8 of 512: 32 us, 3 short items an SM: the
 // chain's latency.
 #include <cuda.h>
 #include <cuda_runtime.h>
