@@ -588,6 +588,61 @@ int pk_attend_cache(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, co
                     const uint32_t *pages_dev, uint64_t page_stride, float *page_weight_dev, void *scratch_dev,
                     size_t scratch_bytes, int32_t *status_dev, pk_stream stream);
 
+/* Device.  pk_attend_cache with a sliding window: a query at position p attends
+ * the positions above p - window up to its own, and the first `sinks` ones up
+ * to its own.  window 0: no limit (pk_attend_cache itself).  Pages that no query
+ * of a request sees are not read, and their slots may be anything; nothing is
+ * added to their weights.  window and sinks below 2^31; the rest, scratch
+ * included (by its own function), as pk_attend_cache. */
+size_t pk_attend_cache_window_scratch_bytes(const pk_kv_cache *kv, uint32_t R, uint32_t n_q, uint32_t q_heads,
+                                            uint64_t page_stride, int weigh, uint32_t window, uint32_t sinks);
+int pk_attend_cache_window(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, const pk_heads *out, float *lse_dev,
+                           uint32_t R, uint32_t n_q, uint32_t q_heads, float scale, uint32_t window, uint32_t sinks,
+                           const int32_t *kv_len_dev, const uint32_t *pages_dev, uint64_t page_stride,
+                           float *page_weight_dev, void *scratch_dev, size_t scratch_bytes, int32_t *status_dev,
+                           pk_stream stream);
+
+/* How positions turn the pairs of a head's first rotary_dim values.  Pair i is
+ * dimensions (i, i + rotary_dim/2), or (2i, 2i + 1) where interleaved; a
+ * position turns it by turns[i] / 2^64 of a whole turn, and amplitude multiplies
+ * what was rotated. */
+typedef struct {
+    const uint64_t *turns_dev; /* [rotary_dim / 2] */
+    uint32_t rotary_dim;       /* a multiple of 16, 16..head_dim */
+    uint32_t interleaved;      /* 0 or 1 */
+    float amplitude;           /* finite */
+} pk_rotary;
+
+/* Host.  The table of a pk_rotary: f_i = base^(-2i / rotary_dim) radians a
+ * position, for long contexts divided by `factor`: all of them where context is
+ * 0, else by parts (Peng et al., "YaRN", 2023): with n = context * f_i / 2 pi
+ * turns over the original context, f_i stays where n >= high, is divided where
+ * n <= low, and between them is the mean of both, f_i weighed by
+ * (n - low) / (high - low).  base > 1, factor >= 1, context >= 0, 0 <= low <
+ * high, all finite; rotary_dim as above. */
+int pk_rotary_turns(uint32_t rotary_dim, double base, double factor, double context, double low, double high,
+                    uint64_t *turns);
+
+/* Device.  Norms of queries and keys, a head at a time, and their rotation, in
+ * one pass:
+ *   q, q_out [n_tokens][q_heads][head_dim], k, k_out [n_tokens][kv_heads][head_dim]
+ *            of dtype; an output may be its own input (the same pointer and
+ *            strides), and must not overlap an input otherwise
+ *   q_weight_dev, k_weight_dev  [head_dim] of dtype, 16-byte aligned, or NULL:
+ *            x becomes x / sqrt(mean(x^2) + eps) * weight over its head; with
+ *            NULL it stays as it is
+ *   tok_off_dev, start_dev  as pk_kv_write: token i of request r has position
+ *            start[r] + i, below 2^31
+ * Angles are exact to 2^-32 of a turn at any position; all else is held in 32
+ * bits and rounded once.  Tokens that belong to no request are not written.
+ * head_dim: 64 or 128; q_heads + kv_heads <= 65536; either may be 0; eps
+ * positive, normal and finite.  Device errors: offsets or start out of range
+ * (PK_ERR_ARG; that token is not written). */
+int pk_rotate(uint32_t dtype, const pk_heads *q, const pk_heads *k, const pk_heads *q_out, const pk_heads *k_out,
+              uint64_t n_tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, const pk_rotary *rotary,
+              const void *q_weight_dev, const void *k_weight_dev, float eps, const int64_t *tok_off_dev,
+              const int32_t *start_dev, uint32_t R, int32_t *status_dev, pk_stream stream);
+
 /* Device.  Cut each request to `budget` pages by accumulated attention
  * weight.  Request r holds n = ceil(kv_len[r] / page_tokens) pages.  n <=
  * budget: all are kept.  Else its first `sinks` and last `recent` pages stay,

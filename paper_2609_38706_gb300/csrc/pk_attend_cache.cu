@@ -59,6 +59,7 @@ struct Args {
     uint32_t splits, split_grans;  // granules of one split
     bool by_length;                // the longest requests' blocks come first
     float scale2, v_scale;         // scale2 = scale * k_scale * log2 e
+    uint32_t window, sinks, sink_grans;  // window 0: none; granules that hold the first `sinks` tokens
     const uint16_t *q;
     int64_t q_ts, q_hs;
     uint16_t *out;
@@ -123,6 +124,14 @@ __device__ __forceinline__ int32_t length_of(const int32_t *kv_len, uint64_t r, 
     return len < 0 || (uint64_t)len > most ? 0 : len;
 }
 
+// With a window a request's granules that some query sees are counted without the gap between those of the first tokens
+// and those of the window: granule v of them is granule v, or v + skip from sink_grans on.
+__device__ __forceinline__ uint32_t gap_of(const Args &a, int32_t len) {
+    const int64_t low = (int64_t)len - a.n_q - a.window + 1;  // first position that the first query's window holds
+    const uint32_t first = low > 0 ? (uint32_t)(low / 16) : 0;
+    return first > a.sink_grans ? first - a.sink_grans : 0;
+}
+
 // How a variant is cut: columns (8 query rows each), granules that a warp takes
 // at once, stages of its ring, CTAs an SM.  Two granules share the waiting, the
 // look for a new reference and the loop around them (338 instructions a granule
@@ -178,7 +187,7 @@ __device__ __forceinline__ uint32_t nth_longest(const int32_t *kv_len, uint32_t 
 // One CTA: one request, KV head, tile of 8 NT query rows and split of the
 // tokens.  Warp w takes the split's steps w, w + kWarps, ... of kGrans granules.
 // Lane = 4 g + c.
-template <int D, int NT, uint32_t DT, bool kWeigh>
+template <int D, int NT, uint32_t DT, bool kWeigh, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Args a) {
     using G = pk::Granule<D>;
     using S = Shape<D, NT>;
@@ -217,7 +226,9 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
     const uint64_t most = a.page_stride * a.page_tokens;
     const int32_t len = length_of(kv_len, r, most);
     if (len != __ldcg(kv_len + r) && tid == 0) pk::set_status(a.status, PK_ERR_ARG);
-    const uint32_t n_gran = ((uint32_t)len + 15) / 16;
+    const uint32_t skip = kWindow ? gap_of(a, len) : 0;
+    auto gran_of = [&](uint32_t v) { return kWindow && v >= a.sink_grans ? v + skip : v; };
+    const uint32_t n_gran = ((uint32_t)len + 15) / 16 - skip;
     const uint32_t g0 = split * a.split_grans, g1 = min(g0 + a.split_grans, n_gran);
     if (a.splits > 1 && g0 >= n_gran) return;  // no partial result: the combination counts the splits itself
     const uint32_t steps = g0 < g1 ? (g1 - g0 + TG - 1) / TG : 0;
@@ -233,8 +244,9 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
     uint64_t where = 0;
     auto find_granules = [&](uint32_t k) {
         ahead = k;
-        const uint32_t gr = g0 + (warp + (k + lane / TG) * kWarps) * TG + lane % TG;
-        if (gr < g1) {
+        const uint32_t at = g0 + (warp + (k + lane / TG) * kWarps) * TG + lane % TG;
+        if (at < g1) {
+            const uint32_t gr = gran_of(at);
             const uint32_t page = pow2 ? gr >> slot_shift : gr / a.page_grans;
             uint64_t slot = __ldcg(pages + page);
             if (slot >= a.n_slots) {
@@ -269,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
     bool wide = false;
     uint32_t up_bits[NT];  // that power of two
     float mul[NT][2];   // for columns 2c, 2c + 1
-    int32_t last[NT][2];
+    int32_t last[NT][2], low[NT][2];  // a column sees the positions low .. last, and those below a.sinks up to last
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const uint32_t row = tile * kRows + nt * 8 + g;
@@ -314,6 +326,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
             mul[nt][j] = a.scale2 * __shfl_sync(0xffffffffu, down, 4 * (2 * c + j));
             const uint32_t cr = tile * kRows + nt * 8 + 2 * c + j;
             last[nt][j] = len - (int32_t)a.n_q + (int32_t)(cr < a.rows ? cr / a.group : a.n_q - 1);
+            low[nt][j] = kWindow ? (int32_t)max((int64_t)last[nt][j] - a.window + 1, (int64_t)0) : 0;
         }
     }
 
@@ -327,7 +340,9 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
         ref[nt][0] = ref[nt][1] = -FLT_MAX;
         sum[nt][0] = sum[nt][1] = 0.0f;
     }
-    const int32_t all_see = len - (int32_t)a.n_q;  // positions up to here are seen by every query
+    // positions all_low .. all_see are seen by every query
+    const int32_t all_see = len - (int32_t)a.n_q;
+    const int32_t all_low = kWindow ? (int32_t)max((int64_t)len - a.window, (int64_t)0) : 0;
     // where this lane's granule sums of the first step go: lanes of g = 0..3 write, column 2c + (g & 1) of granule
     // g >> 1 (of tile nt: + 8 nt)
     float2 *gran_at = nullptr;
@@ -342,7 +357,10 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
     auto step = [&](uint32_t k, uint32_t st, auto edge, auto with_rest) {
         constexpr bool kEdge = decltype(edge)::value, kWide = decltype(with_rest)::value;
         const uint8_t *gr = ring + st * S::kStage;
-        const int32_t pos0 = (int32_t)((g0 + (warp + k * kWarps) * TG) * 16);
+        const uint32_t v0 = g0 + (warp + k * kWarps) * TG;
+        int32_t pos0[TG];  // first positions of the granules
+#pragma unroll
+        for (int h = 0; h < TG; ++h) pos0[h] = (int32_t)(gran_of(v0 + h) * 16);
 
         // S^T = K Q^T: rows g and g + 8 of a granule's 16 are tokens
         float s[TG][NT][4];
@@ -442,7 +460,9 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
                             y = __fmul_rn(s[h][nt][e], mul[nt][e & 1]) - ref[nt][e & 1];
                         else
                             y = fmaf(s[h][nt][e], mul[nt][e & 1], -ref[nt][e & 1]);
-                        if (kEdge && pos0 + 16 * h + (int32_t)(g + 8 * (e >> 1)) > last[nt][e & 1]) y = -INFINITY;
+                        const int32_t pos = pos0[h] + (int32_t)(g + 8 * (e >> 1));
+                        if (kEdge && pos > last[nt][e & 1]) y = -INFINITY;
+                        if (kEdge && kWindow && pos < low[nt][e & 1] && pos >= (int32_t)a.sinks) y = -INFINITY;
                         top = fmaxf(top, y);
                     }
             return top > kTop;
@@ -504,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
                                   : u[0] + __shfl_xor_sync(0xffffffffu, u[0], 8);
                 v += __shfl_xor_sync(0xffffffffu, v, 16);
                 const uint32_t col = nt * 8 + 2 * c + (g & 1);
-                if (g < 2 * TG && tile * kRows + col < a.rows && (!kEdge || pos0 + 16 * (int32_t)(g >> 1) < len))
+                if (g < 2 * TG && tile * kRows + col < a.rows && (!kEdge || (TG == 2 && (g & 2) ? pos0[TG - 1] : pos0[0]) < len))
                     gran_at[(uint64_t)k * (kWarps * TG) * a.gran_rows + nt * 8] =
                         make_float2(v, odd ? ref[nt][1] : ref[nt][0]);
             }
@@ -534,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     const uint32_t tok = 2 * c + (t & 1) + 8 * (t >> 1);
-                    if (pos0 + 16 * h + (int32_t)tok >= len) {
+                    if (pos0[h] + (int32_t)tok >= len) {
                         b[t] = 0;
                     } else if ((b[t] & 0x7f) == 0x7f) {
                         b[t] = 0;
@@ -548,8 +568,9 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
-                            const int32_t see = last[nt][j] - (pos0 + 16 * h) + 1;  // tokens here that it sees
-                            const uint32_t m = see <= 0 ? 0u : see >= 16 ? 0xffffu : (1u << see) - 1;
+                            const auto up_to = [](int32_t n) { return n <= 0 ? 0u : n >= 16 ? 0xffffu : (1u << n) - 1; };
+                            uint32_t m = up_to(last[nt][j] - pos0[h] + 1);  // tokens here that it sees
+                            if (kWindow) m &= ~up_to(low[nt][j] - pos0[h]) | up_to((int32_t)a.sinks - pos0[h]);
                             if (bad & m) {
 #pragma unroll
                                 for (int i = 0; i < kSteps; ++i)
@@ -595,7 +616,10 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
                     pk::mbar_wait(bar_s + 8 * (i % S::kStages), (i / S::kStages) & 1);
                 break;
             }
-            if (decltype(with_rest)::value || (int32_t)((g0 + (warp + k * kWarps) * TG) * 16) + 16 * TG - 1 > all_see)
+            const uint32_t v0 = g0 + (warp + k * kWarps) * TG;
+            const int32_t begin = (int32_t)(gran_of(v0) * 16), end = (int32_t)(gran_of(v0 + TG - 1) * 16 + 16);
+            const bool hides = kWindow && begin < all_low && end > (int32_t)a.sinks;
+            if (decltype(with_rest)::value || end - 1 > all_see || hides)
                 step(k, st, std::true_type{}, with_rest);
             else
                 step(k, st, std::false_type{}, with_rest);
@@ -660,9 +684,10 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
     }
 }
 
-// Splits of one request that hold tokens.
+// Splits of one request that hold tokens that a query sees.
+template <bool kWindow>
 __device__ __forceinline__ uint32_t live_splits(const Args &a, int32_t len) {
-    const uint32_t n_gran = ((uint32_t)len + 15) / 16;
+    const uint32_t n_gran = ((uint32_t)len + 15) / 16 - (kWindow ? gap_of(a, len) : 0);
     return (n_gran + a.split_grans - 1) / a.split_grans;
 }
 
@@ -679,7 +704,7 @@ __host__ __device__ constexpr uint32_t pages_a_warp(uint32_t page_grans) { retur
 // a warp a page, lanes over (head, row), in an order that depends on the sizes
 // alone.  Both need a row's final reference and sum over the splits; the
 // weighing blocks find them again, which costs less than waiting for a launch.
-template <int D, uint32_t DT>
+template <int D, uint32_t DT, bool kWindow>
 __global__ void __launch_bounds__(kFinishThreads) k_cache_finish(const Args a, uint32_t tile_rows, uint32_t join_blocks) {
     __shared__ float2 stat[kStatRows];  // (ref, 1 / sum) of (head, row)
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -696,7 +721,7 @@ __global__ void __launch_bounds__(kFinishThreads) k_cache_finish(const Args a, u
         const uint64_t rh = id / a.rows;
         const uint32_t row = (uint32_t)(id % a.rows);
         const uint32_t r = (uint32_t)(rh / a.kv_heads), head = (uint32_t)(rh % a.kv_heads);
-        const uint32_t n = live_splits(a, length_of(kv_len, r, most));
+        const uint32_t n = live_splits<kWindow>(a, length_of(kv_len, r, most));
         const uint64_t first = (rh * a.row_tiles + row / tile_rows) * a.splits * tile_rows + row % tile_rows;
         float m = -FLT_MAX;
         for (uint32_t s = lane; s < n; s += 32) m = fmaxf(m, __ldcg(part_ml + first + (uint64_t)s * tile_rows).x);
@@ -733,8 +758,12 @@ __global__ void __launch_bounds__(kFinishThreads) k_cache_finish(const Args a, u
     const uint32_t blocks = (uint32_t)((a.page_stride + block_pages - 1) / block_pages);
     const uint32_t id = blockIdx.x - join_blocks, r = id / blocks, page0 = id % blocks * block_pages;
     const int32_t len = length_of(kv_len, r, most);
-    const uint32_t n = live_splits(a, len), n_gran = ((uint32_t)len + 15) / 16;
-    if ((uint64_t)page0 * a.page_grans >= n_gran) return;  // uniform: no token in these pages
+    const uint32_t n = live_splits<kWindow>(a, len), n_gran = ((uint32_t)len + 15) / 16;
+    const uint32_t skip = kWindow ? gap_of(a, len) : 0;  // the granules [sink_grans, sink_grans + skip) nobody sees
+    const uint64_t block_end = ((uint64_t)page0 + block_pages) * a.page_grans;
+    // uniform: no token in these pages, or none that is seen
+    if ((uint64_t)page0 * a.page_grans >= n_gran) return;
+    if (kWindow && (uint64_t)page0 * a.page_grans >= a.sink_grans && block_end <= (uint64_t)a.sink_grans + skip) return;
     const uint32_t total = a.kv_heads * a.rows;
     const uint32_t page = page0 + warp * per, gr0 = page * a.page_grans, gr1 = min(gr0 + per * a.page_grans, n_gran);
     float acc[4] = {};  // of the granules gr0 + i mod 4
@@ -766,12 +795,16 @@ __global__ void __launch_bounds__(kFinishThreads) k_cache_finish(const Args a, u
 #pragma unroll 2
             for (uint32_t gr = gr0; gr < gr1; gr += 4) {
                 float2 y[4];
+                bool in[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t at = !kWindow || gr + i < a.sink_grans ? gr + i : gr + i - skip;  // among those seen
+                    in[i] = gr + i < gr1 && (!kWindow || gr + i < a.sink_grans || gr + i >= a.sink_grans + skip);
+                    y[i] = in[i] ? __ldcg(src + (uint64_t)at * a.gran_rows) : make_float2(0.0f, -FLT_MAX);
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    y[i] = gr + i < gr1 ? __ldcg(src + (uint64_t)(gr + i) * a.gran_rows) : make_float2(0.0f, -FLT_MAX);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (gr + i < gr1) acc[i] += y[i].x * ex2(y[i].y - st.x) * st.y;
+                    if (in[i]) acc[i] += y[i].x * ex2(y[i].y - st.x) * st.y;
             }
         }
     }
@@ -805,12 +838,16 @@ uint64_t up16(uint64_t x) { return (x + 15) & ~15ull; }
 // 67 us, 128 65 us).  Where that leaves places free, shorter ones down to
 // kLeastGrans fill them: the call then lasts as long as one split.
 constexpr uint64_t kWaves = 6, kMinGrans = 128, kLeastGrans = 32;
-Plan plan_of(const pk_kv_cache &kv, uint32_t R, uint32_t n_q, uint32_t q_heads, uint64_t page_stride, bool weigh) {
+Plan plan_of(const pk_kv_cache &kv, uint32_t R, uint32_t n_q, uint32_t q_heads, uint64_t page_stride, bool weigh,
+             uint32_t window, uint32_t sinks) {
     Plan p;
     p.rows = q_heads / kv.kv_heads * n_q;
     p.tile_rows = p.rows <= 8 ? 8 : 16;
     p.row_tiles = (p.rows + p.tile_rows - 1) / p.tile_rows;
     p.max_grans = (uint32_t)(page_stride * kv.page_tokens / 16);
+    // with a window: the first tokens' granules, and those that window + n_q - 1 positions can touch
+    if (window)
+        p.max_grans = (uint32_t)std::min<uint64_t>(p.max_grans, ((uint64_t)sinks + 15) / 16 + ((uint64_t)window + n_q + 14) / 16 + 1);
     const uint64_t units = (uint64_t)R * kv.kv_heads * p.row_tiles;
     auto up = [](uint64_t x, uint64_t by) { return by ? (x + by - 1) / by : 1; };
     uint64_t n = std::min(up(kSlots * kWaves, units), up(p.max_grans, kMinGrans));
@@ -834,22 +871,26 @@ Plan plan_of(const pk_kv_cache &kv, uint32_t R, uint32_t n_q, uint32_t q_heads, 
 
 template <int D, int NT, uint32_t DT>
 cudaError_t launch(const Args &a, const Plan &p, cudaStream_t s) {
-    void (*const kern)(Args) = a.page_weight ? k_attend_cache<D, NT, DT, true> : k_attend_cache<D, NT, DT, false>;
+    const int variant = (a.page_weight != nullptr) + 2 * (a.window != 0);
+    void (*const kerns[4])(Args) = {k_attend_cache<D, NT, DT, false, false>, k_attend_cache<D, NT, DT, true, false>,
+                                    k_attend_cache<D, NT, DT, false, true>, k_attend_cache<D, NT, DT, true, true>};
+    void (*const kern)(Args) = kerns[variant];
     constexpr size_t smem = (size_t)kWarps * Shape<D, NT>::kRing;
-    static std::atomic<uint64_t> seen[2] = {};
-    cudaError_t e = pk_allow_smem(kern, smem, seen[a.page_weight != nullptr]);
+    static std::atomic<uint64_t> seen[4] = {};
+    cudaError_t e = pk_allow_smem(kern, smem, seen[variant]);
     if (e != cudaSuccess) return e;
     e = pk_launch_smem(kern, (unsigned)p.blocks, kThreads, smem, s, a);
     if (e == cudaSuccess && p.join + p.weigh)
-        e = pk_launch(k_cache_finish<D, DT>, (unsigned)(p.join + p.weigh), kFinishThreads, s, a, p.tile_rows, (uint32_t)p.join);
+        e = pk_launch(a.window ? k_cache_finish<D, DT, true> : k_cache_finish<D, DT, false>, (unsigned)(p.join + p.weigh),
+                      kFinishThreads, s, a, p.tile_rows, (uint32_t)p.join);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
 
 uint64_t pk_attend_cache_scratch_bytes_impl(const pk_kv_cache &kv, uint32_t R, uint32_t n_q, uint32_t q_heads,
-                                            uint64_t page_stride, bool weigh) {
-    const Plan p = plan_of(kv, R, n_q, q_heads, page_stride, weigh);
+                                            uint64_t page_stride, bool weigh, uint32_t window, uint32_t sinks) {
+    const Plan p = plan_of(kv, R, n_q, q_heads, page_stride, weigh, window, sinks);
     if (p.blocks > 0x7fffffffull || p.join + p.weigh > 0x7fffffffull) return UINT64_MAX;
     return p.o_bytes + p.ml_bytes + p.gran_bytes;
 }
@@ -857,8 +898,9 @@ uint64_t pk_attend_cache_scratch_bytes_impl(const pk_kv_cache &kv, uint32_t R, u
 cudaError_t pk_launch_attend_cache(const pk_kv_cache &kv, uint32_t dtype, const pk_heads &q, const pk_heads &out,
                                    float *lse, uint32_t R, uint32_t n_q, uint32_t q_heads, float scale,
                                    const int32_t *kv_len, const uint32_t *pages, uint64_t page_stride,
-                                   float *page_weight, void *scratch, int32_t *status, cudaStream_t s) {
-    const Plan p = plan_of(kv, R, n_q, q_heads, page_stride, page_weight);
+                                   float *page_weight, uint32_t window, uint32_t sinks, void *scratch, int32_t *status,
+                                   cudaStream_t s) {
+    const Plan p = plan_of(kv, R, n_q, q_heads, page_stride, page_weight, window, sinks);
     Args a;
     a.pool = static_cast<const uint8_t *>(kv.pool_dev);
     a.page_bytes = pk_kv_page_bytes(kv.page_tokens, kv.kv_heads, kv.head_dim);
@@ -876,10 +918,13 @@ cudaError_t pk_launch_attend_cache(const pk_kv_cache &kv, uint32_t dtype, const 
     // One CTA a request and head, and more of them than the GPU holds: the longest first, so that the last to start are
     // the shortest (128 x 2048 tokens: 65.6 -> 63.5 us; 100 x 1500, D = 64: 36.9 -> 35.2).  The search costs short
     // ones more than it gives (250 x 300: 31.7 -> 38.4 us).
-    a.by_length = p.splits == 1 && R > 1 && R <= kRanked && p.max_grans >= kRankedGrans &&
+    a.by_length = !window && p.splits == 1 && R > 1 && R <= kRanked && p.max_grans >= kRankedGrans &&
                   (uint64_t)R * kv.kv_heads * p.row_tiles > kSlots;
     a.scale2 = (float)((double)scale * kv.k_scale * 1.4426950408889634);
     a.v_scale = kv.v_scale;
+    a.window = window;
+    a.sinks = window ? sinks : 0;
+    a.sink_grans = (a.sinks + 15) / 16;
     a.q = static_cast<const uint16_t *>(q.p);
     a.q_ts = q.tok_stride;
     a.q_hs = q.head_stride;

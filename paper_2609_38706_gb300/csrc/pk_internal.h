@@ -88,10 +88,15 @@ cudaError_t pk_launch_lookup_store(const pk_ctx *ctx, unsigned long long epoch, 
                                    uint64_t key_capacity, int32_t *hit_chunks, uint32_t *slots, int32_t *result,
                                    uint32_t *slot_out, int32_t *status, cudaStream_t s);
 
-// KV pages (pk_kv.cu, pk_attend_prompt.cu, pk_attend_cache.cu, pk_evict_pages.cu).  Arguments checked by pk_kv_host.cpp.
+// KV pages (pk_kv.cu, pk_rotate.cu, pk_attend_prompt.cu, pk_attend_cache.cu, pk_evict_pages.cu).  Arguments checked by pk_kv_host.cpp.
 cudaError_t pk_launch_kv_move(bool write, const pk_kv_cache &kv, uint32_t dtype, const pk_heads &k, const pk_heads &v,
                               uint64_t n_tokens, const int64_t *tok_off, const int32_t *start, uint32_t R,
                               const uint32_t *pages, uint64_t page_stride, int32_t *status, cudaStream_t s);
+cudaError_t pk_launch_rotate(uint32_t dtype, const pk_heads &q, const pk_heads &k, const pk_heads &q_out,
+                             const pk_heads &k_out, uint64_t n_tokens, uint32_t q_heads, uint32_t kv_heads,
+                             uint32_t head_dim, const pk_rotary &rotary, const void *q_weight, const void *k_weight,
+                             float eps, const int64_t *tok_off, const int32_t *start, uint32_t R, int32_t *status,
+                             cudaStream_t s);
 uint64_t pk_attend_prompt_items(uint64_t n_q, uint32_t R, uint32_t q_heads, uint32_t kv_heads);  // blocks of a launch at most
 cudaError_t pk_launch_attend_prompt(uint32_t dtype, const pk_heads &q, const pk_heads &k, const pk_heads &v,
                                     const pk_heads &out, float *lse, uint64_t n_q, uint64_t n_k, const int64_t *q_off,
@@ -99,11 +104,12 @@ cudaError_t pk_launch_attend_prompt(uint32_t dtype, const pk_heads &q, const pk_
                                     uint32_t head_dim, float scale, void *scratch, int32_t *status, cudaStream_t s);
 // UINT64_MAX where a launch would need 2^31 blocks and more.
 uint64_t pk_attend_cache_scratch_bytes_impl(const pk_kv_cache &kv, uint32_t R, uint32_t n_q, uint32_t q_heads,
-                                            uint64_t page_stride, bool weigh);
+                                            uint64_t page_stride, bool weigh, uint32_t window, uint32_t sinks);
 cudaError_t pk_launch_attend_cache(const pk_kv_cache &kv, uint32_t dtype, const pk_heads &q, const pk_heads &out,
                                    float *lse, uint32_t R, uint32_t n_q, uint32_t q_heads, float scale,
                                    const int32_t *kv_len, const uint32_t *pages, uint64_t page_stride,
-                                   float *page_weight, void *scratch, int32_t *status, cudaStream_t s);
+                                   float *page_weight, uint32_t window, uint32_t sinks, void *scratch, int32_t *status,
+                                   cudaStream_t s);
 cudaError_t pk_launch_evict_pages(const uint32_t *pages, const float *weight, const int32_t *kv_len, uint32_t R,
                                   uint64_t page_stride, uint32_t page_tokens, uint32_t budget, uint32_t sinks,
                                   uint32_t recent, uint32_t *pages_out, float *weight_out, int32_t *kv_len_out,

@@ -1,6 +1,6 @@
 // pk_kv_host.cpp -- host half of the KV-page calls: argument checks ahead of
-// the launches of pk_kv.cu, pk_attend_prompt.cu, pk_attend_cache.cu and
-// pk_evict_pages.cu.
+// the launches of pk_kv.cu, pk_rotate.cu, pk_attend_prompt.cu,
+// pk_attend_cache.cu and pk_evict_pages.cu; the table of a rotation.
 #include <cuda_runtime_api.h>
 
 #include <cfloat>
@@ -122,19 +122,32 @@ static bool good_attend(const pk_kv_cache *kv, uint32_t R, uint32_t n_q, uint32_
            page_stride < 1ull << 31;
 }
 
-size_t pk_attend_cache_scratch_bytes(const pk_kv_cache *kv, uint32_t R, uint32_t n_q, uint32_t q_heads,
-                                     uint64_t page_stride, int weigh) {
-    if (!good_attend(kv, R, n_q, q_heads, page_stride)) return 0;
-    const uint64_t need = pk_attend_cache_scratch_bytes_impl(*kv, R, n_q, q_heads, page_stride, weigh != 0);
+// A window that no request can outgrow is none; windows are positions, below 2^31 as they are.
+static bool good_window(uint32_t window, uint32_t sinks) { return window < 1u << 31 && sinks < 1u << 31; }
+static uint32_t window_within(const pk_kv_cache &kv, uint64_t page_stride, uint32_t window) {
+    return window < page_stride * kv.page_tokens ? window : 0;
+}
+
+size_t pk_attend_cache_window_scratch_bytes(const pk_kv_cache *kv, uint32_t R, uint32_t n_q, uint32_t q_heads,
+                                            uint64_t page_stride, int weigh, uint32_t window, uint32_t sinks) {
+    if (!good_attend(kv, R, n_q, q_heads, page_stride) || !good_window(window, sinks)) return 0;
+    const uint64_t need = pk_attend_cache_scratch_bytes_impl(*kv, R, n_q, q_heads, page_stride, weigh != 0,
+                                                             window_within(*kv, page_stride, window), sinks);
     return need == UINT64_MAX ? 0 : (size_t)need;
 }
 
-int pk_attend_cache(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, const pk_heads *out, float *lse_dev,
-                    uint32_t R, uint32_t n_q, uint32_t q_heads, float scale, const int32_t *kv_len_dev,
-                    const uint32_t *pages_dev, uint64_t page_stride, float *page_weight_dev, void *scratch_dev,
-                    size_t scratch_bytes, int32_t *status_dev, pk_stream stream) {
+size_t pk_attend_cache_scratch_bytes(const pk_kv_cache *kv, uint32_t R, uint32_t n_q, uint32_t q_heads,
+                                     uint64_t page_stride, int weigh) {
+    return pk_attend_cache_window_scratch_bytes(kv, R, n_q, q_heads, page_stride, weigh, 0, 0);
+}
+
+int pk_attend_cache_window(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, const pk_heads *out, float *lse_dev,
+                           uint32_t R, uint32_t n_q, uint32_t q_heads, float scale, uint32_t window, uint32_t sinks,
+                           const int32_t *kv_len_dev, const uint32_t *pages_dev, uint64_t page_stride,
+                           float *page_weight_dev, void *scratch_dev, size_t scratch_bytes, int32_t *status_dev,
+                           pk_stream stream) {
     if (!good_cache(kv) || dtype > PK_FP16 || !good_score_scale((double)scale * kv->k_scale)) return PK_ERR_ARG;
-    if (!good_attend(kv, R, n_q, q_heads, page_stride)) return PK_ERR_ARG;
+    if (!good_attend(kv, R, n_q, q_heads, page_stride) || !good_window(window, sinks)) return PK_ERR_ARG;
     const uint64_t rows = (uint64_t)R * n_q;
     if (!good_heads(q, rows, q_heads) || !good_out(out, rows, q_heads, kv->head_dim)) return PK_ERR_ARG;
     if (!aligned(lse_dev, 4) || !aligned(kv_len_dev, 4) || !aligned(pages_dev, 4) || !aligned(page_weight_dev, 4) ||
@@ -142,11 +155,61 @@ int pk_attend_cache(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, co
         return PK_ERR_ARG;
     if (R == 0) return PK_OK;
     if (!kv_len_dev || (page_stride && !pages_dev)) return PK_ERR_ARG;
-    const uint64_t need = pk_attend_cache_scratch_bytes_impl(*kv, R, n_q, q_heads, page_stride, page_weight_dev);
+    window = window_within(*kv, page_stride, window);
+    const uint64_t need = pk_attend_cache_scratch_bytes_impl(*kv, R, n_q, q_heads, page_stride, page_weight_dev, window, sinks);
     if (need == UINT64_MAX || scratch_bytes < need || (need && !scratch_dev)) return PK_ERR_ARG;
     return cuda_rc(pk_launch_attend_cache(*kv, dtype, *q, *out, lse_dev, R, n_q, q_heads, scale, kv_len_dev,
-                                          pages_dev, page_stride, page_weight_dev, scratch_dev, status_dev,
-                                          reinterpret_cast<cudaStream_t>(stream)));
+                                          pages_dev, page_stride, page_weight_dev, window, sinks, scratch_dev,
+                                          status_dev, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+int pk_attend_cache(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, const pk_heads *out, float *lse_dev,
+                    uint32_t R, uint32_t n_q, uint32_t q_heads, float scale, const int32_t *kv_len_dev,
+                    const uint32_t *pages_dev, uint64_t page_stride, float *page_weight_dev, void *scratch_dev,
+                    size_t scratch_bytes, int32_t *status_dev, pk_stream stream) {
+    return pk_attend_cache_window(kv, dtype, q, out, lse_dev, R, n_q, q_heads, scale, 0, 0, kv_len_dev, pages_dev,
+                                  page_stride, page_weight_dev, scratch_dev, scratch_bytes, status_dev, stream);
+}
+
+int pk_rotary_turns(uint32_t rotary_dim, double base, double factor, double context, double low, double high,
+                    uint64_t *turns) {
+    if (!turns || rotary_dim < 16 || rotary_dim > 128 || rotary_dim % 16 || !(base > 1.0) || !std::isfinite(base) ||
+        !(factor >= 1.0) || !std::isfinite(factor) || !(context >= 0.0) || !std::isfinite(context) || !(low >= 0.0) ||
+        !(high > low) || !std::isfinite(high))
+        return PK_ERR_ARG;
+    const double turn = 6.283185307179586476925286766559;  // 2 pi
+    for (uint32_t i = 0; i < rotary_dim / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / rotary_dim);
+        double stays = 0.0;
+        if (context > 0.0) stays = std::fmin(1.0, std::fmax(0.0, (context * f / turn - low) / (high - low)));
+        turns[i] = (uint64_t)std::ldexp((stays * f + (1.0 - stays) * f / factor) / turn, 64);
+    }
+    return PK_OK;
+}
+
+int pk_rotate(uint32_t dtype, const pk_heads *q, const pk_heads *k, const pk_heads *q_out, const pk_heads *k_out,
+              uint64_t n_tokens, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim, const pk_rotary *rotary,
+              const void *q_weight_dev, const void *k_weight_dev, float eps, const int64_t *tok_off_dev,
+              const int32_t *start_dev, uint32_t R, int32_t *status_dev, pk_stream stream) {
+    if (dtype > PK_FP16 || (head_dim != 64 && head_dim != 128) || (uint64_t)q_heads + kv_heads > 65536) return PK_ERR_ARG;
+    if (!rotary || rotary->rotary_dim < 16 || rotary->rotary_dim > head_dim || rotary->rotary_dim % 16 ||
+        rotary->interleaved > 1 || !std::isfinite(rotary->amplitude) || !rotary->turns_dev ||
+        !aligned(rotary->turns_dev, 8) || !std::isnormal(eps) || eps < 0.0f)
+        return PK_ERR_ARG;
+    if (n_tokens >= 1ull << 32) return PK_ERR_ARG;
+    // heads of none: no rows to look at
+    if (!good_heads(q, q_heads ? n_tokens : 0, q_heads) || !good_heads(k, kv_heads ? n_tokens : 0, kv_heads) ||
+        !good_out(q_out, q_heads ? n_tokens : 0, q_heads, head_dim) ||
+        !good_out(k_out, kv_heads ? n_tokens : 0, kv_heads, head_dim))
+        return PK_ERR_ARG;
+    if (!aligned(q_weight_dev, 16) || !aligned(k_weight_dev, 16) || !aligned(tok_off_dev, 8) || !aligned(start_dev, 4) ||
+        !aligned(status_dev, 4))
+        return PK_ERR_ARG;
+    if (R == 0 || n_tokens == 0 || q_heads + kv_heads == 0) return PK_OK;
+    if (!tok_off_dev || !start_dev) return PK_ERR_ARG;
+    return cuda_rc(pk_launch_rotate(dtype, *q, *k, *q_out, *k_out, n_tokens, q_heads, kv_heads, head_dim, *rotary,
+                                    q_weight_dev, k_weight_dev, eps, tok_off_dev, start_dev, R, status_dev,
+                                    reinterpret_cast<cudaStream_t>(stream)));
 }
 
 int pk_evict_pages(const uint32_t *pages_dev, const float *weight_dev, const int32_t *kv_len_dev, uint32_t R,

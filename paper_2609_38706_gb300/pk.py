@@ -74,6 +74,11 @@ class pk_heads(ctypes.Structure):
     _fields_ = [("p", ctypes.c_void_p), ("tok_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
+class pk_rotary(ctypes.Structure):
+    _fields_ = [("turns_dev", ctypes.c_void_p), ("rotary_dim", ctypes.c_uint32), ("interleaved", ctypes.c_uint32),
+                ("amplitude", ctypes.c_float)]
+
+
 _lib = None
 _VP, _U32, _U64, _I32 = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_int32
 
@@ -132,10 +137,16 @@ def lib() -> ctypes.CDLL:
             "pk_kv_page_bytes": (ctypes.c_size_t, [_U32, _U32, _U32]),
             "pk_kv_write": (ctypes.c_int, [_VP, _U32, _VP, _VP, _U64, _VP, _VP, _U32, _VP, _U64, _VP, _VP]),
             "pk_kv_read": (ctypes.c_int, [_VP, _U32, _VP, _VP, _U64, _VP, _VP, _U32, _VP, _U64, _VP, _VP]),
+            "pk_rotary_turns": (ctypes.c_int, [_U32] + [ctypes.c_double] * 5 + [_VP]),
+            "pk_rotate": (ctypes.c_int, [_U32, _VP, _VP, _VP, _VP, _U64, _U32, _U32, _U32, _VP, _VP, _VP, ctypes.c_float,
+                                         _VP, _VP, _U32, _VP, _VP]),
             "pk_attend_prompt_scratch_bytes": (ctypes.c_size_t, [_U32]),
             "pk_attend_prompt": (ctypes.c_int, [_U32, _VP, _VP, _VP, _VP, _VP, _U64, _U64, _VP, _VP, _U32, _U32, _U32,
                                                 _U32, ctypes.c_float, _VP, ctypes.c_size_t, _VP, _VP]),
             "pk_attend_cache_scratch_bytes": (ctypes.c_size_t, [_VP, _U32, _U32, _U32, _U64, ctypes.c_int]),
+            "pk_attend_cache_window_scratch_bytes": (ctypes.c_size_t, [_VP, _U32, _U32, _U32, _U64, ctypes.c_int, _U32, _U32]),
+            "pk_attend_cache_window": (ctypes.c_int, [_VP, _U32, _VP, _VP, _VP, _U32, _U32, _U32, ctypes.c_float, _U32, _U32,
+                                                      _VP, _VP, _U64, _VP, _VP, ctypes.c_size_t, _VP, _VP]),
             "pk_attend_cache": (ctypes.c_int, [_VP, _U32, _VP, _VP, _VP, _U32, _U32, _U32, ctypes.c_float, _VP, _VP,
                                                _U64, _VP, _VP, ctypes.c_size_t, _VP, _VP]),
             "pk_evict_pages": (ctypes.c_int, [_VP, _VP, _VP, _U32, _U64, _U32, _U32, _U32, _U32, _VP, _VP, _VP, _VP,
@@ -616,6 +627,43 @@ def pk_kv_read(kv: pk_kv_cache, k: torch.Tensor, v: torch.Tensor, tok_off: torch
     _kv_move("pk_kv_read", lib().pk_kv_read, kv, k, v, tok_off, start, pages, status, stream)
 
 
+def pk_rotary_turns(rotary_dim: int, base: float, factor: float, context: float, low: float, high: float) -> np.ndarray:
+    """uint64 [rotary_dim / 2], on the host."""
+    if not 0 < rotary_dim <= 128:
+        _refuse("pk_rotary_turns", "rotary_dim is a multiple of 16, up to 128")
+    out = np.zeros(rotary_dim // 2, np.uint64)
+    _check(lib().pk_rotary_turns(rotary_dim, base, factor, context, low, high, out.ctypes.data), "pk_rotary_turns")
+    return out
+
+
+def pk_rotate(q: torch.Tensor, k: torch.Tensor, q_out: torch.Tensor, k_out: torch.Tensor, rotary: pk_rotary,
+              q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor], eps: float, tok_off: torch.Tensor,
+              start: torch.Tensor, status: Optional[torch.Tensor], stream=None) -> None:
+    """q, q_out: [tokens, q_heads, D]; k, k_out: [tokens, kv_heads, D]; weights: [D] or None; tok_off: int64[R+1]; start:
+    int32[R]."""
+    fn = "pk_rotate"
+    dev = _here(fn)
+    qs, ks = q.shape, k.shape
+    if len(qs) != 3 or len(ks) != 3 or qs[0] != ks[0] or qs[2] != ks[2] or q_out.shape != qs or k_out.shape != ks:
+        _refuse(fn, "q, q_out are [tokens, q_heads, D], k, k_out [tokens, kv_heads, D]")
+    R, w = start.numel(), []
+    for t in (q_weight, k_weight):
+        if t is None:
+            w.append(None)
+            continue
+        if t.dtype is not q.dtype or t.requires_grad and torch.is_grad_enabled():
+            _refuse(fn, "weights have the rows' type, and no gradient is computed: detach, or call under torch.no_grad()")
+        w.append(_ints(t, q.dtype, qs[2], dev, fn, "a weight is contiguous, [D]"))
+    rc = lib().pk_rotate(_dtype(fn, q, k, q_out, k_out), ctypes.byref(_heads(q, dev, fn)), ctypes.byref(_heads(k, dev, fn)),
+                         ctypes.byref(_heads(q_out, dev, fn)), ctypes.byref(_heads(k_out, dev, fn)), qs[0], qs[1], ks[1],
+                         qs[2], ctypes.byref(rotary), w[0], w[1], eps,
+                         _ints(tok_off, torch.int64, R + 1, dev, fn, "tok_off is contiguous int64[R+1]"),
+                         _ints(start, torch.int32, R, dev, fn, "start is contiguous int32[R]"), R,
+                         _buffer(status, dev, fn), _stream_of(stream, q))
+    if rc:
+        _check(rc, fn)
+
+
 def pk_attend_prompt_scratch_bytes(R: int) -> int:
     return int(lib().pk_attend_prompt_scratch_bytes(R))
 
@@ -650,12 +698,40 @@ def pk_attend_cache_scratch_bytes(kv: pk_kv_cache, R: int, n_q: int, q_heads: in
     return int(lib().pk_attend_cache_scratch_bytes(ctypes.byref(kv), R, n_q, q_heads, page_stride, int(weigh)))
 
 
+def pk_attend_cache_window_scratch_bytes(kv: pk_kv_cache, R: int, n_q: int, q_heads: int, page_stride: int, weigh: bool,
+                                         window: int, sinks: int) -> int:
+    return int(lib().pk_attend_cache_window_scratch_bytes(ctypes.byref(kv), R, n_q, q_heads, page_stride, int(weigh),
+                                                          *_window("pk_attend_cache_window", window, sinks)))
+
+
+def _window(where: str, window: int, sinks: int):
+    """Both as 32-bit counts: what wraps would be another window."""
+    if not (0 <= window < 1 << 31 and 0 <= sinks < 1 << 31):
+        _refuse(where, "window and sinks are counts below 2^31")
+    return int(window), int(sinks)
+
+
 def pk_attend_cache(kv: pk_kv_cache, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor], n_q: int,
                     kv_len: torch.Tensor, pages: torch.Tensor, scale: float, page_weight: Optional[torch.Tensor],
                     scratch: torch.Tensor, status: torch.Tensor, stream=None) -> None:
     """q, out: [R * n_q, q_heads, D] or [R, n_q, q_heads, D]; lse: float32, R * n_q * q_heads; kv_len: int32[R]; pages:
     int32 and page_weight: float32 [R, page_stride]."""
-    fn = "pk_attend_cache"
+    _attend_cache("pk_attend_cache", lib().pk_attend_cache, (), kv, q, out, lse, n_q, kv_len, pages, scale, page_weight,
+                  scratch, status, stream)
+
+
+def pk_attend_cache_window(kv: pk_kv_cache, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor], n_q: int,
+                           kv_len: torch.Tensor, pages: torch.Tensor, scale: float, window: int, sinks: int,
+                           page_weight: Optional[torch.Tensor], scratch: torch.Tensor, status: torch.Tensor,
+                           stream=None) -> None:
+    """pk_attend_cache's tensors; window 0: no limit."""
+    fn = "pk_attend_cache_window"
+    _attend_cache(fn, lib().pk_attend_cache_window, _window(fn, window, sinks), kv, q, out, lse, n_q, kv_len, pages, scale,
+                  page_weight, scratch, status, stream)
+
+
+def _attend_cache(fn: str, call, limits, kv, q, out, lse, n_q, kv_len, pages, scale, page_weight, scratch, status,
+                  stream) -> None:
     dev = _here(fn, kv)
     R = kv_len.numel()
     qs = q.shape
@@ -671,12 +747,12 @@ def pk_attend_cache(kv: pk_kv_cache, q: torch.Tensor, out: torch.Tensor, lse: Op
         if page_weight.shape != pages.shape:
             _refuse(fn, "page_weight is [R, page_stride]")
         w = _ints(page_weight, torch.float32, R * width, dev, fn, "page_weight is contiguous float32")
-    rc = lib().pk_attend_cache(ctypes.byref(kv), _dtype(fn, q, out), ctypes.byref(_heads(q, dev, fn)),
-                               ctypes.byref(_heads(out, dev, fn)), z, R, n_q, qs[-2], scale,
-                               _ints(kv_len, torch.int32, R, dev, fn, "kv_len is contiguous int32[R]"),
-                               _ints(pages, torch.int32, R * width, dev, fn, "pages is contiguous int32"), width, w,
-                               _buffer(scratch, dev, fn), scratch.numel(), _buffer(status, dev, fn),
-                                _stream_of(stream, q))
+    rc = call(ctypes.byref(kv), _dtype(fn, q, out), ctypes.byref(_heads(q, dev, fn)),
+              ctypes.byref(_heads(out, dev, fn)), z, R, n_q, qs[-2], scale, *limits,
+              _ints(kv_len, torch.int32, R, dev, fn, "kv_len is contiguous int32[R]"),
+              _ints(pages, torch.int32, R * width, dev, fn, "pages is contiguous int32"), width, w,
+              _buffer(scratch, dev, fn), scratch.numel(), _buffer(status, dev, fn),
+              _stream_of(stream, q))
     if rc:
         _check(rc, fn)
 

@@ -258,6 +258,13 @@ class KeyTable:
         return self.entries()
 
 
+def _limits(where: str, window: Optional[int], sinks: int):
+    """(window, sinks) as the library takes them: 0 is no window."""
+    if window is not None and window < 1:
+        raise pk.PKError(pk.PK_ERR_ARG, where + ": a window holds a query's own position at least")
+    return (0 if window is None else window), sinks
+
+
 class KVPages:
     """What the slots of a KeyTable point at: a pool of KV pages held in 4 bits
     (layout and format: pk.h), with its calls.  Page tables are int32
@@ -311,23 +318,34 @@ class KVPages:
         pk.pk_kv_read(self.kv, k, v, tok_off, start, pages, self.status, self.stream)
         return k, v
 
-    def attend(self, q, kv_len, pages, scale: Optional[float] = None, weight: Optional[torch.Tensor] = None):
+    def attend(self, q, kv_len, pages, scale: Optional[float] = None, weight: Optional[torch.Tensor] = None,
+               window: Optional[int] = None, sinks: int = 0):
         """q [R, n_q, q_heads, head_dim] over the pages: (out like q, lse float32 [R, n_q, q_heads]).  weight
-        (float32, like pages) gets each page's attention weight added."""
+        (float32, like pages) gets each page's attention weight added.  With ``window`` a query at position p sees the
+        positions above p - window, and the first ``sinks`` ones; pages out of sight are not read."""
         if q.dim() != 4:
             raise pk.PKError(pk.PK_ERR_ARG, "KVPages.attend: q is [R, n_q, q_heads, head_dim]")
         R, n_q, heads, D = q.shape
-        key = (R, n_q, heads, pages.shape[-1], weight is not None)
+        limits = _limits("KVPages.attend", window, sinks)
+        key = (R, n_q, heads, pages.shape[-1], weight is not None, *limits)
         nbytes = self._scratch_bytes.get(key)
         if nbytes is None:
             if len(self._scratch_bytes) >= 4096:
                 self._scratch_bytes.clear()
-            nbytes = self._scratch_bytes[key] = pk.pk_attend_cache_scratch_bytes(self.kv, *key)
+            nbytes = self._scratch_bytes[key] = pk.pk_attend_cache_window_scratch_bytes(self.kv, *key)
         out, lse, scratch = _empty(q, self.stream, (q.shape, q.dtype), (q.shape[:3], torch.float32),
                                    ((nbytes,), torch.uint8))
-        pk.pk_attend_cache(self.kv, q, out, lse, n_q, kv_len, pages, D ** -0.5 if scale is None else scale, weight,
-                           scratch, self.status, self.stream)
+        scale = D ** -0.5 if scale is None else scale
+        if limits[0]:
+            pk.pk_attend_cache_window(self.kv, q, out, lse, n_q, kv_len, pages, scale, *limits, weight, scratch, self.status,
+                                      self.stream)
+        else:
+            pk.pk_attend_cache(self.kv, q, out, lse, n_q, kv_len, pages, scale, weight, scratch, self.status, self.stream)
         return out, lse
+
+    def rotate(self, q, k, tok_off, start, rotary, q_weight=None, k_weight=None, eps: float = 1e-6, out=None):
+        """rotate on the pool's stream, its device errors in the pool's status word: what write() and attend() take."""
+        return rotate(q, k, tok_off, start, rotary, q_weight, k_weight, eps, out, self.status, self.stream)
 
     def attend_prompt(self, q, k, v, q_off, k_off, scale: Optional[float] = None):
         """attend_prompt on the pool's stream, its device errors in the pool's status word."""
@@ -336,6 +354,45 @@ class KVPages:
     def evict(self, pages, weight, kv_len, budget: int, sinks: int, recent: int):
         """evict_pages for pages of this pool, on its stream, its device errors in the pool's status word."""
         return evict_pages(pages, weight, kv_len, self.page_tokens, budget, sinks, recent, self.status, self.stream)
+
+
+class Rotary:
+    """How positions rotate a head's first ``rotary_dim`` dimensions (pk_rotary): pair i, of dimensions (i, i +
+    rotary_dim/2) or, ``interleaved``, (2i, 2i + 1), by ``base ** (-2 i / rotary_dim)`` radians a position.  For longer
+    contexts than a model was made for these are divided by ``factor``: all of them, or with ``context``, its own context,
+    by parts (pk_rotary_turns); ``amplitude`` multiplies what was rotated.  ``turns`` (uint64 [rotary_dim / 2], fractions of
+    a turn by 2^64) takes the place of base and factor.
+
+    The table is copied to ``device`` once, and that copy is over when the object exists."""
+
+    def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, base: float = 10000.0, interleaved: bool = False,
+                 factor: float = 1.0, context: Optional[float] = None, low: float = 1.0, high: float = 32.0,
+                 amplitude: float = 1.0, turns=None, device="cuda"):
+        self.head_dim, self.rotary_dim = int(head_dim), int(head_dim if rotary_dim is None else rotary_dim)
+        if self.rotary_dim < 16 or self.rotary_dim % 16 or self.rotary_dim > self.head_dim or not np.isfinite(amplitude):
+            raise pk.PKError(pk.PK_ERR_ARG, "Rotary: rotary_dim is a multiple of 16, up to head_dim; amplitude is finite")
+        if turns is None:
+            turns = pk.pk_rotary_turns(self.rotary_dim, base, factor, context or 0.0, low, high)
+        turns = np.ascontiguousarray(turns)
+        if turns.dtype != np.uint64 or turns.shape != (self.rotary_dim // 2,):
+            raise pk.PKError(pk.PK_ERR_ARG, "Rotary: turns is uint64 [rotary_dim / 2]")
+        self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
+        self.table = pk.pk_rotary(self.turns.data_ptr(), self.rotary_dim, int(bool(interleaved)), amplitude)
+
+
+def rotate(q, k, tok_off, start, rotary: Rotary, q_weight: Optional[torch.Tensor] = None,
+           k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, out=None, status: Optional[torch.Tensor] = None,
+           stream=None):
+    """Norms of queries and keys by head (where weights are given) and their rotation, in one pass (pk_rotate): (q, k),
+    new tensors or ``out``, a pair that may be (q, k) themselves.  q [tokens, q_heads, D], k [tokens, kv_heads, D]; token i
+    of request r, row tok_off[r] + i, has position start[r] + i, where KVPages.write puts it.  Rows that belong to no
+    request are unspecified in new tensors, and stay as they are in ``out``.  ``status`` as in attend_prompt
+    (KVPages.rotate passes the pool's)."""
+    if q.shape[-1] != rotary.head_dim or rotary.turns.device != q.device:
+        raise pk.PKError(pk.PK_ERR_ARG, "rotate: rotary is for other heads, or on another device")
+    q_out, k_out = out if out is not None else _empty(q, stream, (q.shape, q.dtype), (k.shape, k.dtype))
+    pk.pk_rotate(q, k, q_out, k_out, rotary.table, q_weight, k_weight, eps, tok_off, start, status, stream)
+    return q_out, k_out
 
 
 def attend_prompt(q, k, v, q_off, k_off, scale: Optional[float] = None, status: Optional[torch.Tensor] = None,
