@@ -602,6 +602,34 @@ int pk_attend_cache_window(const pk_kv_cache *kv, uint32_t dtype, const pk_heads
                            float *page_weight_dev, void *scratch_dev, size_t scratch_bytes, int32_t *status_dev,
                            pk_stream stream);
 
+/* Device.  Attention of a chunk of new tokens a request over its pages, whose
+ * own tokens are written first; chunks are packed one after another.
+ *   q         [n_q][q_heads][head_dim] of dtype; out OUT likewise
+ *   q_off_dev int64[R+1], non-decreasing, within n_q: request r's queries.
+ *             With L of them, query i sits at position kv_len[r] - L + i and
+ *             attends the positions up to its own; with a window (0: none) those
+ *             above its own - window, and the first `sinks` ones
+ *   lse_dev   OUT float32[n_q][q_heads], or NULL
+ *   kv_len_dev, pages_dev  as pk_attend_cache
+ * A query before position 0 gives 0 and -infinity.  Bytes of positions at or
+ * past kv_len are never used, pages that no query of a request sees are not
+ * read, and their slots may be anything.  Rows of q that belong to no request
+ * are not written.  q_heads a multiple of kv_heads, at most 65536; n_q and
+ * page_stride * page_tokens at most 0x7fff0000, n_q * q_heads below 2^34; window
+ * and sinks below 2^31; |scale * k_scale| at most 2.3e38; strides of q below
+ * 2^39.  scratch_dev: pk_attend_chunk_scratch_bytes(...) bytes for the same
+ * arguments, 32-byte aligned.
+ * Device errors: offsets out of order or range (PK_ERR_ARG; nothing is
+ * written); a kv_len out of range (PK_ERR_ARG) counts as 0; a slot out of
+ * range (PK_ERR_ARG) makes out and lse NaN for the queries that see its page,
+ * and for others of its request unspecified numbers or NaN.  PK_ERR_TIMEOUT. */
+size_t pk_attend_chunk_scratch_bytes(const pk_kv_cache *kv, uint64_t n_q, uint32_t R, uint32_t q_heads,
+                                     uint64_t page_stride, uint32_t window, uint32_t sinks);
+int pk_attend_chunk(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, const pk_heads *out, float *lse_dev,
+                    uint64_t n_q, const int64_t *q_off_dev, uint32_t R, uint32_t q_heads, float scale, uint32_t window,
+                    uint32_t sinks, const int32_t *kv_len_dev, const uint32_t *pages_dev, uint64_t page_stride,
+                    void *scratch_dev, size_t scratch_bytes, int32_t *status_dev, pk_stream stream);
+
 /* How positions turn the pairs of a head's first rotary_dim values.  Pair i is
  * dimensions (i, i + rotary_dim/2), or (2i, 2i + 1) where interleaved; a
  * position turns it by turns[i] / 2^64 of a whole turn, and amplitude multiplies

@@ -30,6 +30,7 @@
 
 #include <type_traits>
 
+#include "pk_attend.cuh"
 #include "pk_device.cuh"
 #include "pk_internal.h"
 #include "pk_kv.cuh"
@@ -119,12 +120,6 @@ k_prompt_tiles(const int64_t *q_off, const int64_t *k_off, uint32_t R, uint64_t 
         for (uint64_t r = tid; r <= R; r += kPlanThreads) tile_off[r] = 0;
         if (tid == 0) pk::set_status(status, PK_ERR_ARG);
     }
-}
-
-__device__ __forceinline__ float ex2(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
 }
 
 // Shared memory of a CTA, from a 1024-byte boundary: Q (two tiles), the ring of K and V tiles, then Small.
@@ -268,27 +263,6 @@ __device__ __forceinline__ bool next_taken(Small &sm, uint32_t n, bool reader, u
 // 384 * 168, the launch's own.
 constexpr int kRegsSoftmax = 200, kRegsOther = 104;
 constexpr uint32_t kWarpLoad = 8, kWarpMma = 9, kWarpClean = 10;  // warps 0-7: softmax
-
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ float2 unpack2(uint64_t x) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 
 // One CTA an SM takes one item after another.  Warp roles: one loads Q, K and V by TMA,
 // one issues the matrix products, two look after V at the causal edge, and
@@ -658,7 +632,7 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
         const uint32_t ts = tmem + 128 * t + ((warp & 3) * 32 << 16), to = tmem + 256 + D * t + ((warp & 3) * 32 << 16);
         // a scale of 0 would make a masked -infinity NaN; the smallest normal one gives the same weights
         const float scale2 = fmaxf(fabsf(a.scale2), FLT_MIN);
-        const uint64_t scale22 = pack2(scale2, scale2);
+        const uint64_t scale22 = pk::pack2(scale2, scale2);
         uint32_t ni = 0, items = 0;  // key tiles weighed so far
         bool ok = true;
         while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
@@ -720,21 +694,22 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                 // The weights by the reference so far, and their sum.
                 uint32_t p[2][32];
                 auto weigh = [&](auto masked) {
-                    const uint64_t ref2 = pack2(-ref, -ref);
+                    const uint64_t ref2 = pk::pack2(-ref, -ref);
                     uint64_t sum2[2] = {0, 0};
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         uint32_t(&y)[32] = chunk(c, masked);
 #pragma unroll
                         for (int i = 0; i < 32; i += 2) {
-                            float2 z = unpack2(fma2(pack2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), scale22, ref2));
-                            z.x = ex2(z.x);
-                            z.y = ex2(z.y);
-                            sum2[i / 2 & 1] = add2(sum2[i / 2 & 1], pack2(z.x, z.y));
+                            float2 z = pk::unpack2(
+                                pk::fma2(pk::pack2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), scale22, ref2));
+                            z.x = pk::ex2(z.x);
+                            z.y = pk::ex2(z.y);
+                            sum2[i / 2 & 1] = pk::add2(sum2[i / 2 & 1], pk::pack2(z.x, z.y));
                             p[c / 2][c % 2 * 16 + i / 2] = pk::Elem<DT>::from2(z.x, z.y);
                         }
                     }
-                    const float2 s0 = unpack2(sum2[0]), s1 = unpack2(sum2[1]);
+                    const float2 s0 = pk::unpack2(sum2[0]), s1 = pk::unpack2(sum2[1]);
                     return (s0.x + s1.x) + (s0.y + s1.y);
                 };
                 // The same where a row of the warp has a far reference, which few calls have: by 16 scores, with `fine`.
@@ -751,7 +726,7 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 const bool masked = edge && 16 * c + i + h > see;
-                                w[h] = masked ? 0.0f : ex2(fmaf(__uint_as_float(y[i + h]), scale2, -ref) + fine);
+                                w[h] = masked ? 0.0f : pk::ex2(fmaf(__uint_as_float(y[i + h]), scale2, -ref) + fine);
                                 s += w[h];
                             }
                             p[c / 4][c % 4 * 8 + i / 2] = pk::Elem<DT>::from2(w[0], w[1]);
@@ -773,7 +748,7 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
                     // far: what m's rounding lost comes off again, so the largest weight is 2^kBase or, where kBase
                     // is lost beside that, 1; not a number where m overflowed
                     const float next_fine = !moves ? fine : far ? kBase - fmaf(top, scale2, -m) : 0.0f;
-                    const float f = ex2((ref - next) + (next_fine - fine));
+                    const float f = pk::ex2((ref - next) + (next_fine - fine));
                     ref = next;
                     fine = next_fine;
                     sum *= f;
@@ -862,36 +837,6 @@ k_attend_prompt(const Args a, const __grid_constant__ CUtensorMap map_q, const _
         pk::tmem_fence_after();
         pk::tmem_free(tmem, 512);
     }
-}
-
-using EncodeTiled = decltype(&cuTensorMapEncodeTiled);
-
-EncodeTiled encoder() {
-    static const EncodeTiled fn = []() -> EncodeTiled {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess)
-            return nullptr;
-        return reinterpret_cast<EncodeTiled>(p);
-    }();
-    return fn;
-}
-
-// [tokens][heads][D] as a 3-D map whose box is box_tokens tokens of box_heads heads and 64 dimensions, in the 128-byte
-// swizzle; what lies past the end reads as 0.
-cudaError_t map_of(CUtensorMap *map, const pk_heads &h, uint64_t n, uint32_t heads, uint32_t D, uint32_t dtype,
-                   uint32_t box_tokens, uint32_t box_heads) {
-    const EncodeTiled enc = encoder();
-    if (!enc) return cudaErrorNotSupported;
-    const cuuint64_t dims[3] = {D, heads, n};
-    // a dimension of one entry has no stride
-    const cuuint64_t strides[2] = {heads > 1 ? (cuuint64_t)h.head_stride * 2 : D * 2u, n > 1 ? (cuuint64_t)h.tok_stride * 2 : D * 2u};
-    const cuuint32_t box[3] = {64, box_heads, box_tokens}, unit[3] = {1, 1, 1};
-    const CUresult e = enc(map, dtype == PK_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
-                           h.p, dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return e == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
 template <int D, uint32_t DT, bool kFixed>

@@ -1,6 +1,6 @@
 // pk_kv_host.cpp -- host half of the KV-page calls: argument checks ahead of
 // the launches of pk_kv.cu, pk_rotate.cu, pk_attend_prompt.cu,
-// pk_attend_cache.cu and pk_evict_pages.cu; the table of a rotation.
+// pk_attend_chunk.cu, pk_attend_cache.cu and pk_evict_pages.cu; the table of a rotation.
 #include <cuda_runtime_api.h>
 
 #include <cfloat>
@@ -169,6 +169,43 @@ int pk_attend_cache(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, co
                     size_t scratch_bytes, int32_t *status_dev, pk_stream stream) {
     return pk_attend_cache_window(kv, dtype, q, out, lse_dev, R, n_q, q_heads, scale, 0, 0, kv_len_dev, pages_dev,
                                   page_stride, page_weight_dev, scratch_dev, scratch_bytes, status_dev, stream);
+}
+
+// The shapes that both the scratch size and the launch depend on.
+static bool good_chunk(const pk_kv_cache *kv, uint32_t R, uint64_t n_q, uint32_t q_heads, uint64_t page_stride,
+                       uint32_t window, uint32_t sinks) {
+    return kv && pk_kv_page_bytes(kv->page_tokens, kv->kv_heads, kv->head_dim) != 0 && n_q <= 0x7fff0000ull &&
+           R < 1u << 31 && q_heads >= 1 && q_heads <= 65536 && q_heads % kv->kv_heads == 0 && n_q * q_heads < 1ull << 34 &&
+           page_stride < 1ull << 31 && page_stride * kv->page_tokens <= 0x7fff0000ull && good_window(window, sinks);
+}
+
+size_t pk_attend_chunk_scratch_bytes(const pk_kv_cache *kv, uint64_t n_q, uint32_t R, uint32_t q_heads,
+                                     uint64_t page_stride, uint32_t window, uint32_t sinks) {
+    if (!good_chunk(kv, R, n_q, q_heads, page_stride, window, sinks)) return 0;
+    const uint64_t need = pk_attend_chunk_scratch_bytes_impl(*kv, R, n_q, q_heads, page_stride,
+                                                             window_within(*kv, page_stride, window), sinks);
+    return need == UINT64_MAX ? 0 : (size_t)need;
+}
+
+int pk_attend_chunk(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, const pk_heads *out, float *lse_dev,
+                    uint64_t n_q, const int64_t *q_off_dev, uint32_t R, uint32_t q_heads, float scale, uint32_t window,
+                    uint32_t sinks, const int32_t *kv_len_dev, const uint32_t *pages_dev, uint64_t page_stride,
+                    void *scratch_dev, size_t scratch_bytes, int32_t *status_dev, pk_stream stream) {
+    if (!good_cache(kv) || dtype > PK_FP16 || !good_score_scale((double)scale * kv->k_scale)) return PK_ERR_ARG;
+    if (!good_chunk(kv, R, n_q, q_heads, page_stride, window, sinks)) return PK_ERR_ARG;
+    if (!good_heads(q, n_q, q_heads) || !good_out(out, n_q, q_heads, kv->head_dim)) return PK_ERR_ARG;
+    if (q->tok_stride >= (int64_t)1 << 39 || q->head_stride >= (int64_t)1 << 39) return PK_ERR_ARG;  // a tensor map's
+    if (!aligned(lse_dev, 4) || !aligned(q_off_dev, 8) || !aligned(kv_len_dev, 4) || !aligned(pages_dev, 4) ||
+        !aligned(scratch_dev, 32) || !aligned(status_dev, 4))
+        return PK_ERR_ARG;
+    if (R == 0 || n_q == 0) return PK_OK;
+    if (!q_off_dev || !kv_len_dev || (page_stride && !pages_dev) || !scratch_dev) return PK_ERR_ARG;
+    window = window_within(*kv, page_stride, window);
+    const uint64_t need = pk_attend_chunk_scratch_bytes_impl(*kv, R, n_q, q_heads, page_stride, window, sinks);
+    if (need == UINT64_MAX || scratch_bytes < need) return PK_ERR_ARG;
+    return cuda_rc(pk_launch_attend_chunk(*kv, dtype, *q, *out, lse_dev, n_q, q_off_dev, R, q_heads, scale, window, sinks,
+                                          kv_len_dev, pages_dev, page_stride, scratch_dev, status_dev,
+                                          reinterpret_cast<cudaStream_t>(stream)));
 }
 
 int pk_rotary_turns(uint32_t rotary_dim, double base, double factor, double context, double low, double high,

@@ -147,6 +147,9 @@ def lib() -> ctypes.CDLL:
             "pk_attend_cache_window_scratch_bytes": (ctypes.c_size_t, [_VP, _U32, _U32, _U32, _U64, ctypes.c_int, _U32, _U32]),
             "pk_attend_cache_window": (ctypes.c_int, [_VP, _U32, _VP, _VP, _VP, _U32, _U32, _U32, ctypes.c_float, _U32, _U32,
                                                       _VP, _VP, _U64, _VP, _VP, ctypes.c_size_t, _VP, _VP]),
+            "pk_attend_chunk_scratch_bytes": (ctypes.c_size_t, [_VP, _U64, _U32, _U32, _U64, _U32, _U32]),
+            "pk_attend_chunk": (ctypes.c_int, [_VP, _U32, _VP, _VP, _VP, _U64, _VP, _U32, _U32, ctypes.c_float, _U32, _U32,
+                                               _VP, _VP, _U64, _VP, ctypes.c_size_t, _VP, _VP]),
             "pk_attend_cache": (ctypes.c_int, [_VP, _U32, _VP, _VP, _VP, _U32, _U32, _U32, ctypes.c_float, _VP, _VP,
                                                _U64, _VP, _VP, ctypes.c_size_t, _VP, _VP]),
             "pk_evict_pages": (ctypes.c_int, [_VP, _VP, _VP, _U32, _U64, _U32, _U32, _U32, _U32, _VP, _VP, _VP, _VP,
@@ -753,6 +756,40 @@ def _attend_cache(fn: str, call, limits, kv, q, out, lse, n_q, kv_len, pages, sc
               _ints(pages, torch.int32, R * width, dev, fn, "pages is contiguous int32"), width, w,
               _buffer(scratch, dev, fn), scratch.numel(), _buffer(status, dev, fn),
               _stream_of(stream, q))
+    if rc:
+        _check(rc, fn)
+
+
+def pk_attend_chunk_scratch_bytes(kv: pk_kv_cache, n_q: int, R: int, q_heads: int, page_stride: int, window: int,
+                                  sinks: int) -> int:
+    return int(lib().pk_attend_chunk_scratch_bytes(ctypes.byref(kv), n_q, R, q_heads, page_stride,
+                                                   *_window("pk_attend_chunk", window, sinks)))
+
+
+def pk_attend_chunk(kv: pk_kv_cache, q: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor],
+                    q_off: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor, scale: float, window: int, sinks: int,
+                    scratch: torch.Tensor, status: Optional[torch.Tensor], stream=None) -> None:
+    """q, out: [n_q, q_heads, D]; lse: float32 [n_q, q_heads]; q_off: int64[R+1]; kv_len: int32[R]; pages: int32
+    [R, page_stride]; window 0: no limit."""
+    fn = "pk_attend_chunk"
+    dev = _here(fn, kv)
+    R = kv_len.numel()
+    qs = q.shape
+    if len(qs) != 3 or out.shape != qs or qs[2] != kv.head_dim:
+        _refuse(fn, "q, out are [n_q, q_heads, head_dim]")
+    if pages.dim() != 2 or pages.shape[0] != R:
+        _refuse(fn, "pages is [R, page_stride]")
+    width = pages.shape[1]
+    z = lse
+    if lse is not None:
+        z = _ints(lse, torch.float32, qs[0] * qs[1], dev, fn, "lse is contiguous float32 [n_q, q_heads]")
+    rc = lib().pk_attend_chunk(ctypes.byref(kv), _dtype(fn, q, out), ctypes.byref(_heads(q, dev, fn)),
+                               ctypes.byref(_heads(out, dev, fn)), z, qs[0],
+                               _ints(q_off, torch.int64, R + 1, dev, fn, "q_off is contiguous int64[R+1]"), R, qs[1], scale,
+                               *_window(fn, window, sinks),
+                               _ints(kv_len, torch.int32, R, dev, fn, "kv_len is contiguous int32[R]"),
+                               _ints(pages, torch.int32, R * width, dev, fn, "pages is contiguous int32"), width,
+                               _buffer(scratch, dev, fn), scratch.numel(), _buffer(status, dev, fn), _stream_of(stream, q))
     if rc:
         _check(rc, fn)
 

@@ -343,6 +343,22 @@ class KVPages:
             pk.pk_attend_cache(self.kv, q, out, lse, n_q, kv_len, pages, scale, weight, scratch, self.status, self.stream)
         return out, lse
 
+    def attend_chunk(self, q, q_off, kv_len, pages, scale: Optional[float] = None, window: Optional[int] = None,
+                     sinks: int = 0):
+        """Chunks of new tokens, written before, over the pages: q [n_q, q_heads, head_dim], request r's rows q_off[r] ..
+        q_off[r + 1] at its last positions: (out like q, lse float32 [n_q, q_heads]).  ``window`` and ``sinks`` as in
+        attend."""
+        if q.dim() != 3:
+            raise pk.PKError(pk.PK_ERR_ARG, "KVPages.attend_chunk: q is [n_q, q_heads, head_dim]")
+        n_q, heads, D = q.shape
+        limits = _limits("KVPages.attend_chunk", window, sinks)
+        nbytes = pk.pk_attend_chunk_scratch_bytes(self.kv, n_q, pages.shape[0], heads, pages.shape[-1], *limits)
+        out, lse, scratch = _empty(q, self.stream, (q.shape, q.dtype), (q.shape[:2], torch.float32),
+                                   ((nbytes,), torch.uint8))
+        pk.pk_attend_chunk(self.kv, q, out, lse, q_off, kv_len, pages, D ** -0.5 if scale is None else scale, *limits, scratch,
+                           self.status, self.stream)
+        return out, lse
+
     def rotate(self, q, k, tok_off, start, rotary, q_weight=None, k_weight=None, eps: float = 1e-6, out=None):
         """rotate on the pool's stream, its device errors in the pool's status word: what write() and attend() take."""
         return rotate(q, k, tok_off, start, rotary, q_weight, k_weight, eps, out, self.status, self.stream)
