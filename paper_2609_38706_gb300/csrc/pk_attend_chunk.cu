@@ -154,9 +154,9 @@ __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const Args a) {
 template <int D>
 struct Layout {
     static constexpr uint32_t kTile = 128 * D * 2;  // 128 rows; blocks of [128][64] values, 16 KB each
-    static constexpr uint32_t kStages = D == 128 ? 4 : 8;
+    static constexpr uint32_t kStages = D == 128 ? 3 : 8;
     static constexpr uint32_t kGran = pk::Granule<D>::kBytes;
-    static constexpr uint32_t kGrans = D == 128 ? 14 : 28;
+    static constexpr uint32_t kGrans = D == 128 ? 28 : 32;
     static constexpr uint32_t kRing = 2 * kTile;
     static constexpr uint32_t kGranRing = kRing + kStages * kTile;
     static constexpr uint32_t kBytes = kGranRing + kGrans * kGran;
@@ -164,21 +164,31 @@ struct Layout {
 
 constexpr uint32_t kNotes = 8;       // key tiles whose notes are kept: they are read before the ring has gone round
 constexpr uint32_t kMarked = 1, kLost = 2;
+constexpr uint32_t kMakers = 6;      // warps that make tiles of granules
+
+// A softmax warp's tile of the present item.
+struct TileOf {
+    int32_t causal, hides[2];  // from the first on some query does not see some key; between the others too
+    int32_t off, base;         // position of the request's first query; what a position is more than its place in the piece
+    int32_t sinks, tok0, row0, head0, n_all;
+    int64_t part;              // where the piece's rows go; -1: the item is not cut
+};
 
 struct Small {
     uint64_t full[8], empty[8];             // ring stages: tile ready; no longer read
-    uint64_t gran_full[28], gran_empty[28]; // the same of granules
+    uint64_t gran_full[32], gran_empty[32]; // the same of granules
     uint64_t q_full[2], q_empty[2];
     uint64_t s_full[2], p_ready[2], o_done[2];
     uint64_t over;                          // every product that was issued is done (a matrix warp that gave up)
     uint32_t tmem, abort;
     int32_t work[8][2];                     // by item with keys: key tiles of its two tiles, for the matrix warp; 0, 0 ends it
-    uint8_t gran_lost[28];                  // what stands in a granule's place is another request's
+    uint8_t gran_lost[32];                  // what stands in a granule's place is another request's
     uint32_t split;
-    alignas(4) uint8_t flags[kNotes][4];    // by key tile and unpacking warp: kMarked, kLost
+    alignas(2) uint8_t flags[kNotes][2];    // by key tile and half of its keys: kMarked, kLost
     uint8_t marked[kNotes][128];            // by key, where kMarked: blocks of V that are NaN (0 stands in the tile)
     uint32_t item_end[32];                  // up to 32 requests: items of one KV head in those up to each, and what they are
     int32_t q_start[32], q_len[32], len[32];
+    TileOf tile[8];
 };
 
 // Up to 32 requests every CTA makes the plan itself, a lane a request, and keeps it in shared memory.
@@ -285,59 +295,87 @@ __device__ __forceinline__ bool find_item(const Args &a, const Small &sm, const 
     return it.lq > 0;
 }
 
-// Registers move to the softmax warps: 256 * 200 + 256 * 56 = 512 * 128, the launch's own.
-constexpr int kRegsSoftmax = 200, kRegsOther = 56;
-constexpr uint32_t kWarpLoad = 8, kWarpMma = 9, kWarpUnpack = 12;  // warps 0-7: softmax; 12-15: unpacking
-
-// K or V of a granule as 16-bit rows of a tile, from row `row0` on, in the 128-byte swizzle.  A lane takes 32
-// dimensions of a token.  Eight lanes that store at once have two rows' (D = 128) or four rows' pieces: the upper
-// half of the dimensions goes in another order, so that they lie in eight different 16-byte columns.
-template <int D, bool kBf16>
-__device__ __forceinline__ void unpack(const uint8_t *codes, const uint8_t *scales, uint8_t *tile, uint32_t row0) {
-    constexpr uint32_t kParts = D / 32, kStep = 32 / kParts;
-    const uint32_t lane = threadIdx.x & 31, part = lane % kParts;
-    const bool flip = part >= 2;
-#pragma unroll
-    for (uint32_t r = 0; r < 16; r += kStep) {
-        const uint32_t row = r + lane / kParts;
-        const uint4 u = *reinterpret_cast<const uint4 *>(codes + row * (D / 2) + part * 16);
-        const uint32_t z = pk::e4m3_to_half2(*reinterpret_cast<const uint16_t *>(scales + row * (D / 16) + part * 2));
-        const uint32_t w[4] = {flip ? u.z : u.x, flip ? u.w : u.y, flip ? u.x : u.z, flip ? u.y : u.w};
-        uint32_t by[2];
-        if (kBf16) {
-            // a half's bits, three to the right, are 2^-112 times the value as a bfloat16; the scale makes up for it
-            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&z));
-            const uint32_t lo = pk::Elem<PK_BF16>::from2(f.x * 0x1p112f, f.x * 0x1p112f);
-            const uint32_t hi = pk::Elem<PK_BF16>::from2(f.y * 0x1p112f, f.y * 0x1p112f);
-            by[0] = flip ? hi : lo, by[1] = flip ? lo : hi;
-        } else {
-            const uint32_t lo = __byte_perm(z, z, 0x1010), hi = __byte_perm(z, z, 0x3232);
-            by[0] = flip ? hi : lo, by[1] = flip ? lo : hi;
-        }
-        const uint32_t key = row0 + row;
-        uint8_t *dst = tile + part / 2 * 16384 + key * 128;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t h[4];
-            pk::e2m1x8_to_half2(w[i], h);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (kBf16) {
-                    const uint32_t b = (h[k] >> 3 & 0x0fff0fffu) | (h[k] & 0x80008000u);
-                    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(h[k]) : "r"(b), "r"(by[i / 2]));
-                } else {
-                    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(h[k]) : "r"(h[k]), "r"(by[i / 2]));
-                }
-            }
-            const uint32_t chunk = part % 2 * 4 + (flip ? i ^ 2 : i);
-            *reinterpret_cast<uint4 *>(dst + ((chunk ^ (key & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-        }
-    }
+// Lowest position that the query `tok` of a request sees behind the first tokens; off: position of the request's first.
+__device__ __forceinline__ int32_t low_of(const Args &a, int32_t off, int32_t tok) {
+    return a.window ? (int32_t)max((int64_t)off + tok - a.window + 1, (int64_t)0) : 0;
 }
 
+// Registers move to the softmax warps: 256 * 176 + 256 * 80 = 512 * 128, the launch's own.
+constexpr int kRegsSoftmax = 176, kRegsOther = 80;
+constexpr uint32_t kWarpLoad = 8, kWarpMma = 9, kWarpNote = 10, kWarpUnpack = 12;  // warps 0-7: softmax
+
+// Where a lane finds its codes and scales of K or V in a granule, and where it puts them as 16-bit values in a tile, in
+// the 128-byte swizzle: 32 dimensions of a token, and the same of the token 8 further on for D = 128.  Eight lanes that
+// store at once have two rows' (D = 128) or four rows' pieces: the upper half of the dimensions goes in another order,
+// so that they lie in eight different 16-byte columns.
+template <int D>
+struct Unpack {
+    static constexpr uint32_t kParts = D / 32, kRows = 32 / kParts;
+    uint32_t row, codes[2], scales, pick[2], dst[4];
+
+    __device__ __forceinline__ explicit Unpack(uint32_t lane) {
+        const uint32_t part = lane % kParts, flip = part >= 2 ? 2 : 0;
+        row = lane / kParts;
+#pragma unroll
+        for (uint32_t i = 0; i < 2; ++i) {
+            codes[i] = row * (D / 2) + part * 16 + ((2 * i) ^ flip) * 4;
+            pick[i] = i ^ flip / 2 ? 0x3232 : 0x1010;
+        }
+        scales = row * (D / 16) + part * 2;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+            dst[i] = part / 2 * 16384 + row * 128 + (((part % 2 * 4 + (i ^ flip)) ^ (row & 7)) << 4);
+    }
+
+    // A granule's 16 rows; `tile`: where the first of them lies.  Weights of 0 must not meet a NaN: of V (kClean) rows from
+    // `valid` on, past the request's end, count as 0, and so do blocks marked NaN.
+    template <bool kBf16, bool kClean>
+    __device__ __forceinline__ void granule(const uint8_t *from, const uint8_t *from_scales, uint8_t *tile, int32_t valid) const {
+#pragma unroll
+        for (uint32_t r = 0; r < 16; r += kRows) {
+            uint32_t two = *reinterpret_cast<const uint16_t *>(from_scales + scales + r * (D / 16));
+            if (kClean) {
+                if (((two & 0x7f7f) + 0x0101) & 0x8080) two &= ~__vcmpeq4(two & 0x7f7f, 0x7f7f);
+                if ((int32_t)(row + r) >= valid) two = 0;
+            }
+            const uint32_t z = pk::e4m3_to_half2(two);
+            uint32_t by[2];
+            if (kBf16) {
+                // a half's bits, three to the right, are 2^-112 times the value as a bfloat16; the scale makes up for it
+                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&z));
+                by[0] = pk::Elem<PK_BF16>::from2(f.x * 0x1p112f, f.y * 0x1p112f);
+                by[1] = __byte_perm(by[0], by[0], pick[1]);
+                by[0] = __byte_perm(by[0], by[0], pick[0]);
+            } else {
+                by[0] = __byte_perm(z, z, pick[0]);
+                by[1] = __byte_perm(z, z, pick[1]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+                const uint2 u = *reinterpret_cast<const uint2 *>(from + codes[i / 2] + r * (D / 2));
+                const uint32_t w[2] = {u.x, u.y};
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    uint32_t h[4];
+                    pk::e2m1x8_to_half2(w[n], h);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (kBf16) {
+                            const uint32_t b = (h[k] >> 3 & 0x0fff0fffu) | (h[k] & 0x80008000u);
+                            asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(h[k]) : "r"(b), "r"(by[i / 2]));
+                        } else {
+                            asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(h[k]) : "r"(h[k]), "r"(by[i / 2]));
+                        }
+                    }
+                    *reinterpret_cast<uint4 *>(tile + dst[i + n] + r * 128) = make_uint4(h[0], h[1], h[2], h[3]);
+                }
+            }
+        }
+    }
+};
+
 // One CTA an SM takes one item after another.  Warp roles: one copies Q tiles and
-// granules, four unpack granules into K and V tiles, one issues the matrix
-// products, and two warpgroups of four turn scores into weights, a thread a row,
+// granules, six make K and V tiles of granules, one issues the matrix products, and two warpgroups of four turn scores into weights, a thread a row,
 // for one of the item's two tiles each: while one tile's scores are weighed the
 // other's products run.  TMEM: scores of the tiles (128 columns each; the weights, two
 // to a column, take the place of scores that have been read), then their outputs
@@ -358,12 +396,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
 
     if (tid == 0) {
         for (uint32_t i = 0; i < L::kStages; ++i) {
-            pk::mbar_init(pk::smem_addr(&sm.full[i]), 4);  // the unpacking warps
+            pk::mbar_init(pk::smem_addr(&sm.full[i]), kMakers);
             pk::mbar_init(pk::smem_addr(&sm.empty[i]), 1);
         }
         for (uint32_t i = 0; i < L::kGrans; ++i) {
             pk::mbar_init(pk::smem_addr(&sm.gran_full[i]), 1);
-            pk::mbar_init(pk::smem_addr(&sm.gran_empty[i]), 4);  // the unpacking warps
+            pk::mbar_init(pk::smem_addr(&sm.gran_empty[i]), kMakers);
         }
         for (int t = 0; t < 2; ++t) {
             pk::mbar_init(pk::smem_addr(&sm.q_full[t]), 1);
@@ -489,8 +527,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 for (int t = 0; t < 2; ++t)
                     if (nq[t]) pk::mbar_wait(pk::smem_addr(&sm.q_full[t]), (nq[t] - 1) & 1);
             __syncwarp();
-        } else if (warp >= kWarpUnpack) {
-            const uint32_t w = warp - kWarpUnpack;
+        } else if (warp >= kWarpNote) {
+            // Makers of K and V tiles: two warps look for what the softmax warps have to know of a tile, four unpack it.
+            const uint32_t w = warp - kWarpUnpack, half = warp - kWarpNote;
+            const bool notes = warp < kWarpUnpack;
+            const Unpack<D> lanes(lane);
             uint32_t n = 0, count = 0, tiles = 0, items = 0;  // stages, granules, key tiles, items with keys so far
             bool ok = true;
             auto wait_empty = [&](uint32_t n) {
@@ -500,19 +541,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
             while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
                 if (it.n_all > 0) {
                     // its reader, at most four items behind, sees it by way of the first K tile's barrier
-                    if (w == 0 && lane == 0) {
+                    if (warp == kWarpNote && lane == 0) {
                         sm.work[items & 7][0] = it.n_tiles[0];
                         sm.work[items & 7][1] = it.n_tiles[1];
                     }
                     ++items;
                 }
                 for (int32_t j = 0; j < it.n_all; ++j) {
-                    const uint32_t v0 = 8 * (uint32_t)(it.first + j);
-                    const uint32_t have = min(it.n_gran - v0, 8u), mine = have > 2 * w ? min(have - 2 * w, 2u) : 0;
-                    const uint32_t c0 = count + 2 * w;
-                    uint8_t *gran[2];
-#pragma unroll
-                    for (uint32_t h = 0; h < 2; ++h) gran[h] = smem_c + L::kGranRing + (c0 + h) % L::kGrans * L::kGran;
+                    const uint32_t v0 = 8 * (uint32_t)(it.first + j), have = min(it.n_gran - v0, 8u);
                     // Every warp waits for all of the tile's granules, a lane each, and gives all of them back: a place's
                     // next user may be another warp, and one that has not seen a use of it, or sees it too late, would
                     // take one state of the barrier for another.
@@ -520,45 +556,61 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     ok = lane >= have || pk::mbar_wait(pk::smem_addr(&sm.gran_full[c % L::kGrans]), (c / L::kGrans) & 1);
                     ok = __all_sync(0xffffffffu, ok) && wait_empty(n);
                     if (!ok) break;
-                    // V scales of a token a lane: those past the request's end count as 0, as weights of 0 must not meet a
-                    // NaN; so do blocks marked NaN, which are noted for the queries that see them.
-                    {
-                        const uint32_t h = lane / 16, tok = lane % 16, v = v0 + 2 * w + h;
-                        uint32_t bits = 0, lost = 0;
-                        if (h < mine) {
-                            uint32_t *s = reinterpret_cast<uint32_t *>(gran[h] + G::kVs + tok * G::kScales);
-                            const bool past = (int32_t)(16 * v + tok) + (v >= a.sink_grans ? it.skip : 0) >= it.len;
-                            lost = sm.gran_lost[(c0 + h) % L::kGrans];
+                    auto place = [&](uint32_t g) { return smem_c + L::kGranRing + (count + g) % L::kGrans * L::kGran; };
+                    // tokens of a granule before the request's end
+                    auto valid = [&](uint32_t g) {
+                        return it.len - (int32_t)(16 * (v0 + g)) - (v0 + g >= a.sink_grans ? it.skip : 0);
+                    };
+                    const uint32_t mine = have > 2 * w ? min(have - 2 * w, 2u) : 0;  // granules, of an unpacking warp
+                    uint8_t *tile = smem_c + L::kRing + n % L::kStages * L::kTile + (notes ? 0 : 32 * w * 128);
+                    if (notes) {  // blocks of V marked NaN, two tokens a lane
+                        uint32_t bits[2] = {0, 0}, lost = 0;
 #pragma unroll
-                            for (uint32_t i = 0; i < G::kScales / 4; ++i) {
-                                const uint32_t x = s[i], m = __vcmpeq4(x & 0x7f7f7f7fu, 0x7f7f7f7fu);
-                                if (past || m) s[i] = past ? 0 : x & ~m;
-                                if (!past) bits |= ((m & 1) | (m >> 7 & 2) | (m >> 14 & 4) | (m >> 21 & 8)) << (4 * i);
+                        for (uint32_t i = 0; i < 2; ++i) {
+                            const uint32_t g = 4 * half + 2 * i + lane / 16, tok = lane % 16;
+                            if (g >= have) continue;
+                            const uint32_t *s = reinterpret_cast<const uint32_t *>(place(g) + G::kVs + tok * G::kScales);
+                            lost |= sm.gran_lost[(count + g) % L::kGrans];
+                            if ((int32_t)tok >= valid(g)) continue;
+#pragma unroll
+                            for (uint32_t k = 0; k < G::kScales / 4; ++k) {
+                                const uint32_t m = __vcmpeq4(s[k] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+                                bits[i] |= ((m & 1) | (m >> 7 & 2) | (m >> 14 & 4) | (m >> 21 & 8)) << (4 * k);
                             }
                         }
-                        const bool marked = __any_sync(0xffffffffu, bits != 0), gone = __any_sync(0xffffffffu, lost != 0);
-                        if (marked) sm.marked[tiles % kNotes][32 * w + lane] = (uint8_t)bits;
-                        if (lane == 0) sm.flags[tiles % kNotes][w] = (marked ? kMarked : 0) | (gone ? kLost : 0);
-                        __syncwarp();
+                        const bool marked = __any_sync(0xffffffffu, (bits[0] | bits[1]) != 0);
+                        const bool gone = __any_sync(0xffffffffu, lost != 0);
+                        if (marked) {
+                            sm.marked[tiles % kNotes][64 * half + lane] = (uint8_t)bits[0];
+                            sm.marked[tiles % kNotes][64 * half + 32 + lane] = (uint8_t)bits[1];
+                        }
+                        if (lane == 0) sm.flags[tiles % kNotes][half] = (marked ? kMarked : 0) | (gone ? kLost : 0);
+                    } else {
+#pragma unroll
+                        for (uint32_t h = 0; h < 2; ++h)
+                            if (h < mine)
+                                lanes.template granule<DT == PK_BF16, false>(place(2 * w + h) + G::kK, place(2 * w + h) + G::kKs,
+                                                                             tile + 16 * h * 128, 16);
+                        pk::fence_proxy_async_smem();
                     }
-                    uint8_t *k = smem_c + L::kRing + n % L::kStages * L::kTile;
-                    for (uint32_t h = 0; h < mine; ++h)
-                        unpack<D, DT == PK_BF16>(gran[h] + G::kK, gran[h] + G::kKs, k, 32 * w + 16 * h);
-                    pk::fence_proxy_async();
                     __syncwarp();
                     if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.full[n % L::kStages]));
                     ++n;
                     ok = wait_empty(n);
                     if (!ok) break;
-                    uint8_t *v = smem_c + L::kRing + n % L::kStages * L::kTile;
-                    for (uint32_t h = 0; h < mine; ++h)
-                        unpack<D, false>(gran[h] + G::kV, gran[h] + G::kVs, v, 32 * w + 16 * h);
-                    // rows behind the last granule: weights of 0 must not meet what lies there
-                    for (uint32_t x = mine * 16 * (D / 8) + lane; x < 32 * (D / 8); x += 32) {
-                        const uint32_t row = 32 * w + x / (D / 8), piece = x % (D / 8);
-                        *reinterpret_cast<uint4 *>(v + piece / 8 * 16384 + row * 128 + piece % 8 * 16) = make_uint4(0, 0, 0, 0);
+                    if (!notes) {
+                        tile = smem_c + L::kRing + n % L::kStages * L::kTile + 32 * w * 128;
+#pragma unroll
+                        for (uint32_t h = 0; h < 2; ++h)
+                            if (h < mine)
+                                lanes.template granule<false, true>(place(2 * w + h) + G::kV, place(2 * w + h) + G::kVs,
+                                                                    tile + 16 * h * 128, valid(2 * w + h));
+                        // rows behind the last granule: weights of 0 must not meet what lies there
+                        for (uint32_t x = mine * 16 * (D / 8) + lane; x < 32 * (D / 8); x += 32)
+                            *reinterpret_cast<uint4 *>(tile + x % (D / 8) / 8 * 16384 + x / (D / 8) * 128 + x % 8 * 16) =
+                                make_uint4(0, 0, 0, 0);
+                        pk::fence_proxy_async_smem();
                     }
-                    pk::fence_proxy_async();
                     __syncwarp();
                     if (lane < have) pk::mbar_arrive(pk::smem_addr(&sm.gran_empty[c % L::kGrans]));
                     if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.full[n % L::kStages]));
@@ -571,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
             ok = ok && wait_empty(n);
             if (ok) {  // the matrix warp's end: a stage without a tile
                 if (lane == 0) {
-                    if (w == 0) sm.work[items & 7][0] = sm.work[items & 7][1] = 0;
+                    if (warp == kWarpNote) sm.work[items & 7][0] = sm.work[items & 7][1] = 0;
                     pk::mbar_arrive(pk::smem_addr(&sm.full[n % L::kStages]));
                 }
             } else if (lane == 0) {
@@ -692,28 +744,35 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
         // a scale of 0 would make a masked -infinity NaN; the smallest normal one gives the same weights
         const float scale2 = fmaxf(fabsf(a.scale2), FLT_MIN);
         const uint64_t scale22 = pk::pack2(scale2, scale2);
+        // What is not needed at every tile of the item lies in shared memory: in registers it would push others out.
+        volatile TileOf *mine = &sm.tile[warp];
         uint32_t ni = 0, tiles = 0;  // key tiles weighed so far; key tiles of the CTA's items before the present one
         bool ok = true;
         while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
             const int32_t n_tiles = t ? it.n_tiles[1] : it.n_tiles[0];
-            const int32_t tok0 = it.tok0 + (int32_t)(t * a.tile_tokens), tok = tok0 + row_tok;
-            const int32_t gh = (int32_t)(it.chunk * a.tile_heads) + row_head;
-            const bool on = row_tok < (int32_t)a.tile_tokens && tok < it.lq && gh < (int32_t)a.group;
-            const bool cut = it.pieces > 1;
-            // Places of the list, from the piece's first tile on: the row sees low .. last and those before `sinks`; all
-            // rows of the tile see what lies in all_low .. all_last.
-            const int32_t base = it.first * kKeys, here = it.len - it.lq - it.skip;  // here: place of the request's first query
-            auto low_of = [&](int32_t tok) {  // of the query that is token `tok` of the request
-                return a.window ? (int32_t)max((int64_t)(it.len - it.lq) + tok - a.window + 1, (int64_t)0) - it.skip - base : -base;
-            };
-            const int32_t last = on ? here + tok - base : -1, low = low_of(tok);
-            const int32_t all_last = here + tok0 - base;
-            const int32_t all_low = low_of(min(tok0 + (int32_t)a.tile_tokens, it.lq) - 1), sinks = (int32_t)a.sinks - base;
-            const int64_t q_row = it.q0 + tok;
-            const uint32_t qh = it.head * a.group + gh;
-            const uint64_t part = ((uint64_t)it.index * 2 + t) * kRows + row;
-            const uint32_t n_all = (uint32_t)it.n_all;
-            take_next();
+            bool on;
+            {
+                const int32_t tok0 = it.tok0 + (int32_t)(t * a.tile_tokens), off = it.len - it.lq;
+                const int32_t base = it.first * kKeys + it.skip;  // from positions to places behind the piece's first one
+                const int32_t all_last = off + tok0 - base;
+                const int32_t all_low = low_of(a, off, min(tok0 + (int32_t)a.tile_tokens, it.lq) - 1) - base;
+                const int32_t sinks = (int32_t)a.sinks - it.first * kKeys, gh0 = (int32_t)(it.chunk * a.tile_heads);
+                if (lane == 0) {
+                    mine->causal = ((all_last - (kKeys - 1)) >> 7) + 1;
+                    mine->hides[0] = sinks >> 7;
+                    mine->hides[1] = a.window ? (all_low + kKeys - 1) >> 7 : 0;
+                    mine->off = off;
+                    mine->base = base;
+                    mine->sinks = sinks;
+                    mine->tok0 = tok0;
+                    mine->row0 = it.q0 + tok0;
+                    mine->head0 = it.head * a.group + gh0;
+                    mine->part = it.pieces > 1 ? ((int64_t)it.index * 2 + t) * kRows : -1;
+                    mine->n_all = it.n_all;
+                }
+                on = row_tok < (int32_t)a.tile_tokens && tok0 + row_tok < it.lq && gh0 + row_head < (int32_t)a.group;
+                __syncwarp();
+            }
             // a weight is 2^(score - ref + fine), and fine is 0 but for a reference of kFar and more
             float ref = -FLT_MAX, fine = 0.0f, sum = 0.0f;
             uint32_t marked = 0;  // blocks of 16 dimensions in which the row saw a NaN of V
@@ -723,17 +782,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 ok = pk::mbar_wait_warp(pk::smem_addr(&sm.s_full[t]), ni & 1);
                 if (!ok) break;
                 pk::tmem_fence_after();
-                const int32_t x0 = j * kKeys;
-                const bool edge = x0 + kKeys - 1 > all_last || (x0 < all_low && x0 + kKeys > sinks);
-                const int32_t see = last - x0, from = low - x0, first = sinks - x0;
+                // the row sees the tile's keys up to `see` that are not below `from`, or are below `first`
+                const bool edge = j >= mine->causal || (j >= mine->hides[0] && j < mine->hides[1]);
+                int32_t see = kKeys, from = 0, first = 0;
+                if (edge) {
+                    const int32_t tok = mine->tok0 + row_tok, x0 = j * kKeys;
+                    see = on ? mine->off + tok - mine->base - x0 : -1;
+                    from = low_of(a, mine->off, tok) - mine->base - x0;
+                    first = mine->sinks - x0;
+                }
                 auto hidden = [&](int32_t i) { return i > see || (i < from && i >= first); };
                 const uint32_t note = (tiles + j) % kNotes;
-                const uint32_t flags = *reinterpret_cast<const volatile uint32_t *>(sm.flags[note]);
+                const uint32_t flags = *reinterpret_cast<const volatile uint16_t *>(sm.flags[note]);
                 if (flags) {
-                    lost |= (flags & 0x01010101u * kLost) != 0;
+                    lost |= (flags & 0x0101u * kLost) != 0;
 #pragma unroll 1
                     for (int32_t i = 0; i < kKeys; ++i)
-                        if ((flags >> (i / 32 * 8) & kMarked) && !hidden(i)) marked |= sm.marked[note][i];
+                        if ((flags >> (i / 64 * 8) & kMarked) && !hidden(i)) marked |= sm.marked[note][i];
                 }
                 uint32_t x[3][32];
                 // Chunk c of the scores, 32 keys.  Loads run ahead (1 and 2 behind 0's use, 3 behind 1's).  Masked or
@@ -861,10 +926,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 __syncwarp();
                 if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.p_ready[t]));
             }
-            tiles += n_all;
+            tiles += (uint32_t)mine->n_all;
+            take_next();  // while the last product runs
             if (ok && n_tiles > 0) ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
             if (!ok) break;
             if (lost) sum = __int_as_float(0x7fffffff);
+            const int64_t part = mine->part >= 0 ? mine->part + row : -1;
+            const bool cut = part >= 0;
+            const int64_t q_row = (int64_t)mine->row0 + row_tok;
+            const uint32_t qh = (uint32_t)(mine->head0 + row_head);
             const float inv = cut ? 1.0f : sum == 0.0f ? 0.0f : a.v_scale / sum;
             if (on && cut) a.part_ml[part] = make_float4(ref, fine, sum, 0.0f);
             if (on && !cut && a.lse)

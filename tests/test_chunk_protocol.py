@@ -1,4 +1,4 @@
-"""CPU model of the chunk-attention kernel's barriers: loader, unpacking, matrix and softmax warps of one CTA, which takes one
+"""CPU model of the chunk-attention kernel's barriers: loader, making, matrix and softmax warps of one CTA, which takes one
 item after another, as coroutines under random interleavings, with the copies and the matrix pipe as asynchronous agents.
 Checks that no barrier gets an arrival its phase does not expect, that every product reads what it should, that nothing is
 overwritten while it is read (a key tile's notes among it), that all roles end, and that nothing asynchronous is left then."""
@@ -8,19 +8,19 @@ import pytest
 
 from test_prompt_protocol import Bar
 
-UNPACKERS, NOTES = 4, 8
+MAKERS, NOTES = 6, 8  # of the makers, 0 and 1 take the notes, the others unpack
 
 
 class Cta:
     def __init__(self, items, stages, grans, rng):
         """items: (key tiles of tile 0, of tile 1, granules of the last tile) each."""
         self.items, self.S, self.G, self.rng = items, stages, grans, rng
-        self.full, self.empty = [Bar(UNPACKERS) for _ in range(stages)], [Bar(1) for _ in range(stages)]
-        self.gran_full, self.gran_empty = [Bar(1) for _ in range(grans)], [Bar(UNPACKERS) for _ in range(grans)]
+        self.full, self.empty = [Bar(MAKERS) for _ in range(stages)], [Bar(1) for _ in range(stages)]
+        self.gran_full, self.gran_empty = [Bar(1) for _ in range(grans)], [Bar(MAKERS) for _ in range(grans)]
         self.q_full, self.q_empty, self.s_full, self.o_done = ([Bar(1) for _ in range(2)] for _ in range(4))
         self.p_ready = [Bar(4) for _ in range(2)]
         self.gran, self.q = [None] * grans, [None, None]
-        self.stage = [{} for _ in range(stages)]  # by unpacking warp: what it put there
+        self.stage = [{} for _ in range(stages)]  # by making warp: what it put there
         self.notes = [{} for _ in range(NOTES)]
         self.copies, self.pipe = [], []  # in flight; the pipe runs in order
         self.sp, self.o = [None, None], [None, None]
@@ -65,7 +65,7 @@ class Cta:
             while nq[t] and not self.q_full[t].done((nq[t] - 1) & 1):
                 yield
 
-    def unpacker(self, w):
+    def maker(self, w):
         n, count, tiles, taken = 0, 0, 0, 0
 
         def wait_empty(n):
@@ -80,7 +80,7 @@ class Cta:
                 taken += 1
             for j in range(max(n0, n1)):
                 have = self.grans_of(x, j)
-                mine = [g for g in (2 * w, 2 * w + 1) if g < have]
+                mine = [g for g in (range(4 * w, 4 * w + 4) if w < 2 else (2 * w - 4, 2 * w - 3)) if g < have]
                 for g in range(have):
                     c = count + g
                     while not self.gran_full[c % self.G].done((c // self.G) & 1):
@@ -89,7 +89,7 @@ class Cta:
                     yield from wait_empty(n)
                     for g in mine:
                         assert self.gran[(count + g) % self.G] == (x, j, g)
-                    if kv == "K":
+                    if kv == "K" and w < 2:
                         self.notes[tiles % NOTES][w] = (x, j)
                     self.stage[n % self.S][w] = None
                     yield
@@ -177,7 +177,7 @@ class Cta:
                     yield
                 for _ in range(self.rng.choice((1, 1, 30))):
                     assert self.sp[t] == ("S", x, j)
-                    assert all(self.notes[(tiles + j) % NOTES].get(w) == (x, j) for w in range(UNPACKERS)), "notes gone"
+                    assert all(self.notes[(tiles + j) % NOTES].get(w) == (x, j) for w in (0, 1)), "notes gone"
                     yield
                 if j and self.rng.random() < self.rescale:
                     while not self.o_done[t].done((ni - 1) & 1):
@@ -208,7 +208,7 @@ class Cta:
                 op[1].arrive()
                 return
             kind, t, x, j, st = op
-            want = {w: ("K" if kind == "QK" else "V", x, j) for w in range(UNPACKERS)}
+            want = {w: ("K" if kind == "QK" else "V", x, j) for w in range(MAKERS)}
             assert self.stage[st] == want
             if kind == "QK":
                 assert self.q[t] == x and (self.sp[t] is None or self.sp[t][0] == "P")
@@ -218,7 +218,7 @@ class Cta:
                 self.o[t] = (x, j)
 
     def run(self):
-        roles = [self.loader(), self.mma()] + [self.unpacker(w) for w in range(UNPACKERS)]
+        roles = [self.loader(), self.mma()] + [self.maker(w) for w in range(MAKERS)]
         roles += [self.softmax(t, w) for t in (0, 1) for w in range(4)]
         slow = {id(x): self.rng.choice((1.0, 0.3, 0.03)) for x in roles}
         for _ in range(3000000):
@@ -236,7 +236,7 @@ class Cta:
         assert not self.pipe, "a product or an arrival is left after the CTA's end"
 
 
-@pytest.mark.parametrize("stages,grans", [(4, 14), (8, 28)])
+@pytest.mark.parametrize("stages,grans", [(3, 28), (8, 32)])
 def test_every_interleaving_tried_is_sound(stages, grans):
     rng = random.Random(11)
     for _ in range(100):
@@ -251,6 +251,6 @@ def test_every_interleaving_tried_is_sound(stages, grans):
 def test_many_short_items():
     """Items of one key tile, where the warps run furthest ahead of one another."""
     rng = random.Random(12)
-    for stages, grans in ((4, 14), (8, 28)):
+    for stages, grans in ((3, 28), (8, 32)):
         for _ in range(40):
             Cta([(rng.choice((0, 1)), rng.choice((0, 1)), rng.choice((1, 1, 2))) for _ in range(30)], stages, grans, rng).run()
