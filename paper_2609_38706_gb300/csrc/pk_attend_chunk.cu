@@ -37,6 +37,13 @@ constexpr float kFar = 16777216.0f;  // scores (times log2 e) from here on are f
                                      // one 32-bit reference cannot lie kBase below one
 constexpr int kPlanThreads = 1024;
 
+// A unit that was cut, for k_chunk_join: its rows, and the blocks that had pieces of it.
+struct alignas(32) Cut {
+    int32_t first, last;     // blocks; first -1: none
+    int32_t row0, tokens;    // row of q of its first token; tokens
+    int32_t head0, heads;    // query heads
+};
+
 struct Args {
     const uint8_t *pool;
     uint64_t page_bytes, n_slots, page_stride, positions;  // positions: that a request can hold
@@ -53,13 +60,11 @@ struct Args {
     int64_t o_ts, o_hs;
     bool wide_out;  // every 16 values of out start on 32 bytes
     float *lse;
-    // Keys of an item are cut into pieces of about `split` tiles, so that few rows over many keys fill the GPU.
-    uint32_t target, least;  // pieces that a call is cut into, about (0: none is cut), and tiles of one at least
-    uint64_t *plan;          // [0]: split; [1 + r]: items of one KV head in the requests before r
-    bool listed;             // more than 32 requests: k_chunk_plan made the plan
-    uint32_t most_items;     // no call has more
-    float4 *part_ml;         // [item][2][128]: (ref, fine, sum) of a piece's rows
-    float *part_o;           // [item][2][128][D]
+    uint32_t blocks;  // of k_attend_chunk: the call's work is cut into so many equal shares at most
+    int64_t *plan;    // [R + 2]: work of the requests before each one, then all units, by k_chunk_plan; NULL for up to 32 requests
+    Cut *cuts;        // [blocks]: by block, the unit that its share's beginning cuts, if no share before it begins there too
+    float4 *part_ml;  // [2 blocks][2][128]: (ref, fine, sum) of a piece's rows
+    float *part_o;    // [2 blocks][2][128][D]
     int32_t *status;
 };
 
@@ -72,82 +77,165 @@ __device__ __forceinline__ int32_t good_length(const Args &a, int32_t len) {
     return len < 0 || (uint64_t)len > a.positions ? 0 : len;
 }
 
-// Items of one KV head in a request of n queries, before they are cut.
-__device__ __forceinline__ uint32_t units_of(const Args &a, int64_t n) {
-    return ((uint32_t)n + 2 * a.tile_tokens - 1) / (2 * a.tile_tokens) * a.chunks;
+// The work of a call, on a line: request after request, in one its KV heads (and parts of a group's heads), in one of
+// those its units of 2 tile_tokens queries.  A unit weighs as much as the keys that it goes through and kUnitCost.  The
+// line is cut into equal shares, one for each block: a block takes the units that its share holds, of the first and
+// the last a piece of their keys.  So all blocks are done at about the same time, also where a call is a few rows over
+// many keys (4 x 512 tokens behind 16384, 256 units: 604 -> 550 us against units cut in two).  Where that gains less
+// than the pieces and their joining cost, a block takes the whole units that begin in its share.
+constexpr int64_t kUnitCost = 512;     // a unit's start and end, in keys
+constexpr int64_t kCutCost = 1024;     // one more piece a block, and the joining
+constexpr int64_t kLeastShare = 1024;
+
+struct Req {
+    int32_t q0, lq, len;
+};
+// Units of a request for one KV head and part of a group: their keys grow by `step` from `first` on, within 0 .. most.
+struct Units {
+    int64_t first, most;
+    int32_t step, n;
+
+    __device__ __forceinline__ Units(const Args &a, const Req &q) {
+        step = 2 * (int32_t)a.tile_tokens;
+        n = (int32_t)(((int64_t)q.lq + step - 1) / step);
+        first = (int64_t)q.len - q.lq + step;
+        most = q.len;
+        if (a.window) most = min(most, (int64_t)a.sink_grans * 16 + a.window + step + 15);
+    }
+    __device__ __forceinline__ int64_t weight(int32_t u) const {
+        return kUnitCost + min(max(first + (int64_t)step * u, (int64_t)0), most);
+    }
+    // Weight of the first u units.
+    __device__ __forceinline__ int64_t before(int32_t u) const {
+        const int64_t none = first > 0 ? 0 : -first / step + 1;                          // units without keys
+        const int64_t rising = first >= most ? 0 : (most - first - 1) / step + 1;        // and those with fewer than most
+        const int64_t lo = min(none, (int64_t)u), hi = max(lo, min(rising, (int64_t)u));
+        return kUnitCost * u + first * (hi - lo) + step * ((lo + hi - 1) * (hi - lo) / 2) + most * (u - hi);
+    }
+};
+// Work and units of a request.
+__device__ __forceinline__ int64_t work_of(const Args &a, const Req &q, int64_t &all_units) {
+    const Units units(a, q);
+    all_units = (int64_t)units.n * a.chunks * a.kv_heads;
+    return units.before(units.n) * a.chunks * a.kv_heads;
 }
 
-// Key tiles of a request's last queries, or a few more.
-__device__ __forceinline__ uint32_t tiles_of(const Args &a, int32_t len) {
-    uint64_t grans = ((uint64_t)len + 15) / 16;
-    if (a.window) grans = min(grans, (uint64_t)a.sink_grans + ((uint64_t)a.window + 2 * a.tile_tokens + 14) / 16 + 1);
-    return (uint32_t)((grans + 7) / 8);
+// The shares of `total`: block b has [start(b), start(b + 1)).
+struct Shares {
+    int64_t each;
+    uint32_t more, n;  // the first `more` have one more
+    bool whole;        // no unit is cut
+
+    __device__ __forceinline__ Shares(const Args &a, int64_t total, int64_t units) {
+        n = (uint32_t)min((int64_t)a.blocks, max(total / kLeastShare, (int64_t)1));
+        each = total / n;
+        more = (uint32_t)(total - each * n);
+        whole = units == 0 || (units + n - 1) / n * (total / units) <= each + kCutCost;
+    }
+    __device__ __forceinline__ int64_t start(uint32_t b) const { return each * b + min(b, more); }
+    __device__ __forceinline__ uint32_t block_of(int64_t x) const {
+        const int64_t wide = (each + 1) * more;
+        return x < wide ? (uint32_t)(x / (each + 1)) : more + (uint32_t)((x - wide) / each);
+    }
+};
+
+// Where on the line a piece begins: unit u of part `part` of request r, `pos` of its weight behind its beginning.
+struct Place {
+    uint32_t r, part;
+    int32_t u;
+    int64_t pos;
+};
+// By a whole warp: x lies in request r, whose work begins at `before`.
+__device__ __forceinline__ Place place_of(const Units &units, uint32_t r, int64_t before, int64_t x) {
+    Place p;
+    p.r = r;
+    x -= before;
+    const int64_t one = units.before(units.n);
+    p.part = (uint32_t)(x / one);
+    x -= p.part * one;
+    int32_t lo = 0, hi = units.n;  // before(lo) <= x < before(hi)
+    while (hi - lo > 1) {
+        const int32_t step = (hi - lo + 31) / 32, u = lo + (int32_t)(threadIdx.x & 31) * step;
+        const uint32_t in = __ballot_sync(0xffffffffu, u < hi && units.before(u) <= x);  // lane 0 is; a prefix of the lanes
+        lo += (31 - __clz(in)) * step;
+        hi = min(hi, lo + step);
+    }
+    p.u = lo;
+    p.pos = x - units.before(lo);
+    return p;
 }
 
-// Tiles of a piece, from the sum over the items of their requests' tiles; pieces of an item.
-__device__ __forceinline__ uint32_t split_of(const Args &a, uint64_t total) {
-    if (a.target == 0) return 0x7fffffff;
-    return (uint32_t)max((total + a.target - 1) / a.target, (uint64_t)a.least);
-}
-__device__ __forceinline__ uint32_t pieces_of(uint32_t tiles, uint32_t split) {
-    return tiles <= split ? 1 : (tiles + split - 1) / split;
-}
-
-// The plan of more than 32 requests; of no items where an offset is out of order or range.
+// The plan of more than 32 requests; of no work where an offset is out of order or range.
 __global__ void __launch_bounds__(kPlanThreads) k_chunk_plan(const Args a) {
-    __shared__ uint64_t warp_sum[32];
+    __shared__ int64_t warp_sum[32];
+    __shared__ unsigned long long all_units;
     __shared__ uint32_t bad;
     const uint32_t tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    if (tid == 0) bad = 0;
+    if (tid == 0) bad = 0, all_units = 0;
     const int64_t *q_off = a.q_off;
     const int32_t *kv_len = a.kv_len;
-    uint64_t *plan = a.plan;
+    int64_t *plan = a.plan;
     pk::pdl_wait(q_off, kv_len, plan);
     pk::pdl_launch_dependents();
     __syncthreads();
-    uint32_t split = 0x7fffffff;
-    for (int pass = a.target ? 0 : 1; pass < 2; ++pass) {  // the sum of the tiles, then the items
-        uint64_t base = 0;
-        for (uint64_t r0 = 0; r0 < a.R; r0 += kPlanThreads) {
-            const uint64_t r = r0 + tid;
-            uint64_t n = 0;
-            if (r < a.R) {
-                const int64_t qa = __ldcg(q_off + r), qb = __ldcg(q_off + r + 1);
-                const int32_t l = __ldcg(kv_len + r), len = good_length(a, l);
-                if (pass && l != len) pk::set_status(a.status, PK_ERR_ARG);
-                if (bad_offsets(qa, qb, a.n_q))
-                    bad = 1;
-                else
-                    n = (uint64_t)units_of(a, qb - qa) * (pass ? pieces_of(tiles_of(a, len), split) : a.kv_heads * tiles_of(a, len));
-            }
-            uint64_t scan = n;
-#pragma unroll
-            for (int d = 1; d < 32; d *= 2) {
-                const uint64_t o = __shfl_up_sync(0xffffffffu, scan, d);
-                if (lane >= (uint32_t)d) scan += o;
-            }
-            if (lane == 31) warp_sum[wid] = scan;
-            __syncthreads();
-            uint64_t before = base, total = 0;
-            for (uint32_t w = 0; w < kPlanThreads / 32; ++w) {
-                if (w < wid) before += warp_sum[w];
-                total += warp_sum[w];
-            }
-            if (pass && r < a.R) plan[2 + r] = before + scan;
-            base += total;
-            __syncthreads();
+    int64_t base = 0;
+    for (uint64_t r0 = 0; r0 < a.R; r0 += kPlanThreads) {
+        const uint64_t r = r0 + tid;
+        int64_t n = 0, units = 0;
+        if (r < a.R) {
+            const int64_t qa = __ldcg(q_off + r), qb = __ldcg(q_off + r + 1);
+            const int32_t l = __ldcg(kv_len + r), len = good_length(a, l);
+            if (l != len) pk::set_status(a.status, PK_ERR_ARG);
+            if (bad_offsets(qa, qb, a.n_q))
+                bad = 1;
+            else
+                n = work_of(a, Req{(int32_t)qa, (int32_t)(qb - qa), len}, units);
         }
-        if (pass == 0) split = split_of(a, base);
+#pragma unroll
+        for (int d = 16; d; d /= 2) units += __shfl_xor_sync(0xffffffffu, units, d);
+        if (lane == 0 && units) atomicAdd(&all_units, (unsigned long long)units);
+        int64_t scan = n;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int64_t o = __shfl_up_sync(0xffffffffu, scan, d);
+            if (lane >= (uint32_t)d) scan += o;
+        }
+        if (lane == 31) warp_sum[wid] = scan;
+        __syncthreads();
+        int64_t before = base, total = 0;
+        for (uint32_t w = 0; w < kPlanThreads / 32; ++w) {
+            if (w < wid) before += warp_sum[w];
+            total += warp_sum[w];
+        }
+        if (r < a.R) plan[1 + r] = before + scan;
+        base += total;
+        __syncthreads();
     }
     if (tid == 0) {
-        plan[0] = split;
-        plan[1] = 0;
+        plan[0] = 0;
+        plan[a.R + 1] = (int64_t)all_units;
     }
     if (bad) {
-        for (uint64_t r = tid; r <= a.R; r += kPlanThreads) plan[1 + r] = 0;
+        for (uint64_t r = tid; r <= a.R; r += kPlanThreads) plan[r] = 0;
         if (tid == 0) pk::set_status(a.status, PK_ERR_ARG);
     }
 }
+
+// One piece of a unit: 2 tiles of tile_tokens query tokens times tile_heads heads of one group, and some of their keys.
+struct Item {
+    Place at;
+    Req q;
+    int64_t line, left;   // where the block's share ends; what is left of it behind the piece
+    int32_t skip;         // tokens in the gap, a multiple of 16: place x is position x, or x + skip behind the first granules
+    int32_t first;        // first key tile of the piece
+    int32_t n_tiles[2], n_all;
+    uint32_t n_gran;      // granules of the unit's whole list
+    bool cut, whole;      // not the whole unit; the block takes whole units
+
+    __device__ __forceinline__ uint32_t head(const Args &a) const { return at.part / a.chunks; }
+    __device__ __forceinline__ uint32_t chunk(const Args &a) const { return at.part % a.chunks; }
+    __device__ __forceinline__ int32_t tok0(const Args &a) const { return at.u * 2 * (int32_t)a.tile_tokens; }
+};
 
 // Shared memory of a CTA, from a 1024-byte boundary: Q (two tiles), the ring of K and V tiles in 16 bits, the ring of
 // granules as they lie in the pages, then Small.
@@ -156,7 +244,7 @@ struct Layout {
     static constexpr uint32_t kTile = 128 * D * 2;  // 128 rows; blocks of [128][64] values, 16 KB each
     static constexpr uint32_t kStages = D == 128 ? 3 : 8;
     static constexpr uint32_t kGran = pk::Granule<D>::kBytes;
-    static constexpr uint32_t kGrans = D == 128 ? 28 : 32;
+    static constexpr uint32_t kGrans = D == 128 ? 26 : 32;
     static constexpr uint32_t kRing = 2 * kTile;
     static constexpr uint32_t kGranRing = kRing + kStages * kTile;
     static constexpr uint32_t kBytes = kGranRing + kGrans * kGran;
@@ -171,7 +259,7 @@ struct TileOf {
     int32_t causal, hides[2];  // from the first on some query does not see some key; between the others too
     int32_t off, base;         // position of the request's first query; what a position is more than its place in the piece
     int32_t sinks, tok0, row0, head0, n_all;
-    int64_t part;              // where the piece's rows go; -1: the item is not cut
+    int32_t part;              // where the piece's rows go; -1: the unit is not cut
 };
 
 struct Small {
@@ -183,12 +271,13 @@ struct Small {
     uint32_t tmem, abort;
     int32_t work[8][2];                     // by item with keys: key tiles of its two tiles, for the matrix warp; 0, 0 ends it
     uint8_t gran_lost[32];                  // what stands in a granule's place is another request's
-    uint32_t split;
     alignas(2) uint8_t flags[kNotes][2];    // by key tile and half of its keys: kMarked, kLost
     uint8_t marked[kNotes][128];            // by key, where kMarked: blocks of V that are NaN (0 stands in the tile)
-    uint32_t item_end[32];                  // up to 32 requests: items of one KV head in those up to each, and what they are
-    int32_t q_start[32], q_len[32], len[32];
+    int64_t units;                          // up to 32 requests: all their units, the work of those up to each,
+    int64_t work_end[32];                   // and what they are
+    Req req[32];
     TileOf tile[8];
+    uint32_t item[16][sizeof(Item) / 4];    // by warp: the present item, while its keys are gone through
 };
 
 // Up to 32 requests every CTA makes the plan itself, a lane a request, and keeps it in shared memory.
@@ -204,95 +293,80 @@ __device__ __forceinline__ void plan_here(const Args &a, Small &sm, const int64_
     }
     const bool bad = __any_sync(0xffffffffu, bad_offsets(qa, qb, a.n_q));
     if (bad && lane == 0) pk::set_status(a.status, PK_ERR_ARG);
-    const uint32_t units = bad ? 0 : units_of(a, qb - qa), tiles = tiles_of(a, len);
-    uint64_t total = (uint64_t)units * a.kv_heads * tiles;
+    const Req q = {(int32_t)qa, (int32_t)(qb - qa), len};
+    int64_t units, scan = work_of(a, q, units);
+    if (bad) scan = 0;
 #pragma unroll
-    for (int d = 16; d; d /= 2) total += __shfl_xor_sync(0xffffffffu, total, d);
-    const uint32_t split = split_of(a, total);
-    uint32_t scan = units * pieces_of(tiles, split);
+    for (int d = 16; d; d /= 2) units += __shfl_xor_sync(0xffffffffu, units, d);
+    if (lane == 0) sm.units = units;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
-        const uint32_t o = __shfl_up_sync(0xffffffffu, scan, d);
+        const int64_t o = __shfl_up_sync(0xffffffffu, scan, d);
         if (lane >= (uint32_t)d) scan += o;
     }
-    sm.item_end[lane] = scan;
-    sm.q_start[lane] = (int32_t)qa;
-    sm.q_len[lane] = (int32_t)(qb - qa);
-    sm.len[lane] = len;
-    if (lane == 0) sm.split = split;
-    if (a.target && blockIdx.x == 0) {  // for k_chunk_join
-        if (lane < a.R) a.plan[2 + lane] = scan;
-        if (lane == 0) {
-            a.plan[0] = split;
-            a.plan[1] = 0;
-        }
-    }
+    sm.work_end[lane] = scan;
+    sm.req[lane] = q;
 }
 
-// One item: 2 tiles of tile_tokens query tokens times tile_heads heads of one group, and a piece of their keys.
-struct Item {
-    uint32_t r, head, chunk, index, pieces;
-    int32_t q0, lq, len, tok0;
-    int32_t skip;         // tokens in the gap, a multiple of 16: place x is position x, or x + skip behind the first granules
-    int32_t first;        // first key tile of the piece
-    int32_t n_tiles[2], n_all;
-    uint32_t n_gran;      // granules of the whole list
-};
+// An item that all lanes have, to shared memory and back.
+__device__ __forceinline__ void put_aside(const Item &it, volatile uint32_t *to, uint32_t lane) {
+    uint32_t w[sizeof(Item) / 4];
+    memcpy(w, &it, sizeof(Item));
+    if (lane == 0)
+#pragma unroll
+        for (size_t i = 0; i < sizeof(Item) / 4; ++i) to[i] = w[i];
+}
+__device__ __forceinline__ void take_back(Item &it, const volatile uint32_t *from) {
+    uint32_t w[sizeof(Item) / 4];
+#pragma unroll
+    for (size_t i = 0; i < sizeof(Item) / 4; ++i) w[i] = from[i];
+    memcpy(&it, w, sizeof(Item));
+}
 
-__device__ __forceinline__ bool find_item(const Args &a, const Small &sm, const uint64_t *plan, const int64_t *q_off,
-                                          const int32_t *kv_len, uint32_t index, Item &it) {
-    const uint32_t tile = index / a.kv_heads;
-    it.index = index;
-    it.head = index - tile * a.kv_heads;
-    it.q0 = it.lq = it.len = 0;
-    it.r = 0;
-    uint32_t x = 0, split = 0;  // which of the request's items
-    if (a.listed) {
-        if (tile < __ldcg(plan + 1 + a.R)) {
-            it.r = pk::warp_find_request(reinterpret_cast<const int64_t *>(plan + 1), a.R, (int64_t)tile);
-            it.q0 = (int32_t)__ldcg(q_off + it.r);
-            it.lq = (int32_t)__ldcg(q_off + it.r + 1) - it.q0;
-            it.len = good_length(a, __ldcg(kv_len + it.r));
-            x = (uint32_t)__ldcg(plan + 2 + it.r) - 1 - tile;
-            split = (uint32_t)__ldcg(plan);
-        }
-    } else {
-        const uint32_t lane = threadIdx.x & 31;
-        it.r = __popc(__ballot_sync(0xffffffffu, sm.item_end[lane] <= tile));
-        if (it.r < 32) {  // (requests past R repeat the total)
-            it.q0 = sm.q_start[it.r];
-            it.lq = sm.q_len[it.r];
-            it.len = sm.len[it.r];
-            x = sm.item_end[it.r] - 1 - tile;
-            split = sm.split;
-        }
+__device__ __forceinline__ Shares shares_of(const Args &a, const Small &sm, const int64_t *plan) {
+    return plan ? Shares(a, __ldcg(plan + a.R), __ldcg(plan + a.R + 1)) : Shares(a, sm.work_end[31], sm.units);
+}
+
+// The request that holds place x of the line.
+__device__ __forceinline__ int64_t find_request(const Args &a, const Small &sm, const int64_t *plan, const int64_t *q_off,
+                                                const int32_t *kv_len, int64_t x, Item &it) {
+    if (a.plan) {
+        const uint32_t r = it.at.r = pk::warp_find_request(plan, a.R, x);
+        it.q.q0 = (int32_t)__ldcg(q_off + r);
+        it.q.lq = (int32_t)__ldcg(q_off + r + 1) - it.q.q0;
+        it.q.len = good_length(a, __ldcg(kv_len + r));
+        return __ldcg(plan + r);
     }
-    // the last queries first: they have the most keys
-    it.pieces = pieces_of(tiles_of(a, it.len), split);
-    const uint32_t piece = x % it.pieces;
-    x /= it.pieces;
-    it.chunk = x % a.chunks;
-    it.tok0 = (int32_t)(x / a.chunks) * 2 * (int32_t)a.tile_tokens;
-    const int32_t off = it.len - it.lq;  // position of the request's first query
-    const int64_t low = (int64_t)off + it.tok0 - a.window + 1;
+    const uint32_t lane = threadIdx.x & 31;
+    const uint32_t r = it.at.r = __popc(__ballot_sync(0xffffffffu, sm.work_end[lane] <= x)) & 31;
+    it.q = sm.req[r];
+    return r ? sm.work_end[r - 1] : 0;
+}
+
+// The keys of the piece that begins at it.at and has `room` of the block's share.
+__device__ __forceinline__ void cut_item(const Args &a, const Units &units, int64_t room, Item &it) {
+    const int64_t weight = units.weight(it.at.u), end = it.whole ? weight : min(weight, it.at.pos + room);
+    it.left = room - (end - it.at.pos);
+    it.cut = it.at.pos > 0 || end < weight;
+    const int32_t off = it.q.len - it.q.lq, tok0 = it.tok0(a);  // off: position of the request's first query
+    const int64_t low = (int64_t)off + tok0 - a.window + 1;
     const uint32_t low_gran = a.window && low > 0 ? (uint32_t)(low / 16) : 0;
     it.skip = low_gran > a.sink_grans ? (int32_t)(low_gran - a.sink_grans) * 16 : 0;
     int32_t n[2];
     it.n_gran = 0;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const int32_t t0 = it.tok0 + t * (int32_t)a.tile_tokens, t1 = min(t0 + (int32_t)a.tile_tokens, it.lq);
+        const int32_t t0 = tok0 + t * (int32_t)a.tile_tokens, t1 = min(t0 + (int32_t)a.tile_tokens, it.q.lq);
         const int32_t last = t1 > t0 ? off + t1 - 1 - it.skip : -1;
         n[t] = last >= 0 ? last / kKeys + 1 : 0;
         if (last >= 0) it.n_gran = (uint32_t)last / 16 + 1;
     }
     const int32_t all = max(n[0], n[1]);
-    it.first = (int32_t)((uint64_t)all * piece / it.pieces);
-    const int32_t end = (int32_t)((uint64_t)all * (piece + 1) / it.pieces);
+    it.first = it.cut ? (int32_t)(all * it.at.pos / weight) : 0;
+    const int32_t to = it.cut ? (int32_t)(all * end / weight) : all;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) it.n_tiles[t] = max(min(n[t], end) - it.first, 0);
+    for (int t = 0; t < 2; ++t) it.n_tiles[t] = max(min(n[t], to) - it.first, 0);
     it.n_all = max(it.n_tiles[0], it.n_tiles[1]);
-    return it.lq > 0;
 }
 
 // Lowest position that the query `tok` of a request sees behind the first tokens; off: position of the request's first.
@@ -300,8 +374,8 @@ __device__ __forceinline__ int32_t low_of(const Args &a, int32_t off, int32_t to
     return a.window ? (int32_t)max((int64_t)off + tok - a.window + 1, (int64_t)0) : 0;
 }
 
-// Registers move to the softmax warps: 256 * 176 + 256 * 80 = 512 * 128, the launch's own.
-constexpr int kRegsSoftmax = 176, kRegsOther = 80;
+// Registers move to the softmax warps: 256 * 184 + 256 * 72 = 512 * 128, the launch's own.
+constexpr int kRegsSoftmax = 184, kRegsOther = 72;
 constexpr uint32_t kWarpLoad = 8, kWarpMma = 9, kWarpNote = 10, kWarpUnpack = 12;  // warps 0-7: softmax
 
 // Where a lane finds its codes and scales of K or V in a granule, and where it puts them as 16-bit values in a tile, in
@@ -415,14 +489,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
         sm.abort = 0;
     }
     if (warp == kWarpMma) pk::tmem_alloc(pk::smem_addr(&sm.tmem), 512);
-    const uint64_t *plan = a.plan;
+    const int64_t *plan = a.plan;
     const int64_t *q_off = a.q_off;
     const int32_t *kv_len = a.kv_len;
     const uint32_t *pages = a.pages;
     const uint8_t *pool = a.pool;
     pk::pdl_wait(plan, q_off, kv_len, pages, pool);
     pk::pdl_launch_dependents();
-    if (warp == kWarpLoad && !a.listed) plan_here(a, sm, q_off, kv_len);
+    if (warp == kWarpLoad && !a.plan) plan_here(a, sm, q_off, kv_len);
     pk::tmem_fence_before();
     __syncthreads();
     pk::tmem_fence_after();
@@ -435,14 +509,46 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
     };
 
     Item it;
-    uint32_t turn = 0;  // items before the present one
-    bool more = find_item(a, sm, plan, q_off, kv_len, blockIdx.x, it);
-    // every other turn runs through the blocks backwards: one that got the heaviest item of a turn gets the lightest of
-    // the next
-    auto take_next = [&]() {
-        ++turn;
-        const uint64_t next = (uint64_t)turn * gridDim.x + (turn & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-        more = next < a.most_items && find_item(a, sm, plan, q_off, kv_len, (uint32_t)next, it);
+    bool more;
+    {
+        const Shares shares = shares_of(a, sm, plan);
+        int64_t x = shares.start(min(blockIdx.x, shares.n));
+        it.line = shares.start(min(blockIdx.x + 1, shares.n));
+        it.whole = shares.whole;
+        more = x < it.line;
+        while (more) {
+            const int64_t before = find_request(a, sm, plan, q_off, kv_len, x, it);
+            const Units units(a, it.q);
+            it.at = place_of(units, it.at.r, before, x);
+            if (!it.whole || it.at.pos == 0) {
+                cut_item(a, units, it.line - x, it);
+                break;
+            }
+            x += units.weight(it.at.u) - it.at.pos;  // the next unit
+            more = x < it.line;
+        }
+    }
+    // Each warp finds the block's items for itself.  While it goes through one's keys, what it does not need of it lies
+    // in shared memory, where it does not take registers from the work.
+    auto aside = [&]() {
+        put_aside(it, sm.item[warp], lane);
+        __syncwarp();
+    };
+    auto take_next = [&]() {  // it begins with a unit
+        take_back(it, sm.item[warp]);
+        more = it.left > 0;
+        if (!more) return;
+        Units units(a, it.q);
+        it.at.pos = 0;
+        if (++it.at.u == units.n) {
+            it.at.u = 0;
+            if (++it.at.part == a.kv_heads * a.chunks) {
+                find_request(a, sm, plan, q_off, kv_len, it.line - it.left, it);
+                it.at.part = 0;
+                units = Units(a, it.q);
+            }
+        }
+        cut_item(a, units, it.left, it);
     };
     if (warp >= kWarpLoad) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
@@ -454,14 +560,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
             pk::fence_proxy_async();  // pages written by an earlier kernel are read by the async proxy
             while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
                 const uint32_t v0 = 8 * (uint32_t)it.first, v1 = min(8 * (uint32_t)(it.first + it.n_all), it.n_gran);
-                const uint32_t *row = pages + (uint64_t)it.r * a.page_stride;
+                const uint32_t *row = pages + (uint64_t)it.at.r * a.page_stride;
+                const uint32_t head = it.head(a);
+                const int32_t skip = it.skip, n_all = it.n_all;
+                const bool two[2] = {it.n_tiles[0] > 0, it.n_tiles[1] > 0};
+                const int32_t q_head = (int32_t)(head * a.group + it.chunk(a) * a.tile_heads), q_row = it.q.q0 + it.tok0(a);
+                aside();
                 uint64_t where = 0;  // lane l: address of the granule `base` + l of the list
                 bool lost = false;   // slot 0's bytes stand in for a slot out of range
                 auto find_granules = [&](uint32_t base) {
                     const uint32_t v = base + lane;
                     lost = false;
                     if (v < v1) {
-                        const uint32_t gr = v >= a.sink_grans ? v + (uint32_t)it.skip / 16 : v;
+                        const uint32_t gr = v >= a.sink_grans ? v + (uint32_t)skip / 16 : v;
                         const uint32_t page = pow2 ? gr >> slot_shift : gr / a.page_grans;
                         uint64_t slot = __ldcg(row + page);
                         if (slot >= a.n_slots) {
@@ -470,10 +581,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                             lost = true;
                         }
                         where = reinterpret_cast<uint64_t>(pool) + slot * a.page_bytes +
-                                ((uint64_t)it.head * a.page_grans + (gr - page * a.page_grans)) * L::kGran;
+                                ((uint64_t)head * a.page_grans + (gr - page * a.page_grans)) * L::kGran;
                     }
                 };
-                for (uint32_t v = v0; ok && it.n_all > 0 && v < v1; v += 8) {
+                for (uint32_t v = v0; ok && n_all > 0 && v < v1; v += 8) {
                     if (((v - v0) & 31) == 0) find_granules(v);
                     const uint32_t n = min(v1 - v, 8u), from = ((v - v0) & 31) + (lane & 7);
                     const uint64_t src = __shfl_sync(0xffffffffu, where, from);
@@ -497,16 +608,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                         const uint32_t q_bytes = a.tile_tokens * a.tile_heads * 128 * (D / 64);
 #pragma unroll
                         for (int t = 0; t < 2; ++t) {
-                            if (!ok || it.n_tiles[t] == 0) continue;
+                            if (!ok || !two[t]) continue;
                             ok = nq[t] == 0 || pk::mbar_wait(pk::smem_addr(&sm.q_empty[t]), (nq[t] - 1) & 1);
                             if (!ok) break;
                             const uint32_t bar = pk::smem_addr(&sm.q_full[t]);
                             pk::mbar_expect(bar, q_bytes);
 #pragma unroll
                             for (int b = 0; b < D / 64; ++b)
-                                pk::tile_load3(smem + t * L::kTile + b * 16384, &map_q, b * 64,
-                                               (int)(it.head * a.group + it.chunk * a.tile_heads),
-                                               it.q0 + it.tok0 + t * (int)a.tile_tokens, bar);
+                                pk::tile_load3(smem + t * L::kTile + b * 16384, &map_q, b * 64, q_head,
+                                               q_row + t * (int)a.tile_tokens, bar);
                             ++nq[t];
                         }
                     }
@@ -547,8 +657,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     }
                     ++items;
                 }
-                for (int32_t j = 0; j < it.n_all; ++j) {
-                    const uint32_t v0 = 8 * (uint32_t)(it.first + j), have = min(it.n_gran - v0, 8u);
+                const int32_t n_all = it.n_all, skip = it.skip, len = it.q.len;
+                const uint32_t first = (uint32_t)it.first, n_gran = it.n_gran;
+                aside();
+                for (int32_t j = 0; j < n_all; ++j) {
+                    const uint32_t v0 = 8 * (first + j), have = min(n_gran - v0, 8u);
                     // Every warp waits for all of the tile's granules, a lane each, and gives all of them back: a place's
                     // next user may be another warp, and one that has not seen a use of it, or sees it too late, would
                     // take one state of the barrier for another.
@@ -559,7 +672,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     auto place = [&](uint32_t g) { return smem_c + L::kGranRing + (count + g) % L::kGrans * L::kGran; };
                     // tokens of a granule before the request's end
                     auto valid = [&](uint32_t g) {
-                        return it.len - (int32_t)(16 * (v0 + g)) - (v0 + g >= a.sink_grans ? it.skip : 0);
+                        return len - (int32_t)(16 * (v0 + g)) - (v0 + g >= a.sink_grans ? skip : 0);
                     };
                     const uint32_t mine = have > 2 * w ? min(have - 2 * w, 2u) : 0;  // granules, of an unpacking warp
                     uint8_t *tile = smem_c + L::kRing + n % L::kStages * L::kTile + (notes ? 0 : 32 * w * 128);
@@ -637,6 +750,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
             uint32_t ring = 0, use = 0;             // next ring stage, and how often the ring has been gone round
             uint32_t ni0 = 0, ni1 = 0, nq0 = 0, nq1 = 0;  // key tiles and Q tiles used so far, by tile
             bool ok = true;
+            if (a.blocks > 1) {  // what k_chunk_join has to know of the unit that this share's beginning cuts
+                const Shares shares = shares_of(a, sm, plan);
+                Cut cut = {-1, 0, 0, 0, 0, 0};
+                if (more && it.at.pos > 0) {
+                    const Units units(a, it.q);
+                    const int64_t unit = shares.start(blockIdx.x) - it.at.pos;  // where it begins
+                    const uint32_t before = shares.block_of(unit);
+                    const int32_t tok0 = it.tok0(a);
+                    const uint32_t head0 = it.chunk(a) * a.tile_heads;
+                    if (before + 1 == blockIdx.x)
+                        cut = Cut{(int32_t)before, (int32_t)shares.block_of(unit + units.weight(it.at.u) - 1), it.q.q0 + tok0,
+                                  min(it.q.lq - tok0, units.step), (int32_t)(it.head(a) * a.group + head0),
+                                  (int32_t)min(a.group - head0, a.tile_heads)};
+                }
+                if (lane == 0) a.cuts[blockIdx.x] = cut;
+            }
             auto wait_full = [&](uint32_t st, uint32_t round) {
                 return pk::mbar_wait_warp(pk::smem_addr(&sm.full[st]), round & 1);
             };
@@ -752,11 +881,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
             const int32_t n_tiles = t ? it.n_tiles[1] : it.n_tiles[0];
             bool on;
             {
-                const int32_t tok0 = it.tok0 + (int32_t)(t * a.tile_tokens), off = it.len - it.lq;
+                const int32_t tok0 = it.tok0(a) + (int32_t)(t * a.tile_tokens), off = it.q.len - it.q.lq;
                 const int32_t base = it.first * kKeys + it.skip;  // from positions to places behind the piece's first one
                 const int32_t all_last = off + tok0 - base;
-                const int32_t all_low = low_of(a, off, min(tok0 + (int32_t)a.tile_tokens, it.lq) - 1) - base;
-                const int32_t sinks = (int32_t)a.sinks - it.first * kKeys, gh0 = (int32_t)(it.chunk * a.tile_heads);
+                const int32_t all_low = low_of(a, off, min(tok0 + (int32_t)a.tile_tokens, it.q.lq) - 1) - base;
+                const int32_t sinks = (int32_t)a.sinks - it.first * kKeys, gh0 = (int32_t)(it.chunk(a) * a.tile_heads);
                 if (lane == 0) {
                     mine->causal = ((all_last - (kKeys - 1)) >> 7) + 1;
                     mine->hides[0] = sinks >> 7;
@@ -765,13 +894,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     mine->base = base;
                     mine->sinks = sinks;
                     mine->tok0 = tok0;
-                    mine->row0 = it.q0 + tok0;
-                    mine->head0 = it.head * a.group + gh0;
-                    mine->part = it.pieces > 1 ? ((int64_t)it.index * 2 + t) * kRows : -1;
+                    mine->row0 = it.q.q0 + tok0;
+                    mine->head0 = (int32_t)(it.head(a) * a.group) + gh0;
+                    // a block has one piece at most that begins inside a unit, and one that only ends there
+                    mine->part = it.cut ? (int32_t)(((2 * blockIdx.x + (it.at.pos == 0)) * 2 + t) * kRows) : -1;
                     mine->n_all = it.n_all;
                 }
-                on = row_tok < (int32_t)a.tile_tokens && tok0 + row_tok < it.lq && gh0 + row_head < (int32_t)a.group;
-                __syncwarp();
+                on = row_tok < (int32_t)a.tile_tokens && tok0 + row_tok < it.q.lq && gh0 + row_head < (int32_t)a.group;
+                aside();
             }
             // a weight is 2^(score - ref + fine), and fine is 0 but for a reference of kFar and more
             float ref = -FLT_MAX, fine = 0.0f, sum = 0.0f;
@@ -784,12 +914,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 pk::tmem_fence_after();
                 // the row sees the tile's keys up to `see` that are not below `from`, or are below `first`
                 const bool edge = j >= mine->causal || (j >= mine->hides[0] && j < mine->hides[1]);
-                int32_t see = kKeys, from = 0, first = 0;
+                int32_t see = kKeys - 1, from = 0, first = 0;
                 if (edge) {
                     const int32_t tok = mine->tok0 + row_tok, x0 = j * kKeys;
-                    see = on ? mine->off + tok - mine->base - x0 : -1;
-                    from = low_of(a, mine->off, tok) - mine->base - x0;
-                    first = mine->sinks - x0;
+                    if (on) {
+                        see = mine->off + tok - mine->base - x0;
+                        from = low_of(a, mine->off, tok) - mine->base - x0;
+                        first = mine->sinks - x0;
+                    }
                 }
                 auto hidden = [&](int32_t i) { return i > see || (i < from && i >= first); };
                 const uint32_t note = (tiles + j) % kNotes;
@@ -801,6 +933,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                         if ((flags >> (i / 64 * 8) & kMarked) && !hidden(i)) marked |= sm.marked[note][i];
                 }
                 uint32_t x[3][32];
+                // -infinity for the keys of a chunk of 32 that the row does not see; most chunks of an edge tile are seen
+                // whole by all of a warp's rows.
+                auto mask = [&](int c, uint32_t(&y)[32]) {
+                    auto up_to = [&](int32_t n) { n -= 32 * c; return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; };
+                    const uint32_t seen = up_to(see + 1) & (~up_to(from) | up_to(first));
+                    if (__all_sync(0xffffffffu, seen == ~0u)) return;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (!(seen & 1u << i)) y[i] = 0xff800000u;
+                };
                 // Chunk c of the scores, 32 keys.  Loads run ahead (1 and 2 behind 0's use, 3 behind 1's).  Masked or
                 // not is known at compile time.
                 auto chunk = [&](int c, auto masked) -> uint32_t(&)[32] {
@@ -814,11 +956,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                         pk::tmem_wait_load(x[2]);
                         pk::tmem_load32(ts + 96, x[0]);
                     }
-                    if (decltype(masked)::value) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (hidden(32 * c + i)) y[i] = 0xff800000u;
-                    }
+                    if (decltype(masked)::value) mask(c, y);
                     return y;
                 };
                 auto largest = [&](auto masked) {
@@ -878,11 +1016,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     if (__any_sync(0xffffffffu, fine != 0.0f)) return weigh_far();
                     return edge ? weigh(std::true_type{}) : weigh(std::false_type{});
                 };
-                // Moves the reference of the rows that `over` names to their largest score; their sum and output so
-                // far are rescaled.  That score's weight is then a power of two, which rounding leaves as it is: a
-                // row with one key, or one that outweighs the others, gets its value of V and no more error.
-                auto move_ref = [&](bool over) {
-                    const float top = edge ? largest(std::true_type{}) : largest(std::false_type{}), m = top * scale2;
+                // Moves the reference of the rows that `over` names to the score `top`; their sum so far is rescaled.
+                // Returns the factor.  That score's weight is then a power of two, which rounding leaves as it is: a row
+                // with one key, or one that outweighs the others, gets its value of V and no more error.
+                auto move_ref = [&](bool over, float top) {
+                    const float m = top * scale2;
                     const bool moves = over && m > -INFINITY, far = moves && fabsf(m) >= kFar;
                     const float next = !moves ? ref : far ? m : m - kBase;
                     // far: what m's rounding lost comes off again, so the largest weight is 2^kBase or, where kBase
@@ -892,32 +1030,40 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     ref = next;
                     fine = next_fine;
                     sum *= f;
-                    if (j == 0) return;
-                    ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
-                    if (!ok) return;
-                    pk::tmem_fence_after();
-#pragma unroll 1
-                    for (int d = 0; d < D / 32; ++d) {
-                        pk::tmem_load32(to + 32 * d, x[0]);
-                        pk::tmem_wait_load(x[0]);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) x[0][i] = __float_as_uint(__uint_as_float(x[0][i]) * f);
-                        pk::tmem_store32(to + 32 * d, x[0]);
-                    }
+                    return f;
                 };
-                if (j == 0) move_ref(on);
+                if (j == 0) {  // from 32 keys alone: mostly no other is 2^11 times as heavy as the heaviest of them
+                    pk::tmem_load32(ts, x[0]);
+                    pk::tmem_wait_load(x[0]);
+                    if (edge) mask(0, x[0]);
+                    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) m4[i & 3] = fmaxf(m4[i & 3], __uint_as_float(x[0][i]));
+                    move_ref(on, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])));
+                }
                 // One pass over the scores takes the weights by the reference so far, with no look at the scores
                 // first: a weight that has outgrown it shows in the sum, and only then the reference is moved and
                 // the pass done again.  A row that saw no key yet (its window begins further on) has the lowest
                 // reference, by which any weight is infinite.  Once does: behind a move no weight is above
-                // 2^(kBase + 2).  Rows without a query have no say.
+                // 2^(kBase + 2).  Rows without a query, whose scores may be anything, have no say.
                 float part_sum = weigh_any();
                 if (__any_sync(0xffffffffu, on && part_sum > kTop)) {
-                    move_ref(on && part_sum > kTop);
-                    if (!ok) break;
+                    const float f = move_ref(on && part_sum > kTop, edge ? largest(std::true_type{}) : largest(std::false_type{}));
+                    if (j > 0) {  // the output so far too
+                        ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
+                        if (!ok) break;
+                        pk::tmem_fence_after();
+#pragma unroll 1
+                        for (int d = 0; d < D / 32; ++d) {
+                            pk::tmem_load32(to + 32 * d, x[0]);
+                            pk::tmem_wait_load(x[0]);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[0][i] = __float_as_uint(__uint_as_float(x[0][i]) * f);
+                            pk::tmem_store32(to + 32 * d, x[0]);
+                        }
+                    }
                     part_sum = weigh_any();
                 }
-                if (!ok) break;
                 sum += part_sum;
                 pk::tmem_store32(ts, p[0]);  // over the scores, which every pass is done with
                 pk::tmem_store32(ts + 32, p[1]);
@@ -931,8 +1077,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
             if (ok && n_tiles > 0) ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
             if (!ok) break;
             if (lost) sum = __int_as_float(0x7fffffff);
-            const int64_t part = mine->part >= 0 ? mine->part + row : -1;
-            const bool cut = part >= 0;
+            const bool cut = mine->part >= 0;
+            const uint64_t part = cut ? (uint64_t)(mine->part + row) : 0;
             const int64_t q_row = (int64_t)mine->row0 + row_tok;
             const uint32_t qh = (uint32_t)(mine->head0 + row_head);
             const float inv = cut ? 1.0f : sum == 0.0f ? 0.0f : a.v_scale / sum;
@@ -984,102 +1130,98 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
     }
 }
 
-// Joins the pieces of the rows whose keys were cut, a warp a row, in the order of the keys.
-constexpr int kJoinThreads = 256;
+// Joins the pieces of the units that were cut, in the order of their keys: kJoinBlocks for a unit, a warp a row.
+constexpr int kJoinThreads = 256, kJoinBlocks = 8;
 template <int D, uint32_t DT>
 __global__ void __launch_bounds__(kJoinThreads) k_chunk_join(const Args a) {
-    const uint64_t *plan = a.plan;
-    const int64_t *q_off = a.q_off;
-    const int32_t *kv_len = a.kv_len;
+    const Cut *cuts = a.cuts;
     const float4 *ml = a.part_ml;
     const float *po = a.part_o;
-    pk::pdl_wait(plan, q_off, kv_len, ml, po);
+    pk::pdl_wait(cuts, ml, po);
     pk::pdl_launch_dependents();
-    const uint32_t lane = threadIdx.x & 31;
-    const uint64_t id = (uint64_t)blockIdx.x * (kJoinThreads / 32) + threadIdx.x / 32, token = id / a.q_heads;
-    const uint32_t qh = (uint32_t)(id % a.q_heads);
-    if (token >= a.n_q || __ldcg(plan + 1 + a.R) == 0) return;  // uniform; no items where an offset is bad
-    const uint32_t r = pk::warp_find_request(q_off, a.R, (int64_t)token);
-    const int64_t qa = __ldcg(q_off + r), qb = __ldcg(q_off + r + 1);
-    if ((int64_t)token < qa || (int64_t)token >= qb) return;
-    const uint32_t pieces = pieces_of(tiles_of(a, good_length(a, __ldcg(kv_len + r))), (uint32_t)__ldcg(plan));
-    if (pieces == 1) return;  // the row is written
-    const uint32_t tok = (uint32_t)((int64_t)token - qa), head = qh / a.group, gh = qh % a.group;
-    const uint32_t t = tok / a.tile_tokens % 2;
-    const uint32_t row = tok % a.tile_tokens * a.tile_heads + gh % a.tile_heads;
-    const uint32_t x = (tok / (2 * a.tile_tokens) * a.chunks + gh / a.tile_heads) * pieces;
-    const uint64_t end = __ldcg(plan + 2 + r);
-    auto part_of = [&](uint32_t piece) {
-        return (((end - 1 - (x + piece)) * a.kv_heads + head) * 2 + t) * (uint64_t)kRows + row;
-    };
-    // the exponent of a piece's weights is ref - fine, which 32 bits may not hold: differences are taken part by part
-    float ref = -FLT_MAX, fine = 0.0f;
-    for (uint32_t p = 0; p < pieces; ++p) {
-        const float4 y = __ldcg(ml + part_of(p));
-        if ((y.x - ref) - (y.y - fine) > 0.0f) ref = y.x, fine = y.y;
-    }
-    constexpr int kPer = D / 32;
-    float sum = 0.0f, o[kPer] = {};
-#pragma unroll 4
-    for (uint32_t p = 0; p < pieces; ++p) {
-        const uint64_t at = part_of(p);
-        const float4 y = __ldcg(ml + at);
-        float z[kPer];
-#pragma unroll
-        for (int i = 0; i < kPer; i += 2) {
-            const float2 u = __ldcg(reinterpret_cast<const float2 *>(po + at * D + lane * kPer + i));
-            z[i] = u.x, z[i + 1] = u.y;
+    cuts += blockIdx.x / kJoinBlocks + 1;
+    const int4 where = __ldcg(reinterpret_cast<const int4 *>(cuts));
+    const int2 heads = __ldcg(reinterpret_cast<const int2 *>(cuts) + 2);
+    if (where.x < 0) return;  // uniform
+    const uint32_t lane = threadIdx.x & 31, b0 = (uint32_t)where.x, n = (uint32_t)where.y - b0 + 1;
+    for (uint32_t row = blockIdx.x % kJoinBlocks + threadIdx.x / 32 * kJoinBlocks; row < 2 * kRows;
+         row += kJoinBlocks * (kJoinThreads / 32)) {
+        const uint32_t in = row % kRows, tok = in / a.tile_heads, gh = in % a.tile_heads, t = row / kRows;
+        if (tok >= a.tile_tokens || t * a.tile_tokens + tok >= (uint32_t)where.w || gh >= (uint32_t)heads.y) continue;
+        const int64_t token = (int64_t)where.z + t * a.tile_tokens + tok;
+        const uint32_t qh = (uint32_t)heads.x + gh;
+        auto part_of = [&](uint32_t i) { return (uint64_t)(2 * (b0 + i) + (i == 0)) * 2 * kRows + row; };
+        // The exponent of a piece's weights is ref - fine, which 32 bits may not hold: differences are taken part by part.
+        auto more = [](float2 x, float2 y) { return (x.x - y.x) - (x.y - y.y); };
+        float2 top = make_float2(-FLT_MAX, 0.0f);
+        for (uint32_t i = lane; i < n; i += 32) {
+            const float4 y = __ldcg(ml + part_of(i));
+            if (more(make_float2(y.x, y.y), top) > 0.0f) top = make_float2(y.x, y.y);
         }
-        if (y.z == 0.0f) continue;  // a piece without a key that the row sees
-        const float f = pk::ex2((y.x - ref) - (y.y - fine));
-        sum += f * y.z;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) o[i] += f * z[i];
+        for (int d = 16; d; d /= 2) {
+            const float2 y = make_float2(__shfl_xor_sync(0xffffffffu, top.x, d), __shfl_xor_sync(0xffffffffu, top.y, d));
+            if (more(y, top) > 0.0f) top = y;
+        }
+        const float ref = __shfl_sync(0xffffffffu, top.x, 0), fine = __shfl_sync(0xffffffffu, top.y, 0);
+        constexpr int kPer = D / 32;
+        float sum = 0.0f, o[kPer] = {};
+        for (uint32_t i0 = 0; i0 < n; i0 += 32) {
+            const float4 y = i0 + lane < n ? __ldcg(ml + part_of(i0 + lane)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            const float f = y.z == 0.0f ? 0.0f : pk::ex2(more(make_float2(y.x, y.y), make_float2(ref, fine)));
+#pragma unroll 8
+            for (uint32_t i = 0; i < min(n - i0, 32u); ++i) {
+                const float w = __shfl_sync(0xffffffffu, f, i);
+                sum += w * __shfl_sync(0xffffffffu, y.z, i);
+                const uint64_t at = part_of(i0 + i) * D + lane * kPer;
+#pragma unroll
+                for (int k = 0; k < kPer; k += 2) {
+                    const float2 u = __ldcg(reinterpret_cast<const float2 *>(po + at + k));
+                    o[k] += w * u.x;
+                    o[k + 1] += w * u.y;
+                }
+            }
+        }
+        const float inv = sum == 0.0f ? 0.0f : a.v_scale / sum;
+#pragma unroll
+        for (int i = 0; i < kPer; i += 2)
+            *reinterpret_cast<uint32_t *>(a.out + token * a.o_ts + (int64_t)qh * a.o_hs + lane * kPer + i) =
+                pk::Elem<DT>::from2(o[i] * inv, o[i + 1] * inv);
+        if (lane == 0 && a.lse)
+            a.lse[token * a.q_heads + qh] = sum == 0.0f ? -INFINITY : (ref - fine + log2f(sum)) * 0.69314718055994531f;
     }
-    const float inv = sum == 0.0f ? 0.0f : a.v_scale / sum;
-#pragma unroll
-    for (int i = 0; i < kPer; i += 2)
-        *reinterpret_cast<uint32_t *>(a.out + (int64_t)token * a.o_ts + (int64_t)qh * a.o_hs + lane * kPer + i) =
-            pk::Elem<DT>::from2(o[i] * inv, o[i + 1] * inv);
-    if (lane == 0 && a.lse)
-        a.lse[token * a.q_heads + qh] = sum == 0.0f ? -INFINITY : (ref - fine + log2f(sum)) * 0.69314718055994531f;
 }
 
-// How the call is cut: what the host knows are bounds, the kernels see the lengths.
+// What the host knows of a call are bounds; the kernels see the lengths.
 struct Plan {
-    uint64_t units, items;  // at most: before the keys are cut, and behind
-    uint32_t target, least;
-    uint64_t plan_bytes, ml_bytes, o_bytes;
+    uint64_t units, blocks;  // at most
+    uint64_t plan_bytes, cut_bytes, ml_bytes, o_bytes;
 };
 
 constexpr uint64_t kSms = 152;
-constexpr uint32_t kLeastTiles = 4;
 Plan plan_of(const pk_kv_cache &kv, uint32_t R, uint64_t n_q, uint32_t q_heads, uint64_t page_stride, uint32_t window,
              uint32_t sinks) {
     Plan p;
     p.units = pk_attend_prompt_items(n_q, R, q_heads, kv.kv_heads);
-    p.least = kLeastTiles;
-    uint64_t grans = (page_stride * kv.page_tokens + 15) / 16;
-    if (window) grans = std::min<uint64_t>(grans, ((uint64_t)sinks + 15) / 16 + ((uint64_t)window + 2 * kRows + 14) / 16 + 1);
-    const uint64_t most = ((grans + 7) / 8 + p.least - 1) / p.least;  // pieces of an item
-    p.target = p.units <= 2 * kSms && most > 1 ? 2 * kSms : 0;
-    p.items = p.target ? std::min(p.units + p.target, p.units * most) : p.units;
-    p.plan_bytes = (((uint64_t)R + 2) * 8 + 31) & ~31ull;
-    p.ml_bytes = p.target ? p.items * 2 * kRows * 16 : 0;
-    p.o_bytes = p.target ? p.items * 2 * kRows * kv.head_dim * 4 : 0;
+    uint64_t keys = page_stride * kv.page_tokens;
+    if (window) keys = std::min<uint64_t>(keys, (uint64_t)sinks + 15 + window + 2 * kRows + 15);
+    const uint64_t share = (uint64_t)kUnitCost + keys;  // of a unit
+    p.blocks = p.units > kSms * kLeastShare ? kSms : std::min(kSms, std::max<uint64_t>(p.units * share / kLeastShare, 1));
+    p.plan_bytes = R > 32 ? (((uint64_t)R + 2) * 8 + 31) & ~31ull : 0;
+    p.cut_bytes = p.blocks * sizeof(Cut);
+    p.ml_bytes = p.blocks > 1 ? 2 * p.blocks * 2 * kRows * 16 : 0;
+    p.o_bytes = p.blocks > 1 ? 2 * p.blocks * 2 * kRows * kv.head_dim * 4 : 0;
     return p;
 }
 
 template <int D, uint32_t DT>
-cudaError_t launch(const Args &a, unsigned grid, const CUtensorMap &mq, cudaStream_t s) {
+cudaError_t launch(const Args &a, const CUtensorMap &mq, cudaStream_t s) {
     constexpr size_t smem = Layout<D>::kBytes + sizeof(Small);
     static_assert(smem <= 227 * 1024, "shared memory of a block");
     static std::atomic<uint64_t> seen{0};
     cudaError_t e = pk_allow_smem(k_attend_chunk<D, DT>, smem, seen);
-    if (e == cudaSuccess) e = pk_launch_smem(k_attend_chunk<D, DT>, grid, kThreads, smem, s, a, mq);
-    if (e == cudaSuccess && a.target)
-        e = pk_launch(k_chunk_join<D, DT>, (unsigned)((a.n_q * a.q_heads + kJoinThreads / 32 - 1) / (kJoinThreads / 32)),
-                      kJoinThreads, s, a);
+    if (e == cudaSuccess) e = pk_launch_smem(k_attend_chunk<D, DT>, a.blocks, kThreads, smem, s, a, mq);
+    if (e == cudaSuccess && a.blocks > 1) e = pk_launch(k_chunk_join<D, DT>, (a.blocks - 1) * (unsigned)kJoinBlocks, kJoinThreads, s, a);
     return e;
 }
 
@@ -1088,8 +1230,8 @@ cudaError_t launch(const Args &a, unsigned grid, const CUtensorMap &mq, cudaStre
 uint64_t pk_attend_chunk_scratch_bytes_impl(const pk_kv_cache &kv, uint32_t R, uint64_t n_q, uint32_t q_heads,
                                             uint64_t page_stride, uint32_t window, uint32_t sinks) {
     const Plan p = plan_of(kv, R, n_q, q_heads, page_stride, window, sinks);
-    if (p.items > 0x7fffffffull) return UINT64_MAX;
-    return p.plan_bytes + p.ml_bytes + p.o_bytes;
+    if (p.units > 0x7fffffffull) return UINT64_MAX;
+    return p.plan_bytes + p.cut_bytes + p.ml_bytes + p.o_bytes;
 }
 
 cudaError_t pk_launch_attend_chunk(const pk_kv_cache &kv, uint32_t dtype, const pk_heads &q, const pk_heads &out,
@@ -1126,26 +1268,20 @@ cudaError_t pk_launch_attend_chunk(const pk_kv_cache &kv, uint32_t dtype, const 
     a.o_hs = out.head_stride;
     a.wide_out = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0 && a.o_ts % 16 == 0 && a.o_hs % 16 == 0;
     a.lse = lse;
-    a.target = p.target;
-    a.least = p.least;
-    a.listed = R > 32;
-    a.most_items = (uint32_t)p.items;
+    a.blocks = (uint32_t)p.blocks;
     uint8_t *at = static_cast<uint8_t *>(scratch);
-    a.plan = reinterpret_cast<uint64_t *>(at);
-    a.part_ml = reinterpret_cast<float4 *>(at + p.plan_bytes);
-    a.part_o = reinterpret_cast<float *>(at + p.plan_bytes + p.ml_bytes);
+    a.plan = R > 32 ? reinterpret_cast<int64_t *>(at) : nullptr;
+    a.cuts = reinterpret_cast<Cut *>(at + p.plan_bytes);
+    a.part_ml = reinterpret_cast<float4 *>(at + p.plan_bytes + p.cut_bytes);
+    a.part_o = reinterpret_cast<float *>(at + p.plan_bytes + p.cut_bytes + p.ml_bytes);
     a.status = status;
-    int device = 0, sms = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     CUtensorMap mq;
-    if (e == cudaSuccess) e = map_of(&mq, q, n_q, q_heads, kv.head_dim, dtype, a.tile_tokens, a.tile_heads);
-    if (e == cudaSuccess && a.listed) e = pk_launch(k_chunk_plan, 1, kPlanThreads, s, a);
+    cudaError_t e = map_of(&mq, q, n_q, q_heads, kv.head_dim, dtype, a.tile_tokens, a.tile_heads);
+    if (e == cudaSuccess && a.plan) e = pk_launch(k_chunk_plan, 1, kPlanThreads, s, a);
     if (e != cudaSuccess) return e;
-    const unsigned grid = (unsigned)std::min<uint64_t>(p.items, (uint64_t)sms);
     if (kv.head_dim == 128)
-        e = dtype == PK_BF16 ? launch<128, PK_BF16>(a, grid, mq, s) : launch<128, PK_FP16>(a, grid, mq, s);
+        e = dtype == PK_BF16 ? launch<128, PK_BF16>(a, mq, s) : launch<128, PK_FP16>(a, mq, s);
     else
-        e = dtype == PK_BF16 ? launch<64, PK_BF16>(a, grid, mq, s) : launch<64, PK_FP16>(a, grid, mq, s);
+        e = dtype == PK_BF16 ? launch<64, PK_BF16>(a, mq, s) : launch<64, PK_FP16>(a, mq, s);
     return e != cudaSuccess ? e : cudaGetLastError();
 }

@@ -236,7 +236,7 @@ class Cta:
         assert not self.pipe, "a product or an arrival is left after the CTA's end"
 
 
-@pytest.mark.parametrize("stages,grans", [(3, 28), (8, 32)])
+@pytest.mark.parametrize("stages,grans", [(3, 26), (8, 32)])
 def test_every_interleaving_tried_is_sound(stages, grans):
     rng = random.Random(11)
     for _ in range(100):
@@ -251,6 +251,6 @@ def test_every_interleaving_tried_is_sound(stages, grans):
 def test_many_short_items():
     """Items of one key tile, where the warps run furthest ahead of one another."""
     rng = random.Random(12)
-    for stages, grans in ((3, 28), (8, 32)):
+    for stages, grans in ((3, 26), (8, 32)):
         for _ in range(40):
             Cta([(rng.choice((0, 1)), rng.choice((0, 1)), rng.choice((1, 1, 2))) for _ in range(30)], stages, grans, rng).run()
