@@ -130,7 +130,8 @@ struct Shares {
         n = (uint32_t)min((int64_t)a.blocks, max(total / kLeastShare, (int64_t)1));
         each = total / n;
         more = (uint32_t)(total - each * n);
-        whole = units == 0 || (units + n - 1) / n * (total / units) <= each + kCutCost;
+        const int64_t one = units ? total / units : 0;
+        whole = max((units + n - 1) / n * one, each + one / 2) <= each + kCutCost;
     }
     __device__ __forceinline__ int64_t start(uint32_t b) const { return each * b + min(b, more); }
     __device__ __forceinline__ uint32_t block_of(int64_t x) const {
@@ -244,7 +245,7 @@ struct Layout {
     static constexpr uint32_t kTile = 128 * D * 2;  // 128 rows; blocks of [128][64] values, 16 KB each
     static constexpr uint32_t kStages = D == 128 ? 3 : 8;
     static constexpr uint32_t kGran = pk::Granule<D>::kBytes;
-    static constexpr uint32_t kGrans = D == 128 ? 26 : 32;
+    static constexpr uint32_t kGrans = D == 128 ? 28 : 32;
     static constexpr uint32_t kRing = 2 * kTile;
     static constexpr uint32_t kGranRing = kRing + kStages * kTile;
     static constexpr uint32_t kBytes = kGranRing + kGrans * kGran;
@@ -253,13 +254,20 @@ struct Layout {
 constexpr uint32_t kNotes = 8;       // key tiles whose notes are kept: they are read before the ring has gone round
 constexpr uint32_t kMarked = 1, kLost = 2;
 constexpr uint32_t kMakers = 6;      // warps that make tiles of granules
+constexpr uint32_t kItems = 4;       // items that the loading warp is ahead at most
 
-// A softmax warp's tile of the present item.
-struct TileOf {
-    int32_t causal, hides[2];  // from the first on some query does not see some key; between the others too
-    int32_t off, base;         // position of the request's first query; what a position is more than its place in the piece
-    int32_t sinks, tok0, row0, head0, n_all;
-    int32_t part;              // where the piece's rows go; -1: the unit is not cut
+// What the other warps have to know of an item, from the loading warp.
+struct Piece {
+    struct Tile {
+        int32_t causal, hides[2];  // key tiles from the first on hide some key from some query; those between the others too
+        int32_t off, base;         // position of the request's first query; what a position is more than its place in the piece
+        int32_t sinks;             // place behind the first tokens
+        int32_t tok0, row0, tokens, head0, heads;  // first token of the request, its row; how many; the same of query heads
+        int32_t part;              // where the rows of a piece go; -1: the unit is not cut
+    } tile[2];
+    int32_t n_tiles[2], n_all;     // key tiles; n_all -1: no item, the end
+    int32_t first, skip, len;
+    uint32_t n_gran;
 };
 
 struct Small {
@@ -267,17 +275,16 @@ struct Small {
     uint64_t gran_full[32], gran_empty[32]; // the same of granules
     uint64_t q_full[2], q_empty[2];
     uint64_t s_full[2], p_ready[2], o_done[2];
+    uint64_t item_full[kItems], item_empty[kItems];
     uint64_t over;                          // every product that was issued is done (a matrix warp that gave up)
     uint32_t tmem, abort;
-    int32_t work[8][2];                     // by item with keys: key tiles of its two tiles, for the matrix warp; 0, 0 ends it
     uint8_t gran_lost[32];                  // what stands in a granule's place is another request's
     alignas(2) uint8_t flags[kNotes][2];    // by key tile and half of its keys: kMarked, kLost
     uint8_t marked[kNotes][128];            // by key, where kMarked: blocks of V that are NaN (0 stands in the tile)
     int64_t units;                          // up to 32 requests: all their units, the work of those up to each,
     int64_t work_end[32];                   // and what they are
     Req req[32];
-    TileOf tile[8];
-    uint32_t item[16][sizeof(Item) / 4];    // by warp: the present item, while its keys are gone through
+    Piece piece[kItems];
 };
 
 // Up to 32 requests every CTA makes the plan itself, a lane a request, and keeps it in shared memory.
@@ -306,21 +313,6 @@ __device__ __forceinline__ void plan_here(const Args &a, Small &sm, const int64_
     }
     sm.work_end[lane] = scan;
     sm.req[lane] = q;
-}
-
-// An item that all lanes have, to shared memory and back.
-__device__ __forceinline__ void put_aside(const Item &it, volatile uint32_t *to, uint32_t lane) {
-    uint32_t w[sizeof(Item) / 4];
-    memcpy(w, &it, sizeof(Item));
-    if (lane == 0)
-#pragma unroll
-        for (size_t i = 0; i < sizeof(Item) / 4; ++i) to[i] = w[i];
-}
-__device__ __forceinline__ void take_back(Item &it, const volatile uint32_t *from) {
-    uint32_t w[sizeof(Item) / 4];
-#pragma unroll
-    for (size_t i = 0; i < sizeof(Item) / 4; ++i) w[i] = from[i];
-    memcpy(&it, w, sizeof(Item));
 }
 
 __device__ __forceinline__ Shares shares_of(const Args &a, const Small &sm, const int64_t *plan) {
@@ -374,14 +366,14 @@ __device__ __forceinline__ int32_t low_of(const Args &a, int32_t off, int32_t to
     return a.window ? (int32_t)max((int64_t)off + tok - a.window + 1, (int64_t)0) : 0;
 }
 
-// Registers move to the softmax warps: 256 * 184 + 256 * 72 = 512 * 128, the launch's own.
-constexpr int kRegsSoftmax = 184, kRegsOther = 72;
-constexpr uint32_t kWarpLoad = 8, kWarpMma = 9, kWarpNote = 10, kWarpUnpack = 12;  // warps 0-7: softmax
+// Registers move to the softmax warps: 256 * 200 + 256 * 56 = 512 * 128, the launch's own.
+constexpr int kRegsSoftmax = 200, kRegsOther = 56;
+constexpr uint32_t kWarpLoad = 8, kWarpMma = 9, kWarpMake = 10;  // warps 0-7: softmax; from 10: makers
 
 // Where a lane finds its codes and scales of K or V in a granule, and where it puts them as 16-bit values in a tile, in
-// the 128-byte swizzle: 32 dimensions of a token, and the same of the token 8 further on for D = 128.  Eight lanes that
-// store at once have two rows' (D = 128) or four rows' pieces: the upper half of the dimensions goes in another order,
-// so that they lie in eight different 16-byte columns.
+// the 128-byte swizzle: 32 dimensions of a token, so that a warp takes 8 tokens (D = 128) or 16 at a step.  Eight lanes
+// that store at once have two rows' (D = 128) or four rows' pieces: the upper half of the dimensions goes in another
+// order, so that they lie in eight different 16-byte columns.
 template <int D>
 struct Unpack {
     static constexpr uint32_t kParts = D / 32, kRows = 32 / kParts;
@@ -401,50 +393,52 @@ struct Unpack {
             dst[i] = part / 2 * 16384 + row * 128 + (((part % 2 * 4 + (i ^ flip)) ^ (row & 7)) << 4);
     }
 
-    // A granule's 16 rows; `tile`: where the first of them lies.  Weights of 0 must not meet a NaN: of V (kClean) rows from
-    // `valid` on, past the request's end, count as 0, and so do blocks marked NaN.
+    // kRows tokens from row r of a granule on; `tile`: where row r goes.  Weights of 0 must not meet a NaN: of V (kClean)
+    // the granule's rows from `valid` on, past the request's end, count as 0, and so do blocks marked NaN.
     template <bool kBf16, bool kClean>
-    __device__ __forceinline__ void granule(const uint8_t *from, const uint8_t *from_scales, uint8_t *tile, int32_t valid) const {
+    __device__ __forceinline__ void step(const uint8_t *from, const uint8_t *from_scales, uint8_t *tile, uint32_t r,
+                                         int32_t valid) const {
+        uint32_t two = *reinterpret_cast<const uint16_t *>(from_scales + scales + r * (D / 16));
+        if (kClean) {
+            if (((two & 0x7f7f) + 0x0101) & 0x8080) two &= ~__vcmpeq4(two & 0x7f7f, 0x7f7f);
+            if ((int32_t)(row + r) >= valid) two = 0;
+        }
+        const uint32_t z = pk::e4m3_to_half2(two);
+        uint32_t by[2];
+        if (kBf16) {
+            // a half's bits, three to the right, are 2^-112 times the value as a bfloat16; the scale makes up for it
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&z));
+            by[0] = pk::Elem<PK_BF16>::from2(f.x * 0x1p112f, f.y * 0x1p112f);
+            by[1] = __byte_perm(by[0], by[0], pick[1]);
+            by[0] = __byte_perm(by[0], by[0], pick[0]);
+        } else {
+            by[0] = __byte_perm(z, z, pick[0]);
+            by[1] = __byte_perm(z, z, pick[1]);
+        }
 #pragma unroll
-        for (uint32_t r = 0; r < 16; r += kRows) {
-            uint32_t two = *reinterpret_cast<const uint16_t *>(from_scales + scales + r * (D / 16));
-            if (kClean) {
-                if (((two & 0x7f7f) + 0x0101) & 0x8080) two &= ~__vcmpeq4(two & 0x7f7f, 0x7f7f);
-                if ((int32_t)(row + r) >= valid) two = 0;
-            }
-            const uint32_t z = pk::e4m3_to_half2(two);
-            uint32_t by[2];
-            if (kBf16) {
-                // a half's bits, three to the right, are 2^-112 times the value as a bfloat16; the scale makes up for it
-                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&z));
-                by[0] = pk::Elem<PK_BF16>::from2(f.x * 0x1p112f, f.y * 0x1p112f);
-                by[1] = __byte_perm(by[0], by[0], pick[1]);
-                by[0] = __byte_perm(by[0], by[0], pick[0]);
-            } else {
-                by[0] = __byte_perm(z, z, pick[0]);
-                by[1] = __byte_perm(z, z, pick[1]);
-            }
+        for (int i = 0; i < 4; i += 2) {
+            const uint2 u = *reinterpret_cast<const uint2 *>(from + codes[i / 2] + r * (D / 2));
+            const uint32_t w[2] = {u.x, u.y};
 #pragma unroll
-            for (int i = 0; i < 4; i += 2) {
-                const uint2 u = *reinterpret_cast<const uint2 *>(from + codes[i / 2] + r * (D / 2));
-                const uint32_t w[2] = {u.x, u.y};
+            for (int n = 0; n < 2; ++n) {
+                uint32_t h[4];
+                pk::e2m1x8_to_half2(w[n], h);
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    uint32_t h[4];
-                    pk::e2m1x8_to_half2(w[n], h);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (kBf16) {
-                            const uint32_t b = (h[k] >> 3 & 0x0fff0fffu) | (h[k] & 0x80008000u);
-                            asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(h[k]) : "r"(b), "r"(by[i / 2]));
-                        } else {
-                            asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(h[k]) : "r"(h[k]), "r"(by[i / 2]));
-                        }
+                for (int k = 0; k < 4; ++k) {
+                    if (kBf16) {
+                        const uint32_t b = (h[k] >> 3 & 0x0fff0fffu) | (h[k] & 0x80008000u);
+                        asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(h[k]) : "r"(b), "r"(by[i / 2]));
+                    } else {
+                        asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(h[k]) : "r"(h[k]), "r"(by[i / 2]));
                     }
-                    *reinterpret_cast<uint4 *>(tile + dst[i + n] + r * 128) = make_uint4(h[0], h[1], h[2], h[3]);
                 }
+                *reinterpret_cast<uint4 *>(tile + dst[i + n]) = make_uint4(h[0], h[1], h[2], h[3]);
             }
         }
+    }
+    __device__ __forceinline__ void zero(uint8_t *tile) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(tile + dst[i]) = make_uint4(0, 0, 0, 0);
     }
 };
 
@@ -484,6 +478,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
             pk::mbar_init(pk::smem_addr(&sm.p_ready[t]), 4);
             pk::mbar_init(pk::smem_addr(&sm.o_done[t]), 1);
         }
+        for (uint32_t i = 0; i < kItems; ++i) {
+            pk::mbar_init(pk::smem_addr(&sm.item_full[i]), 1);
+            pk::mbar_init(pk::smem_addr(&sm.item_empty[i]), 8 + kMakers + 1);  // all that read it
+        }
         pk::mbar_init(pk::smem_addr(&sm.over), 1);
         pk::mbar_fence_init();
         sm.abort = 0;
@@ -496,7 +494,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
     const uint8_t *pool = a.pool;
     pk::pdl_wait(plan, q_off, kv_len, pages, pool);
     pk::pdl_launch_dependents();
-    if (warp == kWarpLoad && !a.plan) plan_here(a, sm, q_off, kv_len);
     pk::tmem_fence_before();
     __syncthreads();
     pk::tmem_fence_after();
@@ -508,47 +505,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
         pk::set_status(a.status, PK_ERR_TIMEOUT);
     };
 
-    Item it;
-    bool more;
-    {
-        const Shares shares = shares_of(a, sm, plan);
-        int64_t x = shares.start(min(blockIdx.x, shares.n));
-        it.line = shares.start(min(blockIdx.x + 1, shares.n));
-        it.whole = shares.whole;
-        more = x < it.line;
-        while (more) {
-            const int64_t before = find_request(a, sm, plan, q_off, kv_len, x, it);
-            const Units units(a, it.q);
-            it.at = place_of(units, it.at.r, before, x);
-            if (!it.whole || it.at.pos == 0) {
-                cut_item(a, units, it.line - x, it);
-                break;
-            }
-            x += units.weight(it.at.u) - it.at.pos;  // the next unit
-            more = x < it.line;
-        }
-    }
-    // Each warp finds the block's items for itself.  While it goes through one's keys, what it does not need of it lies
-    // in shared memory, where it does not take registers from the work.
-    auto aside = [&]() {
-        put_aside(it, sm.item[warp], lane);
-        __syncwarp();
+    // The loading warp's n-th item; back to it.
+    auto wait_item = [&](uint32_t n) {
+        return pk::mbar_wait_warp(pk::smem_addr(&sm.item_full[n % kItems]), n / kItems & 1);
     };
-    auto take_next = [&]() {  // it begins with a unit
-        take_back(it, sm.item[warp]);
-        more = it.left > 0;
-        if (!more) return;
-        Units units(a, it.q);
-        it.at.pos = 0;
-        if (++it.at.u == units.n) {
-            it.at.u = 0;
-            if (++it.at.part == a.kv_heads * a.chunks) {
-                find_request(a, sm, plan, q_off, kv_len, it.line - it.left, it);
-                it.at.part = 0;
-                units = Units(a, it.q);
-            }
-        }
-        cut_item(a, units, it.left, it);
+    auto return_item = [&](uint32_t n) {
+        __syncwarp();
+        if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.item_empty[n % kItems]));
     };
     if (warp >= kWarpLoad) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
@@ -557,15 +520,109 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
             bool ok = true, sent = false;        // sent: a copy that `count` does not hold
             const uint32_t slot_shift = 31 - __clz(a.page_grans);
             const bool pow2 = (a.page_grans & (a.page_grans - 1)) == 0;
+            if (!plan) {
+                plan_here(a, sm, q_off, kv_len);
+                __syncwarp();
+            }
+            Item it;
+            bool more;
+            {
+                const Shares shares = shares_of(a, sm, plan);
+                int64_t x = shares.start(min(blockIdx.x, shares.n));
+                it.line = shares.start(min(blockIdx.x + 1, shares.n));
+                it.whole = shares.whole;
+                more = x < it.line;
+                while (more) {
+                    const int64_t before = find_request(a, sm, plan, q_off, kv_len, x, it);
+                    const Units units(a, it.q);
+                    it.at = place_of(units, it.at.r, before, x);
+                    if (!it.whole || it.at.pos == 0) {
+                        cut_item(a, units, it.line - x, it);
+                        break;
+                    }
+                    x += units.weight(it.at.u) - it.at.pos;  // the next unit
+                    more = x < it.line;
+                }
+                if (a.blocks > 1) {  // what k_chunk_join has to know of the unit that this share's beginning cuts
+                    Cut cut = {-1, 0, 0, 0, 0, 0};
+                    if (more && it.at.pos > 0) {
+                        const Units units(a, it.q);
+                        const int64_t unit = x - it.at.pos;  // where it begins
+                        const uint32_t before = shares.block_of(unit);
+                        const int32_t tok0 = it.tok0(a);
+                        const uint32_t head0 = it.chunk(a) * a.tile_heads;
+                        if (before + 1 == blockIdx.x)
+                            cut = Cut{(int32_t)before, (int32_t)shares.block_of(unit + units.weight(it.at.u) - 1), it.q.q0 + tok0,
+                                      min(it.q.lq - tok0, units.step), (int32_t)(it.head(a) * a.group + head0),
+                                      (int32_t)min(a.group - head0, a.tile_heads)};
+                    }
+                    if (lane == 0) a.cuts[blockIdx.x] = cut;
+                }
+            }
+            auto take_next = [&]() {  // it begins with a unit
+                more = it.left > 0;
+                if (!more) return;
+                Units units(a, it.q);
+                it.at.pos = 0;
+                if (++it.at.u == units.n) {
+                    it.at.u = 0;
+                    if (++it.at.part == a.kv_heads * a.chunks) {
+                        find_request(a, sm, plan, q_off, kv_len, it.line - it.left, it);
+                        it.at.part = 0;
+                        units = Units(a, it.q);
+                    }
+                }
+                cut_item(a, units, it.left, it);
+            };
+            auto tell = [&](Piece &to) {  // a lane a tile
+                const int32_t tok0 = it.tok0(a) + (int32_t)(lane * a.tile_tokens), off = it.q.len - it.q.lq;
+                const int32_t base = it.first * kKeys + it.skip;  // from positions to places behind the piece's first one
+                const int32_t all_last = off + tok0 - base;       // all queries of the tile see what lies up to here
+                const int32_t all_low = low_of(a, off, min(tok0 + (int32_t)a.tile_tokens, it.q.lq) - 1) - base;  // and from here
+                const int32_t sinks = (int32_t)a.sinks - it.first * kKeys, gh0 = (int32_t)(it.chunk(a) * a.tile_heads);
+                if (lane < 2) {
+                    Piece::Tile &t = to.tile[lane];
+                    t.causal = ((all_last - (kKeys - 1)) >> 7) + 1;
+                    t.hides[0] = sinks >> 7;
+                    t.hides[1] = a.window ? (all_low + kKeys - 1) >> 7 : 0;
+                    t.off = off;
+                    t.base = base;
+                    t.sinks = sinks;
+                    t.tok0 = tok0;
+                    t.row0 = it.q.q0 + tok0;
+                    t.tokens = min((int32_t)a.tile_tokens, it.q.lq - tok0);
+                    t.head0 = (int32_t)(it.head(a) * a.group) + gh0;
+                    t.heads = (int32_t)a.group - gh0;
+                    // a block has one piece at most that begins inside a unit, and one that only ends there
+                    t.part = it.cut ? (int32_t)(((2 * blockIdx.x + (it.at.pos == 0)) * 2 + lane) * kRows) : -1;
+                    to.n_tiles[lane] = it.n_tiles[lane];
+                }
+                if (lane == 0) {
+                    to.n_all = it.n_all;
+                    to.first = it.first;
+                    to.skip = it.skip;
+                    to.len = it.q.len;
+                    to.n_gran = it.n_gran;
+                }
+            };
             pk::fence_proxy_async();  // pages written by an earlier kernel are read by the async proxy
-            while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
+            for (uint32_t items = 0; ok && !__any_sync(0xffffffffu, *abort != 0); ++items) {
+                const uint32_t at = items % kItems;
+                ok = items < kItems || pk::mbar_wait_warp(pk::smem_addr(&sm.item_empty[at]), (items / kItems + 1) & 1);
+                if (!ok) break;
+                if (more)
+                    tell(sm.piece[at]);
+                else if (lane == 0)
+                    sm.piece[at].n_all = -1;
+                __syncwarp();
+                if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.item_full[at]));
+                if (!more) break;
                 const uint32_t v0 = 8 * (uint32_t)it.first, v1 = min(8 * (uint32_t)(it.first + it.n_all), it.n_gran);
                 const uint32_t *row = pages + (uint64_t)it.at.r * a.page_stride;
                 const uint32_t head = it.head(a);
                 const int32_t skip = it.skip, n_all = it.n_all;
                 const bool two[2] = {it.n_tiles[0] > 0, it.n_tiles[1] > 0};
                 const int32_t q_head = (int32_t)(head * a.group + it.chunk(a) * a.tile_heads), q_row = it.q.q0 + it.tok0(a);
-                aside();
                 uint64_t where = 0;  // lane l: address of the granule `base` + l of the list
                 bool lost = false;   // slot 0's bytes stand in for a slot out of range
                 auto find_granules = [&](uint32_t base) {
@@ -637,29 +694,27 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 for (int t = 0; t < 2; ++t)
                     if (nq[t]) pk::mbar_wait(pk::smem_addr(&sm.q_full[t]), (nq[t] - 1) & 1);
             __syncwarp();
-        } else if (warp >= kWarpNote) {
-            // Makers of K and V tiles: two warps look for what the softmax warps have to know of a tile, four unpack it.
-            const uint32_t w = warp - kWarpUnpack, half = warp - kWarpNote;
-            const bool notes = warp < kWarpUnpack;
-            const Unpack<D> lanes(lane);
-            uint32_t n = 0, count = 0, tiles = 0, items = 0;  // stages, granules, key tiles, items with keys so far
+        } else if (warp >= kWarpMake) {
+            // Makers of K and V tiles: a tile's steps go round the six; the last two, which have fewer, look for what the
+            // softmax warps have to know of it.
+            using U = Unpack<D>;
+            constexpr uint32_t kPerGran = 16 / U::kRows, kSteps = 8 * kPerGran;
+            const uint32_t mine = warp - kWarpMake;
+            const U lanes(lane);
+            uint32_t n = 0, count = 0, tiles = 0;  // stages, granules, key tiles so far
             bool ok = true;
             auto wait_empty = [&](uint32_t n) {
                 return n < L::kStages ||
                        pk::mbar_wait_warp(pk::smem_addr(&sm.empty[n % L::kStages]), (n / L::kStages + 1) & 1);
             };
-            while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
-                if (it.n_all > 0) {
-                    // its reader, at most four items behind, sees it by way of the first K tile's barrier
-                    if (warp == kWarpNote && lane == 0) {
-                        sm.work[items & 7][0] = it.n_tiles[0];
-                        sm.work[items & 7][1] = it.n_tiles[1];
-                    }
-                    ++items;
-                }
-                const int32_t n_all = it.n_all, skip = it.skip, len = it.q.len;
+            for (uint32_t items = 0; ok && !__any_sync(0xffffffffu, *abort != 0); ++items) {
+                ok = wait_item(items);
+                if (!ok) break;
+                const volatile Piece &it = sm.piece[items % kItems];
+                const int32_t n_all = it.n_all, skip = it.skip, len = it.len;
                 const uint32_t first = (uint32_t)it.first, n_gran = it.n_gran;
-                aside();
+                return_item(items);
+                if (n_all < 0) break;
                 for (int32_t j = 0; j < n_all; ++j) {
                     const uint32_t v0 = 8 * (first + j), have = min(n_gran - v0, 8u);
                     // Every warp waits for all of the tile's granules, a lane each, and gives all of them back: a place's
@@ -671,12 +726,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     if (!ok) break;
                     auto place = [&](uint32_t g) { return smem_c + L::kGranRing + (count + g) % L::kGrans * L::kGran; };
                     // tokens of a granule before the request's end
-                    auto valid = [&](uint32_t g) {
-                        return len - (int32_t)(16 * (v0 + g)) - (v0 + g >= a.sink_grans ? skip : 0);
-                    };
-                    const uint32_t mine = have > 2 * w ? min(have - 2 * w, 2u) : 0;  // granules, of an unpacking warp
-                    uint8_t *tile = smem_c + L::kRing + n % L::kStages * L::kTile + (notes ? 0 : 32 * w * 128);
-                    if (notes) {  // blocks of V marked NaN, two tokens a lane
+                    auto valid = [&](uint32_t g) { return len - (int32_t)(16 * (v0 + g)) - (v0 + g >= a.sink_grans ? skip : 0); };
+                    uint8_t *tile = smem_c + L::kRing + n % L::kStages * L::kTile;
+#pragma unroll
+                    for (uint32_t s = mine; s < kSteps; s += kMakers) {
+                        const uint32_t g = s / kPerGran, r = s % kPerGran * U::kRows;
+                        if (g < have)
+                            lanes.template step<DT == PK_BF16, false>(place(g) + G::kK, place(g) + G::kKs, tile + s * U::kRows * 128, r, 16);
+                    }
+                    pk::fence_proxy_async_smem();
+                    if (mine >= kMakers - 2) {  // blocks of V marked NaN, two tokens a lane
+                        const uint32_t half = mine - (kMakers - 2);
                         uint32_t bits[2] = {0, 0}, lost = 0;
 #pragma unroll
                         for (uint32_t i = 0; i < 2; ++i) {
@@ -698,32 +758,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                             sm.marked[tiles % kNotes][64 * half + 32 + lane] = (uint8_t)bits[1];
                         }
                         if (lane == 0) sm.flags[tiles % kNotes][half] = (marked ? kMarked : 0) | (gone ? kLost : 0);
-                    } else {
-#pragma unroll
-                        for (uint32_t h = 0; h < 2; ++h)
-                            if (h < mine)
-                                lanes.template granule<DT == PK_BF16, false>(place(2 * w + h) + G::kK, place(2 * w + h) + G::kKs,
-                                                                             tile + 16 * h * 128, 16);
-                        pk::fence_proxy_async_smem();
                     }
                     __syncwarp();
                     if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.full[n % L::kStages]));
                     ++n;
                     ok = wait_empty(n);
                     if (!ok) break;
-                    if (!notes) {
-                        tile = smem_c + L::kRing + n % L::kStages * L::kTile + 32 * w * 128;
+                    tile = smem_c + L::kRing + n % L::kStages * L::kTile;
 #pragma unroll
-                        for (uint32_t h = 0; h < 2; ++h)
-                            if (h < mine)
-                                lanes.template granule<false, true>(place(2 * w + h) + G::kV, place(2 * w + h) + G::kVs,
-                                                                    tile + 16 * h * 128, valid(2 * w + h));
-                        // rows behind the last granule: weights of 0 must not meet what lies there
-                        for (uint32_t x = mine * 16 * (D / 8) + lane; x < 32 * (D / 8); x += 32)
-                            *reinterpret_cast<uint4 *>(tile + x % (D / 8) / 8 * 16384 + x / (D / 8) * 128 + x % 8 * 16) =
-                                make_uint4(0, 0, 0, 0);
-                        pk::fence_proxy_async_smem();
+                    for (uint32_t s = mine; s < kSteps; s += kMakers) {
+                        const uint32_t g = s / kPerGran, r = s % kPerGran * U::kRows;
+                        if (g < have)
+                            lanes.template step<false, true>(place(g) + G::kV, place(g) + G::kVs, tile + s * U::kRows * 128, r, valid(g));
+                        else  // behind the last granule: weights of 0 must not meet what lies there
+                            lanes.zero(tile + s * U::kRows * 128);
                     }
+                    pk::fence_proxy_async_smem();
                     __syncwarp();
                     if (lane < have) pk::mbar_arrive(pk::smem_addr(&sm.gran_empty[c % L::kGrans]));
                     if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.full[n % L::kStages]));
@@ -731,17 +781,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     count += have;
                     ++tiles;
                 }
-                if (ok) take_next();
             }
-            ok = ok && wait_empty(n);
-            if (ok) {  // the matrix warp's end: a stage without a tile
-                if (lane == 0) {
-                    if (warp == kWarpNote) sm.work[items & 7][0] = sm.work[items & 7][1] = 0;
-                    pk::mbar_arrive(pk::smem_addr(&sm.full[n % L::kStages]));
-                }
-            } else if (lane == 0) {
-                give_up();
-            }
+            if (!ok && lane == 0) give_up();
             __syncwarp();
         } else if (warp == kWarpMma) {
             const uint32_t qk_kind = pk::mma_idesc(DT == PK_BF16, 128, 128, false) |
@@ -750,22 +791,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
             uint32_t ring = 0, use = 0;             // next ring stage, and how often the ring has been gone round
             uint32_t ni0 = 0, ni1 = 0, nq0 = 0, nq1 = 0;  // key tiles and Q tiles used so far, by tile
             bool ok = true;
-            if (a.blocks > 1) {  // what k_chunk_join has to know of the unit that this share's beginning cuts
-                const Shares shares = shares_of(a, sm, plan);
-                Cut cut = {-1, 0, 0, 0, 0, 0};
-                if (more && it.at.pos > 0) {
-                    const Units units(a, it.q);
-                    const int64_t unit = shares.start(blockIdx.x) - it.at.pos;  // where it begins
-                    const uint32_t before = shares.block_of(unit);
-                    const int32_t tok0 = it.tok0(a);
-                    const uint32_t head0 = it.chunk(a) * a.tile_heads;
-                    if (before + 1 == blockIdx.x)
-                        cut = Cut{(int32_t)before, (int32_t)shares.block_of(unit + units.weight(it.at.u) - 1), it.q.q0 + tok0,
-                                  min(it.q.lq - tok0, units.step), (int32_t)(it.head(a) * a.group + head0),
-                                  (int32_t)min(a.group - head0, a.tile_heads)};
-                }
-                if (lane == 0) a.cuts[blockIdx.x] = cut;
-            }
             auto wait_full = [&](uint32_t st, uint32_t round) {
                 return pk::mbar_wait_warp(pk::smem_addr(&sm.full[st]), round & 1);
             };
@@ -801,12 +826,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 __syncwarp();
             };
             for (uint32_t items = 0; ok && !__any_sync(0xffffffffu, *abort != 0); ++items) {
+                ok = wait_item(items);
+                if (!ok) break;
+                const volatile Piece &it = sm.piece[items % kItems];
+                const int32_t n0 = (int32_t)pk::uniform(it.n_tiles[0]), n1 = (int32_t)pk::uniform(it.n_tiles[1]);
+                const int32_t n_all = (int32_t)pk::uniform(it.n_all);
+                return_item(items);
+                if (n_all < 0) break;
+                if (n_all == 0) continue;
                 ok = wait_full(ring, use);
                 if (!ok) break;
-                const int32_t n0 = (int32_t)pk::uniform(sm.work[items & 7][0]);
-                const int32_t n1 = (int32_t)pk::uniform(sm.work[items & 7][1]);
-                const int32_t n_all = max(n0, n1);
-                if (n_all == 0) break;
                 if (n0 > 0 && (ok = pk::mbar_wait_warp(pk::smem_addr(&sm.q_full[0]), nq0++ & 1))) {
                     pk::tmem_fence_after();
                     qk(0, ring, n0 == 1);
@@ -873,36 +902,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
         // a scale of 0 would make a masked -infinity NaN; the smallest normal one gives the same weights
         const float scale2 = fmaxf(fabsf(a.scale2), FLT_MIN);
         const uint64_t scale22 = pk::pack2(scale2, scale2);
-        // What is not needed at every tile of the item lies in shared memory: in registers it would push others out.
-        volatile TileOf *mine = &sm.tile[warp];
         uint32_t ni = 0, tiles = 0;  // key tiles weighed so far; key tiles of the CTA's items before the present one
         bool ok = true;
-        while (more && ok && !__any_sync(0xffffffffu, *abort != 0)) {
-            const int32_t n_tiles = t ? it.n_tiles[1] : it.n_tiles[0];
-            bool on;
-            {
-                const int32_t tok0 = it.tok0(a) + (int32_t)(t * a.tile_tokens), off = it.q.len - it.q.lq;
-                const int32_t base = it.first * kKeys + it.skip;  // from positions to places behind the piece's first one
-                const int32_t all_last = off + tok0 - base;
-                const int32_t all_low = low_of(a, off, min(tok0 + (int32_t)a.tile_tokens, it.q.lq) - 1) - base;
-                const int32_t sinks = (int32_t)a.sinks - it.first * kKeys, gh0 = (int32_t)(it.chunk(a) * a.tile_heads);
-                if (lane == 0) {
-                    mine->causal = ((all_last - (kKeys - 1)) >> 7) + 1;
-                    mine->hides[0] = sinks >> 7;
-                    mine->hides[1] = a.window ? (all_low + kKeys - 1) >> 7 : 0;
-                    mine->off = off;
-                    mine->base = base;
-                    mine->sinks = sinks;
-                    mine->tok0 = tok0;
-                    mine->row0 = it.q.q0 + tok0;
-                    mine->head0 = (int32_t)(it.head(a) * a.group) + gh0;
-                    // a block has one piece at most that begins inside a unit, and one that only ends there
-                    mine->part = it.cut ? (int32_t)(((2 * blockIdx.x + (it.at.pos == 0)) * 2 + t) * kRows) : -1;
-                    mine->n_all = it.n_all;
-                }
-                on = row_tok < (int32_t)a.tile_tokens && tok0 + row_tok < it.q.lq && gh0 + row_head < (int32_t)a.group;
-                aside();
-            }
+        for (uint32_t items = 0; ok && !__any_sync(0xffffffffu, *abort != 0); ++items) {
+            ok = wait_item(items);
+            if (!ok) break;
+            const volatile Piece &it = sm.piece[items % kItems];
+            const volatile Piece::Tile *mine = &it.tile[t];
+            if (it.n_all < 0) break;
+            const int32_t n_tiles = it.n_tiles[t];
+            const bool on = row_tok < mine->tokens && row_tok < (int32_t)a.tile_tokens && row_head < mine->heads;
             // a weight is 2^(score - ref + fine), and fine is 0 but for a reference of kFar and more
             float ref = -FLT_MAX, fine = 0.0f, sum = 0.0f;
             uint32_t marked = 0;  // blocks of 16 dimensions in which the row saw a NaN of V
@@ -1072,8 +1081,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 __syncwarp();
                 if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.p_ready[t]));
             }
-            tiles += (uint32_t)mine->n_all;
-            take_next();  // while the last product runs
+            tiles += (uint32_t)it.n_all;
             if (ok && n_tiles > 0) ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
             if (!ok) break;
             if (lost) sum = __int_as_float(0x7fffffff);
@@ -1118,7 +1126,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     pk::store32(dst + 16 * c, a.wide_out, w);
                 }
             }
-            __syncwarp();
+            return_item(items);
         }
         if (!ok && lane == 0) give_up();
     }
@@ -1169,7 +1177,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_chunk_join(const Args a) {
         for (uint32_t i0 = 0; i0 < n; i0 += 32) {
             const float4 y = i0 + lane < n ? __ldcg(ml + part_of(i0 + lane)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             const float f = y.z == 0.0f ? 0.0f : pk::ex2(more(make_float2(y.x, y.y), make_float2(ref, fine)));
-#pragma unroll 8
+#pragma unroll 4
             for (uint32_t i = 0; i < min(n - i0, 32u); ++i) {
                 const float w = __shfl_sync(0xffffffffu, f, i);
                 sum += w * __shfl_sync(0xffffffffu, y.z, i);

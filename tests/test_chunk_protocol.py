@@ -8,7 +8,7 @@ import pytest
 
 from test_prompt_protocol import Bar
 
-MAKERS, NOTES = 6, 8  # of the makers, 0 and 1 take the notes, the others unpack
+MAKERS, NOTES, AHEAD = 6, 8, 4  # the last two makers take the notes too
 
 
 class Cta:
@@ -24,10 +24,16 @@ class Cta:
         self.notes = [{} for _ in range(NOTES)]
         self.copies, self.pipe = [], []  # in flight; the pipe runs in order
         self.sp, self.o = [None, None], [None, None]
-        self.work = [None] * 8
+        self.work = [None] * AHEAD
+        self.item_full, self.item_empty = [Bar(1) for _ in range(AHEAD)], [Bar(8 + MAKERS + 1) for _ in range(AHEAD)]
         self.stored = [set(), set()]
         self.speed = rng.choice((0.5, 0.02)), rng.choice((0.5, 0.05))
         self.rescale = rng.choice((0.0, 0.3))
+
+    def read_item(self, n):
+        while not self.item_full[n % AHEAD].done(n // AHEAD & 1):
+            yield
+        return self.work[n % AHEAD]
 
     def grans_of(self, x, j):
         n0, n1, tail = self.items[x]
@@ -35,7 +41,15 @@ class Cta:
 
     def loader(self):
         count, nq = 0, [0, 0]
-        for x, (n0, n1, _) in enumerate(self.items):
+        for x in range(len(self.items) + 1):
+            while x >= AHEAD and not self.item_empty[x % AHEAD].done((x // AHEAD + 1) & 1):
+                yield
+            self.work[x % AHEAD] = x if x < len(self.items) else "end"
+            yield
+            self.item_full[x % AHEAD].arrive()
+            if x == len(self.items):
+                break
+            n0, n1, _ = self.items[x]
             for j in range(max(n0, n1)):
                 lanes = list(range(self.grans_of(x, j)))
                 self.rng.shuffle(lanes)
@@ -67,20 +81,26 @@ class Cta:
 
     def maker(self, w):
         n, count, tiles, taken = 0, 0, 0, 0
+        steps = 16 if self.S == 3 else 8
+        grans = sorted({s * 8 // steps for s in range(w, steps, MAKERS)})  # that it unpacks a part of
 
         def wait_empty(n):
             while n >= self.S and not self.empty[n % self.S].done((n // self.S + 1) & 1):
                 yield
 
-        for x, (n0, n1, _) in enumerate(self.items):
-            if max(n0, n1):
-                if w == 0:
-                    assert self.work[taken & 7] is None, "an item's note overwritten before it was read"
-                    self.work[taken & 7] = x
-                taken += 1
+        while True:
+            x = yield from self.read_item(taken)
+            yield
+            assert self.work[taken % AHEAD] == x
+            self.item_empty[taken % AHEAD].arrive()
+            taken += 1
+            if x == "end":
+                return
+            n0, n1, _ = self.items[x]
             for j in range(max(n0, n1)):
                 have = self.grans_of(x, j)
-                mine = [g for g in (range(4 * w, 4 * w + 4) if w < 2 else (2 * w - 4, 2 * w - 3)) if g < have]
+                notes = w - (MAKERS - 2)
+                mine = [g for g in sorted({*grans, *(range(4 * notes, 4 * notes + 4) if notes >= 0 else ())}) if g < have]
                 for g in range(have):
                     c = count + g
                     while not self.gran_full[c % self.G].done((c // self.G) & 1):
@@ -89,7 +109,7 @@ class Cta:
                     yield from wait_empty(n)
                     for g in mine:
                         assert self.gran[(count + g) % self.G] == (x, j, g)
-                    if kv == "K" and w < 2:
+                    if kv == "K" and notes >= 0:
                         self.notes[tiles % NOTES][w] = (x, j)
                     self.stage[n % self.S][w] = None
                     yield
@@ -102,10 +122,6 @@ class Cta:
                     yield
                 count += have
                 tiles += 1
-        yield from wait_empty(n)
-        if w == 0:
-            self.work[taken & 7] = "end"
-        self.full[n % self.S].arrive()
 
     def mma(self):
         base, ni, nq, taken = 0, [0, 0], [0, 0], 0
@@ -126,14 +142,18 @@ class Cta:
             self.pipe.append(("commit", self.empty[n % self.S]))
 
         while True:
-            yield from wait_full(base)
-            x = self.work[taken & 7]
-            self.work[taken & 7] = None
+            x = yield from self.read_item(taken)
+            yield
+            assert self.work[taken % AHEAD] == x
+            self.item_empty[taken % AHEAD].arrive()
             taken += 1
             if x == "end":
                 break
             n0, n1, _ = self.items[x]
             nt, n_all = (n0, n1), max(n0, n1)
+            if n_all == 0:
+                continue
+            yield from wait_full(base)
             for t in (0, 1):
                 if nt[t]:
                     while not self.q_full[t].done(nq[t] & 1):
@@ -170,14 +190,18 @@ class Cta:
                     yield
 
     def softmax(self, t, warp):
-        ni, tiles = 0, 0
-        for x, item in enumerate(self.items):
+        ni, tiles, taken = 0, 0, 0
+        while True:
+            x = yield from self.read_item(taken)
+            if x == "end":
+                return
+            item = self.items[x]
             for j in range(item[t]):
                 while not self.s_full[t].done(ni & 1):
                     yield
                 for _ in range(self.rng.choice((1, 1, 30))):
                     assert self.sp[t] == ("S", x, j)
-                    assert all(self.notes[(tiles + j) % NOTES].get(w) == (x, j) for w in (0, 1)), "notes gone"
+                    assert all(self.notes[(tiles + j) % NOTES].get(w) == (x, j) for w in (MAKERS - 2, MAKERS - 1)), "notes gone"
                     yield
                 if j and self.rng.random() < self.rescale:
                     while not self.o_done[t].done((ni - 1) & 1):
@@ -196,6 +220,9 @@ class Cta:
                 for _ in range(self.rng.choice((1, 1, 40))):
                     assert self.o[t] == (x, item[t] - 1), "O overwritten before it was read"
                     yield
+            assert self.work[taken % AHEAD] == x, "an item overwritten before all had read it"
+            self.item_empty[taken % AHEAD].arrive()
+            taken += 1
 
     def agents(self):
         if self.copies and self.rng.random() < self.speed[0]:
@@ -236,7 +263,7 @@ class Cta:
         assert not self.pipe, "a product or an arrival is left after the CTA's end"
 
 
-@pytest.mark.parametrize("stages,grans", [(3, 26), (8, 32)])
+@pytest.mark.parametrize("stages,grans", [(3, 28), (8, 32)])
 def test_every_interleaving_tried_is_sound(stages, grans):
     rng = random.Random(11)
     for _ in range(100):
@@ -251,6 +278,6 @@ def test_every_interleaving_tried_is_sound(stages, grans):
 def test_many_short_items():
     """Items of one key tile, where the warps run furthest ahead of one another."""
     rng = random.Random(12)
-    for stages, grans in ((3, 26), (8, 32)):
+    for stages, grans in ((3, 28), (8, 32)):
         for _ in range(40):
             Cta([(rng.choice((0, 1)), rng.choice((0, 1)), rng.choice((1, 1, 2))) for _ in range(30)], stages, grans, rng).run()
