@@ -84,7 +84,7 @@ __device__ __forceinline__ int32_t good_length(const Args &a, int32_t len) {
 // many keys (4 x 512 tokens behind 16384, 256 units: 604 -> 550 us against units cut in two).  Where that gains less
 // than the pieces and their joining cost, a block takes the whole units that begin in its share.
 constexpr int64_t kUnitCost = 512;     // a unit's start and end, in keys
-constexpr int64_t kCutCost = 1024;     // one more piece a block, and the joining
+constexpr int64_t kCutCost = 2048;     // one more piece a block, and the joining
 constexpr int64_t kLeastShare = 1024;
 
 struct Req {
@@ -131,7 +131,7 @@ struct Shares {
         each = total / n;
         more = (uint32_t)(total - each * n);
         const int64_t one = units ? total / units : 0;
-        whole = max((units + n - 1) / n * one, each + one / 2) <= each + kCutCost;
+        whole = max((units + n - 1) / n * one, each + one / 4) <= each + kCutCost;
     }
     __device__ __forceinline__ int64_t start(uint32_t b) const { return each * b + min(b, more); }
     __device__ __forceinline__ uint32_t block_of(int64_t x) const {
@@ -728,7 +728,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     // tokens of a granule before the request's end
                     auto valid = [&](uint32_t g) { return len - (int32_t)(16 * (v0 + g)) - (v0 + g >= a.sink_grans ? skip : 0); };
                     uint8_t *tile = smem_c + L::kRing + n % L::kStages * L::kTile;
-#pragma unroll
+#pragma unroll 1
                     for (uint32_t s = mine; s < kSteps; s += kMakers) {
                         const uint32_t g = s / kPerGran, r = s % kPerGran * U::kRows;
                         if (g < have)
@@ -765,7 +765,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     ok = wait_empty(n);
                     if (!ok) break;
                     tile = smem_c + L::kRing + n % L::kStages * L::kTile;
-#pragma unroll
+#pragma unroll 1
                     for (uint32_t s = mine; s < kSteps; s += kMakers) {
                         const uint32_t g = s / kPerGran, r = s % kPerGran * U::kRows;
                         if (g < have)
@@ -968,13 +968,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     if (decltype(masked)::value) mask(c, y);
                     return y;
                 };
-                auto largest = [&](auto masked) {
+                // The largest score of the first n chunks.
+                auto largest = [&](int n) {
                     float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+                    for (int c = 0; c < n; ++c) {
+                        pk::tmem_load32(ts + 32 * c, x[0]);
+                        pk::tmem_wait_load(x[0]);
+                        if (edge) mask(c, x[0]);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t(&y)[32] = chunk(c, masked);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) m4[i & 3] = fmaxf(m4[i & 3], __uint_as_float(y[i]));
+                        for (int i = 0; i < 32; ++i) m4[i & 3] = fmaxf(m4[i & 3], __uint_as_float(x[0][i]));
                     }
                     return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
                 };
@@ -1003,22 +1006,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 auto weigh_far = [&]() {
                     float s = 0.0f;
                     uint32_t(&y)[16] = reinterpret_cast<uint32_t(&)[16]>(x[0]);
-#pragma unroll
+                    uint32_t w[64];  // by way of memory: a loop, as its code would take the place of what is run often
+#pragma unroll 1
                     for (int c = 0; c < 8; ++c) {
                         pk::tmem_load16(ts + 16 * c, y);
                         pk::tmem_wait_load(y);
 #pragma unroll
                         for (int i = 0; i < 16; i += 2) {
-                            float w[2];
+                            float f[2];
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
                                 const bool off = edge && hidden(16 * c + i + h);
-                                w[h] = off ? 0.0f : pk::ex2(fmaf(__uint_as_float(y[i + h]), scale2, -ref) + fine);
-                                s += w[h];
+                                f[h] = off ? 0.0f : pk::ex2(fmaf(__uint_as_float(y[i + h]), scale2, -ref) + fine);
+                                s += f[h];
                             }
-                            p[c / 4][c % 4 * 8 + i / 2] = pk::Elem<PK_FP16>::from2(w[0], w[1]);
+                            w[8 * c + i / 2] = pk::Elem<PK_FP16>::from2(f[0], f[1]);
                         }
                     }
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) p[i / 32][i % 32] = w[i];
                     return s;
                 };
                 auto weigh_any = [&]() {
@@ -1041,15 +1047,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     sum *= f;
                     return f;
                 };
-                if (j == 0) {  // from 32 keys alone: mostly no other is 2^11 times as heavy as the heaviest of them
-                    pk::tmem_load32(ts, x[0]);
-                    pk::tmem_wait_load(x[0]);
-                    if (edge) mask(0, x[0]);
-                    float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) m4[i & 3] = fmaxf(m4[i & 3], __uint_as_float(x[0][i]));
-                    move_ref(on, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])));
-                }
+                // from 32 keys alone: mostly no other is 2^11 times as heavy as the heaviest of them
+                if (j == 0) move_ref(on, largest(1));
                 // One pass over the scores takes the weights by the reference so far, with no look at the scores
                 // first: a weight that has outgrown it shows in the sum, and only then the reference is moved and
                 // the pass done again.  A row that saw no key yet (its window begins further on) has the lowest
@@ -1057,7 +1056,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 // 2^(kBase + 2).  Rows without a query, whose scores may be anything, have no say.
                 float part_sum = weigh_any();
                 if (__any_sync(0xffffffffu, on && part_sum > kTop)) {
-                    const float f = move_ref(on && part_sum > kTop, edge ? largest(std::true_type{}) : largest(std::false_type{}));
+                    const float f = move_ref(on && part_sum > kTop, largest(4));
                     if (j > 0) {  // the output so far too
                         ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
                         if (!ok) break;
@@ -1095,35 +1094,37 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 a.lse[q_row * a.q_heads + qh] = sum == 0.0f ? -INFINITY : (ref - fine + log2f(sum)) * 0.69314718055994531f;
             uint16_t *dst = a.out + q_row * a.o_ts + (int64_t)qh * a.o_hs;
             pk::tmem_fence_after();
-            // 16 columns of the output, the next ones on their way meanwhile
-            uint32_t y[2][16];
-            if (n_tiles > 0) pk::tmem_load16(to, y[0]);
-#pragma unroll
-            for (int c = 0; c < D / 16; ++c) {  // no load is left in flight over a loop's end
-                uint32_t(&z)[16] = y[c & 1];
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t z[32];
                 if (n_tiles > 0) {  // else O was never written
                     __syncwarp();
+                    pk::tmem_load32(to + 32 * c, z);
                     pk::tmem_wait_load(z);
-                    if (c + 1 < D / 16) pk::tmem_load16(to + 16 * (c + 1), y[(c + 1) & 1]);
                 }
                 if (!on) continue;
-                const bool none = n_tiles == 0 || inv == 0.0f, nan = marked >> c & 1;
-                float f[16];
+                const bool none = n_tiles == 0 || inv == 0.0f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    f[i] = nan ? __int_as_float(0x7fffffff) : none ? 0.0f : __uint_as_float(z[i]) * inv;
+                for (int i = 0; i < 32; ++i) {
+                    const float f = none ? 0.0f : __uint_as_float(z[i]) * inv;
+                    z[i] = __float_as_uint(marked >> (2 * c + i / 16) & 1 ? __int_as_float(0x7fffffff) : f);
+                }
                 uint32_t w[8];
                 if (cut) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+                    for (int h = 0; h < 4; ++h) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(f[8 * h + i]);
-                        pk::store32(reinterpret_cast<uint16_t *>(a.part_o + part * D + 16 * c + 8 * h), true, w);
+                        for (int i = 0; i < 8; ++i) w[i] = z[8 * h + i];
+                        pk::store32(reinterpret_cast<uint16_t *>(a.part_o + part * D + 32 * c + 8 * h), true, w);
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 16; i += 2) w[i / 2] = pk::Elem<DT>::from2(f[i], f[i + 1]);
-                    pk::store32(dst + 16 * c, a.wide_out, w);
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2)
+                            w[i / 2] = pk::Elem<DT>::from2(__uint_as_float(z[16 * h + i]), __uint_as_float(z[16 * h + i + 1]));
+                        pk::store32(dst + 32 * c + 16 * h, a.wide_out, w);
+                    }
                 }
             }
             return_item(items);
