@@ -635,7 +635,7 @@ int pk_attend_chunk(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, co
  * position turns it by turns[i] / 2^64 of a whole turn, and amplitude multiplies
  * what was rotated. */
 typedef struct {
-    const uint64_t *turns_dev; /* [rotary_dim / 2] */
+    const uint64_t *turns_dev; /* [rotary_dim / 2]; 16-byte aligned */
     uint32_t rotary_dim;       /* a multiple of 16, 16..head_dim */
     uint32_t interleaved;      /* 0 or 1 */
     float amplitude;           /* finite */

@@ -14,7 +14,9 @@ __device__ __forceinline__ void set_status(int32_t *status, int32_t code) {
 // key_off with key_off[0] <= g < key_off[R].  Called by all 32 lanes of a warp
 // with the same g: each level probes 32 positions at once, so R = 2^14
 // requests resolve in 3 rounds of independent loads instead of 14 dependent
-// ones.
+// ones.  kCached: through L1, for kernels whose warps would all ask the L2 for
+// the same few lines.
+template <bool kCached = false>
 __device__ __forceinline__ uint32_t warp_find_request(const int64_t *key_off, uint32_t R,
                                                       int64_t g) {
     const uint32_t lane = threadIdx.x & 31;
@@ -24,7 +26,7 @@ __device__ __forceinline__ uint32_t warp_find_request(const int64_t *key_off, ui
         const uint32_t step = span > 32 ? span / 32 : 1;  // span <= 32: every candidate probed at once
         uint32_t p = lo + (lane + 1) * step;
         if (p > hi - 1) p = hi - 1;
-        const bool le = __ldcg(key_off + p) <= g;
+        const bool le = (kCached ? key_off[p] : __ldcg(key_off + p)) <= g;
         const uint32_t ball = __ballot_sync(0xffffffffu, le);
         // probes are non-decreasing in lane, so the set lanes form a prefix
         const int last = 31 - __clz(ball);  // -1 if none

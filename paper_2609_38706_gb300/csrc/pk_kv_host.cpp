@@ -231,7 +231,7 @@ int pk_rotate(uint32_t dtype, const pk_heads *q, const pk_heads *k, const pk_hea
     if (dtype > PK_FP16 || (head_dim != 64 && head_dim != 128) || (uint64_t)q_heads + kv_heads > 65536) return PK_ERR_ARG;
     if (!rotary || rotary->rotary_dim < 16 || rotary->rotary_dim > head_dim || rotary->rotary_dim % 16 ||
         rotary->interleaved > 1 || !std::isfinite(rotary->amplitude) || !rotary->turns_dev ||
-        !aligned(rotary->turns_dev, 8) || !std::isnormal(eps) || eps < 0.0f)
+        !aligned(rotary->turns_dev, 16) || !std::isnormal(eps) || eps < 0.0f)
         return PK_ERR_ARG;
     if (n_tokens >= 1ull << 32) return PK_ERR_ARG;
     // heads of none: no rows to look at

@@ -58,7 +58,7 @@ __device__ __forceinline__ void pieces_of(uint32_t c, uint32_t rotary_dim, uint3
 // D/16 lanes a head, 512/D heads a warp at a time; a warp takes part_steps such
 // steps of one token's heads, queries first.
 template <int D, uint32_t DT, bool kHalves>
-__global__ void __launch_bounds__(kThreads) k_rotate(const Rotate a) {
+__global__ void __launch_bounds__(kThreads, 4) k_rotate(const Rotate a) {
     constexpr uint32_t kLanes = D / 16, kHeads = 32 / kLanes;
     using E = pk::Elem<DT>;
     const uint32_t lane = threadIdx.x & 31, c = lane % kLanes;
@@ -72,6 +72,22 @@ __global__ void __launch_bounds__(kThreads) k_rotate(const Rotate a) {
     pk::pdl_wait(tok_off, start, turns, xq, xk, wq, wk);
     pk::pdl_launch_dependents();
 
+    uint32_t at[2];
+    pieces_of<kHalves>(c, a.rotary_dim, at);
+    // A step's rows, on their way while the one before is worked on, the first while its request is looked for.
+    const uint32_t all = a.heads[0] + a.heads[1], end = min((first_step + a.part_steps) * kHeads, all);
+    uint4 next[2] = {};
+    auto load = [&](uint32_t h) {
+        if (h >= end || t >= a.n_tokens) return;
+        const bool key = h >= a.heads[0];
+        const uint32_t in = key ? h - a.heads[0] : h;
+        const uint16_t *src = (key ? xk : xq) + (int64_t)t * a.x_ts[key] + (int64_t)in * a.x_hs[key];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) next[i] = __ldcg(reinterpret_cast<const uint4 *>(src + at[i]));
+    };
+    uint32_t h = first_step * kHeads + lane / kLanes;
+    load(h);
+
     // every request's offsets are looked at once, whatever the tokens do
     for (uint64_t r = (uint64_t)blockIdx.x * kThreads + threadIdx.x; r < a.R; r += (uint64_t)gridDim.x * kThreads) {
         const int64_t o0 = __ldcg(tok_off + r), o1 = __ldcg(tok_off + r + 1), s = __ldcg(start + r);
@@ -80,23 +96,27 @@ __global__ void __launch_bounds__(kThreads) k_rotate(const Rotate a) {
     }
     if (t >= a.n_tokens) return;  // uniform per warp
 
-    const uint32_t r = pk::warp_find_request(tok_off, a.R, (int64_t)t);
-    const int64_t o0 = __ldcg(tok_off + r), o1 = __ldcg(tok_off + r + 1), s = __ldcg(start + r);
+    // Through L1, as the table and the weights below: a few lines that every warp reads are a queue at the L2 (8 x 6144
+    // tokens of 40 heads: 262 -> 171 us).
+    const uint32_t r = pk::warp_find_request<true>(tok_off, a.R, (int64_t)t);
+    const int64_t o0 = tok_off[r], o1 = tok_off[r + 1], s = start[r];
     const int64_t pos = s + ((int64_t)t - o0);
     // a token of no request, or of bad offsets, is left as it is
     if (o0 < 0 || (int64_t)t < o0 || (int64_t)t >= o1 || (uint64_t)o1 > a.n_tokens || s < 0 || pos >= (int64_t)1 << 31)
         return;
 
-    uint32_t at[2];
-    pieces_of<kHalves>(c, a.rotary_dim, at);
     const bool rotated = c < a.rotary_dim / 16;
     float cs[8], sn[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint64_t turn = rotated ? __ldcg(turns + 8 * c + i) * (uint64_t)pos : 0;
-        sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &sn[i], &cs[i]);
-        sn[i] *= a.amplitude;
-        cs[i] *= a.amplitude;
+    for (int i = 0; i < 8; i += 2) {
+        const ulonglong2 f = rotated ? *reinterpret_cast<const ulonglong2 *>(turns + 8 * c + i) : make_ulonglong2(0, 0);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint64_t turn = (k ? f.y : f.x) * (uint64_t)pos;
+            sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &sn[i + k], &cs[i + k]);
+            sn[i + k] *= a.amplitude;
+            cs[i + k] *= a.amplitude;
+        }
     }
     uint4 w[2][2];
 #pragma unroll
@@ -106,15 +126,10 @@ __global__ void __launch_bounds__(kThreads) k_rotate(const Rotate a) {
         for (int i = 0; i < 2; ++i) w[j][i] = p ? *reinterpret_cast<const uint4 *>(p + at[i]) : make_uint4(0, 0, 0, 0);
     }
 
-    const uint32_t all = a.heads[0] + a.heads[1];
-    for (uint32_t step = first_step; step < first_step + a.part_steps && step * kHeads < all; ++step) {
-        const uint32_t h = step * kHeads + lane / kLanes;
-        const bool on = h < all, key = h >= a.heads[0];
-        const uint32_t in = key ? h - a.heads[0] : h;
-        const uint16_t *src = (key ? xk : xq) + (int64_t)t * a.x_ts[key] + (int64_t)in * a.x_hs[key];
-        uint4 v[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) v[i] = on ? __ldcg(reinterpret_cast<const uint4 *>(src + at[i])) : make_uint4(0, 0, 0, 0);
+    for (uint32_t h0 = first_step * kHeads; h0 < end; h0 += kHeads, h += kHeads) {
+        const bool on = h < end, key = h >= a.heads[0];
+        const uint4 v[2] = {next[0], next[1]};
+        load(h + kHeads);
         float x[2][8];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -174,6 +189,7 @@ __global__ void __launch_bounds__(kThreads) k_rotate(const Rotate a) {
             }
         }
         if (!on) continue;
+        const uint32_t in = key ? h - a.heads[0] : h;
         uint16_t *dst = (key ? a.y[1] : a.y[0]) + (int64_t)t * a.y_ts[key] + (int64_t)in * a.y_hs[key];
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -210,9 +226,13 @@ cudaError_t pk_launch_rotate(uint32_t dtype, const pk_heads &q, const pk_heads &
     a.start = start;
     a.R = R;
     a.status = status;
+    // A token's heads to one warp, which then has its angles once; to more, each with fewer steps one behind the other,
+    // while that leaves SMs without work (64 tokens of 40 heads: 9.1 -> 3.2 us).
     const uint32_t steps = (q_heads + kv_heads + 512 / head_dim - 1) / (512 / head_dim);
-    a.part_steps = steps;
-    a.parts = 1;
+    a.part_steps = 1;
+    while (a.part_steps < steps && n_tokens * steps / a.part_steps > 152 * 48) a.part_steps *= 2;
+    if (a.part_steps > steps) a.part_steps = steps;
+    a.parts = (steps + a.part_steps - 1) / a.part_steps;
     const uint64_t blocks = (n_tokens * a.parts + kThreads / 32 - 1) / (kThreads / 32);
     if (blocks > 0x7fffffffull) return cudaErrorInvalidValue;
     void (*const kernels[2][2][2])(Rotate) = {
