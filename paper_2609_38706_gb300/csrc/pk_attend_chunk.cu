@@ -84,8 +84,8 @@ __device__ __forceinline__ int32_t good_length(const Args &a, int32_t len) {
 // many keys (4 x 512 tokens behind 16384, 256 units: 604 -> 550 us against units cut in two).  Where that gains less
 // than the pieces and their joining cost, a block takes the whole units that begin in its share.
 constexpr int64_t kUnitCost = 512;     // a unit's start and end, in keys
-constexpr int64_t kCutCost = 2048;     // one more piece a block, and the joining
-constexpr int64_t kLeastShare = 1024;
+constexpr int64_t kCutCost = 768;      // one more piece a block, and the joining
+constexpr int64_t kLeastShare = 640;
 
 struct Req {
     int32_t q0, lq, len;
@@ -1140,7 +1140,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
 }
 
 // Joins the pieces of the units that were cut, in the order of their keys: kJoinBlocks for a unit, a warp a row.
-constexpr int kJoinThreads = 256, kJoinBlocks = 8;
+constexpr int kJoinThreads = 256, kJoinBlocks = 16;
 template <int D, uint32_t DT>
 __global__ void __launch_bounds__(kJoinThreads) k_chunk_join(const Args a) {
     const Cut *cuts = a.cuts;
@@ -1153,51 +1153,75 @@ __global__ void __launch_bounds__(kJoinThreads) k_chunk_join(const Args a) {
     const int2 heads = __ldcg(reinterpret_cast<const int2 *>(cuts) + 2);
     if (where.x < 0) return;  // uniform
     const uint32_t lane = threadIdx.x & 31, b0 = (uint32_t)where.x, n = (uint32_t)where.y - b0 + 1;
-    for (uint32_t row = blockIdx.x % kJoinBlocks + threadIdx.x / 32 * kJoinBlocks; row < 2 * kRows;
-         row += kJoinBlocks * (kJoinThreads / 32)) {
-        const uint32_t in = row % kRows, tok = in / a.tile_heads, gh = in % a.tile_heads, t = row / kRows;
-        if (tok >= a.tile_tokens || t * a.tile_tokens + tok >= (uint32_t)where.w || gh >= (uint32_t)heads.y) continue;
-        const int64_t token = (int64_t)where.z + t * a.tile_tokens + tok;
-        const uint32_t qh = (uint32_t)heads.x + gh;
-        auto part_of = [&](uint32_t i) { return (uint64_t)(2 * (b0 + i) + (i == 0)) * 2 * kRows + row; };
-        // The exponent of a piece's weights is ref - fine, which 32 bits may not hold: differences are taken part by part.
-        auto more = [](float2 x, float2 y) { return (x.x - y.x) - (x.y - y.y); };
-        float2 top = make_float2(-FLT_MAX, 0.0f);
-        for (uint32_t i = lane; i < n; i += 32) {
-            const float4 y = __ldcg(ml + part_of(i));
-            if (more(make_float2(y.x, y.y), top) > 0.0f) top = make_float2(y.x, y.y);
-        }
+    // The exponent of a piece's weights is ref - fine, which 32 bits may not hold: differences are taken part by part.
+    auto more = [](float2 x, float2 y) { return (x.x - y.x) - (x.y - y.y); };
+    constexpr int kAtOnce = 2 * kRows / kJoinBlocks / (kJoinThreads / 32);  // rows of a warp, whose loads go out together
+    constexpr int kPer = D / 32;
+    const uint32_t row0 = (blockIdx.x % kJoinBlocks * (kJoinThreads / 32) + threadIdx.x / 32) * kAtOnce;
+    auto part_of = [&](uint32_t i, int k) { return (uint64_t)(2 * (b0 + i) + (i == 0)) * 2 * kRows + row0 + k; };
+    float2 top[kAtOnce];
+    float sum[kAtOnce] = {}, o[kAtOnce][kPer] = {};
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) top[k] = make_float2(-FLT_MAX, 0.0f);
+    for (uint32_t i = lane; i < n; i += 32) {
+        float4 y[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) y[k] = __ldcg(ml + part_of(i, k));
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+            if (more(make_float2(y[k].x, y[k].y), top[k]) > 0.0f) top[k] = make_float2(y[k].x, y[k].y);
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
 #pragma unroll
         for (int d = 16; d; d /= 2) {
-            const float2 y = make_float2(__shfl_xor_sync(0xffffffffu, top.x, d), __shfl_xor_sync(0xffffffffu, top.y, d));
-            if (more(y, top) > 0.0f) top = y;
+            const float2 y = make_float2(__shfl_xor_sync(0xffffffffu, top[k].x, d), __shfl_xor_sync(0xffffffffu, top[k].y, d));
+            if (more(y, top[k]) > 0.0f) top[k] = y;
         }
-        const float ref = __shfl_sync(0xffffffffu, top.x, 0), fine = __shfl_sync(0xffffffffu, top.y, 0);
-        constexpr int kPer = D / 32;
-        float sum = 0.0f, o[kPer] = {};
-        for (uint32_t i0 = 0; i0 < n; i0 += 32) {
-            const float4 y = i0 + lane < n ? __ldcg(ml + part_of(i0 + lane)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            const float f = y.z == 0.0f ? 0.0f : pk::ex2(more(make_float2(y.x, y.y), make_float2(ref, fine)));
-#pragma unroll 4
-            for (uint32_t i = 0; i < min(n - i0, 32u); ++i) {
-                const float w = __shfl_sync(0xffffffffu, f, i);
-                sum += w * __shfl_sync(0xffffffffu, y.z, i);
-                const uint64_t at = part_of(i0 + i) * D + lane * kPer;
+        top[k] = make_float2(__shfl_sync(0xffffffffu, top[k].x, 0), __shfl_sync(0xffffffffu, top[k].y, 0));
+    }
+    for (uint32_t i0 = 0; i0 < n; i0 += 32) {
+        float f[kAtOnce], l[kAtOnce];
 #pragma unroll
-                for (int k = 0; k < kPer; k += 2) {
-                    const float2 u = __ldcg(reinterpret_cast<const float2 *>(po + at + k));
-                    o[k] += w * u.x;
-                    o[k + 1] += w * u.y;
+        for (int k = 0; k < kAtOnce; ++k) {
+            const float4 y = i0 + lane < n ? __ldcg(ml + part_of(i0 + lane, k)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            f[k] = y.z == 0.0f ? 0.0f : pk::ex2(more(make_float2(y.x, y.y), top[k]));
+            l[k] = y.z;
+        }
+#pragma unroll 2
+        for (uint32_t i = 0; i < min(n - i0, 32u); ++i) {
+            float2 u[kAtOnce][kPer / 2];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+                for (int e = 0; e < kPer; e += 2)
+                    u[k][e / 2] = __ldcg(reinterpret_cast<const float2 *>(po + part_of(i0 + i, k) * D + lane * kPer + e));
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const float w = __shfl_sync(0xffffffffu, f[k], i);
+                sum[k] += w * __shfl_sync(0xffffffffu, l[k], i);
+#pragma unroll
+                for (int e = 0; e < kPer; e += 2) {
+                    o[k][e] += w * u[k][e / 2].x;
+                    o[k][e + 1] += w * u[k][e / 2].y;
                 }
             }
         }
-        const float inv = sum == 0.0f ? 0.0f : a.v_scale / sum;
+    }
 #pragma unroll
-        for (int i = 0; i < kPer; i += 2)
-            *reinterpret_cast<uint32_t *>(a.out + token * a.o_ts + (int64_t)qh * a.o_hs + lane * kPer + i) =
-                pk::Elem<DT>::from2(o[i] * inv, o[i + 1] * inv);
+    for (int k = 0; k < kAtOnce; ++k) {
+        const uint32_t row = row0 + k, in = row % kRows, tok = in / a.tile_heads, gh = in % a.tile_heads, t = row / kRows;
+        if (tok >= a.tile_tokens || t * a.tile_tokens + tok >= (uint32_t)where.w || gh >= (uint32_t)heads.y) continue;
+        const int64_t token = (int64_t)where.z + t * a.tile_tokens + tok;
+        const uint32_t qh = (uint32_t)heads.x + gh;
+        const float inv = sum[k] == 0.0f ? 0.0f : a.v_scale / sum[k];
+#pragma unroll
+        for (int e = 0; e < kPer; e += 2)
+            *reinterpret_cast<uint32_t *>(a.out + token * a.o_ts + (int64_t)qh * a.o_hs + lane * kPer + e) =
+                pk::Elem<DT>::from2(o[k][e] * inv, o[k][e + 1] * inv);
         if (lane == 0 && a.lse)
-            a.lse[token * a.q_heads + qh] = sum == 0.0f ? -INFINITY : (ref - fine + log2f(sum)) * 0.69314718055994531f;
+            a.lse[token * a.q_heads + qh] =
+                sum[k] == 0.0f ? -INFINITY : (top[k].x - top[k].y + log2f(sum[k])) * 0.69314718055994531f;
     }
 }
 
