@@ -916,11 +916,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
             float ref = -FLT_MAX, fine = 0.0f, sum = 0.0f;
             uint32_t marked = 0;  // blocks of 16 dimensions in which the row saw a NaN of V
             bool lost = false;    // it saw a token whose slot is out of range
+            bool far_off = false; // a row of the warp has a far reference
 #pragma unroll 1
             for (int32_t j = 0; ok && j < n_tiles; ++j, ++ni) {
-                ok = pk::mbar_wait_warp(pk::smem_addr(&sm.s_full[t]), ni & 1);
-                if (!ok) break;
-                pk::tmem_fence_after();
                 // the row sees the tile's keys up to `see` that are not below `from`, or are below `first`
                 const bool edge = j >= mine->causal || (j >= mine->hides[0] && j < mine->hides[1]);
                 int32_t see = kKeys - 1, from = 0, first = 0;
@@ -933,15 +931,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     }
                 }
                 auto hidden = [&](int32_t i) { return i > see || (i < from && i >= first); };
-                const uint32_t note = (tiles + j) % kNotes;
-                const uint32_t flags = *reinterpret_cast<const volatile uint16_t *>(sm.flags[note]);
-                if (flags) {
-                    lost |= (flags & 0x0101u * kLost) != 0;
-#pragma unroll 1
-                    for (int32_t i = 0; i < kKeys; ++i)
-                        if ((flags >> (i / 64 * 8) & kMarked) && !hidden(i)) marked |= sm.marked[note][i];
-                }
                 uint32_t x[3][32];
+                ok = pk::mbar_wait_warp(pk::smem_addr(&sm.s_full[t]), ni & 1);
+                if (!ok) break;
+                pk::tmem_fence_after();
+                pk::tmem_load32(ts, x[0]);
                 // -infinity for the keys of a chunk of 32 that the row does not see; most chunks of an edge tile are seen
                 // whole by all of a warp's rows.
                 auto mask = [&](int c, uint32_t(&y)[32]) {
@@ -955,8 +949,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 // Chunk c of the scores, 32 keys.  Loads run ahead (1 and 2 behind 0's use, 3 behind 1's).  Masked or
                 // not is known at compile time.
                 auto chunk = [&](int c, auto masked) -> uint32_t(&)[32] {
-                    if (c == 0) pk::tmem_load32(ts, x[0]);
-                    uint32_t(&y)[32] = x[c % 3];
+                    uint32_t(&y)[32] = x[c % 3];  // (0's is on its way)
                     if (c != 2) pk::tmem_wait_load(y);
                     if (c == 0) {
                         pk::tmem_load32(ts + 32, x[1]);
@@ -979,13 +972,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
 #pragma unroll
                         for (int i = 0; i < 32; ++i) m4[i & 3] = fmaxf(m4[i & 3], __uint_as_float(x[0][i]));
                     }
+                    pk::tmem_load32(ts, x[0]);  // for what comes next
                     return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
                 };
                 // The weights by the reference so far, and their sum.
                 uint32_t p[2][32];
                 auto weigh = [&](auto masked) {
                     const uint64_t ref2 = pk::pack2(-ref, -ref);
-                    uint64_t sum2[2] = {0, 0};
+                    uint64_t sum2[4] = {0, 0, 0, 0};
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         uint32_t(&y)[32] = chunk(c, masked);
@@ -995,11 +989,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                                 pk::fma2(pk::pack2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), scale22, ref2));
                             z.x = pk::ex2(z.x);
                             z.y = pk::ex2(z.y);
-                            sum2[i / 2 & 1] = pk::add2(sum2[i / 2 & 1], pk::pack2(z.x, z.y));
+                            sum2[i / 2 & 3] = pk::add2(sum2[i / 2 & 3], pk::pack2(z.x, z.y));
                             p[c / 2][c % 2 * 16 + i / 2] = pk::Elem<PK_FP16>::from2(z.x, z.y);
                         }
                     }
-                    const float2 s0 = pk::unpack2(sum2[0]), s1 = pk::unpack2(sum2[1]);
+                    const float2 s0 = pk::unpack2(pk::add2(sum2[0], sum2[2])), s1 = pk::unpack2(pk::add2(sum2[1], sum2[3]));
                     return (s0.x + s1.x) + (s0.y + s1.y);
                 };
                 // The same where a row of the warp has a far reference, which few calls have: by 16 scores, with `fine`.
@@ -1028,7 +1022,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     return s;
                 };
                 auto weigh_any = [&]() {
-                    if (__any_sync(0xffffffffu, fine != 0.0f)) return weigh_far();
+                    if (far_off) return weigh_far();
                     return edge ? weigh(std::true_type{}) : weigh(std::false_type{});
                 };
                 // Moves the reference of the rows that `over` names to the score `top`; their sum so far is rescaled.
@@ -1044,6 +1038,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     const float f = pk::ex2((ref - next) + (next_fine - fine));
                     ref = next;
                     fine = next_fine;
+                    far_off = __any_sync(0xffffffffu, fine != 0.0f);
                     sum *= f;
                     return f;
                 };
@@ -1063,12 +1058,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                         pk::tmem_fence_after();
 #pragma unroll 1
                         for (int d = 0; d < D / 32; ++d) {
-                            pk::tmem_load32(to + 32 * d, x[0]);
-                            pk::tmem_wait_load(x[0]);
+                            pk::tmem_load32(to + 32 * d, x[1]);
+                            pk::tmem_wait_load(x[1]);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) x[0][i] = __float_as_uint(__uint_as_float(x[0][i]) * f);
-                            pk::tmem_store32(to + 32 * d, x[0]);
+                            for (int i = 0; i < 32; ++i) x[1][i] = __float_as_uint(__uint_as_float(x[1][i]) * f);
+                            pk::tmem_store32(to + 32 * d, x[1]);
                         }
+                        pk::tmem_load32(ts, x[0]);
                     }
                     part_sum = weigh_any();
                 }
@@ -1079,6 +1075,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 pk::tmem_fence_before();
                 __syncwarp();
                 if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.p_ready[t]));
+                const uint32_t note = (tiles + j) % kNotes;
+                const uint32_t flags = *reinterpret_cast<const volatile uint16_t *>(sm.flags[note]);
+                if (flags) {
+                    lost |= (flags & 0x0101u * kLost) != 0;
+#pragma unroll 1
+                    for (int32_t i = 0; i < kKeys; ++i)
+                        if ((flags >> (i / 64 * 8) & kMarked) && !hidden(i)) marked |= sm.marked[note][i];
+                }
             }
             tiles += (uint32_t)it.n_all;
             if (ok && n_tiles > 0) ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);
