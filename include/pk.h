@@ -623,7 +623,7 @@ int pk_attend_cache_window(const pk_kv_cache *kv, uint32_t dtype, const pk_heads
  * written); a kv_len out of range (PK_ERR_ARG) counts as 0; a slot out of
  * range (PK_ERR_ARG) makes out and lse NaN for the queries that see its page,
  * and for others of its request unspecified numbers or NaN.  PK_ERR_TIMEOUT. */
-size_t pk_attend_chunk_scratch_bytes(const pk_kv_cache *kv, uint64_t n_q, uint32_t R, uint32_t q_heads,
+size_t pk_attend_chunk_scratch_bytes(const pk_kv_cache *kv, uint32_t dtype, uint64_t n_q, uint32_t R, uint32_t q_heads,
                                      uint64_t page_stride, uint32_t window, uint32_t sinks);
 int pk_attend_chunk(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, const pk_heads *out, float *lse_dev,
                     uint64_t n_q, const int64_t *q_off_dev, uint32_t R, uint32_t q_heads, float scale, uint32_t window,

@@ -3,8 +3,11 @@
 //
 // out = v_scale sum_j p_j V_j / sum_j p_j over the keys j that a query sees, p_j =
 // 2^(s_j - ref), s_j = scale k_scale log2(e) q . K_j; K and V are code * scale, which
-// has six significant bits: exact in a half and in a bfloat16.  K takes the type of
-// q, which the matrix instruction wants, V and the weights are halves for either.
+// has six significant bits: exact in a half and in a bfloat16.  All products are of
+// halves: queries in bfloat16 are scaled by a power of two a row first, which
+// leaves them as they are (k_chunk_queries); where one row's values lie too far
+// apart for that, the call's products with K are of bfloat16s, to which K costs
+// more to unpack (470 | 439 us for 4 x 512 tokens behind 16384).
 // ref moves as in pk_attend_prompt.cu: only when a tile's weights of a row sum to
 // more than 2^15.
 //
@@ -48,6 +51,12 @@ struct Args {
     const uint8_t *pool;
     uint64_t page_bytes, n_slots, page_stride, positions;  // positions: that a request can hold
     uint32_t page_grans;  // granules of one head in a page
+    const uint16_t *q;
+    int64_t q_ts, q_hs;
+    uint16_t *half_q;   // [n_q][q_heads][D], queries in bfloat16 as halves; times row_down they are what they were
+    float *row_down;    // [n_q][q_heads]
+    uint8_t *too_wide;  // by block of k_chunk_queries: a row that halves do not hold
+    uint32_t query_blocks;
     const int64_t *q_off;
     const int32_t *kv_len;
     const uint32_t *pages;
@@ -238,6 +247,58 @@ struct Item {
     __device__ __forceinline__ int32_t tok0(const Args &a) const { return at.u * 2 * (int32_t)a.tile_tokens; }
 };
 
+// Queries in bfloat16 as halves, times the power of two that brings a row's largest value to [2^14, 2^15): all values down
+// to 2^-31 of it keep their 8 bits.  8 values a lane.
+constexpr int kQueryThreads = 256;
+constexpr uint32_t kQueryBlocks = 1024;
+template <int D>
+__global__ void __launch_bounds__(kQueryThreads) k_chunk_queries(const Args a) {
+    constexpr uint32_t kLanes = D / 8, kRowsAtOnce = kQueryThreads / kLanes;
+    const uint16_t *q = a.q;
+    pk::pdl_wait(q);
+    pk::pdl_launch_dependents();
+    const uint64_t rows = a.n_q * a.q_heads;
+    const uint32_t c = threadIdx.x % kLanes;
+    bool wide = false;
+    for (uint64_t row0 = (uint64_t)blockIdx.x * kRowsAtOnce; row0 < rows; row0 += (uint64_t)gridDim.x * kRowsAtOnce) {
+        const uint64_t row = row0 + threadIdx.x / kLanes;
+        const bool on = row < rows;
+        const uint64_t token = on ? row / a.q_heads : 0;
+        const uint32_t h = on ? (uint32_t)(row - token * a.q_heads) : 0;
+        const uint4 u = on ? __ldcg(reinterpret_cast<const uint4 *>(q + (int64_t)token * a.q_ts + (int64_t)h * a.q_hs + c * 8))
+                           : make_uint4(0, 0, 0, 0);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        float x[8], top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = pk::Elem<PK_BF16>::to2(w[i]);
+            x[2 * i] = f.x, x[2 * i + 1] = f.y;
+        }
+        uint32_t bits = 0;  // of the largest magnitude, found on the bits, which finds a NaN too
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bits = max(bits, __float_as_uint(x[i]) & 0x7fffffffu);
+#pragma unroll
+        for (uint32_t d = 1; d < kLanes; d *= 2) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, d));
+        top = __uint_as_float(bits);
+        const int e = top == 0.0f || bits >= 0x7f800000u ? 14 : max((int)(bits >> 23) - 127, -110);  // 2^e <= top
+        const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
+        uint32_t out[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float lo = x[2 * i] * up, hi = x[2 * i + 1] * up;
+            const __half2 had = __floats2half2_rn(lo, hi);
+            wide |= !(__low2float(had) == lo && __high2float(had) == hi);
+            out[i] = *reinterpret_cast<const uint32_t *>(&had);
+        }
+        wide |= bits >= 0x7f800000u;
+        if (!on) continue;
+        *reinterpret_cast<uint4 *>(a.half_q + row * D + c * 8) = make_uint4(out[0], out[1], out[2], out[3]);
+        if (c == 0) a.row_down[row] = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
+    }
+    const int any = __syncthreads_or(wide);
+    if (threadIdx.x == 0) a.too_wide[blockIdx.x] = (uint8_t)(any != 0);
+}
+
 // Shared memory of a CTA, from a 1024-byte boundary: Q (two tiles), the ring of K and V tiles in 16 bits, the ring of
 // granules as they lie in the pages, then Small.
 template <int D>
@@ -268,6 +329,7 @@ struct Piece {
     int32_t n_tiles[2], n_all;     // key tiles; n_all -1: no item, the end
     int32_t first, skip, len;
     uint32_t n_gran;
+    int32_t halves;                // the call's queries are halves
 };
 
 struct Small {
@@ -449,7 +511,8 @@ struct Unpack {
 // to a column, take the place of scores that have been read), then their outputs
 // (D columns each).  Every counter of a barrier's use runs on over the items.
 template <int D, uint32_t DT>
-__global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, const __grid_constant__ CUtensorMap map_q) {
+__global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, const __grid_constant__ CUtensorMap map_q,
+                                                               const __grid_constant__ CUtensorMap map_half) {
     using L = Layout<D>;
     using G = pk::Granule<D>;
     // all the shared memory that the kernel has, so that it starts on the swizzle's 1024 bytes
@@ -492,7 +555,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
     const int32_t *kv_len = a.kv_len;
     const uint32_t *pages = a.pages;
     const uint8_t *pool = a.pool;
-    pk::pdl_wait(plan, q_off, kv_len, pages, pool);
+    const float *row_down = a.row_down;
+    const uint8_t *too_wide = a.too_wide;
+    pk::pdl_wait(plan, q_off, kv_len, pages, pool, row_down, too_wide);
     pk::pdl_launch_dependents();
     pk::tmem_fence_before();
     __syncthreads();
@@ -524,6 +589,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 plan_here(a, sm, q_off, kv_len);
                 __syncwarp();
             }
+            bool halves = true;
+            if (DT == PK_BF16) {
+                uint32_t wide = 0;
+                for (uint32_t i = lane; i < a.query_blocks; i += 32) wide |= __ldcg(too_wide + i);
+                halves = !__any_sync(0xffffffffu, wide != 0);
+            }
+            const CUtensorMap *map = DT == PK_BF16 && halves ? &map_half : &map_q;
             Item it;
             bool more;
             {
@@ -603,6 +675,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     to.skip = it.skip;
                     to.len = it.q.len;
                     to.n_gran = it.n_gran;
+                    to.halves = halves;
                 }
             };
             pk::fence_proxy_async();  // pages written by an earlier kernel are read by the async proxy
@@ -672,7 +745,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                             pk::mbar_expect(bar, q_bytes);
 #pragma unroll
                             for (int b = 0; b < D / 64; ++b)
-                                pk::tile_load3(smem + t * L::kTile + b * 16384, &map_q, b * 64, q_head,
+                                pk::tile_load3(smem + t * L::kTile + b * 16384, map, b * 64, q_head,
                                                q_row + t * (int)a.tile_tokens, bar);
                             ++nq[t];
                         }
@@ -711,7 +784,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 ok = wait_item(items);
                 if (!ok) break;
                 const volatile Piece &it = sm.piece[items % kItems];
-                const int32_t n_all = it.n_all, skip = it.skip, len = it.len;
+                const int32_t n_all = it.n_all, skip = it.skip, len = it.len, halves = it.halves;
                 const uint32_t first = (uint32_t)it.first, n_gran = it.n_gran;
                 return_item(items);
                 if (n_all < 0) break;
@@ -731,8 +804,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
 #pragma unroll 1
                     for (uint32_t s = mine; s < kSteps; s += kMakers) {
                         const uint32_t g = s / kPerGran, r = s % kPerGran * U::kRows;
-                        if (g < have)
-                            lanes.template step<DT == PK_BF16, false>(place(g) + G::kK, place(g) + G::kKs, tile + s * U::kRows * 128, r, 16);
+                        if (g >= have) continue;
+                        if (DT == PK_FP16 || halves)
+                            lanes.template step<false, false>(place(g) + G::kK, place(g) + G::kKs, tile + s * U::kRows * 128, r, 16);
+                        else
+                            lanes.template step<true, false>(place(g) + G::kK, place(g) + G::kKs, tile + s * U::kRows * 128, r, 16);
                     }
                     pk::fence_proxy_async_smem();
                     if (mine >= kMakers - 2) {  // blocks of V marked NaN, two tokens a lane
@@ -785,8 +861,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
             if (!ok && lane == 0) give_up();
             __syncwarp();
         } else if (warp == kWarpMma) {
-            const uint32_t qk_kind = pk::mma_idesc(DT == PK_BF16, 128, 128, false) |
-                                     (a.scale2 < 0.0f ? 1u << 13 : 0u);  // a negative scale negates Q
+            uint32_t qk_kind = 0;
             constexpr uint32_t kPv = pk::mma_idesc(false, 128, D, true);
             uint32_t ring = 0, use = 0;             // next ring stage, and how often the ring has been gone round
             uint32_t ni0 = 0, ni1 = 0, nq0 = 0, nq1 = 0;  // key tiles and Q tiles used so far, by tile
@@ -831,6 +906,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 const volatile Piece &it = sm.piece[items % kItems];
                 const int32_t n0 = (int32_t)pk::uniform(it.n_tiles[0]), n1 = (int32_t)pk::uniform(it.n_tiles[1]);
                 const int32_t n_all = (int32_t)pk::uniform(it.n_all);
+                qk_kind = pk::mma_idesc(DT == PK_BF16 && !pk::uniform(it.halves), 128, 128, false) |
+                          (a.scale2 < 0.0f ? 1u << 13 : 0u);  // a negative scale negates Q
                 return_item(items);
                 if (n_all < 0) break;
                 if (n_all == 0) continue;
@@ -899,9 +976,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
         const int32_t row = tid & 127;  // TMEM lane
         const int32_t row_tok = row / (int32_t)a.tile_heads, row_head = row % (int32_t)a.tile_heads;
         const uint32_t ts = tmem + 128 * t + ((warp & 3) * 32 << 16), to = tmem + 256 + D * t + ((warp & 3) * 32 << 16);
-        // a scale of 0 would make a masked -infinity NaN; the smallest normal one gives the same weights
-        const float scale2 = fmaxf(fabsf(a.scale2), FLT_MIN);
-        const uint64_t scale22 = pk::pack2(scale2, scale2);
         uint32_t ni = 0, tiles = 0;  // key tiles weighed so far; key tiles of the CTA's items before the present one
         bool ok = true;
         for (uint32_t items = 0; ok && !__any_sync(0xffffffffu, *abort != 0); ++items) {
@@ -911,7 +985,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
             const volatile Piece::Tile *mine = &it.tile[t];
             if (it.n_all < 0) break;
             const int32_t n_tiles = it.n_tiles[t];
+            float scale2 = fabsf(a.scale2);
             const bool on = row_tok < mine->tokens && row_tok < (int32_t)a.tile_tokens && row_head < mine->heads;
+            if (DT == PK_BF16 && on && it.halves)
+                scale2 *= __ldcg(row_down + (int64_t)(mine->row0 + row_tok) * a.q_heads + mine->head0 + row_head);
+            // a scale of 0 would make a masked -infinity NaN; the smallest normal one gives the same weights
+            scale2 = fmaxf(scale2, FLT_MIN);
+            const uint64_t scale22 = pk::pack2(scale2, scale2);
             // a weight is 2^(score - ref + fine), and fine is 0 but for a reference of kFar and more
             float ref = -FLT_MAX, fine = 0.0f, sum = 0.0f;
             uint32_t marked = 0;  // blocks of 16 dimensions in which the row saw a NaN of V
@@ -1232,12 +1312,12 @@ __global__ void __launch_bounds__(kJoinThreads) k_chunk_join(const Args a) {
 // What the host knows of a call are bounds; the kernels see the lengths.
 struct Plan {
     uint64_t units, blocks;  // at most
-    uint64_t plan_bytes, cut_bytes, ml_bytes, o_bytes;
+    uint64_t plan_bytes, cut_bytes, ml_bytes, o_bytes, wide_bytes, down_bytes, half_bytes;
 };
 
 constexpr uint64_t kSms = 152;
-Plan plan_of(const pk_kv_cache &kv, uint32_t R, uint64_t n_q, uint32_t q_heads, uint64_t page_stride, uint32_t window,
-             uint32_t sinks) {
+Plan plan_of(const pk_kv_cache &kv, uint32_t dtype, uint32_t R, uint64_t n_q, uint32_t q_heads, uint64_t page_stride,
+             uint32_t window, uint32_t sinks) {
     Plan p;
     p.units = pk_attend_prompt_items(n_q, R, q_heads, kv.kv_heads);
     uint64_t keys = page_stride * kv.page_tokens;
@@ -1248,27 +1328,32 @@ Plan plan_of(const pk_kv_cache &kv, uint32_t R, uint64_t n_q, uint32_t q_heads, 
     p.cut_bytes = p.blocks * sizeof(Cut);
     p.ml_bytes = p.blocks > 1 ? 2 * p.blocks * 2 * kRows * 16 : 0;
     p.o_bytes = p.blocks > 1 ? 2 * p.blocks * 2 * kRows * kv.head_dim * 4 : 0;
+    const uint64_t rows = dtype == PK_BF16 ? n_q * q_heads : 0;
+    p.wide_bytes = rows ? kQueryBlocks : 0;
+    p.down_bytes = (rows * 4 + 31) & ~31ull;
+    p.half_bytes = rows * kv.head_dim * 2;
     return p;
 }
 
 template <int D, uint32_t DT>
-cudaError_t launch(const Args &a, const CUtensorMap &mq, cudaStream_t s) {
+cudaError_t launch(const Args &a, const CUtensorMap &mq, const CUtensorMap &mh, cudaStream_t s) {
     constexpr size_t smem = Layout<D>::kBytes + sizeof(Small);
     static_assert(smem <= 227 * 1024, "shared memory of a block");
     static std::atomic<uint64_t> seen{0};
     cudaError_t e = pk_allow_smem(k_attend_chunk<D, DT>, smem, seen);
-    if (e == cudaSuccess) e = pk_launch_smem(k_attend_chunk<D, DT>, a.blocks, kThreads, smem, s, a, mq);
+    if (e == cudaSuccess && DT == PK_BF16) e = pk_launch(k_chunk_queries<D>, a.query_blocks, kQueryThreads, s, a);
+    if (e == cudaSuccess) e = pk_launch_smem(k_attend_chunk<D, DT>, a.blocks, kThreads, smem, s, a, mq, mh);
     if (e == cudaSuccess && a.blocks > 1) e = pk_launch(k_chunk_join<D, DT>, (a.blocks - 1) * (unsigned)kJoinBlocks, kJoinThreads, s, a);
     return e;
 }
 
 }  // namespace
 
-uint64_t pk_attend_chunk_scratch_bytes_impl(const pk_kv_cache &kv, uint32_t R, uint64_t n_q, uint32_t q_heads,
+uint64_t pk_attend_chunk_scratch_bytes_impl(const pk_kv_cache &kv, uint32_t dtype, uint32_t R, uint64_t n_q, uint32_t q_heads,
                                             uint64_t page_stride, uint32_t window, uint32_t sinks) {
-    const Plan p = plan_of(kv, R, n_q, q_heads, page_stride, window, sinks);
+    const Plan p = plan_of(kv, dtype, R, n_q, q_heads, page_stride, window, sinks);
     if (p.units > 0x7fffffffull) return UINT64_MAX;
-    return p.plan_bytes + p.cut_bytes + p.ml_bytes + p.o_bytes;
+    return p.plan_bytes + p.cut_bytes + p.ml_bytes + p.o_bytes + p.wide_bytes + p.down_bytes + p.half_bytes;
 }
 
 cudaError_t pk_launch_attend_chunk(const pk_kv_cache &kv, uint32_t dtype, const pk_heads &q, const pk_heads &out,
@@ -1276,8 +1361,11 @@ cudaError_t pk_launch_attend_chunk(const pk_kv_cache &kv, uint32_t dtype, const 
                                    float scale, uint32_t window, uint32_t sinks, const int32_t *kv_len,
                                    const uint32_t *pages, uint64_t page_stride, void *scratch, int32_t *status,
                                    cudaStream_t s) {
-    const Plan p = plan_of(kv, R, n_q, q_heads, page_stride, window, sinks);
+    const Plan p = plan_of(kv, dtype, R, n_q, q_heads, page_stride, window, sinks);
     Args a;
+    a.q = static_cast<const uint16_t *>(q.p);
+    a.q_ts = q.tok_stride;
+    a.q_hs = q.head_stride;
     a.pool = static_cast<const uint8_t *>(kv.pool_dev);
     a.page_bytes = pk_kv_page_bytes(kv.page_tokens, kv.kv_heads, kv.head_dim);
     a.n_slots = kv.n_slots;
@@ -1311,14 +1399,23 @@ cudaError_t pk_launch_attend_chunk(const pk_kv_cache &kv, uint32_t dtype, const 
     a.cuts = reinterpret_cast<Cut *>(at + p.plan_bytes);
     a.part_ml = reinterpret_cast<float4 *>(at + p.plan_bytes + p.cut_bytes);
     a.part_o = reinterpret_cast<float *>(at + p.plan_bytes + p.cut_bytes + p.ml_bytes);
+    at += p.plan_bytes + p.cut_bytes + p.ml_bytes + p.o_bytes;
+    a.too_wide = at;
+    a.row_down = reinterpret_cast<float *>(at + p.wide_bytes);
+    a.half_q = reinterpret_cast<uint16_t *>(at + p.wide_bytes + p.down_bytes);
+    const uint64_t query_rows = kQueryThreads / (kv.head_dim / 8);  // of a block at once
+    a.query_blocks = (uint32_t)std::min<uint64_t>((n_q * q_heads + query_rows - 1) / query_rows, kQueryBlocks);
     a.status = status;
-    CUtensorMap mq;
+    CUtensorMap mq, mh{};
     cudaError_t e = map_of(&mq, q, n_q, q_heads, kv.head_dim, dtype, a.tile_tokens, a.tile_heads);
+    if (e == cudaSuccess && dtype == PK_BF16)
+        e = map_of(&mh, pk_heads{a.half_q, (int64_t)q_heads * kv.head_dim, kv.head_dim}, n_q, q_heads, kv.head_dim, PK_FP16,
+                   a.tile_tokens, a.tile_heads);
     if (e == cudaSuccess && a.plan) e = pk_launch(k_chunk_plan, 1, kPlanThreads, s, a);
     if (e != cudaSuccess) return e;
     if (kv.head_dim == 128)
-        e = dtype == PK_BF16 ? launch<128, PK_BF16>(a, mq, s) : launch<128, PK_FP16>(a, mq, s);
+        e = dtype == PK_BF16 ? launch<128, PK_BF16>(a, mq, mh, s) : launch<128, PK_FP16>(a, mq, mh, s);
     else
-        e = dtype == PK_BF16 ? launch<64, PK_BF16>(a, mq, s) : launch<64, PK_FP16>(a, mq, s);
+        e = dtype == PK_BF16 ? launch<64, PK_BF16>(a, mq, mh, s) : launch<64, PK_FP16>(a, mq, mh, s);
     return e != cudaSuccess ? e : cudaGetLastError();
 }

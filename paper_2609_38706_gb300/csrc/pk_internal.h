@@ -112,8 +112,8 @@ cudaError_t pk_launch_attend_cache(const pk_kv_cache &kv, uint32_t dtype, const 
                                    float *page_weight, uint32_t window, uint32_t sinks, void *scratch, int32_t *status,
                                    cudaStream_t s);
 // UINT64_MAX as above.
-uint64_t pk_attend_chunk_scratch_bytes_impl(const pk_kv_cache &kv, uint32_t R, uint64_t n_q, uint32_t q_heads,
-                                            uint64_t page_stride, uint32_t window, uint32_t sinks);
+uint64_t pk_attend_chunk_scratch_bytes_impl(const pk_kv_cache &kv, uint32_t dtype, uint32_t R, uint64_t n_q,
+                                            uint32_t q_heads, uint64_t page_stride, uint32_t window, uint32_t sinks);
 cudaError_t pk_launch_attend_chunk(const pk_kv_cache &kv, uint32_t dtype, const pk_heads &q, const pk_heads &out,
                                    float *lse, uint64_t n_q, const int64_t *q_off, uint32_t R, uint32_t q_heads,
                                    float scale, uint32_t window, uint32_t sinks, const int32_t *kv_len,

@@ -179,10 +179,10 @@ static bool good_chunk(const pk_kv_cache *kv, uint32_t R, uint64_t n_q, uint32_t
            page_stride < 1ull << 31 && page_stride * kv->page_tokens <= 0x7fff0000ull && good_window(window, sinks);
 }
 
-size_t pk_attend_chunk_scratch_bytes(const pk_kv_cache *kv, uint64_t n_q, uint32_t R, uint32_t q_heads,
+size_t pk_attend_chunk_scratch_bytes(const pk_kv_cache *kv, uint32_t dtype, uint64_t n_q, uint32_t R, uint32_t q_heads,
                                      uint64_t page_stride, uint32_t window, uint32_t sinks) {
-    if (!good_chunk(kv, R, n_q, q_heads, page_stride, window, sinks)) return 0;
-    const uint64_t need = pk_attend_chunk_scratch_bytes_impl(*kv, R, n_q, q_heads, page_stride,
+    if (dtype > PK_FP16 || !good_chunk(kv, R, n_q, q_heads, page_stride, window, sinks)) return 0;
+    const uint64_t need = pk_attend_chunk_scratch_bytes_impl(*kv, dtype, R, n_q, q_heads, page_stride,
                                                              window_within(*kv, page_stride, window), sinks);
     return need == UINT64_MAX ? 0 : (size_t)need;
 }
@@ -201,7 +201,7 @@ int pk_attend_chunk(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, co
     if (R == 0 || n_q == 0) return PK_OK;
     if (!q_off_dev || !kv_len_dev || (page_stride && !pages_dev) || !scratch_dev) return PK_ERR_ARG;
     window = window_within(*kv, page_stride, window);
-    const uint64_t need = pk_attend_chunk_scratch_bytes_impl(*kv, R, n_q, q_heads, page_stride, window, sinks);
+    const uint64_t need = pk_attend_chunk_scratch_bytes_impl(*kv, dtype, R, n_q, q_heads, page_stride, window, sinks);
     if (need == UINT64_MAX || scratch_bytes < need) return PK_ERR_ARG;
     return cuda_rc(pk_launch_attend_chunk(*kv, dtype, *q, *out, lse_dev, n_q, q_off_dev, R, q_heads, scale, window, sinks,
                                           kv_len_dev, pages_dev, page_stride, scratch_dev, status_dev,

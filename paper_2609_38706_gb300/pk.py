@@ -147,7 +147,7 @@ def lib() -> ctypes.CDLL:
             "pk_attend_cache_window_scratch_bytes": (ctypes.c_size_t, [_VP, _U32, _U32, _U32, _U64, ctypes.c_int, _U32, _U32]),
             "pk_attend_cache_window": (ctypes.c_int, [_VP, _U32, _VP, _VP, _VP, _U32, _U32, _U32, ctypes.c_float, _U32, _U32,
                                                       _VP, _VP, _U64, _VP, _VP, ctypes.c_size_t, _VP, _VP]),
-            "pk_attend_chunk_scratch_bytes": (ctypes.c_size_t, [_VP, _U64, _U32, _U32, _U64, _U32, _U32]),
+            "pk_attend_chunk_scratch_bytes": (ctypes.c_size_t, [_VP, _U32, _U64, _U32, _U32, _U64, _U32, _U32]),
             "pk_attend_chunk": (ctypes.c_int, [_VP, _U32, _VP, _VP, _VP, _U64, _VP, _U32, _U32, ctypes.c_float, _U32, _U32,
                                                _VP, _VP, _U64, _VP, ctypes.c_size_t, _VP, _VP]),
             "pk_attend_cache": (ctypes.c_int, [_VP, _U32, _VP, _VP, _VP, _U32, _U32, _U32, ctypes.c_float, _VP, _VP,
@@ -760,9 +760,9 @@ def _attend_cache(fn: str, call, limits, kv, q, out, lse, n_q, kv_len, pages, sc
         _check(rc, fn)
 
 
-def pk_attend_chunk_scratch_bytes(kv: pk_kv_cache, n_q: int, R: int, q_heads: int, page_stride: int, window: int,
-                                  sinks: int) -> int:
-    return int(lib().pk_attend_chunk_scratch_bytes(ctypes.byref(kv), n_q, R, q_heads, page_stride,
+def pk_attend_chunk_scratch_bytes(kv: pk_kv_cache, dtype: torch.dtype, n_q: int, R: int, q_heads: int, page_stride: int,
+                                  window: int, sinks: int) -> int:
+    return int(lib().pk_attend_chunk_scratch_bytes(ctypes.byref(kv), _KV_DTYPES.get(dtype, 2), n_q, R, q_heads, page_stride,
                                                    *_window("pk_attend_chunk", window, sinks)))
 
 

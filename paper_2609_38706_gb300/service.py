@@ -352,7 +352,12 @@ class KVPages:
             raise pk.PKError(pk.PK_ERR_ARG, "KVPages.attend_chunk: q is [n_q, q_heads, head_dim]")
         n_q, heads, D = q.shape
         limits = _limits("KVPages.attend_chunk", window, sinks)
-        nbytes = pk.pk_attend_chunk_scratch_bytes(self.kv, n_q, pages.shape[0], heads, pages.shape[-1], *limits)
+        key = (q.dtype, n_q, pages.shape[0], heads, pages.shape[-1], *limits)
+        nbytes = self._scratch_bytes.get(key)
+        if nbytes is None:
+            if len(self._scratch_bytes) >= 4096:
+                self._scratch_bytes.clear()
+            nbytes = self._scratch_bytes[key] = pk.pk_attend_chunk_scratch_bytes(self.kv, *key)
         out, lse, scratch = _empty(q, self.stream, (q.shape, q.dtype), (q.shape[:2], torch.float32),
                                    ((nbytes,), torch.uint8))
         pk.pk_attend_chunk(self.kv, q, out, lse, q_off, kv_len, pages, D ** -0.5 if scale is None else scale, *limits, scratch,

@@ -43,15 +43,18 @@ def test_nothing_to_do(pk):
 
 
 def test_chunk_scratch(pk):
+    import torch
     kv = pk.pk_kv_cache(FAKE, 1 << 20, 256, 8, 128, 1.0, 1.0)
-    size = lambda n, R, stride, w=0, s=0: pk.pk_attend_chunk_scratch_bytes(kv, n, R, 32, stride, w, s)  # noqa: E731
+    size = lambda n, R, stride, w=0, s=0: pk.pk_attend_chunk_scratch_bytes(kv, torch.float16, n, R, 32, stride, w, s)  # noqa: E731
     assert 0 < size(1, 1, 1) < size(16, 1, 512) < 1 << 27        # pieces of at most as many units as there are blocks
     assert size(1 << 20, 4, 512) == size(1 << 10, 4, 512)
     assert size(16, 1, 512, 128, 4) < size(16, 1, 512)           # a window is four tiles
     assert size(16, 1, 512, 512 * 256, 4) == size(16, 1, 512)    # one that no request outgrows is none
     one = pk.pk_kv_cache(FAKE, 4, 16, 1, 64, 1.0, 1.0)
-    assert pk.pk_attend_chunk_scratch_bytes(one, 1, 1, 1, 1, 0, 0) < 4096  # one block: nothing is cut
+    assert pk.pk_attend_chunk_scratch_bytes(one, torch.float16, 1, 1, 1, 1, 0, 0) < 4096  # one block: nothing is cut
     assert all(x % 16 == 0 for x in (size(16, 1, 512), size(16, 40, 512)))
+    assert pk.pk_attend_chunk_scratch_bytes(kv, torch.bfloat16, 100, 1, 32, 2, 0, 0) - size(100, 1, 2) >= 100 * 32 * (256 + 4)
+    assert pk.pk_attend_chunk_scratch_bytes(kv, torch.float32, 100, 1, 32, 2, 0, 0) == 0
     for bad in ((1 << 31, 1, 4, 0, 0), (4, 1, 4, 1 << 31, 0)):
         try:
             assert size(*bad) == 0

@@ -188,7 +188,7 @@ def test_errors_reported(new, lens):
     # offsets out of order or range: nothing is written
     for o in ([0, a, sum(new) + 1], [0, a, a - 1], [-1, a, sum(new)], [5, 2, sum(new)], [0, 2 ** 62, sum(new)]):
         out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
-        scratch = torch.zeros(pk.pk_attend_chunk_scratch_bytes(kv.kv, q.shape[0], 2, H * G, pages.shape[1], 0, 0), dtype=torch.uint8, device="cuda")
+        scratch = torch.zeros(pk.pk_attend_chunk_scratch_bytes(kv.kv, q.dtype, q.shape[0], 2, H * G, pages.shape[1], 0, 0), dtype=torch.uint8, device="cuda")
         pk.pk_attend_chunk(kv.kv, q, out, lse, dev(np.array(o)), n, dev(pages), 1.0, 0, 0, scratch, kv.status)
         assert kv.take_status() == pk.PK_ERR_ARG, o
         assert bool((out == 7).all()) and bool((lse == 7).all()), o
@@ -206,7 +206,7 @@ def test_errors_of_many_requests(R_):
     off = np.arange(0, 2 * R_ + 1, 2)
     off[R_ - 1] = -5
     out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
-    scratch = torch.zeros(pk.pk_attend_chunk_scratch_bytes(kv.kv, q.shape[0], R_, 2, pages.shape[1], 0, 0), dtype=torch.uint8, device="cuda")
+    scratch = torch.zeros(pk.pk_attend_chunk_scratch_bytes(kv.kv, q.dtype, q.shape[0], R_, 2, pages.shape[1], 0, 0), dtype=torch.uint8, device="cuda")
     pk.pk_attend_chunk(kv.kv, q, out, lse, dev(off), dev(np.array(lens, np.int32)), dev(pages), 1.0, 0, 0, scratch, kv.status)
     assert kv.take_status() == pk.PK_ERR_ARG and bool((out == 7).all()) and bool((lse == 7).all())
 
@@ -222,7 +222,7 @@ def test_strides_and_rows_of_no_request():
     want, _ = kv.attend_chunk(q[2:27].contiguous(), offsets(new), n, dev(pages))
     wide = torch.full((30, H * G + 1, D), 7.0, dtype=torch.float16, device="cuda")
     out = wide[:, : H * G]
-    scratch = torch.zeros(pk.pk_attend_chunk_scratch_bytes(kv.kv, 30, 2, H * G, pages.shape[1], 0, 0), dtype=torch.uint8, device="cuda")
+    scratch = torch.zeros(pk.pk_attend_chunk_scratch_bytes(kv.kv, q.dtype, 30, 2, H * G, pages.shape[1], 0, 0), dtype=torch.uint8, device="cuda")
     pk.pk_attend_chunk(kv.kv, q, out, None, off, n, dev(pages), D ** -0.5, 0, 0, scratch, kv.status)
     kv.check()
     assert torch.equal(out[2:27], want)
@@ -249,6 +249,46 @@ def test_far_scores_keep_their_order(m, n):
             if top[1] - top[0] > 2 * room + 100:  # no other key weighs anything
                 got = out[i, 0].double().cpu().numpy()
                 assert np.all(np.abs(got - v[s.argmax(), 0]) <= 2.0 ** -8 * np.abs(v[s.argmax(), 0]))
+
+
+@pytest.mark.parametrize("far,D,window", [(2.0 ** 27, 64, None), (2.0 ** 30, 128, 300), (2.0 ** 45, 64, 300), (2.0 ** 60, 128, None)])
+def test_wide_queries(far, D, window):
+    """Rows with one large value, behind which K holds nothing, beside ordinary ones: these keep their bits, also where halves
+    cannot hold both."""
+    m, n, C, H, G = 20, 700, 16, 1, 2
+    pool, pages, rng = make([n], C, H, D, 5)
+    pool.reshape(-1, C // 16, 16 * (D + D // 8))[:, :, 0: 8 * D: D // 2] &= 0xF0  # K: dimension 0 holds nothing
+    q = torch.from_numpy(rng.standard_normal((m, G, D))).to(torch.bfloat16)
+    q[3:, :, 0] = far
+    kv = cache(pool, C, H, D)
+    out, lse = kv.attend_chunk(q.cuda(), offsets([m]), dev(np.array([n], np.int32)), dev(pages), window=window, sinks=2)
+    kv.check()
+    small = np.where(np.arange(D) == 0, 0, q.double().numpy())
+    small[:3] = q[:3].double().numpy()
+    ref, rl, mag, err, _ = reference(pool, pages, [m], [n], small, C, H, D, D ** -0.5, window, 2)
+    check(out, lse, ref, rl, mag, err, "bf16", n)
+
+
+@pytest.mark.parametrize("small", [2.0 ** -100, 2.0 ** -130, 0.0])
+def test_tiny_and_infinite_queries(small):
+    """Rows of tiny values weigh all keys alike; an infinity or NaN reaches its own row only."""
+    m, n, C, H, G, D = 6, 300, 16, 1, 1, 64
+    pool, pages, rng = make([n], C, H, D, 5)
+    q = torch.from_numpy(rng.standard_normal((m, G, D))).to(torch.bfloat16)
+    q[1] *= small
+    kv = cache(pool, C, H, D)
+    args = (offsets([m]), dev(np.array([n], np.int32)), dev(pages))
+    out, lse = kv.attend_chunk(q.cuda(), *args)
+    ref, rl, mag, err, _ = reference(pool, pages, [m], [n], q.double().numpy(), C, H, D, D ** -0.5)
+    check(out, lse, ref, rl, mag, err, "bf16", n)
+    for bad in (float("inf"), float("nan")):
+        odd = q.clone()
+        odd[4, 0, 9] = bad
+        got, glse = kv.attend_chunk(odd.cuda(), *args)
+        kv.check()
+        keep = [0, 1, 2, 3, 5]
+        check(got[keep], glse[keep], ref[keep], rl[keep], mag[keep], err, "bf16", n)
+        assert bool(got[4].isnan().any())
 
 
 def test_one_token_chunks_are_decode_steps():
