@@ -13,6 +13,7 @@ device tensors that a caller passes, and reads of what it gets, the caller order
 from __future__ import annotations
 
 import contextlib
+import operator
 from typing import Optional
 
 import numpy as np
@@ -262,7 +263,7 @@ def _limits(where: str, window: Optional[int], sinks: int):
     """(window, sinks) as the library takes them: 0 is no window."""
     if window is not None and window < 1:
         raise pk.PKError(pk.PK_ERR_ARG, where + ": a window holds a query's own position at least")
-    return (0 if window is None else window), sinks
+    return 0 if window is None else operator.index(window), operator.index(sinks)
 
 
 class KVPages:
@@ -412,6 +413,8 @@ def rotate(q, k, tok_off, start, rotary: Rotary, q_weight: Optional[torch.Tensor
     if q.shape[-1] != rotary.head_dim or rotary.turns.device != q.device:
         raise pk.PKError(pk.PK_ERR_ARG, "rotate: rotary is for other heads, or on another device")
     q_out, k_out = out if out is not None else _empty(q, stream, (q.shape, q.dtype), (k.shape, k.dtype))
+    if stream is not None:  # the table belongs to the stream that it was made on
+        rotary.turns.record_stream(_stream(stream))
     pk.pk_rotate(q, k, q_out, k_out, rotary.table, q_weight, k_weight, eps, tok_off, start, status, stream)
     return q_out, k_out
 

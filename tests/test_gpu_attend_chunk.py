@@ -374,3 +374,51 @@ def test_refusals():
     with pytest.raises(pk.PKError):  # scratch of another call
         pk.pk_attend_chunk(kv.kv, q, torch.empty_like(q), None, ok["q_off"], ok["kv_len"], ok["pages"], 1.0, 0, 0,
                            torch.zeros(8, dtype=torch.uint8, device="cuda"), kv.status)
+
+
+def test_pool_past_32_bits():
+    """Pages whose bytes lie behind 4 GiB answer as the same pages in a small pool, in chunks and in windowed steps."""
+    from paper_2609_38706_gb300.service import KVPages
+    new, lens, C, H, D = [30, 2], [300, 90], 256, 8, 128
+    pool, pages, rng = make(lens, C, H, D, 4)
+    q = torch.from_numpy(rng.standard_normal((32, 16, D))).to(torch.bfloat16).cuda()
+    small = cache(pool, C, H, D)
+    n_slots = (1 << 32) // pool.shape[1] + 40
+    big = KVPages(n_slots, C, H, D)
+    base = n_slots - pool.shape[0]
+    big.pool[base:] = dev(pool)
+    off, n = offsets(new), dev(np.array(lens, np.int32))
+    for window, sinks in ((None, 0), (60, 2)):
+        a = small.attend_chunk(q, off, n, dev(pages), window=window, sinks=sinks)
+        b = big.attend_chunk(q, off, n, dev(pages + base), window=window, sinks=sinks)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    one = q[:2].view(2, 1, 16, D)
+    a = small.attend(one, n, dev(pages), window=60, sinks=2)
+    b = big.attend(one, n, dev(pages + base), window=60, sinks=2)
+    big.check()
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("new,lens,window", [([700] * 6, [900] * 6, None), ([64] * 50, [400] * 50, 100), ([2000], [2000], None),
+                                             ([1] * 300, [33] * 300, None), ([9] * 3, [20000, 150, 9000], 15000)])
+def test_many_shapes_against_small_calls(new, lens, window):
+    """Calls whose work is cut in many ways: each request alone, in a call of its own, is cut elsewhere; both are within the
+    bounds that the small cases hold to, so they differ by two of them at most."""
+    C, H, G, D = 16, 2, 2, 64
+    pool, pages, rng = make(lens, C, H, D, 6)
+    kv = cache(pool, C, H, D)
+    q = torch.from_numpy(rng.standard_normal((sum(new), H * G, D))).to(torch.float16).cuda()
+    n, p = dev(np.array(lens, np.int32)), dev(pages)
+    out, lse = kv.attend_chunk(q, offsets(new), n, p, window=window, sinks=4)
+    a = 0
+    for r, m in enumerate(new):
+        if r % max(1, len(new) // 5) == 0:
+            o, l = kv.attend_chunk(q[a: a + m].contiguous(), offsets([m]), n[r: r + 1].clone(), p[r: r + 1].clone(), window=window, sinks=4)
+            k, v = R.get_tokens(pool, pages[r], lens[r], C, H, D)
+            err = R.score_error(q[a: a + m].double().cpu().numpy(), k, D ** -0.5)
+            # mag, a mean of magnitudes, is at most the largest
+            bound = 2 * R.out_bound(o.double().cpu().numpy(), np.abs(v).max(), R.U["fp16"], R.U["fp16"], err, lens[r])
+            assert np.all(np.abs((out[a: a + m].double() - o.double()).cpu().numpy()) <= bound)
+            assert np.all(np.abs((lse[a: a + m] - l).double().cpu().numpy()) <= 2 * R.lse_bound(l.double().cpu().numpy(), err, lens[r]))
+        a += m
+    kv.check()
