@@ -60,6 +60,7 @@ struct Args {
     bool by_length;                // the longest requests' blocks come first
     float scale2, v_scale;         // scale2 = scale * k_scale * log2 e
     uint32_t window, sinks, sink_grans;  // window 0: none; granules that hold the first `sinks` tokens
+    uint32_t weigh_blocks, sink_blocks;  // of k_cache_finish: that weigh a request's pages; of them for the first tokens' pages
     const uint16_t *q;
     int64_t q_ts, q_hs;
     uint16_t *out;
@@ -755,11 +756,18 @@ __global__ void __launch_bounds__(kFinishThreads) k_cache_finish(const Args a, u
         return;
     }
     const uint32_t per = pages_a_warp(a.page_grans), block_pages = kFinishWarps * per;
-    const uint32_t blocks = (uint32_t)((a.page_stride + block_pages - 1) / block_pages);
-    const uint32_t id = blockIdx.x - join_blocks, r = id / blocks, page0 = id % blocks * block_pages;
+    const uint32_t blocks = a.weigh_blocks;
+    const uint32_t id = blockIdx.x - join_blocks, r = id / blocks;
     const int32_t len = length_of(kv_len, r, most);
     const uint32_t n = live_splits<kWindow>(a, len), n_gran = ((uint32_t)len + 15) / 16;
     const uint32_t skip = kWindow ? gap_of(a, len) : 0;  // the granules [sink_grans, sink_grans + skip) nobody sees
+    // with a window: blocks of pages for the first tokens, then those from the window's first page on. A block for every
+    // page of the table, most with nothing to do: 52.1 against 48.9 us at 128 x 8192 tokens behind a window of 1024.
+    uint32_t block = id % blocks;
+    if (kWindow && block >= a.sink_blocks)
+        block += max((a.sink_grans + skip) / a.page_grans / block_pages, a.sink_blocks) - a.sink_blocks;
+    if ((uint64_t)block * block_pages >= a.page_stride) return;  // uniform
+    const uint32_t page0 = block * block_pages;
     const uint64_t block_end = ((uint64_t)page0 + block_pages) * a.page_grans;
     // uniform: no token in these pages, or none that is seen
     if ((uint64_t)page0 * a.page_grans >= n_gran) return;
@@ -826,6 +834,7 @@ struct Plan {
     uint32_t rows, tile_rows, row_tiles, splits, split_grans, max_grans;
     uint64_t part_rows, o_bytes, ml_bytes, gran_bytes;
     uint64_t blocks, join, weigh;  // of k_attend_cache; of k_cache_finish
+    uint32_t weigh_blocks, sink_blocks;
 };
 
 uint64_t up16(uint64_t x) { return (x + 15) & ~15ull; }
@@ -865,7 +874,15 @@ Plan plan_of(const pk_kv_cache &kv, uint32_t R, uint32_t n_q, uint32_t q_heads, 
     p.blocks = units * p.splits;
     p.join = p.splits > 1 ? ((uint64_t)R * kv.kv_heads * p.rows + kFinishWarps - 1) / kFinishWarps : 0;
     const uint64_t block_pages = kFinishWarps * pages_a_warp(kv.page_tokens / 16);
-    p.weigh = weigh ? (page_stride + block_pages - 1) / block_pages * R : 0;
+    uint64_t weigh_blocks = up(page_stride, block_pages);
+    p.sink_blocks = 0;
+    if (window) {
+        p.sink_blocks = (uint32_t)std::min<uint64_t>(up(up(sinks, kv.page_tokens), block_pages), weigh_blocks);
+        const uint64_t pages = ((uint64_t)window + n_q) / kv.page_tokens + 2;  // that a request's windows touch, at most
+        weigh_blocks = std::min<uint64_t>(weigh_blocks, p.sink_blocks + pages / block_pages + 2);
+    }
+    p.weigh_blocks = (uint32_t)weigh_blocks;
+    p.weigh = weigh ? weigh_blocks * R : 0;
     return p;
 }
 
@@ -925,6 +942,8 @@ cudaError_t pk_launch_attend_cache(const pk_kv_cache &kv, uint32_t dtype, const 
     a.window = window;
     a.sinks = window ? sinks : 0;
     a.sink_grans = (a.sinks + 15) / 16;
+    a.weigh_blocks = p.weigh_blocks;
+    a.sink_blocks = p.sink_blocks;
     a.q = static_cast<const uint16_t *>(q.p);
     a.q_ts = q.tok_stride;
     a.q_hs = q.head_stride;
