@@ -617,7 +617,7 @@ int pk_attend_cache_window(const pk_kv_cache *kv, uint32_t dtype, const pk_heads
  * are not written.  q_heads a multiple of kv_heads, at most 65536; n_q and
  * page_stride * page_tokens at most 0x7fff0000, n_q * q_heads below 2^34; window
  * and sinks below 2^31; |scale * k_scale| at most 2.3e38; strides of q below
- * 2^39.  scratch_dev: pk_attend_chunk_scratch_bytes(...) bytes for the same
+ * 2^39; out overlaps no input.  scratch_dev: pk_attend_chunk_scratch_bytes(...) bytes for the same
  * arguments, 32-byte aligned.
  * Device errors: offsets out of order or range (PK_ERR_ARG; nothing is
  * written); a kv_len out of range (PK_ERR_ARG) counts as 0; a slot out of

@@ -6,8 +6,9 @@
 // has six significant bits: exact in a half and in a bfloat16.  All products are of
 // halves: queries in bfloat16 are scaled by a power of two a row first, which
 // leaves them as they are (k_chunk_queries); where one row's values lie too far
-// apart for that, the call's products with K are of bfloat16s, to which K costs
-// more to unpack (470 | 439 us for 4 x 512 tokens behind 16384).
+// apart for that, or the call is too short to be worth it, the call's products
+// with K are of bfloat16s, to which K costs more to unpack (476 | 438 us for
+// 4 x 512 tokens behind 16384).
 // ref moves as in pk_attend_prompt.cu: only when a tile's weights of a row sum to
 // more than 2^15.
 //
@@ -56,7 +57,7 @@ struct Args {
     uint16_t *half_q;   // [n_q][q_heads][D], queries in bfloat16 as halves; times row_down they are what they were
     float *row_down;    // [n_q][q_heads]
     uint8_t *too_wide;  // by block of k_chunk_queries: a row that halves do not hold
-    uint32_t query_blocks;
+    uint32_t query_blocks;  // 0: the products with K take bfloat16s
     const int64_t *q_off;
     const int32_t *kv_len;
     const uint32_t *pages;
@@ -248,55 +249,70 @@ struct Item {
 };
 
 // Queries in bfloat16 as halves, times the power of two that brings a row's largest value to [2^14, 2^15): all values down
-// to 2^-31 of it keep their 8 bits.  8 values a lane.
-constexpr int kQueryThreads = 256;
+// to 2^-31 of it keep their 8 bits.  8 values a lane, of four rows at once, so that four loads are on their way.
+constexpr int kQueryThreads = 256, kQueryRows = 4;
 constexpr uint32_t kQueryBlocks = 1024;
 template <int D>
 __global__ void __launch_bounds__(kQueryThreads) k_chunk_queries(const Args a) {
     constexpr uint32_t kLanes = D / 8, kRowsAtOnce = kQueryThreads / kLanes;
     const uint16_t *q = a.q;
-    pk::pdl_wait(q);
+    const int64_t *q_off = a.q_off;
+    pk::pdl_wait(q, q_off);
     pk::pdl_launch_dependents();
     const uint64_t rows = a.n_q * a.q_heads;
+    const int64_t q_first = __ldcg(q_off), q_end = __ldcg(q_off + a.R);  // rows of no request may hold anything
     const uint32_t c = threadIdx.x % kLanes;
     bool wide = false;
-    for (uint64_t row0 = (uint64_t)blockIdx.x * kRowsAtOnce; row0 < rows; row0 += (uint64_t)gridDim.x * kRowsAtOnce) {
-        const uint64_t row = row0 + threadIdx.x / kLanes;
-        const bool on = row < rows;
-        const uint64_t token = on ? row / a.q_heads : 0;
-        const uint32_t h = on ? (uint32_t)(row - token * a.q_heads) : 0;
-        const uint4 u = on ? __ldcg(reinterpret_cast<const uint4 *>(q + (int64_t)token * a.q_ts + (int64_t)h * a.q_hs + c * 8))
+    constexpr uint32_t kBlockRows = kRowsAtOnce * kQueryRows;
+    for (uint64_t first = (uint64_t)blockIdx.x * kBlockRows; first < rows; first += (uint64_t)gridDim.x * kBlockRows) {
+        const uint64_t row0 = first + threadIdx.x / kLanes;
+        uint4 all[kQueryRows];
+        bool on[kQueryRows];
+#pragma unroll
+        for (uint32_t k = 0; k < kQueryRows; ++k) {
+            const uint64_t row = row0 + k * kRowsAtOnce, token = row / a.q_heads;
+            on[k] = row < rows;
+            all[k] = on[k] ? __ldcg(reinterpret_cast<const uint4 *>(q + (int64_t)token * a.q_ts +
+                                                                   (int64_t)(row - token * a.q_heads) * a.q_hs + c * 8))
                            : make_uint4(0, 0, 0, 0);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-        float x[8], top = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = pk::Elem<PK_BF16>::to2(w[i]);
-            x[2 * i] = f.x, x[2 * i + 1] = f.y;
+            on[k] = on[k] && (int64_t)token >= q_first && (int64_t)token < q_end;
         }
-        uint32_t bits = 0;  // of the largest magnitude, found on the bits, which finds a NaN too
 #pragma unroll
-        for (int i = 0; i < 8; ++i) bits = max(bits, __float_as_uint(x[i]) & 0x7fffffffu);
+        for (uint32_t k = 0; k < kQueryRows; ++k) {
+            const uint64_t row = row0 + k * kRowsAtOnce;
+            const uint32_t w[4] = {all[k].x, all[k].y, all[k].z, all[k].w};
+            float x[8];
 #pragma unroll
-        for (uint32_t d = 1; d < kLanes; d *= 2) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, d));
-        top = __uint_as_float(bits);
-        const int e = top == 0.0f || bits >= 0x7f800000u ? 14 : max((int)(bits >> 23) - 127, -110);  // 2^e <= top
-        const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
-        uint32_t out[4];
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = pk::Elem<PK_BF16>::to2(w[i]);
+                x[2 * i] = f.x, x[2 * i + 1] = f.y;
+            }
+            uint32_t bits = 0;  // of the largest magnitude, found on the bits, which finds a NaN too
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float lo = x[2 * i] * up, hi = x[2 * i + 1] * up;
-            const __half2 had = __floats2half2_rn(lo, hi);
-            wide |= !(__low2float(had) == lo && __high2float(had) == hi);
-            out[i] = *reinterpret_cast<const uint32_t *>(&had);
+            for (int i = 0; i < 8; ++i) bits = max(bits, __float_as_uint(x[i]) & 0x7fffffffu);
+#pragma unroll
+            for (uint32_t d = 1; d < kLanes; d *= 2) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, d));
+            const int e = bits == 0 || bits >= 0x7f800000u ? 14 : max((int)(bits >> 23) - 127, -110);  // 2^e <= the largest
+            const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
+            uint32_t out[4];
+            bool odd = bits >= 0x7f800000u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float lo = x[2 * i] * up, hi = x[2 * i + 1] * up;
+                const __half2 had = __floats2half2_rn(lo, hi);
+                odd |= !(__low2float(had) == lo && __high2float(had) == hi);
+                out[i] = *reinterpret_cast<const uint32_t *>(&had);
+            }
+            if (!on[k]) continue;
+            wide |= odd;
+            *reinterpret_cast<uint4 *>(a.half_q + row * D + c * 8) = make_uint4(out[0], out[1], out[2], out[3]);
+            if (c == 0) a.row_down[row] = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
         }
-        wide |= bits >= 0x7f800000u;
-        if (!on) continue;
-        *reinterpret_cast<uint4 *>(a.half_q + row * D + c * 8) = make_uint4(out[0], out[1], out[2], out[3]);
-        if (c == 0) a.row_down[row] = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
     }
     const int any = __syncthreads_or(wide);
     if (threadIdx.x == 0) a.too_wide[blockIdx.x] = (uint8_t)(any != 0);
+    if (blockIdx.x == 0)  // all are read
+        for (uint32_t i = gridDim.x + threadIdx.x; i < kQueryBlocks; i += kQueryThreads) a.too_wide[i] = 0;
 }
 
 // Shared memory of a CTA, from a 1024-byte boundary: Q (two tiles), the ring of K and V tiles in 16 bits, the ring of
@@ -589,11 +605,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 plan_here(a, sm, q_off, kv_len);
                 __syncwarp();
             }
-            bool halves = true;
-            if (DT == PK_BF16) {
+            bool halves = DT == PK_FP16 || a.query_blocks;
+            if (DT == PK_BF16) {  // uniform
                 uint32_t wide = 0;
-                for (uint32_t i = lane; i < a.query_blocks; i += 32) wide |= __ldcg(too_wide + i);
-                halves = !__any_sync(0xffffffffu, wide != 0);
+                if (halves) {
+#pragma unroll
+                    for (uint32_t i = 0; i < kQueryBlocks / 512; ++i) {
+                        const uint4 u = __ldcg(reinterpret_cast<const uint4 *>(too_wide) + 32 * i + lane);
+                        wide |= u.x | u.y | u.z | u.w;
+                    }
+                }
+                halves &= !__any_sync(0xffffffffu, wide != 0);
             }
             const CUtensorMap *map = DT == PK_BF16 && halves ? &map_half : &map_q;
             Item it;
@@ -1312,10 +1334,14 @@ __global__ void __launch_bounds__(kJoinThreads) k_chunk_join(const Args a) {
 // What the host knows of a call are bounds; the kernels see the lengths.
 struct Plan {
     uint64_t units, blocks;  // at most
-    uint64_t plan_bytes, cut_bytes, ml_bytes, o_bytes, wide_bytes, down_bytes, half_bytes;
+    uint64_t plan_bytes, cut_bytes, ml_bytes, o_bytes, wide_bytes, down_bytes, half_bytes;  // wide_bytes 0: no halves
 };
 
 constexpr uint64_t kSms = 152;
+// Keys that a call's units go through (half of them at head_dim 64) from which on halves of its queries pay for their
+// making, as bfloat16s | halves: 400 tokens of 2 requests behind 4000 (0.5 M keys) 82 | 84 us, 1 x 40 behind 60000 (1.0 M)
+// 129 | 122, 4 x 500 behind 4000 (1.2 M) 156 | 153, head_dim 64 12 x 700 behind 2048 (1.2 M) 136 | 141.
+constexpr uint64_t kWorthHalves = 3ull << 18;
 Plan plan_of(const pk_kv_cache &kv, uint32_t dtype, uint32_t R, uint64_t n_q, uint32_t q_heads, uint64_t page_stride,
              uint32_t window, uint32_t sinks) {
     Plan p;
@@ -1328,7 +1354,8 @@ Plan plan_of(const pk_kv_cache &kv, uint32_t dtype, uint32_t R, uint64_t n_q, ui
     p.cut_bytes = p.blocks * sizeof(Cut);
     p.ml_bytes = p.blocks > 1 ? 2 * p.blocks * 2 * kRows * 16 : 0;
     p.o_bytes = p.blocks > 1 ? 2 * p.blocks * 2 * kRows * kv.head_dim * 4 : 0;
-    const uint64_t rows = dtype == PK_BF16 ? n_q * q_heads : 0;
+    const bool halves = dtype == PK_BF16 && keys && p.units >= kWorthHalves * 128 / kv.head_dim / keys;
+    const uint64_t rows = halves ? n_q * q_heads : 0;
     p.wide_bytes = rows ? kQueryBlocks : 0;
     p.down_bytes = (rows * 4 + 31) & ~31ull;
     p.half_bytes = rows * kv.head_dim * 2;
@@ -1341,7 +1368,7 @@ cudaError_t launch(const Args &a, const CUtensorMap &mq, const CUtensorMap &mh, 
     static_assert(smem <= 227 * 1024, "shared memory of a block");
     static std::atomic<uint64_t> seen{0};
     cudaError_t e = pk_allow_smem(k_attend_chunk<D, DT>, smem, seen);
-    if (e == cudaSuccess && DT == PK_BF16) e = pk_launch(k_chunk_queries<D>, a.query_blocks, kQueryThreads, s, a);
+    if (e == cudaSuccess && a.query_blocks) e = pk_launch(k_chunk_queries<D>, a.query_blocks, kQueryThreads, s, a);
     if (e == cudaSuccess) e = pk_launch_smem(k_attend_chunk<D, DT>, a.blocks, kThreads, smem, s, a, mq, mh);
     if (e == cudaSuccess && a.blocks > 1) e = pk_launch(k_chunk_join<D, DT>, (a.blocks - 1) * (unsigned)kJoinBlocks, kJoinThreads, s, a);
     return e;
@@ -1403,12 +1430,12 @@ cudaError_t pk_launch_attend_chunk(const pk_kv_cache &kv, uint32_t dtype, const 
     a.too_wide = at;
     a.row_down = reinterpret_cast<float *>(at + p.wide_bytes);
     a.half_q = reinterpret_cast<uint16_t *>(at + p.wide_bytes + p.down_bytes);
-    const uint64_t query_rows = kQueryThreads / (kv.head_dim / 8);  // of a block at once
-    a.query_blocks = (uint32_t)std::min<uint64_t>((n_q * q_heads + query_rows - 1) / query_rows, kQueryBlocks);
+    const uint64_t query_rows = kQueryThreads / (kv.head_dim / 8) * kQueryRows;  // of a block at once
+    a.query_blocks = p.wide_bytes ? (uint32_t)std::min<uint64_t>((n_q * q_heads + query_rows - 1) / query_rows, kQueryBlocks) : 0;
     a.status = status;
     CUtensorMap mq, mh{};
     cudaError_t e = map_of(&mq, q, n_q, q_heads, kv.head_dim, dtype, a.tile_tokens, a.tile_heads);
-    if (e == cudaSuccess && dtype == PK_BF16)
+    if (e == cudaSuccess && a.query_blocks)
         e = map_of(&mh, pk_heads{a.half_q, (int64_t)q_heads * kv.head_dim, kv.head_dim}, n_q, q_heads, kv.head_dim, PK_FP16,
                    a.tile_tokens, a.tile_heads);
     if (e == cudaSuccess && a.plan) e = pk_launch(k_chunk_plan, 1, kPlanThreads, s, a);

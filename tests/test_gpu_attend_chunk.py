@@ -251,8 +251,14 @@ def test_far_scores_keep_their_order(m, n):
                 assert np.all(np.abs(got - v[s.argmax(), 0]) <= 2.0 ** -8 * np.abs(v[s.argmax(), 0]))
 
 
+def roomy(pages, D=64):
+    """The same pages with room in the table for so many more that queries are worth making halves of."""
+    return np.concatenate([pages, np.full((pages.shape[0], 2 ** 20 // D * 8), -1, pages.dtype)], 1)
+
+
+@pytest.mark.parametrize("room", [False, True])
 @pytest.mark.parametrize("far,D,window", [(2.0 ** 27, 64, None), (2.0 ** 30, 128, 300), (2.0 ** 45, 64, 300), (2.0 ** 60, 128, None)])
-def test_wide_queries(far, D, window):
+def test_wide_queries(far, D, window, room):
     """Rows with one large value, behind which K holds nothing, beside ordinary ones: these keep their bits, also where halves
     cannot hold both."""
     m, n, C, H, G = 20, 700, 16, 1, 2
@@ -261,7 +267,8 @@ def test_wide_queries(far, D, window):
     q = torch.from_numpy(rng.standard_normal((m, G, D))).to(torch.bfloat16)
     q[3:, :, 0] = far
     kv = cache(pool, C, H, D)
-    out, lse = kv.attend_chunk(q.cuda(), offsets([m]), dev(np.array([n], np.int32)), dev(pages), window=window, sinks=2)
+    out, lse = kv.attend_chunk(q.cuda(), offsets([m]), dev(np.array([n], np.int32)), dev(roomy(pages) if room else pages),
+                               window=window, sinks=2)
     kv.check()
     small = np.where(np.arange(D) == 0, 0, q.double().numpy())
     small[:3] = q[:3].double().numpy()
@@ -269,15 +276,16 @@ def test_wide_queries(far, D, window):
     check(out, lse, ref, rl, mag, err, "bf16", n)
 
 
+@pytest.mark.parametrize("room", [False, True])
 @pytest.mark.parametrize("small", [2.0 ** -100, 2.0 ** -130, 0.0])
-def test_tiny_and_infinite_queries(small):
+def test_tiny_and_infinite_queries(small, room):
     """Rows of tiny values weigh all keys alike; an infinity or NaN reaches its own row only."""
     m, n, C, H, G, D = 6, 300, 16, 1, 1, 64
     pool, pages, rng = make([n], C, H, D, 5)
     q = torch.from_numpy(rng.standard_normal((m, G, D))).to(torch.bfloat16)
     q[1] *= small
     kv = cache(pool, C, H, D)
-    args = (offsets([m]), dev(np.array([n], np.int32)), dev(pages))
+    args = (offsets([m]), dev(np.array([n], np.int32)), dev(roomy(pages) if room else pages))
     out, lse = kv.attend_chunk(q.cuda(), *args)
     ref, rl, mag, err, _ = reference(pool, pages, [m], [n], q.double().numpy(), C, H, D, D ** -0.5)
     check(out, lse, ref, rl, mag, err, "bf16", n)
@@ -289,6 +297,33 @@ def test_tiny_and_infinite_queries(small):
         keep = [0, 1, 2, 3, 5]
         check(got[keep], glse[keep], ref[keep], rl[keep], mag[keep], err, "bf16", n)
         assert bool(got[4].isnan().any())
+
+
+@pytest.mark.parametrize("new,lens,C,H,G,D,window", [([40, 5, 0, 7], [40, 3, 0, 300], 48, 2, 3, 64, None), ([130, 257], [130, 300], 16, 1, 1, 128, None),
+                                                     ([2, 9] * 20, [30, 9] * 20, 16, 1, 2, 64, None), ([700], [700], 16, 1, 130, 64, None),
+                                                     ([33, 64, 65], [500, 64, 1000], 256, 2, 4, 128, 17)])
+def test_queries_as_halves_or_not_are_the_same(new, lens, C, H, G, D, window):
+    """A table with room for long requests has the call make halves of its queries, which are as exact: the same products,
+    in sums that may be cut at other keys only.  Rows of no request, here NaN, have no say."""
+    from paper_2609_38706_gb300 import pk
+    pool, pages, rng = make(lens, C, H, D, 8, spare=2)
+    n_q, dt = sum(new), torch.bfloat16
+    q = torch.full((n_q + 70, H * G, D), float("nan"), dtype=dt, device="cuda")
+    q[3: 3 + n_q] = torch.from_numpy(rng.standard_normal((n_q, H * G, D)) * 10.0 ** rng.uniform(-3, 1, (n_q, H * G, 1))).to(dt).cuda()
+    off, n, kv, got = offsets(new) + 3, dev(np.array(lens, np.int32)), cache(pool, C, H, D), []
+    for table in (pages, roomy(pages)):
+        table = dev(table)
+        out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+        nbytes = pk.pk_attend_chunk_scratch_bytes(kv.kv, dt, q.shape[0], len(new), H * G, table.shape[1], window or 0, 2)
+        pk.pk_attend_chunk(kv.kv, q, out, lse, off, n, table, D ** -0.5, window or 0, 2,
+                           torch.zeros(nbytes, dtype=torch.uint8, device="cuda"), kv.status)
+        kv.check()
+        assert bool((out[:3] == 7).all()) and bool((out[3 + n_q:] == 7).all()) and bool((lse[3 + n_q:] == 7).all())
+        got.append((nbytes, out[3: 3 + n_q].clone(), lse[3: 3 + n_q].clone()))
+    assert window or got[1][0] - got[0][0] >= q.numel() * 2  # a window bounds the keys whatever the table holds
+    ref, rl, mag, err, _ = reference(pool, pages, new, lens, q[3: 3 + n_q].double().cpu().numpy(), C, H, D, D ** -0.5, window, 2)
+    for _, out, lse in got:
+        check(out, lse, ref, rl, mag, err, "bf16", max(lens))
 
 
 def test_one_token_chunks_are_decode_steps():
