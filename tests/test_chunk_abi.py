@@ -53,7 +53,8 @@ def test_chunk_scratch(pk):
     one = pk.pk_kv_cache(FAKE, 4, 16, 1, 64, 1.0, 1.0)
     assert pk.pk_attend_chunk_scratch_bytes(one, torch.float16, 1, 1, 1, 1, 0, 0) < 4096  # one block: nothing is cut
     assert all(x % 16 == 0 for x in (size(16, 1, 512), size(16, 40, 512)))
-    assert pk.pk_attend_chunk_scratch_bytes(kv, torch.bfloat16, 100, 1, 32, 2, 0, 0) - size(100, 1, 2) >= 100 * 32 * (256 + 4)
+    halves = [pk.pk_attend_chunk_scratch_bytes(kv, torch.bfloat16, 100, 1, 32, n, 0, 0) - size(100, 1, n) for n in (2, 512)]
+    assert halves[0] == 0 and halves[1] >= 100 * 32 * (256 + 4)  # of queries in bfloat16, where the call is long enough
     assert pk.pk_attend_chunk_scratch_bytes(kv, torch.float32, 100, 1, 32, 2, 0, 0) == 0
     for bad in ((1 << 31, 1, 4, 0, 0), (4, 1, 4, 1 << 31, 0)):
         try:
