@@ -1245,10 +1245,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
     }
 }
 
-// Joins the pieces of the units that were cut, in the order of their keys: kJoinBlocks for a unit, a warp a row.
-constexpr int kJoinThreads = 256, kJoinBlocks = 16;
+// Joins the pieces of the units that were cut, in the order of their keys: kJoinBlocks for a unit, a warp two rows.  Most
+// units have two pieces, whose rows are on their way before their weights are known (1 x 40 tokens behind 120000, ten
+// pieces a unit: 208 -> 201 us; 4 x 500 behind 4000: 153 -> 150).  It costs 17 to 20 us there, for 40 MB from the L2: rows
+// of a warp 1 | 2 | 4 are 153 | 150 | 155 us, and more warps an SM by fewer registers nothing.
+constexpr int kJoinThreads = 256, kJoinRows = 2, kJoinBlocks = 2 * kRows / (kJoinThreads / 32 * kJoinRows);
 template <int D, uint32_t DT>
 __global__ void __launch_bounds__(kJoinThreads) k_chunk_join(const Args a) {
+    using V = std::conditional_t<D == 128, float4, float2>;  // of a row, a lane's part
+    constexpr int kPer = D / 32;
     const Cut *cuts = a.cuts;
     const float4 *ml = a.part_ml;
     const float *po = a.part_o;
@@ -1259,72 +1264,89 @@ __global__ void __launch_bounds__(kJoinThreads) k_chunk_join(const Args a) {
     const int2 heads = __ldcg(reinterpret_cast<const int2 *>(cuts) + 2);
     if (where.x < 0) return;  // uniform
     const uint32_t lane = threadIdx.x & 31, b0 = (uint32_t)where.x, n = (uint32_t)where.y - b0 + 1;
-    // The exponent of a piece's weights is ref - fine, which 32 bits may not hold: differences are taken part by part.
-    auto more = [](float2 x, float2 y) { return (x.x - y.x) - (x.y - y.y); };
-    constexpr int kAtOnce = 2 * kRows / kJoinBlocks / (kJoinThreads / 32);  // rows of a warp, whose loads go out together
-    constexpr int kPer = D / 32;
-    const uint32_t row0 = (blockIdx.x % kJoinBlocks * (kJoinThreads / 32) + threadIdx.x / 32) * kAtOnce;
+    const uint32_t row0 = (blockIdx.x % kJoinBlocks * (kJoinThreads / 32) + threadIdx.x / 32) * kJoinRows;
+    auto token_of = [&](int k) { return (row0 + k) / kRows * a.tile_tokens + (row0 + k) % kRows / a.tile_heads; };
+    auto is_row = [&](int k) {
+        const uint32_t in = (row0 + k) % kRows;
+        return in / a.tile_heads < a.tile_tokens && token_of(k) < (uint32_t)where.w && in % a.tile_heads < (uint32_t)heads.y;
+    };
+    if (!is_row(0) && !is_row(1)) return;  // uniform per warp
+    static_assert(kJoinRows == 2, "rows of a warp");
     auto part_of = [&](uint32_t i, int k) { return (uint64_t)(2 * (b0 + i) + (i == 0)) * 2 * kRows + row0 + k; };
-    float2 top[kAtOnce];
-    float sum[kAtOnce] = {}, o[kAtOnce][kPer] = {};
+    V u[2][kJoinRows];
+    auto load = [&](uint32_t i) {
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) top[k] = make_float2(-FLT_MAX, 0.0f);
-    for (uint32_t i = lane; i < n; i += 32) {
-        float4 y[kAtOnce];
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) y[k] = __ldcg(ml + part_of(i, k));
+            for (int k = 0; k < kJoinRows; ++k)
+                if (i + j < n) u[j][k] = __ldcg(reinterpret_cast<const V *>(po + part_of(i + j, k) * D) + lane);
+    };
+    // (ref, fine, sum) of piece i0 + lane.  The exponent of a piece's weights is ref - fine, which 32 bits may not hold:
+    // differences are taken part by part.
+    float4 y[kJoinRows];
+    auto look = [&](uint32_t i0) {
 #pragma unroll
-        for (int k = 0; k < kAtOnce; ++k)
+        for (int k = 0; k < kJoinRows; ++k)
+            y[k] = i0 + lane < n ? __ldcg(ml + part_of(i0 + lane, k)) : make_float4(-FLT_MAX, 0.0f, 0.0f, 0.0f);
+    };
+    auto more = [](float2 x, float2 y) { return (x.x - y.x) - (x.y - y.y); };
+    look(0);
+    load(0);
+    float2 top[kJoinRows];
+#pragma unroll
+    for (int k = 0; k < kJoinRows; ++k) top[k] = make_float2(y[k].x, y[k].y);
+    for (uint32_t i0 = 32; i0 < n; i0 += 32) {
+        look(i0);
+#pragma unroll
+        for (int k = 0; k < kJoinRows; ++k)
             if (more(make_float2(y[k].x, y[k].y), top[k]) > 0.0f) top[k] = make_float2(y[k].x, y[k].y);
     }
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
+    for (int k = 0; k < kJoinRows; ++k) {
 #pragma unroll
         for (int d = 16; d; d /= 2) {
-            const float2 y = make_float2(__shfl_xor_sync(0xffffffffu, top[k].x, d), __shfl_xor_sync(0xffffffffu, top[k].y, d));
-            if (more(y, top[k]) > 0.0f) top[k] = y;
+            const float2 z = make_float2(__shfl_xor_sync(0xffffffffu, top[k].x, d), __shfl_xor_sync(0xffffffffu, top[k].y, d));
+            if (more(z, top[k]) > 0.0f) top[k] = z;
         }
         top[k] = make_float2(__shfl_sync(0xffffffffu, top[k].x, 0), __shfl_sync(0xffffffffu, top[k].y, 0));
     }
+    float sum[kJoinRows] = {}, o[kJoinRows][kPer] = {};
     for (uint32_t i0 = 0; i0 < n; i0 += 32) {
-        float f[kAtOnce], l[kAtOnce];
+        if (n > 32) look(i0);
+        float f[kJoinRows];
 #pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
-            const float4 y = i0 + lane < n ? __ldcg(ml + part_of(i0 + lane, k)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            f[k] = y.z == 0.0f ? 0.0f : pk::ex2(more(make_float2(y.x, y.y), top[k]));
-            l[k] = y.z;
-        }
-#pragma unroll 2
-        for (uint32_t i = 0; i < min(n - i0, 32u); ++i) {
-            float2 u[kAtOnce][kPer / 2];
+        for (int k = 0; k < kJoinRows; ++k)
+            f[k] = y[k].z == 0.0f ? 0.0f : pk::ex2(more(make_float2(y[k].x, y[k].y), top[k]));
+        for (uint32_t i = i0; i < min(n, i0 + 32); i += 2) {
+            if (i) load(i);
 #pragma unroll
-            for (int k = 0; k < kAtOnce; ++k)
+            for (int j = 0; j < 2; ++j) {
+                if (i + j >= n) break;
 #pragma unroll
-                for (int e = 0; e < kPer; e += 2)
-                    u[k][e / 2] = __ldcg(reinterpret_cast<const float2 *>(po + part_of(i0 + i, k) * D + lane * kPer + e));
+                for (int k = 0; k < kJoinRows; ++k) {
+                    const float w = __shfl_sync(0xffffffffu, f[k], (i + j) & 31);
+                    sum[k] += w * __shfl_sync(0xffffffffu, y[k].z, (i + j) & 31);
+                    const float(&v)[kPer] = reinterpret_cast<const float(&)[kPer]>(u[j][k]);
 #pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) {
-                const float w = __shfl_sync(0xffffffffu, f[k], i);
-                sum[k] += w * __shfl_sync(0xffffffffu, l[k], i);
-#pragma unroll
-                for (int e = 0; e < kPer; e += 2) {
-                    o[k][e] += w * u[k][e / 2].x;
-                    o[k][e + 1] += w * u[k][e / 2].y;
+                    for (int e = 0; e < kPer; ++e) o[k][e] += w * v[e];
                 }
             }
         }
     }
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-        const uint32_t row = row0 + k, in = row % kRows, tok = in / a.tile_heads, gh = in % a.tile_heads, t = row / kRows;
-        if (tok >= a.tile_tokens || t * a.tile_tokens + tok >= (uint32_t)where.w || gh >= (uint32_t)heads.y) continue;
-        const int64_t token = (int64_t)where.z + t * a.tile_tokens + tok;
-        const uint32_t qh = (uint32_t)heads.x + gh;
+    for (int k = 0; k < kJoinRows; ++k) {
+        if (!is_row(k)) continue;
+        const int64_t token = (int64_t)where.z + token_of(k);
+        const uint32_t qh = (uint32_t)heads.x + (row0 + k) % kRows % a.tile_heads;
         const float inv = sum[k] == 0.0f ? 0.0f : a.v_scale / sum[k];
+        uint32_t w[kPer / 2];
 #pragma unroll
-        for (int e = 0; e < kPer; e += 2)
-            *reinterpret_cast<uint32_t *>(a.out + token * a.o_ts + (int64_t)qh * a.o_hs + lane * kPer + e) =
-                pk::Elem<DT>::from2(o[k][e] * inv, o[k][e + 1] * inv);
+        for (int e = 0; e < kPer; e += 2) w[e / 2] = pk::Elem<DT>::from2(o[k][e] * inv, o[k][e + 1] * inv);
+        uint32_t *dst = reinterpret_cast<uint32_t *>(a.out + token * a.o_ts + (int64_t)qh * a.o_hs + lane * kPer);
+        if constexpr (kPer == 4)
+            *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
+        else
+            *dst = w[0];
         if (lane == 0 && a.lse)
             a.lse[token * a.q_heads + qh] =
                 sum[k] == 0.0f ? -INFINITY : (top[k].x - top[k].y + log2f(sum[k])) * 0.69314718055994531f;
