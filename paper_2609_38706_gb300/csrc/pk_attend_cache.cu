@@ -24,7 +24,11 @@
 // for both launches, 25 of it the join, 5.4 TB/s of pages; the attention takes 76%
 // of the memory's cycles and 65% of the issue slots (dequantising is 58% of the
 // ALU's).  128 requests of up to 2048: 62.5 us, 5 of it the page weights: 1024 CTAs
-// of unequal lengths for 608 places.  Short caches: two launches, 8 us.
+// of unequal lengths for 608 places.  Short caches: two launches, 8 us.  With a
+// window the granules that no query sees are left out of the count, so the work is
+// that of a short cache: 128 requests of 8192 tokens, window 1024, 49 us, 9 of it the
+// page weights; 2 or 3 splits of such windows are 59 or 65 us, 2 or 3 warps a CTA 53 to
+// 55 (with one split 52, but 135 for 77 at 64 x 8192, window 4096).
 #include <cuda_runtime.h>
 #include <float.h>
 

@@ -16,6 +16,14 @@
 // granules (16 tokens) of the first tokens and those from the first query's window
 // on are one list, cut into tiles of 128 keys.  In its places a query sees last and
 // below, down to low, and those before `sinks`.
+//
+// What bounds it is a tile's chain: scores, weights, product.  A key tile meets two
+// tiles of 128 rows, so that unpacking it is paid once for 256 rows, and takes 3560
+// cycles at head_dim 128, of which the products are 2048 (tensor pipe 55-61% busy,
+// issue slots 52-58%, memory 5%); a warp's scores and weights of one tile are a chain
+// of 1650 to 2000 cycles.  Full lengths, bf16, 32 heads over 8: 4 x 512 tokens behind
+// 16384 434 us (1.29 PFLOP/s), 2048 behind 60000 1455 us (1.41); head_dim 64, 12 heads
+// over 4: 12 x 700 behind 2048 119 us (0.52: the same chain for half of the products).
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <float.h>
@@ -93,8 +101,11 @@ __device__ __forceinline__ int32_t good_length(const Args &a, int32_t len) {
 // the last a piece of their keys.  So all blocks are done at about the same time, also where a call is a few rows over
 // many keys (4 x 512 tokens behind 16384, 256 units: 604 -> 550 us against units cut in two).  Where that gains less
 // than the pieces and their joining cost, a block takes the whole units that begin in its share.
-constexpr int64_t kUnitCost = 512;     // a unit's start and end, in keys
-constexpr int64_t kCutCost = 768;      // one more piece a block, and the joining
+// All three in keys.  A unit's start and end: 256 | 512 | 1024 are 65 | 65 | 86 us for 8 x 600 tokens behind 9000, window 1000
+// (head_dim 64).  One more piece a block, and the joining: 768 | 1536 are 112 | 128 for 2 x 2000 behind 2000, 150 | 157 for
+// 4 x 500 behind 4000, and 123 | 114 for 5 x 400 behind 2500.  Shares of 320 to 1280 keys at least are alike.
+constexpr int64_t kUnitCost = 512;
+constexpr int64_t kCutCost = 768;
 constexpr int64_t kLeastShare = 640;
 
 struct Req {
@@ -316,7 +327,9 @@ __global__ void __launch_bounds__(kQueryThreads) k_chunk_queries(const Args a) {
 }
 
 // Shared memory of a CTA, from a 1024-byte boundary: Q (two tiles), the ring of K and V tiles in 16 bits, the ring of
-// granules as they lie in the pages, then Small.
+// granules as they lie in the pages, then Small.  As much as fits: 2 | 3 stages at head_dim 128 are 578 | 435 us for 4 x 512
+// tokens behind 16384 (at 64 4 | 8 are even, 285 | 292 for 12 x 1500 behind 2048, 122 | 121 for 12 x 700), 16 | 28 granules
+// 219 | 202 us for 1 x 40 behind 120000, and 143 | 121 at head_dim 64 for 12 x 700.
 template <int D>
 struct Layout {
     static constexpr uint32_t kTile = 128 * D * 2;  // 128 rows; blocks of [128][64] values, 16 KB each
@@ -521,9 +534,12 @@ struct Unpack {
 };
 
 // One CTA an SM takes one item after another.  Warp roles: one copies Q tiles and
-// granules, six make K and V tiles of granules, one issues the matrix products, and two warpgroups of four turn scores into weights, a thread a row,
-// for one of the item's two tiles each: while one tile's scores are weighed the
-// other's products run.  TMEM: scores of the tiles (128 columns each; the weights, two
+// granules, six make K and V tiles of granules, one issues the matrix products, and
+// two warpgroups of four turn scores into weights, a thread a row, for one of the
+// item's two tiles each: while one tile's scores are weighed the other's products
+// run.  What is run seldom is loops, not unrolled: code that pushes the rest out of
+// the instruction cache costs more than it (4 x 2048 tokens behind 32768, window
+// 4096: 592 -> 499 us).  TMEM: scores of the tiles (128 columns each; the weights, two
 // to a column, take the place of scores that have been read), then their outputs
 // (D columns each).  Every counter of a barrier's use runs on over the items.
 template <int D, uint32_t DT>
@@ -1173,18 +1189,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 sum += part_sum;
                 pk::tmem_store32(ts, p[0]);  // over the scores, which every pass is done with
                 pk::tmem_store32(ts + 32, p[1]);
-                pk::tmem_wait_store();
-                pk::tmem_fence_before();
-                __syncwarp();
-                if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.p_ready[t]));
+                // The tile's notes, before it is given up: behind it the makers can go round while the other tile's products,
+                // for which nobody waits for this warp, take their tiles.
                 const uint32_t note = (tiles + j) % kNotes;
                 const uint32_t flags = *reinterpret_cast<const volatile uint16_t *>(sm.flags[note]);
+                pk::tmem_wait_store();
+                pk::tmem_fence_before();
                 if (flags) {
                     lost |= (flags & 0x0101u * kLost) != 0;
 #pragma unroll 1
                     for (int32_t i = 0; i < kKeys; ++i)
                         if ((flags >> (i / 64 * 8) & kMarked) && !hidden(i)) marked |= sm.marked[note][i];
                 }
+                __syncwarp();
+                if (lane == 0) pk::mbar_arrive(pk::smem_addr(&sm.p_ready[t]));
             }
             tiles += (uint32_t)it.n_all;
             if (ok && n_tiles > 0) ok = pk::mbar_wait_warp(pk::smem_addr(&sm.o_done[t]), (ni - 1) & 1);

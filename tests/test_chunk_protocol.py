@@ -210,10 +210,10 @@ class Cta:
                 self.stored[t].add((warp, x, j))
                 if all((w, x, j) in self.stored[t] for w in range(4)):
                     self.sp[t] = ("P", x, j)
-                self.p_ready[t].arrive()
                 for _ in range(self.rng.choice((1, 1, 60))):
                     assert all(self.notes[(tiles + j) % NOTES].get(w) == (x, j) for w in (MAKERS - 2, MAKERS - 1)), "notes gone"
                     yield
+                self.p_ready[t].arrive()
                 ni += 1
             tiles += max(item[:2])
             if item[t]:
@@ -283,3 +283,15 @@ def test_many_short_items():
     for stages, grans in ((3, 28), (8, 32)):
         for _ in range(20):
             Cta([(rng.choice((0, 1)), rng.choice((0, 1)), rng.choice((1, 1, 2))) for _ in range(30)], stages, grans, rng).run()
+
+
+@pytest.mark.parametrize("stages,grans", [(3, 28), (8, 32)])
+def test_long_items_of_one_tile_alone(stages, grans):
+    """Items that one of the two warpgroups has no part in, while it still reads the notes of its last tile."""
+    rng = random.Random(13)
+    for _ in range(40):
+        items = []
+        for _ in range(3):
+            items += [rng.choice(((1, 1), (2, 2), (0, 1), (1, 0))) + (8,)]
+            items += [rng.choice(((10, 0), (9, 0), (0, 12))) + (1,)] * rng.randint(1, 2)
+        Cta(items, stages, grans, rng).run()
