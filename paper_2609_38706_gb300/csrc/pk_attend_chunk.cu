@@ -1064,21 +1064,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     for (int i = 0; i < 32; ++i)
                         if (!(seen & 1u << i)) y[i] = 0xff800000u;
                 };
-                // Chunk c of the scores, 32 keys.  Loads run ahead (1 and 2 behind 0's use, 3 behind 1's).  Masked or
-                // not is known at compile time.
-                auto chunk = [&](int c, auto masked) -> uint32_t(&)[32] {
-                    uint32_t(&y)[32] = x[c % 3];  // (0's is on its way)
-                    if (c != 2) pk::tmem_wait_load(y);
-                    if (c == 0) {
-                        pk::tmem_load32(ts + 32, x[1]);
-                        pk::tmem_load32(ts + 64, x[2]);
-                    } else if (c == 1) {
-                        pk::tmem_wait_load(x[2]);
-                        pk::tmem_load32(ts + 96, x[0]);
-                    }
-                    if (decltype(masked)::value) mask(c, y);
-                    return y;
-                };
                 // The largest score of the first n chunks.
                 auto largest = [&](int n) {
                     float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -1095,24 +1080,51 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 };
                 // The weights by the reference so far, and their sum.
                 uint32_t p[2][32];
-                auto weigh = [&](auto masked) {
-                    const uint64_t ref2 = pk::pack2(-ref, -ref);
-                    uint64_t sum2[4] = {0, 0, 0, 0};
+                uint64_t ref2, sum2[4];
+                auto weigh_chunk = [&](const uint32_t(&y)[32], uint32_t *to) {  // 32 keys
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        float2 z = pk::unpack2(
+                            pk::fma2(pk::pack2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), scale22, ref2));
+                        z.x = pk::ex2(z.x);
+                        z.y = pk::ex2(z.y);
+                        sum2[i / 2 & 3] = pk::add2(sum2[i / 2 & 3], pk::pack2(z.x, z.y));
+                        to[i / 2] = pk::Elem<PK_FP16>::from2(z.x, z.y);
+                    }
+                };
+                auto weigh = [&]() {  // loads run ahead: 1 and 2 behind 0's use, 3 behind 1's (0's is on its way)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        uint32_t(&y)[32] = chunk(c, masked);
+                        if (c != 2) pk::tmem_wait_load(x[c % 3]);
+                        if (c == 0) {
+                            pk::tmem_load32(ts + 32, x[1]);
+                            pk::tmem_load32(ts + 64, x[2]);
+                        } else if (c == 1) {
+                            pk::tmem_wait_load(x[2]);
+                            pk::tmem_load32(ts + 96, x[0]);
+                        }
+                        weigh_chunk(x[c % 3], p[c / 2] + c % 2 * 16);
+                    }
+                };
+                // The same of an edge tile, in a loop of 64 keys: less code (against four chunks in a row, head_dim 64, bf16,
+                // 12 x 1500 tokens behind 2048: 292 -> 260 us; for all tiles it is more for its moves: 4 x 512 behind 16384,
+                // head_dim 128: 435 -> 446).
+                auto weigh_edge = [&]() {
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) {
+                        pk::tmem_wait_load(x[0]);
+                        pk::tmem_load32(ts + 64 * h + 32, x[1]);
+                        mask(2 * h, x[0]);
+                        weigh_chunk(x[0], p[1]);
+                        pk::tmem_wait_load(x[1]);
+                        if (h == 0) pk::tmem_load32(ts + 64, x[0]);
+                        mask(2 * h + 1, x[1]);
+                        weigh_chunk(x[1], p[1] + 16);
+                        if (h == 0) {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            float2 z = pk::unpack2(
-                                pk::fma2(pk::pack2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), scale22, ref2));
-                            z.x = pk::ex2(z.x);
-                            z.y = pk::ex2(z.y);
-                            sum2[i / 2 & 3] = pk::add2(sum2[i / 2 & 3], pk::pack2(z.x, z.y));
-                            p[c / 2][c % 2 * 16 + i / 2] = pk::Elem<PK_FP16>::from2(z.x, z.y);
+                            for (int i = 0; i < 32; ++i) p[0][i] = p[1][i];
                         }
                     }
-                    const float2 s0 = pk::unpack2(pk::add2(sum2[0], sum2[2])), s1 = pk::unpack2(pk::add2(sum2[1], sum2[3]));
-                    return (s0.x + s1.x) + (s0.y + s1.y);
                 };
                 // The same where a row of the warp has a far reference, which few calls have: by 16 scores, with `fine`.
                 auto weigh_far = [&]() {
@@ -1141,7 +1153,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                 };
                 auto weigh_any = [&]() {
                     if (far_off) return weigh_far();
-                    return edge ? weigh(std::true_type{}) : weigh(std::false_type{});
+                    ref2 = pk::pack2(-ref, -ref);
+                    sum2[0] = sum2[1] = sum2[2] = sum2[3] = 0;
+                    edge ? weigh_edge() : weigh();
+                    const float2 s0 = pk::unpack2(pk::add2(sum2[0], sum2[2])), s1 = pk::unpack2(pk::add2(sum2[1], sum2[3]));
+                    return (s0.x + s1.x) + (s0.y + s1.y);
                 };
                 // Moves the reference of the rows that `over` names to the score `top`; their sum so far is rescaled.
                 // Returns the factor.  That score's weight is then a power of two, which rounding leaves as it is: a row
