@@ -22,7 +22,7 @@
 // cycles at head_dim 128, of which the products are 2048 (tensor pipe 55-61% busy,
 // issue slots 52-58%, memory 5%); a warp's scores and weights of one tile are a chain
 // of 1650 to 2000 cycles.  Full lengths, bf16, 32 heads over 8: 4 x 512 tokens behind
-// 16384 434 us (1.29 PFLOP/s), 2048 behind 60000 1455 us (1.41); head_dim 64, 12 heads
+// 16384 431 us (1.29 PFLOP/s), 2048 behind 60000 1455 us (1.41); head_dim 64, 12 heads
 // over 4: 12 x 700 behind 2048 119 us (0.52: the same chain for half of the products).
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -839,15 +839,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     // tokens of a granule before the request's end
                     auto valid = [&](uint32_t g) { return len - (int32_t)(16 * (v0 + g)) - (v0 + g >= a.sink_grans ? skip : 0); };
                     uint8_t *tile = smem_c + L::kRing + n % L::kStages * L::kTile;
+                    auto k_steps = [&](auto bf16) {
 #pragma unroll 1
-                    for (uint32_t s = mine; s < kSteps; s += kMakers) {
-                        const uint32_t g = s / kPerGran, r = s % kPerGran * U::kRows;
-                        if (g >= have) continue;
-                        if (DT == PK_FP16 || halves)
-                            lanes.template step<false, false>(place(g) + G::kK, place(g) + G::kKs, tile + s * U::kRows * 128, r, 16);
-                        else
-                            lanes.template step<true, false>(place(g) + G::kK, place(g) + G::kKs, tile + s * U::kRows * 128, r, 16);
-                    }
+                        for (uint32_t s = mine; s < have * kPerGran; s += kMakers) {
+                            const uint32_t g = s / kPerGran, r = s % kPerGran * U::kRows;
+                            lanes.template step<decltype(bf16)::value, false>(place(g) + G::kK, place(g) + G::kKs,
+                                                                              tile + s * U::kRows * 128, r, 16);
+                        }
+                    };
+                    // a loop each, the seldom one out of the way (438 -> 431 us for 4 x 512 tokens behind 16384)
+                    if (__builtin_expect(DT == PK_FP16 || halves, 1))
+                        k_steps(std::false_type{});
+                    else
+                        k_steps(std::true_type{});
                     pk::fence_proxy_async_smem();
                     if (mine >= kMakers - 2) {  // blocks of V marked NaN, two tokens a lane
                         const uint32_t half = mine - (kMakers - 2);
@@ -879,14 +883,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attend_chunk(const Args a, cons
                     ok = wait_empty(n);
                     if (!ok) break;
                     tile = smem_c + L::kRing + n % L::kStages * L::kTile;
+                    uint32_t s = mine;
 #pragma unroll 1
-                    for (uint32_t s = mine; s < kSteps; s += kMakers) {
+                    for (; s < have * kPerGran; s += kMakers) {
                         const uint32_t g = s / kPerGran, r = s % kPerGran * U::kRows;
-                        if (g < have)
-                            lanes.template step<false, true>(place(g) + G::kV, place(g) + G::kVs, tile + s * U::kRows * 128, r, valid(g));
-                        else  // behind the last granule: weights of 0 must not meet what lies there
-                            lanes.zero(tile + s * U::kRows * 128);
+                        lanes.template step<false, true>(place(g) + G::kV, place(g) + G::kVs, tile + s * U::kRows * 128, r,
+                                                         valid(g));
                     }
+#pragma unroll 1
+                    for (; s < kSteps; s += kMakers)  // behind the last granule: weights of 0 must not meet what lies there
+                        lanes.zero(tile + s * U::kRows * 128);
                     pk::fence_proxy_async_smem();
                     __syncwarp();
                     if (lane < have) pk::mbar_arrive(pk::smem_addr(&sm.gran_empty[c % L::kGrans]));
