@@ -7,7 +7,7 @@
 // halves: queries in bfloat16 are scaled by a power of two a row first, which
 // leaves them as they are (k_chunk_queries); where one row's values lie too far
 // apart for that, or the call is too short to be worth it, the call's products
-// with K are of bfloat16s, to which K costs more to unpack (476 | 438 us for
+// with K are of bfloat16s, to which K costs more to unpack (460 | 429 us for
 // 4 x 512 tokens behind 16384).
 // ref moves as in pk_attend_prompt.cu: only when a tile's weights of a row sum to
 // more than 2^15.
@@ -22,8 +22,8 @@
 // cycles at head_dim 128, of which the products are 2048 (tensor pipe 55-61% busy,
 // issue slots 52-58%, memory 5%); a warp's scores and weights of one tile are a chain
 // of 1650 to 2000 cycles.  Full lengths, bf16, 32 heads over 8: 4 x 512 tokens behind
-// 16384 431 us (1.29 PFLOP/s), 2048 behind 60000 1455 us (1.41); head_dim 64, 12 heads
-// over 4: 12 x 700 behind 2048 119 us (0.52: the same chain for half of the products).
+// 16384 430 us (1.30 PFLOP/s), 2048 behind 60000 1441 us (1.42); head_dim 64, 12 heads
+// over 4: 12 x 700 behind 2048 117 us (0.53: the same chain for half of the products).
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <float.h>
@@ -1401,8 +1401,8 @@ struct Plan {
 
 constexpr uint64_t kSms = 152;
 // Keys that a call's units go through (half of them at head_dim 64) from which on halves of its queries pay for their
-// making, as bfloat16s | halves: 400 tokens of 2 requests behind 4000 (0.5 M keys) 82 | 84 us, 1 x 40 behind 60000 (1.0 M)
-// 129 | 122, 4 x 500 behind 4000 (1.2 M) 156 | 153, head_dim 64 12 x 700 behind 2048 (1.2 M) 136 | 141.
+// making, as bfloat16s | halves: 400 tokens of 2 requests behind 4000 (0.5 M keys) 77 | 80 us, 1 x 40 behind 60000 (1.0 M)
+// 118 | 112, 4 x 500 behind 4000 (1.2 M) 147 | 148, head_dim 64 12 x 700 behind 2048 (1.2 M) 130 | 132.
 constexpr uint64_t kWorthHalves = 3ull << 18;
 Plan plan_of(const pk_kv_cache &kv, uint32_t dtype, uint32_t R, uint64_t n_q, uint32_t q_heads, uint64_t page_stride,
              uint32_t window, uint32_t sinks) {
