@@ -127,3 +127,21 @@ def test_captured_step():
                 o, l = step()
                 want.append((o.clone(), l.clone(), weight.clone()))
     layer.kv.check()
+
+
+def test_the_readmes_lines_run():
+    import os
+    import re
+    from paper_2609_38706_gb300.service import KVPages
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    block = next(b for b in re.findall(r"```python\n(.*?)```", text, re.S) if "kv.rotate(" in b)
+    x = lambda n, h: torch.randn((n, h, 128), device="cuda").to(torch.bfloat16)  # noqa: E731
+    off, w = dev(np.array([0, 40, 60])), torch.ones(128, dtype=torch.bfloat16, device="cuda")
+    env = dict(kv=KVPages(8, 16, 2, 128), q=x(60, 4), k=x(60, 2), v=x(60, 2), tok_off=off, q_off=off, q_weight=w, k_weight=w,
+               start=dev(np.zeros(2, np.int32)), pages=dev(np.arange(6, dtype=np.int32).reshape(2, 3)),
+               kv_len=dev(np.array([40, 20], np.int32)))
+    for line in block.strip().split("\n"):
+        if "kv.attend(" in line:
+            env["q"] = env["q"][:2].unsqueeze(1)
+        exec(line, env)
+    assert env["out"].shape == (2, 1, 4, 128) and bool(env["out"].isfinite().all())
