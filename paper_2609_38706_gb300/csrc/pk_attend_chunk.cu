@@ -18,8 +18,8 @@
 // below, down to low, and those before `sinks`.
 //
 // What bounds it is a tile's chain: scores, weights, product.  A key tile meets two
-// tiles of 128 rows, so that unpacking it is paid once for 256 rows, and takes 3560
-// cycles at head_dim 128, of which the products are 2048 (tensor pipe 55-61% busy,
+// tiles of 128 rows, so that unpacking it is paid once for 256 rows, and takes 3500
+// cycles at head_dim 128, of which the products are 2048 (tensor pipe 56-62% busy,
 // issue slots 52-58%, memory 5%); a warp's scores and weights of one tile are a chain
 // of 1650 to 2000 cycles.  Full lengths, bf16, 32 heads over 8: 4 x 512 tokens behind
 // 16384 430 us (1.30 PFLOP/s), 2048 behind 60000 1441 us (1.42); head_dim 64, 12 heads
