@@ -6,7 +6,7 @@
 // has six significant bits: exact in a half and in a bfloat16.  All products are of
 // halves: queries in bfloat16 are scaled by a power of two a row first, which
 // leaves them as they are (k_chunk_queries); where one row's values lie too far
-// apart for that, or the call is too short to be worth it, the call's products
+// apart for that, or a row has too few keys to be worth it, the call's products
 // with K are of bfloat16s, to which K costs more to unpack (460 | 429 us for
 // 4 x 512 tokens behind 16384).
 // ref moves as in pk_attend_prompt.cu: only when a tile's weights of a row sum to
@@ -1404,6 +1404,10 @@ constexpr uint64_t kSms = 152;
 // making, as bfloat16s | halves: 400 tokens of 2 requests behind 4000 (0.5 M keys) 77 | 80 us, 1 x 40 behind 60000 (1.0 M)
 // 118 | 112, 4 x 500 behind 4000 (1.2 M) 147 | 148, head_dim 64 12 x 700 behind 2048 (1.2 M) 130 | 132.
 constexpr uint64_t kWorthHalves = 3ull << 18;
+// And keys of one unit at least (twice as many at head_dim 64): what is made is a row's, what it saves a key's. 16 x 1024
+// tokens alone 215 | 262 us, 8 x 4096 behind 8192 with a window of 2048 985 | 1037, 4 x 2048 behind 32768 with one of 4096
+// 487 | 478, 1 x 8192 alone 489 | 476; head_dim 64 12 x 1500 behind 2048 253 | 260, 6 x 3000 behind 4000 541 | 538.
+constexpr uint64_t kHalfKeys = 4096;
 Plan plan_of(const pk_kv_cache &kv, uint32_t dtype, uint32_t R, uint64_t n_q, uint32_t q_heads, uint64_t page_stride,
              uint32_t window, uint32_t sinks) {
     Plan p;
@@ -1416,7 +1420,8 @@ Plan plan_of(const pk_kv_cache &kv, uint32_t dtype, uint32_t R, uint64_t n_q, ui
     p.cut_bytes = p.blocks * sizeof(Cut);
     p.ml_bytes = p.blocks > 1 ? 2 * p.blocks * 2 * kRows * 16 : 0;
     p.o_bytes = p.blocks > 1 ? 2 * p.blocks * 2 * kRows * kv.head_dim * 4 : 0;
-    const bool halves = dtype == PK_BF16 && keys && p.units >= kWorthHalves * 128 / kv.head_dim / keys;
+    const bool halves = dtype == PK_BF16 && keys >= kHalfKeys * 128 / kv.head_dim &&
+                        p.units >= kWorthHalves * 128 / kv.head_dim / keys;
     const uint64_t rows = halves ? n_q * q_heads : 0;
     p.wide_bytes = rows ? kQueryBlocks : 0;
     p.down_bytes = (rows * 4 + 31) & ~31ull;
