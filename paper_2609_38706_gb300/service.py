@@ -385,7 +385,8 @@ class Rotary:
     by parts (pk_rotary_turns); ``amplitude`` multiplies what was rotated.  ``turns`` (uint64 [rotary_dim / 2], fractions of
     a turn by 2^64) takes the place of base and factor.
 
-    The table is copied to ``device`` once, and that copy is over when the object exists."""
+    The table is copied to ``device`` once, and that copy is over when the object exists.  Its memory is not given out again
+    before the calls that read it have run, on whatever stream."""
 
     def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, base: float = 10000.0, interleaved: bool = False,
                  factor: float = 1.0, context: Optional[float] = None, low: float = 1.0, high: float = 32.0,
@@ -399,6 +400,7 @@ class Rotary:
         if turns.dtype != np.uint64 or turns.shape != (self.rotary_dim // 2,):
             raise pk.PKError(pk.PK_ERR_ARG, "Rotary: turns is uint64 [rotary_dim / 2]")
         self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
+        self.made_on = pk._stream_of(None, self.turns) if self.turns.is_cuda else None
         self.table = pk.pk_rotary(self.turns.data_ptr(), self.rotary_dim, int(bool(interleaved)), amplitude)
 
 
@@ -413,8 +415,8 @@ def rotate(q, k, tok_off, start, rotary: Rotary, q_weight: Optional[torch.Tensor
     if q.shape[-1] != rotary.head_dim or rotary.turns.device != q.device:
         raise pk.PKError(pk.PK_ERR_ARG, "rotate: rotary is for other heads, or on another device")
     q_out, k_out = out if out is not None else _empty(q, stream, (q.shape, q.dtype), (k.shape, k.dtype))
-    if stream is not None:  # the table belongs to the stream that it was made on
-        rotary.turns.record_stream(_stream(stream))
+    if pk._stream_of(stream, rotary.turns) != rotary.made_on:  # the table belongs to the stream that it was made on
+        rotary.turns.record_stream(torch.cuda.current_stream(rotary.turns.device) if stream is None else _stream(stream))
     pk.pk_rotate(q, k, q_out, k_out, rotary.table, q_weight, k_weight, eps, tok_off, start, status, stream)
     return q_out, k_out
 
