@@ -6,7 +6,8 @@
 // has six significant bits: exact in a half and in a bfloat16.  All products are of
 // halves: queries in bfloat16 are scaled by a power of two a row first, which
 // leaves them as they are (k_chunk_queries); where one row's values lie too far
-// apart for that, or a row has too few keys to be worth it, the call's products
+// apart for that, its power of two times the scale leaves 32 bits, or a request
+// could not hold enough keys for it to be worth it (kHalfKeys), the call's products
 // with K are of bfloat16s, to which K costs more to unpack (460 | 429 us for
 // 4 x 512 tokens behind 16384).
 // ref moves as in pk_attend_prompt.cu: only when a tile's weights of a row sum to
@@ -305,8 +306,10 @@ __global__ void __launch_bounds__(kQueryThreads) k_chunk_queries(const Args a) {
             for (uint32_t d = 1; d < kLanes; d *= 2) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, d));
             const int e = bits == 0 || bits >= 0x7f800000u ? 14 : max((int)(bits >> 23) - 127, -110);  // 2^e <= the largest
             const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
+            const float down = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
             uint32_t out[4];
-            bool odd = bits >= 0x7f800000u;
+            // a row's factor of scores past 32 bits would make NaN of a score of 0: bfloat16s need none
+            bool odd = bits >= 0x7f800000u || fabsf(a.scale2) * down > FLT_MAX;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float lo = x[2 * i] * up, hi = x[2 * i + 1] * up;
@@ -317,7 +320,7 @@ __global__ void __launch_bounds__(kQueryThreads) k_chunk_queries(const Args a) {
             if (!on[k]) continue;
             wide |= odd;
             *reinterpret_cast<uint4 *>(a.half_q + row * D + c * 8) = make_uint4(out[0], out[1], out[2], out[3]);
-            if (c == 0) a.row_down[row] = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
+            if (c == 0) a.row_down[row] = down;
         }
     }
     const int any = __syncthreads_or(wide);
