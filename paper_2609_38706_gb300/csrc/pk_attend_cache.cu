@@ -328,7 +328,8 @@ __global__ void __launch_bounds__(kThreads, 16 / kWarps) k_attend_cache(const Ar
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            mul[nt][j] = a.scale2 * __shfl_sync(0xffffffffu, down, 4 * (2 * c + j));
+            // past 32 bits it would make NaN of a score of 0; scores that are made smaller, all beyond 2^50, keep their order
+            mul[nt][j] = fminf(fmaxf(a.scale2 * __shfl_sync(0xffffffffu, down, 4 * (2 * c + j)), -FLT_MAX), FLT_MAX);
             const uint32_t cr = tile * kRows + nt * 8 + 2 * c + j;
             last[nt][j] = len - (int32_t)a.n_q + (int32_t)(cr < a.rows ? cr / a.group : a.n_q - 1);
             low[nt][j] = kWindow ? (int32_t)max((int64_t)last[nt][j] - a.window + 1, (int64_t)0) : 0;

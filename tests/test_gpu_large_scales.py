@@ -47,3 +47,24 @@ def test_chunks(dtype, top, scale, D, window, room):
                                window=window, sinks=3)
     kv.check()
     check(out, lse, *reference(pool, pages, new, lens, np.zeros(q.shape), C, H, D, 1.0, window, 3)[:4], dtype, max(lens))
+
+
+@pytest.mark.parametrize("weigh", [False, True])
+@pytest.mark.parametrize("D,G,n_q,window", [(64, 1, 1, None), (128, 3, 1, 70), (128, 4, 5, None), (64, 2, 3, 70)])
+@pytest.mark.parametrize("dtype,top,scale", TOPS)
+def test_steps(dtype, top, scale, D, G, n_q, window, weigh):
+    """The same of a decode step's queries, whose page weights add up to one for each query that sees a key."""
+    lens, C, H = [300, 2], 16, 2
+    pool, pages, rng = flat(lens, C, H, D, 6)
+    q = large(rng, (len(lens), n_q, H * G, D), top, dtype)
+    q[0, 0, 0] *= 2.0 ** -20 if dtype == "bf16" else 0.0
+    kv = cache(pool, C, H, D)
+    weight = torch.zeros(pages.shape, dtype=torch.float32, device="cuda") if weigh else None
+    out, lse = kv.attend(q.cuda(), dev(np.array(lens, np.int32)), dev(pages), scale, weight, window=window, sinks=3)
+    kv.check()
+    shape = (len(lens) * n_q, H * G, D)
+    check(out.view(shape), lse.view(shape[:2]),
+          *reference(pool, pages, [n_q] * len(lens), lens, np.zeros(shape), C, H, D, 1.0, window, 3)[:4], dtype, max(lens))
+    if weigh:
+        total = sum(min(n, n_q) for n in lens) * H * G
+        assert abs(float(weight.sum()) - total) <= total * (max(lens) + 64) * 2.0 ** -23  # sums of 32 bits
