@@ -651,6 +651,18 @@ typedef struct {
 int pk_rotary_turns(uint32_t rotary_dim, double base, double factor, double context, double low, double high,
                     uint64_t *turns);
 
+/* Host.  pk_rotary_turns by parts with the ramp over the pair's index instead of
+ * its turns, between ends that are rounded outwards.  The two tables differ by up
+ * to half and more of a frequency, so a model takes the one that it was tuned
+ * with.  i(n) = rotary_dim * ln(context / (2 pi n)) / (2 ln base) is the index
+ * whose pair makes n turns over the original context.  With first =
+ * max(floor(i(high)), 0) and last = min(ceil(i(low)), rotary_dim - 1), f_i stays
+ * where i <= first, is divided where i >= last, and between them is the mean of
+ * both, f_i weighed by (last - i) / (last - first).  Arguments as above, but
+ * context > 0 and low > 0; refused where last < first. */
+int pk_rotary_turns_by_index(uint32_t rotary_dim, double base, double factor, double context, double low, double high,
+                             uint64_t *turns);
+
 /* Device.  Norms of queries and keys, a head at a time, and their rotation, in
  * one pass:
  *   q, q_out [n_tokens][q_heads][head_dim], k, k_out [n_tokens][kv_heads][head_dim]

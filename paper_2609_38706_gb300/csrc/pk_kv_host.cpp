@@ -208,19 +208,41 @@ int pk_attend_chunk(const pk_kv_cache *kv, uint32_t dtype, const pk_heads *q, co
                                           reinterpret_cast<cudaStream_t>(stream)));
 }
 
+static const double kTurn = 6.283185307179586476925286766559;  // 2 pi
+
+static bool good_turns(uint32_t rotary_dim, double base, double factor, double context, double low, double high,
+                       const uint64_t *turns) {
+    return turns && rotary_dim >= 16 && rotary_dim <= 128 && rotary_dim % 16 == 0 && base > 1.0 && std::isfinite(base) &&
+           factor >= 1.0 && std::isfinite(factor) && context >= 0.0 && std::isfinite(context) && low >= 0.0 && high > low &&
+           std::isfinite(high);
+}
+
+// Part `stays` of f as it is, the rest divided.
+static uint64_t turns_of(double f, double factor, double stays) {
+    return (uint64_t)std::ldexp((stays * f + (1.0 - stays) * f / factor) / kTurn, 64);
+}
+
 int pk_rotary_turns(uint32_t rotary_dim, double base, double factor, double context, double low, double high,
                     uint64_t *turns) {
-    if (!turns || rotary_dim < 16 || rotary_dim > 128 || rotary_dim % 16 || !(base > 1.0) || !std::isfinite(base) ||
-        !(factor >= 1.0) || !std::isfinite(factor) || !(context >= 0.0) || !std::isfinite(context) || !(low >= 0.0) ||
-        !(high > low) || !std::isfinite(high))
-        return PK_ERR_ARG;
-    const double turn = 6.283185307179586476925286766559;  // 2 pi
+    if (!good_turns(rotary_dim, base, factor, context, low, high, turns)) return PK_ERR_ARG;
     for (uint32_t i = 0; i < rotary_dim / 2; ++i) {
         const double f = std::pow(base, -2.0 * i / rotary_dim);
         double stays = 0.0;
-        if (context > 0.0) stays = std::fmin(1.0, std::fmax(0.0, (context * f / turn - low) / (high - low)));
-        turns[i] = (uint64_t)std::ldexp((stays * f + (1.0 - stays) * f / factor) / turn, 64);
+        if (context > 0.0) stays = std::fmin(1.0, std::fmax(0.0, (context * f / kTurn - low) / (high - low)));
+        turns[i] = turns_of(f, factor, stays);
     }
+    return PK_OK;
+}
+
+int pk_rotary_turns_by_index(uint32_t rotary_dim, double base, double factor, double context, double low, double high,
+                             uint64_t *turns) {
+    if (!good_turns(rotary_dim, base, factor, context, low, high, turns) || context == 0.0 || low == 0.0) return PK_ERR_ARG;
+    auto index = [&](double n) { return rotary_dim * std::log(context / (kTurn * n)) / (2.0 * std::log(base)); };
+    const double first = std::fmax(std::floor(index(high)), 0.0), last = std::fmin(std::ceil(index(low)), rotary_dim - 1.0);
+    if (last < first) return PK_ERR_ARG;
+    for (uint32_t i = 0; i < rotary_dim / 2; ++i)
+        turns[i] = turns_of(std::pow(base, -2.0 * i / rotary_dim), factor,
+                            i <= first ? 1.0 : i >= last ? 0.0 : (last - i) / (last - first));
     return PK_OK;
 }
 

@@ -138,6 +138,7 @@ def lib() -> ctypes.CDLL:
             "pk_kv_write": (ctypes.c_int, [_VP, _U32, _VP, _VP, _U64, _VP, _VP, _U32, _VP, _U64, _VP, _VP]),
             "pk_kv_read": (ctypes.c_int, [_VP, _U32, _VP, _VP, _U64, _VP, _VP, _U32, _VP, _U64, _VP, _VP]),
             "pk_rotary_turns": (ctypes.c_int, [_U32] + [ctypes.c_double] * 5 + [_VP]),
+            "pk_rotary_turns_by_index": (ctypes.c_int, [_U32] + [ctypes.c_double] * 5 + [_VP]),
             "pk_rotate": (ctypes.c_int, [_U32, _VP, _VP, _VP, _VP, _U64, _U32, _U32, _U32, _VP, _VP, _VP, ctypes.c_float,
                                          _VP, _VP, _U32, _VP, _VP]),
             "pk_attend_prompt_scratch_bytes": (ctypes.c_size_t, [_U32]),
@@ -632,10 +633,19 @@ def pk_kv_read(kv: pk_kv_cache, k: torch.Tensor, v: torch.Tensor, tok_off: torch
 
 def pk_rotary_turns(rotary_dim: int, base: float, factor: float, context: float, low: float, high: float) -> np.ndarray:
     """uint64 [rotary_dim / 2], on the host."""
+    return _turns("pk_rotary_turns", rotary_dim, base, factor, context, low, high)
+
+
+def pk_rotary_turns_by_index(rotary_dim: int, base: float, factor: float, context: float, low: float, high: float) -> np.ndarray:
+    """As pk_rotary_turns."""
+    return _turns("pk_rotary_turns_by_index", rotary_dim, base, factor, context, low, high)
+
+
+def _turns(fn: str, rotary_dim: int, *args) -> np.ndarray:
     if not 0 < rotary_dim <= 128:
-        _refuse("pk_rotary_turns", "rotary_dim is a multiple of 16, up to 128")
+        _refuse(fn, "rotary_dim is a multiple of 16, up to 128")
     out = np.zeros(rotary_dim // 2, np.uint64)
-    _check(lib().pk_rotary_turns(rotary_dim, base, factor, context, low, high, out.ctypes.data), "pk_rotary_turns")
+    _check(getattr(lib(), fn)(rotary_dim, *args, out.ctypes.data), fn)
     return out
 
 

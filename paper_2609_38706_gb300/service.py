@@ -382,20 +382,25 @@ class Rotary:
     """How positions rotate a head's first ``rotary_dim`` dimensions (pk_rotary): pair i, of dimensions (i, i +
     rotary_dim/2) or, ``interleaved``, (2i, 2i + 1), by ``base ** (-2 i / rotary_dim)`` radians a position.  For longer
     contexts than a model was made for these are divided by ``factor``: all of them, or with ``context``, its own context,
-    by parts (pk_rotary_turns); ``amplitude`` multiplies what was rotated.  ``turns`` (uint64 [rotary_dim / 2], fractions of
-    a turn by 2^64) takes the place of base and factor.
+    by parts; ``amplitude`` multiplies what was rotated.  The parts' ramp runs over a pair's turns in that context
+    (pk_rotary_turns), or with ``ramp="index"`` over its index, between rounded ends (pk_rotary_turns_by_index): the angles
+    differ much, and a model takes those that it was tuned with.  ``turns`` (uint64 [rotary_dim / 2], fractions of a turn by
+    2^64) takes the place of base and factor.
 
     The table is copied to ``device`` once, and that copy is over when the object exists.  Its memory is not given out again
     before the calls that read it have run, on whatever stream."""
 
     def __init__(self, head_dim: int, rotary_dim: Optional[int] = None, base: float = 10000.0, interleaved: bool = False,
                  factor: float = 1.0, context: Optional[float] = None, low: float = 1.0, high: float = 32.0,
-                 amplitude: float = 1.0, turns=None, device="cuda"):
+                 amplitude: float = 1.0, turns=None, device="cuda", ramp: str = "turns"):
         self.head_dim, self.rotary_dim = int(head_dim), int(head_dim if rotary_dim is None else rotary_dim)
         if self.rotary_dim < 16 or self.rotary_dim % 16 or self.rotary_dim > self.head_dim or not np.isfinite(amplitude):
             raise pk.PKError(pk.PK_ERR_ARG, "Rotary: rotary_dim is a multiple of 16, up to head_dim; amplitude is finite")
+        if ramp not in ("turns", "index"):
+            raise pk.PKError(pk.PK_ERR_ARG, "Rotary: the ramp is over turns or index")
         if turns is None:
-            turns = pk.pk_rotary_turns(self.rotary_dim, base, factor, context or 0.0, low, high)
+            make = pk.pk_rotary_turns if ramp == "turns" else pk.pk_rotary_turns_by_index
+            turns = make(self.rotary_dim, base, factor, context or 0.0, low, high)
         turns = np.ascontiguousarray(turns)
         if turns.dtype != np.uint64 or turns.shape != (self.rotary_dim // 2,):
             raise pk.PKError(pk.PK_ERR_ARG, "Rotary: turns is uint64 [rotary_dim / 2]")
