@@ -673,8 +673,12 @@ int pk_rotary_turns_by_index(uint32_t rotary_dim, double base, double factor, do
  *            NULL it stays as it is
  *   tok_off_dev, start_dev  as pk_kv_write: token i of request r has position
  *            start[r] + i, below 2^31
- * Angles are exact to 2^-32 of a turn at any position; all else is held in 32
- * bits and rounded once.  Tokens that belong to no request are not written.
+ * A position times an entry of turns_dev is exact modulo a turn; the angle is that
+ * to 2^-25 of a turn (its upper 32 bits, rounded to 24).  An entry's own error counts
+ * once a position: those of pk_rotary_turns and pk_rotary_turns_by_index lie within
+ * 2^-51 of a turn of their formula (by turns: where high is twice low and more).
+ * All else is held in 32 bits and rounded once.  Tokens that belong to no request
+ * are not written.
  * head_dim: 64 or 128; q_heads + kv_heads <= 65536; either may be 0; eps
  * positive, normal and finite.  Device errors: offsets or start out of range
  * (PK_ERR_ARG; that token is not written). */

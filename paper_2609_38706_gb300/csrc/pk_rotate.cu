@@ -6,8 +6,9 @@
 //
 // An angle is held in turns: f_i is a 64-bit fraction of a turn, so pos * f_i mod
 // 2^64 is the product's part behind the whole turns, exact for any position, where
-// a 32-bit product would be off by 0.004 rad at position 100000.  Its upper half
-// goes to sincospi.  All else is 32-bit arithmetic, rounded once, at the end.
+// a 32-bit product would be off by 0.004 rad at position 100000.  Its upper half,
+// rounded to 24 bits (2^-26 of a turn at most), goes to sincospi.  All else is
+// 32-bit arithmetic, rounded once, at the end.
 //
 // A lane holds the 16 values of 8 pairs of one head, so that nothing but the norm's
 // sum crosses lanes, and the angles, which are a token's, serve all its heads.  The
