@@ -6,8 +6,8 @@
 // has six significant bits: exact in a half and in a bfloat16.  All products are of
 // halves: queries in bfloat16 are scaled by a power of two a row first, which
 // leaves them as they are (k_chunk_queries); where one row's values lie too far
-// apart for that, its power of two times the scale leaves 32 bits, or a request
-// could not hold enough keys for it to be worth it (kHalfKeys), the call's products
+// apart for that, the scale is so large that a row's power of two times it may leave
+// 32 bits, or a row has too few keys to be worth it, the call's products
 // with K are of bfloat16s, to which K costs more to unpack (460 | 429 us for
 // 4 x 512 tokens behind 16384).
 // ref moves as in pk_attend_prompt.cu: only when a tile's weights of a row sum to
@@ -30,6 +30,7 @@
 #include <float.h>
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "pk_attend.cuh"
@@ -306,10 +307,8 @@ __global__ void __launch_bounds__(kQueryThreads) k_chunk_queries(const Args a) {
             for (uint32_t d = 1; d < kLanes; d *= 2) bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, d));
             const int e = bits == 0 || bits >= 0x7f800000u ? 14 : max((int)(bits >> 23) - 127, -110);  // 2^e <= the largest
             const float up = __uint_as_float((uint32_t)(14 - e + 127) << 23);
-            const float down = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
             uint32_t out[4];
-            // a row's factor of scores past 32 bits would make NaN of a score of 0: bfloat16s need none
-            bool odd = bits >= 0x7f800000u || fabsf(a.scale2) * down > FLT_MAX;
+            bool odd = bits >= 0x7f800000u;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float lo = x[2 * i] * up, hi = x[2 * i + 1] * up;
@@ -320,7 +319,7 @@ __global__ void __launch_bounds__(kQueryThreads) k_chunk_queries(const Args a) {
             if (!on[k]) continue;
             wide |= odd;
             *reinterpret_cast<uint4 *>(a.half_q + row * D + c * 8) = make_uint4(out[0], out[1], out[2], out[3]);
-            if (c == 0) a.row_down[row] = down;
+            if (c == 0) a.row_down[row] = __uint_as_float((uint32_t)(e - 14 + 127) << 23);
         }
     }
     const int any = __syncthreads_or(wide);
@@ -1501,7 +1500,10 @@ cudaError_t pk_launch_attend_chunk(const pk_kv_cache &kv, uint32_t dtype, const 
     a.row_down = reinterpret_cast<float *>(at + p.wide_bytes);
     a.half_q = reinterpret_cast<uint16_t *>(at + p.wide_bytes + p.down_bytes);
     const uint64_t query_rows = kQueryThreads / (kv.head_dim / 8) * kQueryRows;  // of a block at once
-    a.query_blocks = p.wide_bytes ? (uint32_t)std::min<uint64_t>((n_q * q_heads + query_rows - 1) / query_rows, kQueryBlocks) : 0;
+    // A row's factor of scores is scale2 * 2^(e - 14), e up to 127: where that can leave 32 bits, which would make NaN of a
+    // score of 0, the call takes bfloat16 products, which need no factor.
+    const bool halves = p.wide_bytes && std::fabs(a.scale2) < 0x1p15f;
+    a.query_blocks = halves ? (uint32_t)std::min<uint64_t>((n_q * q_heads + query_rows - 1) / query_rows, kQueryBlocks) : 0;
     a.status = status;
     CUtensorMap mq, mh{};
     cudaError_t e = map_of(&mq, q, n_q, q_heads, kv.head_dim, dtype, a.tile_tokens, a.tile_heads);
