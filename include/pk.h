@@ -618,7 +618,10 @@ int pk_attend_cache_window(const pk_kv_cache *kv, uint32_t dtype, const pk_heads
  * page_stride * page_tokens at most 0x7fff0000, n_q * q_heads below 2^34; window
  * and sinks below 2^31; |scale * k_scale| at most 2.3e38; strides of q below
  * 2^39; out overlaps no input.  scratch_dev: pk_attend_chunk_scratch_bytes(...) bytes for the same
- * arguments, 32-byte aligned.
+ * arguments, 32-byte aligned.  Sums of q times (code * block scale) are held in
+ * 32 bits, which queries in bfloat16 of 2^109 and more can leave.  Work is shared
+ * out by a call's mean request: one very long request among many short ones is
+ * faster in a call of its own.
  * Device errors: offsets out of order or range (PK_ERR_ARG; nothing is
  * written); a kv_len out of range (PK_ERR_ARG) counts as 0; a slot out of
  * range (PK_ERR_ARG) makes out and lse NaN for the queries that see its page,

@@ -939,7 +939,9 @@ cudaError_t pk_launch_attend_cache(const pk_kv_cache &kv, uint32_t dtype, const 
     a.split_grans = p.split_grans;
     // One CTA a request and head, and more of them than the GPU holds: the longest first, so that the last to start are
     // the shortest (128 x 2048 tokens: 65.6 -> 63.5 us; 100 x 1500, D = 64: 36.9 -> 35.2).  The search costs short
-    // ones more than it gives (250 x 300: 31.7 -> 38.4 us).
+    // ones more than it gives (250 x 300: 31.7 -> 38.4 us).  Behind a window most requests weigh the same, and it costs
+    // more than it gives (window 1024: 128 x 8192 tokens 50.9 -> 53.6, 250 x up to 1200, D = 64, 21.7 -> 23.1), but for
+    // lengths about the window (128 x up to 1500: 46.9 -> 43.6; window 4096, 128 x up to 4096: even).
     a.by_length = !window && p.splits == 1 && R > 1 && R <= kRanked && p.max_grans >= kRankedGrans &&
                   (uint64_t)R * kv.kv_heads * p.row_tiles > kSlots;
     a.scale2 = (float)((double)scale * kv.k_scale * 1.4426950408889634);

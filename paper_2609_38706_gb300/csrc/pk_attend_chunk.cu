@@ -7,11 +7,19 @@
 // halves: queries in bfloat16 are scaled by a power of two a row first, which
 // leaves them as they are (k_chunk_queries); where one row's values lie too far
 // apart for that, the scale is so large that a row's power of two times it may leave
-// 32 bits, or a row has too few keys to be worth it, the call's products
-// with K are of bfloat16s, to which K costs more to unpack (460 | 429 us for
-// 4 x 512 tokens behind 16384).
+// 32 bits, or the page table is too narrow for them to be worth it (kHalfKeys), the
+// call's products with K are of bfloat16s, to which K costs more to unpack (460 |
+// 429 us for 4 x 512 tokens behind 16384).  Those sum q . (code * scale) in 32 bits,
+// which queries of 2^109 and more can leave.
 // ref moves as in pk_attend_prompt.cu: only when a tile's weights of a row sum to
 // more than 2^15.
+//
+// Weights are rounded to halves for the product with V, whatever q's type: half a
+// step is 2^-11 of a weight where bfloat16s are off by 2^-8 at the same rate; 32-bit
+// weights would take V in 32 bits too and twice the product's time.  The largest one
+// is 2^kBase and more (1 behind a far reference), so those that a half does not hold
+// (below 2^-14, down to 0 from 2^-25 on) cost N keys at most N 2^-29 (2^-25) of their
+// values.  A row's sum takes its weights unrounded, in 32 bits.
 //
 // Keys are counted without the gap that a window leaves: of a tile of queries the
 // granules (16 tokens) of the first tokens and those from the first query's window
@@ -102,7 +110,9 @@ __device__ __forceinline__ int32_t good_length(const Args &a, int32_t len) {
 // line is cut into equal shares, one for each block: a block takes the units that its share holds, of the first and
 // the last a piece of their keys.  So all blocks are done at about the same time, also where a call is a few rows over
 // many keys (4 x 512 tokens behind 16384, 256 units: 604 -> 550 us against units cut in two).  Where that gains less
-// than the pieces and their joining cost, a block takes the whole units that begin in its share.
+// than the pieces and their joining cost, a block takes the whole units that begin in its share.  That is judged by the
+// mean unit, and is too good for a long request among many short ones, whose units are far above it: 40 tokens behind
+// 60000 with 63 requests of 100 alone take 842 us, the two kinds in calls of their own 73 and 55.
 // All three in keys.  A unit's start and end: 256 | 512 | 1024 are 65 | 65 | 86 us for 8 x 600 tokens behind 9000, window 1000
 // (head_dim 64).  One more piece a block, and the joining: 768 | 1536 are 112 | 128 for 2 x 2000 behind 2000, 150 | 157 for
 // 4 x 500 behind 4000, and 123 | 114 for 5 x 400 behind 2500.  Shares of 320 to 1280 keys at least are alike.
@@ -1406,9 +1416,11 @@ constexpr uint64_t kSms = 152;
 // making, as bfloat16s | halves: 400 tokens of 2 requests behind 4000 (0.5 M keys) 77 | 80 us, 1 x 40 behind 60000 (1.0 M)
 // 118 | 112, 4 x 500 behind 4000 (1.2 M) 147 | 148, head_dim 64 12 x 700 behind 2048 (1.2 M) 130 | 132.
 constexpr uint64_t kWorthHalves = 3ull << 18;
-// And keys of one unit at least (twice as many at head_dim 64): what is made is a row's, what it saves a key's. 16 x 1024
-// tokens alone 215 | 262 us, 8 x 4096 behind 8192 with a window of 2048 985 | 1037, 4 x 2048 behind 32768 with one of 4096
-// 487 | 478, 1 x 8192 alone 489 | 476; head_dim 64 12 x 1500 behind 2048 253 | 260, 6 x 3000 behind 4000 541 | 538.
+// And keys that a unit can have at least (twice as many at head_dim 64): what is made is a row's, what it saves a key's.
+// 16 x 1024 tokens alone 215 | 262 us, 8 x 4096 behind 8192 with a window of 2048 985 | 1037, 4 x 2048 behind 32768 with
+// one of 4096 487 | 478, 1 x 8192 alone 489 | 476; head_dim 64 12 x 1500 behind 2048 253 | 260, 6 x 3000 behind 4000
+// 541 | 538.  The host knows the page table's width and the window, not the lengths: in a table for 4096 tokens and more
+// 16 x 1024 alone make halves too and take 263 us.
 constexpr uint64_t kHalfKeys = 4096;
 Plan plan_of(const pk_kv_cache &kv, uint32_t dtype, uint32_t R, uint64_t n_q, uint32_t q_heads, uint64_t page_stride,
              uint32_t window, uint32_t sinks) {

@@ -348,7 +348,7 @@ class KVPages:
                      sinks: int = 0):
         """Chunks of new tokens, written before, over the pages: q [n_q, q_heads, head_dim], request r's rows q_off[r] ..
         q_off[r + 1] at its last positions: (out like q, lse float32 [n_q, q_heads]).  ``window`` and ``sinks`` as in
-        attend."""
+        attend.  One very long request among many short ones is faster in a call of its own."""
         if q.dim() != 3:
             raise pk.PKError(pk.PK_ERR_ARG, "KVPages.attend_chunk: q is [n_q, q_heads, head_dim]")
         n_q, heads, D = q.shape
